@@ -61,7 +61,10 @@ typedef enum {
 typedef enum {
     IGC_ACTIVATION_SIGMOID = 0, /* 1 / (1 + exp(-x)) */
     IGC_ACTIVATION_RELU = 1,    /* max(x, 0) */
-    IGC_ACTIVATION_TANH = 2
+    IGC_ACTIVATION_TANH = 2,
+    /* of the matrix products below only (the other functions refuse them) */
+    IGC_ACTIVATION_GELU = 3,    /* x (1 + erf(x / sqrt(2))) / 2 */
+    IGC_ACTIVATION_SILU = 4     /* x / (1 + exp(-x)) */
 } igcActivationMode;
 
 typedef enum {
@@ -444,6 +447,103 @@ igcStatus igcPoolingBackward(igcHandle_t handle, igcPoolingDescriptor_t poolDesc
                              igcTensorDescriptor_t dyDesc, const void *dy,
                              igcTensorDescriptor_t xDesc, const void *x,
                              const void *beta, igcTensorDescriptor_t dxDesc, void *dx);
+
+/* ---- feed-forward blocks: layer norm and matrix products over tokens ------------------------
+ * The functions below see a tensor as a matrix: every position (n,h,w) is a row, its feature
+ * maps are the columns.  Feature maps must lie next to each other (stride 1) and the positions
+ * be evenly spaced in the order n, h, w, with any distance between rows (tokens (M,C,1,1), a
+ * slice of a wider buffer, N,H,W,C images); anything else is NOT_SUPPORTED.  A tensor may
+ * exceed 2 GiB.  alpha, beta and paramBeta are HOST floats (doubles for double tensors).
+ * Sums are accumulated in fp32 (fp64 for double tensors) in a fixed order: results are
+ * bitwise repeatable.  Outputs must not overlap inputs or each other except where said;
+ * an output is read only where its factor is not 0.  Errors as for the other functions:
+ * BAD_PARAM for null pointers, mismatched dimensions, aliasing output strides, misaligned
+ * pointers; NOT_INITIALIZED; NOT_SUPPORTED; EXECUTION_FAILED; validation precedes any GPU call.
+ *
+ * igcLayerNormForward: per row, over its C feature maps,
+ *   y = alpha * ((x - mean) * invStd * scale + shift) + beta * y,
+ *   mean = sum(x) / C,  invStd = 1 / sqrt(sum((x - mean)^2) / C + epsilon).
+ * x and y: float or bfloat16, each its own, or both double.  scale, shift (C values) and mean,
+ * invStd (one value per row): packed floats (doubles for double x), each may be NULL: no scale,
+ * no shift, not kept.  epsilon >= 0, finite.  y may be x itself (same type, same descriptor). */
+igcStatus igcLayerNormForward(igcHandle_t handle, const void *alpha,
+                              igcTensorDescriptor_t xDesc, const void *x,
+                              const void *scale, const void *shift, double epsilon,
+                              const void *beta, igcTensorDescriptor_t yDesc, void *y,
+                              void *mean, void *invStd);
+
+/* With h = (x - mean) * invStd, q = dy * scale, and averages over a row's C feature maps:
+ *   dx     = alpha * invStd * (q - average(q) - h * average(q * h)) + beta * r
+ *   dscale = alpha * sum over the rows of dy * h + paramBeta * dscale
+ *   dshift = alpha * sum over the rows of dy     + paramBeta * dshift
+ * mean and invStd as the forward pass kept them.  x and dy: types as x and y above; dx and r:
+ * x's type.  r is the gradient that reaches x past the norm; read only where *beta != 0 (else
+ * rDesc and r may be NULL); dx may be r itself (same descriptor).  scale may be NULL (1), dscale and dshift too
+ * (not computed).  workSpace (device, 16-byte aligned, contents mean nothing): with the bytes
+ * the query reports the sums over the rows are taken in ranges side by side; NULL or less: the
+ * same sums to rounding, slower. */
+igcStatus igcGetLayerNormBackwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                               igcTensorDescriptor_t dyDesc,
+                                               igcTensorDescriptor_t dxDesc, size_t *sizeInBytes);
+igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha,
+                               igcTensorDescriptor_t xDesc, const void *x,
+                               igcTensorDescriptor_t dyDesc, const void *dy,
+                               const void *scale, const void *mean, const void *invStd,
+                               void *workSpace, size_t workSpaceSizeInBytes,
+                               const void *beta, igcTensorDescriptor_t rDesc, const void *r,
+                               igcTensorDescriptor_t dxDesc, void *dx,
+                               const void *paramBeta, void *dscale, void *dshift);
+
+/* Matrix product with bias, activation and residual:
+ *   z = alpha * x w^T + bias,   y = f(z) + beta * r
+ * x: M rows of C, w: filter K x C x 1 x 1, y, z and r: M rows of K.  x and w bfloat16 with y
+ * bfloat16 or float, or all float; z and r have y's type, z is laid out by yDesc.  bias: K
+ * packed floats or NULL; activation: an igcActivationMode or IGC_ACTIVATION_IDENTITY; z: NULL
+ * where it is not kept; f is applied before z is rounded.  r is read only where *beta != 0
+ * (else rDesc and r may be NULL) and may be y itself (same descriptor).  Double:
+ * NOT_SUPPORTED.  workSpace (device, 16-byte aligned, contents mean nothing): as many bytes as
+ * the query reports, or NULL / less: same result to rounding, slower. */
+igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                           igcFilterDescriptor_t wDesc,
+                                           igcTensorDescriptor_t yDesc, size_t *sizeInBytes);
+igcStatus igcLinearForward(igcHandle_t handle, const void *alpha,
+                           igcTensorDescriptor_t xDesc, const void *x,
+                           igcFilterDescriptor_t wDesc, const void *w,
+                           void *workSpace, size_t workSpaceSizeInBytes,
+                           const void *bias, int activation, const void *beta,
+                           igcTensorDescriptor_t rDesc, const void *r,
+                           igcTensorDescriptor_t yDesc, void *z, void *y);
+
+/* Gradient with respect to x, and on through the activation in front of the product:
+ *   dx = alpha * (dy w) * f'(z) + beta * r
+ * dy: M rows of K; dx, z and r: M rows of C; z is what f was applied to (the z that the product
+ * before this one kept).  Types: (dy, w, dx) as (x, w, y) above, z and r as dx.  With
+ * IGC_ACTIVATION_IDENTITY zDesc and z may be NULL, with *beta == 0 rDesc and r; r may be dx
+ * itself (same descriptor).  The rectifier's f' is 1 where z > 0, else 0. */
+igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDescriptor_t wDesc,
+                                                igcTensorDescriptor_t dyDesc,
+                                                igcTensorDescriptor_t dxDesc, size_t *sizeInBytes);
+igcStatus igcLinearBackwardData(igcHandle_t handle, const void *alpha,
+                                igcFilterDescriptor_t wDesc, const void *w,
+                                igcTensorDescriptor_t dyDesc, const void *dy,
+                                void *workSpace, size_t workSpaceSizeInBytes,
+                                int activation, igcTensorDescriptor_t zDesc, const void *z,
+                                const void *beta, igcTensorDescriptor_t rDesc, const void *r,
+                                igcTensorDescriptor_t dxDesc, void *dx);
+
+/* Gradients with respect to w and the bias:
+ *   dw = alpha * dy^T x + beta * dw,   dbias = alpha * (column sums of dy) + beta * dbias
+ * x: M rows of C, dy: M rows of K, dw: filter K x C x 1 x 1, dbias: K packed floats or NULL.
+ * Types: (x, dy, dw) as (x, w, y) above. */
+igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                                  igcTensorDescriptor_t dyDesc,
+                                                  igcFilterDescriptor_t dwDesc, size_t *sizeInBytes);
+igcStatus igcLinearBackwardFilter(igcHandle_t handle, const void *alpha,
+                                  igcTensorDescriptor_t xDesc, const void *x,
+                                  igcTensorDescriptor_t dyDesc, const void *dy,
+                                  void *workSpace, size_t workSpaceSizeInBytes,
+                                  const void *beta, igcFilterDescriptor_t dwDesc, void *dw,
+                                  void *dbias);
 
 /* ---- introspection and tuning (host only; no GPU call) ----------------------------
  * The launch plan the library derives for a problem: the tile of the lowered

@@ -19,11 +19,14 @@ __all__ = [
     "get_backward_filter_workspace_size", "convolution_backward_filter",
     "PoolingDescriptor", "get_pooling_output_dim", "activation_forward", "activation_backward", "add_tensor",
     "softmax_forward", "pooling_forward", "softmax_backward", "pooling_backward", "transform_tensor", "convolution_bias_activation_forward", "IGC_ACTIVATION_IDENTITY",
-    "IGC_ACTIVATION_SIGMOID", "IGC_ACTIVATION_RELU", "IGC_ACTIVATION_TANH", "IGC_SOFTMAX_MODE_INSTANCE",
+    "IGC_ACTIVATION_SIGMOID", "IGC_ACTIVATION_RELU", "IGC_ACTIVATION_TANH", "IGC_ACTIVATION_GELU", "IGC_ACTIVATION_SILU", "IGC_SOFTMAX_MODE_INSTANCE",
     "IGC_SOFTMAX_MODE_CHANNEL", "IGC_POOLING_MAX", "IGC_POOLING_AVERAGE",
     "kernel_names", "magic_divisor", "magic_divide", "tensor_descriptor_for",
     "get_device_properties", "measure_matrix_rate", "measure_matrix_rate_operands", "convolution_backward_filter_no_alloc", "NOALLOC_SCRATCH_BYTES",
     "get_backward_bias_workspace_size", "convolution_backward_bias", "set_compute_units", "get_compute_units", "get_forward_address_reach", "get_backward_data_address_reach",
+    "layer_norm_forward", "get_layer_norm_backward_workspace_size", "layer_norm_backward",
+    "get_linear_forward_workspace_size", "linear_forward", "get_linear_backward_data_workspace_size", "linear_backward_data",
+    "get_linear_backward_filter_workspace_size", "linear_backward_filter",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -34,6 +37,7 @@ LIB_PATH = os.path.join(HERE, "libigconv.so")
 IGC_DATA_FLOAT, IGC_DATA_BFLOAT16, IGC_DATA_DOUBLE = 0, 1, 2
 IGC_CONVOLUTION, IGC_CROSS_CORRELATION = 0, 1
 IGC_ACTIVATION_SIGMOID, IGC_ACTIVATION_RELU, IGC_ACTIVATION_TANH = 0, 1, 2
+IGC_ACTIVATION_GELU, IGC_ACTIVATION_SILU = 3, 4      # of the linear_* functions only
 IGC_ACTIVATION_IDENTITY = -1
 IGC_SOFTMAX_MODE_INSTANCE, IGC_SOFTMAX_MODE_CHANNEL = 0, 1
 IGC_POOLING_MAX, IGC_POOLING_AVERAGE = 0, 1
@@ -92,6 +96,15 @@ DECLARED_SYMBOLS = {
     "igcTransformTensor": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "igcPoolingBackward": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "igcConvolutionBiasActivationForward": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp, _i, _vp, _vp]),
+    "igcLayerNormForward": (_i, [_vp] * 6 + [ctypes.c_double] + [_vp] * 5),
+    "igcGetLayerNormBackwardWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
+    "igcLayerNormBackward": (_i, [_vp] * 10 + [_sz] + [_vp] * 8),
+    "igcGetLinearForwardWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
+    "igcLinearForward": (_i, [_vp] * 7 + [_sz, _vp, _i] + [_vp] * 6),
+    "igcGetLinearBackwardDataWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
+    "igcLinearBackwardData": (_i, [_vp] * 7 + [_sz, _i] + [_vp] * 7),
+    "igcGetLinearBackwardFilterWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
+    "igcLinearBackwardFilter": (_i, [_vp] * 7 + [_sz] + [_vp] * 4),
     "igcGetConvolutionForwardPlan": (_i, [_vp, _vp, _vp, _vp, _vp, _P(igcConvolutionForwardPlan)]),
     "igcGetKernelCount": (_i, []),
     "igcGetKernelName": (ctypes.c_char_p, [_i]),
@@ -408,6 +421,81 @@ def convolution_bias_activation_forward(handle, alpha, xdesc, x_ptr, wdesc, w_pt
     return lib().igcConvolutionBiasActivationForward(
         handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), wdesc.ptr, _vp(w_ptr), conv.ptr, _vp(ws_ptr) if ws_ptr else None,
         ws_bytes, ctypes.byref(b), _vp(bias_ptr), activation, ydesc.ptr, _vp(y_ptr))
+
+
+def _desc_ptr(desc):
+    return None if desc is None else desc.ptr
+
+
+def layer_norm_forward(handle, alpha, xdesc, x_ptr, scale_ptr, shift_ptr, epsilon, beta, ydesc, y_ptr, mean_ptr=0, invstd_ptr=0):
+    """igcLayerNormForward; scale, shift, mean and invstd pointers may be 0."""
+    a, b = _scalars(ydesc, alpha, beta)
+    return lib().igcLayerNormForward(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), _vp(scale_ptr), _vp(shift_ptr), epsilon,
+                                     ctypes.byref(b), ydesc.ptr, _vp(y_ptr), _vp(mean_ptr), _vp(invstd_ptr))
+
+
+def get_layer_norm_backward_workspace_size(handle, xdesc, dydesc, dxdesc):
+    out = _sz()
+    check(lib().igcGetLayerNormBackwardWorkspaceSize(handle.ptr, xdesc.ptr, dydesc.ptr, dxdesc.ptr, ctypes.byref(out)),
+          "igcGetLayerNormBackwardWorkspaceSize")
+    return out.value
+
+
+def layer_norm_backward(handle, alpha, xdesc, x_ptr, dydesc, dy_ptr, scale_ptr, mean_ptr, invstd_ptr, workspace_ptr, workspace_bytes,
+                        beta, rdesc, r_ptr, dxdesc, dx_ptr, param_beta, dscale_ptr, dshift_ptr):
+    """igcLayerNormBackward; rdesc may be None where beta is 0, scale, dscale and dshift pointers may be 0."""
+    a, b = _scalars(dxdesc, alpha, beta)
+    pb = type(a)(param_beta)
+    return lib().igcLayerNormBackward(
+        handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), dydesc.ptr, _vp(dy_ptr), _vp(scale_ptr), _vp(mean_ptr), _vp(invstd_ptr),
+        _vp(workspace_ptr), workspace_bytes, ctypes.byref(b), _desc_ptr(rdesc), _vp(r_ptr), dxdesc.ptr, _vp(dx_ptr), ctypes.byref(pb),
+        _vp(dscale_ptr), _vp(dshift_ptr))
+
+
+def get_linear_forward_workspace_size(handle, xdesc, wdesc, ydesc):
+    out = _sz()
+    check(lib().igcGetLinearForwardWorkspaceSize(handle.ptr, xdesc.ptr, wdesc.ptr, ydesc.ptr, ctypes.byref(out)),
+          "igcGetLinearForwardWorkspaceSize")
+    return out.value
+
+
+def linear_forward(handle, alpha, xdesc, x_ptr, wdesc, w_ptr, workspace_ptr, workspace_bytes, bias_ptr, activation, beta, rdesc, r_ptr,
+                   ydesc, z_ptr, y_ptr):
+    """igcLinearForward; rdesc may be None where beta is 0, bias and z pointers may be 0, activation -1 for none."""
+    a, b = _scalars(ydesc, alpha, beta)
+    return lib().igcLinearForward(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), wdesc.ptr, _vp(w_ptr), _vp(workspace_ptr),
+                                  workspace_bytes, _vp(bias_ptr), activation, ctypes.byref(b), _desc_ptr(rdesc), _vp(r_ptr), ydesc.ptr,
+                                  _vp(z_ptr), _vp(y_ptr))
+
+
+def get_linear_backward_data_workspace_size(handle, wdesc, dydesc, dxdesc):
+    out = _sz()
+    check(lib().igcGetLinearBackwardDataWorkspaceSize(handle.ptr, wdesc.ptr, dydesc.ptr, dxdesc.ptr, ctypes.byref(out)),
+          "igcGetLinearBackwardDataWorkspaceSize")
+    return out.value
+
+
+def linear_backward_data(handle, alpha, wdesc, w_ptr, dydesc, dy_ptr, workspace_ptr, workspace_bytes, activation, zdesc, z_ptr, beta,
+                         rdesc, r_ptr, dxdesc, dx_ptr):
+    """igcLinearBackwardData; zdesc may be None for activation -1, rdesc where beta is 0."""
+    a, b = _scalars(dxdesc, alpha, beta)
+    return lib().igcLinearBackwardData(handle.ptr, ctypes.byref(a), wdesc.ptr, _vp(w_ptr), dydesc.ptr, _vp(dy_ptr), _vp(workspace_ptr),
+                                       workspace_bytes, activation, _desc_ptr(zdesc), _vp(z_ptr), ctypes.byref(b), _desc_ptr(rdesc),
+                                       _vp(r_ptr), dxdesc.ptr, _vp(dx_ptr))
+
+
+def get_linear_backward_filter_workspace_size(handle, xdesc, dydesc, dwdesc):
+    out = _sz()
+    check(lib().igcGetLinearBackwardFilterWorkspaceSize(handle.ptr, xdesc.ptr, dydesc.ptr, dwdesc.ptr, ctypes.byref(out)),
+          "igcGetLinearBackwardFilterWorkspaceSize")
+    return out.value
+
+
+def linear_backward_filter(handle, alpha, xdesc, x_ptr, dydesc, dy_ptr, workspace_ptr, workspace_bytes, beta, dwdesc, dw_ptr, dbias_ptr=0):
+    """igcLinearBackwardFilter; the dbias pointer may be 0."""
+    a, b = _scalars(dwdesc, alpha, beta)
+    return lib().igcLinearBackwardFilter(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), dydesc.ptr, _vp(dy_ptr), _vp(workspace_ptr),
+                                         workspace_bytes, ctypes.byref(b), dwdesc.ptr, _vp(dw_ptr), _vp(dbias_ptr))
 
 
 def kernel_names():

@@ -1,0 +1,117 @@
+// Products of token matrices with their epilogue: launch constants, and the arithmetic after the product.  Internal.
+#ifndef IGCONV_LINEAR_H_
+#define IGCONV_LINEAR_H_
+
+#include "igconv_rows.h"
+
+namespace igc {
+
+// D[m][n] = sum_k A(m,k) B(n,k); element (m,k) of A lies at a + m * am + k * ak, one of the two strides being 1, likewise B.
+//   forward          A = x (rows: tokens, k: features in),        B = w (rows: features out)
+//   backward data    A = dy (rows: tokens, k: features out),      B = w read along its other index (rows: features in)
+//   backward filter  A = dy (rows: features out, k: tokens),      B = x (rows: features in)
+struct LinearArgs {
+    const void *a, *b;
+    long long am, ak, bn, bk;
+    int M, N, K;
+    // after the product: t = alpha D + bias[n]; z[m][n] = t where z is kept; t = f(t) (forward) or t f'(zin[m][n]) (backward
+    // data); y[m][n] = t + beta r[m][n]
+    float alpha, beta;
+    const float *bias;
+    int act;
+    const void *zin;
+    void *z;
+    const void *r;
+    void *y;
+    long long zs, rs, ys;   // elements between rows (z is laid out as y is)
+};
+
+// ---- activations -----------------------------------------------------------------------------------------------------
+// FINE: to float's last digits, for float results.  Otherwise for results that are rounded to bfloat16 (half a step: 2^-9 of
+// the value): the normal distribution function then comes from the polynomial in 1 / (1 + p|v|) of Abramowitz and Stegun
+// (Handbook of Mathematical Functions, 7.1.26: absolute error 1.5e-7), one exponential and one reciprocal instead of the
+// library function's two ranges, since the epilogue's arithmetic does not overlap the matrix instructions of its own wave.
+__device__ __forceinline__ float fast_exp(float v) { return __expf(v); }
+__device__ __forceinline__ float fast_rcp(float v) { return __builtin_amdgcn_rcpf(v); }
+
+// Phi(v) = (1 + erf(v / sqrt 2)) / 2, and exp(-v v / 2) with it
+template <bool FINE>
+__device__ __forceinline__ float normal_cdf(float v, float *bell) {
+    if constexpr (FINE) {
+        *bell = expf(-0.5f * v * v);
+        return 0.5f * erfcf(-v * 0.70710678118654752f);
+    } else {
+        const float e = fast_exp(-0.5f * v * v);
+        const float t = fast_rcp(1.f + 0.3275911f * 0.70710678118654752f * __builtin_fabsf(v));
+        const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+        *bell = e;
+        return v < 0.f ? tail : 1.f - tail;
+    }
+}
+
+template <bool FINE>
+__device__ __forceinline__ float logistic(float v) {
+    if constexpr (FINE) return 1.f / (1.f + expf(-v));
+    else return fast_rcp(1.f + fast_exp(-v));
+}
+
+// v times a factor that is 0 where v is -infinity: the limit, not 0 * infinity
+__device__ __forceinline__ float gated(float v, float factor) { return factor == 0.f ? 0.f : v * factor; }
+
+template <bool FINE>
+__device__ __forceinline__ float activation(int act, float v) {
+    float bell;
+    switch (act) {
+    case IGC_ACTIVATION_SIGMOID: return logistic<FINE>(v);
+    case IGC_ACTIVATION_RELU: return v > 0.f ? v : (v != v ? v : 0.f);
+    case IGC_ACTIVATION_TANH:
+        if constexpr (FINE) return tanhf(v);
+        else   // (close to 0 the difference would lose v's digits: two terms of the series)
+            return __builtin_fabsf(v) < 0.03f ? v * (1.f - v * v * (1.f / 3.f)) : 1.f - 2.f * fast_rcp(1.f + fast_exp(2.f * v));
+    case IGC_ACTIVATION_GELU: return gated(v, normal_cdf<FINE>(v, &bell));
+    case IGC_ACTIVATION_SILU: return gated(v, logistic<FINE>(v));
+    default: return v;
+    }
+}
+
+template <bool FINE>
+__device__ __forceinline__ float activation_slope(int act, float v) {
+    float bell;
+    switch (act) {
+    case IGC_ACTIVATION_SIGMOID: {
+        // e / (1 + e)^2 with e = exp(-|v|): s (1 - s) would lose the digits of 1 - s
+        const float e = FINE ? expf(-__builtin_fabsf(v)) : fast_exp(-__builtin_fabsf(v)), d = 1.f / (1.f + e);
+        return e * d * d;
+    }
+    case IGC_ACTIVATION_RELU: return v > 0.f ? 1.f : 0.f;
+    case IGC_ACTIVATION_TANH: {
+        const float e = FINE ? expf(-2.f * __builtin_fabsf(v)) : fast_exp(-2.f * __builtin_fabsf(v)), d = 1.f / (1.f + e);
+        return 4.f * e * d * d;
+    }
+    case IGC_ACTIVATION_GELU: {
+        const float cdf = normal_cdf<FINE>(v, &bell);
+        return cdf + gated(v, bell * 0.39894228040143268f);
+    }
+    case IGC_ACTIVATION_SILU: {
+        const float s = logistic<FINE>(v);
+        return s + gated(v, s * (1.f - s));
+    }
+    default: return 1.f;
+    }
+}
+
+// one result, element by element (the kernels that hold several neighbours of a row store them together)
+template <class TO>
+__device__ __forceinline__ void finish_element(const LinearArgs &a, int m, int n, float d) {
+    constexpr bool FINE = sizeof(TO) == 4;
+    float v = a.alpha * d;
+    if (a.bias) v += a.bias[n];
+    if (a.z) static_cast<TO *>(a.z)[m * a.zs + n] = Stored<TO>::narrow(v);
+    if (a.zin) v *= activation_slope<FINE>(a.act, Stored<TO>::widen(static_cast<const TO *>(a.zin)[m * a.zs + n]));
+    else v = activation<FINE>(a.act, v);
+    if (a.beta != 0.f) v += a.beta * Stored<TO>::widen(static_cast<const TO *>(a.r)[m * a.rs + n]);
+    static_cast<TO *>(a.y)[m * a.ys + n] = Stored<TO>::narrow(v);
+}
+
+}  // namespace igc
+#endif
