@@ -26,6 +26,31 @@ struct LinearArgs {
     long long zs, rs, ys;   // elements between rows (z is laid out as y is)
 };
 
+constexpr int kTileStep = 64;                     // reduction indices per step
+constexpr int kMaxPairs = 6;
+
+struct TileArgs : LinearArgs {
+    int tilesM, tilesN, group;     // tiles are taken `group` rows of tiles at a time
+    int tilesPerXcd;
+    int splits, stepsPerSplit;     // the reduction in ranges of steps
+    float *parts;                  // [split][M][partsRow] (partsRow: N rounded up to 8), where splits > 1
+    long long partsRow;
+    int vec;                       // the epilogue's matrices allow 16-byte accesses at every eighth column
+    // the operands' parts: the products of a pair of parts are summed one after the other
+    int pairs;
+    long long planeA[kMaxPairs], planeB[kMaxPairs];   // elements
+};
+
+// Tile shapes of linear_tiles_kernel (igconv_linear_tiles.hpp).  sa, sb: the operand's reduction index runs along its rows.
+struct TileKernel {
+    int bm, bn, threads;
+    const void *kernel;
+};
+constexpr int kTileShapes = 2;
+TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent
+TileKernel tile_kernel_rows_columns(int shape, bool f32_out);  // backward data: B strided
+TileKernel tile_kernel_columns(int shape, bool f32_out);       // backward filter: both strided
+
 // ---- activations -----------------------------------------------------------------------------------------------------
 // FINE: to float's last digits, for float results.  Otherwise for results that are rounded to bfloat16 (half a step: 2^-9 of
 // the value): the normal distribution function then comes from the polynomial in 1 / (1 + p|v|) of Abramowitz and Stegun
@@ -97,6 +122,20 @@ __device__ __forceinline__ float activation_slope(int act, float v) {
         return s + gated(v, s * (1.f - s));
     }
     default: return 1.f;
+    }
+}
+
+// f(the activation as a constant): one branch for several elements
+template <int V> struct Constant { static constexpr int value = V; };
+template <class F>
+__device__ __forceinline__ void by_activation(int act, F f) {
+    switch (act) {
+    case IGC_ACTIVATION_SIGMOID: f(Constant<IGC_ACTIVATION_SIGMOID>()); break;
+    case IGC_ACTIVATION_RELU: f(Constant<IGC_ACTIVATION_RELU>()); break;
+    case IGC_ACTIVATION_TANH: f(Constant<IGC_ACTIVATION_TANH>()); break;
+    case IGC_ACTIVATION_GELU: f(Constant<IGC_ACTIVATION_GELU>()); break;
+    case IGC_ACTIVATION_SILU: f(Constant<IGC_ACTIVATION_SILU>()); break;
+    default: break;
     }
 }
 

@@ -5,7 +5,7 @@
 //   backward filter  dw = alpha dy^T x + beta dw,  dbias = alpha (column sums of dy) + beta dbias
 //
 // Products of bfloat16 are accumulated in fp32 by the matrix instructions, in a fixed order.
-#include "igconv_linear.h"
+#include "igconv_linear_tiles.hpp"
 
 namespace igc {
 namespace {
@@ -16,7 +16,6 @@ namespace {
 constexpr int kAnyTile = 64, kAnyStep = 32;
 
 using f32x16 = float __attribute__((ext_vector_type(16)));
-using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 
 template <class T> struct AnyTile;
 template <> struct AnyTile<float> {
@@ -164,13 +163,131 @@ igcStatus check_beside(igcTensorDescriptor_t out, igcTensorDescriptor_t d, const
     return IGC_STATUS_SUCCESS;
 }
 
-igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a) {
+// ---- the sum of the ranges' parts, with the epilogue --------------------------------------------------------------------
+// a thread per eight neighbours of a row
+template <class TO>
+__global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
+    const long long groups = p.partsRow / 8, id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)(id / groups), n = (int)(id % groups) * 8;
+    if (m >= p.M) return;
+    Eight d = load8<float>(p.parts, (long long)m * p.partsRow + n);
+    for (int s = 1; s < p.splits; ++s) {
+        const Eight q = load8<float>(p.parts, ((long long)s * p.M + m) * p.partsRow + n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d.v[e] += q.v[e];
+    }
+    Eight bias;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias.v[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.f;
+    if (p.vec && n + 8 <= p.N) {
+        finish8<TO>(p, m, n, d, bias);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (n + e < p.N) finish_element<TO>(p, m, n + e, d.v[e]);
+    }
+}
+
+// ---- the choice of a tile and of the ranges -------------------------------------------------------------------------------
+struct TilePlan {
+    bool tiles = false;      // (else the kernel for any layout)
+    TileKernel k{};
+    int tilesM = 0, tilesN = 0, splits = 1, stepsPerSplit = 0;
+    size_t bytes = 0;        // of workspace: the ranges' parts
+};
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
+    return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
+}
+
+// rows on 16-byte boundaries, whole 16-byte pieces, a tile's or step's reach within 31 bits
+bool tile_operand(long long rows, long long cols, long long stride) {
+    return cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride >= cols)) && stride < (1ll << 22);
+}
+
+TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, size_t room) {
+    TilePlan best;
+    if (in != IGC_DATA_BFLOAT16) return best;
+    const bool sa = a.ak != 1, sb = a.bk != 1;
+    if (!(sa ? tile_operand(a.K, a.M, a.ak) : tile_operand(a.M, a.K, a.am)) || !(sb ? tile_operand(a.K, a.N, a.bk) : tile_operand(a.N, a.K, a.bn))) return best;
+    const int steps = (a.K + kTileStep - 1) / kTileStep;
+    double cost = 1e300;
+    for (int shape = 0; shape < kTileShapes; ++shape) {
+        const TileKernel k = tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT);
+        const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn, at_once = h->computeUnits * (shape == 0 ? 1 : 2);
+        for (int splits = 1; splits <= 32 && splits * 4 <= std::max(steps, 4); ++splits) {
+            const int per = (steps + splits - 1) / splits;
+            if ((steps + per - 1) / per != splits) continue;
+            const size_t bytes = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0;
+            if (bytes > room) break;
+            const double rounds = (double)((tm * tn * splits + at_once - 1) / at_once);
+            const double c = rounds * (per + 6) * (shape == 0 ? 1.0 : 0.62) + (splits > 1 ? 4.0 + (double)bytes * 2 / 4e6 : 0.0);
+            if (c < cost) {
+                cost = c;
+                best.tiles = true;
+                best.k = k;
+                best.tilesM = (int)tm; best.tilesN = (int)tn; best.splits = splits; best.stepsPerSplit = per; best.bytes = bytes;
+            }
+        }
+    }
+    return best;
+}
+
+bool on16(const void *p) { return (uintptr_t)p % 16 == 0; }
+
+igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes) {
+    if (on16(a.a) && on16(a.b)) {
+        const TilePlan pl = plan_tiles(handle, in, out, a, workSpace && on16(workSpace) ? bytes : 0);
+        if (pl.tiles) {
+            TileArgs t{};
+            static_cast<LinearArgs &>(t) = a;
+            t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
+            t.group = std::min(pl.tilesM, 4);
+            t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
+            const long long units = (long long)pl.tilesM * pl.tilesN * pl.splits;
+            t.tilesPerXcd = (int)((units + 7) / 8);
+            t.parts = static_cast<float *>(workSpace);
+            t.partsRow = round_up(a.N, 8);
+            const long long per16 = 16 / elem_size(out);
+            t.vec = on16(a.y) && a.ys % per16 == 0 && (!a.z || on16(a.z)) && (!a.zin || (on16(a.zin) && a.zs % per16 == 0)) &&
+                    (a.beta == 0.f || (on16(a.r) && a.rs % per16 == 0));
+            t.pairs = 1;
+            const igcStatus rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+            if (rc != IGC_STATUS_SUCCESS || pl.splits == 1) return rc;
+            const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
+                                                    : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
+            return launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
+        }
+    }
     const long long tiles = (long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile);
     if (tiles >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
     return by_types(in, out, [&](auto ti, auto to) {
         return launch_kernel(reinterpret_cast<const void *>(&linear_any_kernel<decltype(ti), decltype(to)>), a, dim3((unsigned)tiles), 256, handle->stream);
     });
 }
+
+// the passes as D[m][n] = sum_k A(m,k) B(n,k)
+LinearArgs forward_sizes(const Matrix &x, const igcFilterStruct &w) {
+    LinearArgs a{};
+    a.am = x.stride; a.ak = 1; a.bn = w.c; a.bk = 1;
+    a.M = (int)x.rows; a.N = w.k; a.K = w.c;
+    return a;
+}
+LinearArgs backward_data_sizes(const Matrix &dy, const igcFilterStruct &w) {
+    LinearArgs a{};
+    a.am = dy.stride; a.ak = 1; a.bn = 1; a.bk = w.c;
+    a.M = (int)dy.rows; a.N = w.c; a.K = w.k;
+    return a;
+}
+LinearArgs backward_filter_sizes(const Matrix &x, const Matrix &dy, const igcFilterStruct &dw) {
+    LinearArgs a{};
+    a.am = 1; a.ak = dy.stride; a.bn = 1; a.bk = x.stride;
+    a.M = dw.k; a.N = dw.c; a.K = (int)x.rows;
+    return a;
+}
+constexpr size_t kNoLimit = ~(size_t)0;
 
 }  // namespace
 }  // namespace igc
@@ -185,7 +302,7 @@ igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescript
     Matrix x, y;
     const igcStatus st = check_linear(xDesc, wDesc, yDesc, false, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = 0;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -196,22 +313,21 @@ igcStatus igcLinearForward(igcHandle_t handle, const void *alpha, igcTensorDescr
     Matrix mx, my, mr;
     igcStatus st = check_linear(xDesc, wDesc, yDesc, false, &mx, &my);
     if (st != IGC_STATUS_SUCCESS) return st;
-    LinearArgs a{};
+    LinearArgs a = forward_sizes(mx, *wDesc);
     a.alpha = *static_cast<const float *>(alpha);
     a.beta = *static_cast<const float *>(beta);
     if (a.beta != 0.f && (st = check_beside(yDesc, rDesc, r, &mr)) != IGC_STATUS_SUCCESS) return st;
     if (misaligned(x, xDesc->dtype) || misaligned(w, wDesc->dtype) || misaligned(y, yDesc->dtype) || misaligned(z, yDesc->dtype) ||
         misaligned(bias, IGC_DATA_FLOAT))
         return IGC_STATUS_BAD_PARAM;
-    a.a = x; a.am = mx.stride; a.ak = 1;
-    a.b = w; a.bn = wDesc->c; a.bk = 1;
-    a.M = (int)mx.rows; a.N = wDesc->k; a.K = wDesc->c;
+    a.a = x;
+    a.b = w;
     a.bias = static_cast<const float *>(bias);
     a.act = activation;
     a.z = z; a.zs = my.stride;
     a.r = r; a.rs = mr.stride;
     a.y = y; a.ys = my.stride;
-    return run_product(handle, xDesc->dtype, yDesc->dtype, a);
+    return run_product(handle, xDesc->dtype, yDesc->dtype, a, workSpace, workSpaceSizeInBytes);
 }
 
 igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDescriptor_t wDesc, igcTensorDescriptor_t dyDesc,
@@ -220,7 +336,7 @@ igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDes
     Matrix dy, dx;
     const igcStatus st = check_linear(dyDesc, wDesc, dxDesc, true, &dy, &dx);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = 0;
+    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -232,21 +348,20 @@ igcStatus igcLinearBackwardData(igcHandle_t handle, const void *alpha, igcFilter
     Matrix mdy, mdx, mz, mr;
     igcStatus st = check_linear(dyDesc, wDesc, dxDesc, true, &mdy, &mdx);
     if (st != IGC_STATUS_SUCCESS) return st;
-    LinearArgs a{};
+    LinearArgs a = backward_data_sizes(mdy, *wDesc);
     a.alpha = *static_cast<const float *>(alpha);
     a.beta = *static_cast<const float *>(beta);
     const bool slope = activation != IGC_ACTIVATION_IDENTITY;
     if (slope && (st = check_beside(dxDesc, zDesc, z, &mz)) != IGC_STATUS_SUCCESS) return st;
     if (a.beta != 0.f && (st = check_beside(dxDesc, rDesc, r, &mr)) != IGC_STATUS_SUCCESS) return st;
     if (misaligned(w, wDesc->dtype) || misaligned(dy, dyDesc->dtype) || misaligned(dx, dxDesc->dtype)) return IGC_STATUS_BAD_PARAM;
-    a.a = dy; a.am = mdy.stride; a.ak = 1;
-    a.b = w; a.bn = 1; a.bk = wDesc->c;
-    a.M = (int)mdy.rows; a.N = wDesc->c; a.K = wDesc->k;
+    a.a = dy;
+    a.b = w;
     a.act = activation;
     a.zin = slope ? z : nullptr; a.zs = mz.stride;
     a.r = r; a.rs = mr.stride;
     a.y = dx; a.ys = mdx.stride;
-    return run_product(handle, dyDesc->dtype, dxDesc->dtype, a);
+    return run_product(handle, dyDesc->dtype, dxDesc->dtype, a, workSpace, workSpaceSizeInBytes);
 }
 
 igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc, igcTensorDescriptor_t dyDesc,
@@ -255,7 +370,7 @@ igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorD
     Matrix x, dy;
     const igcStatus st = check_linear_filter(xDesc, dyDesc, dwDesc, &x, &dy);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = 0;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -268,16 +383,15 @@ igcStatus igcLinearBackwardFilter(igcHandle_t handle, const void *alpha, igcTens
     if (st != IGC_STATUS_SUCCESS) return st;
     if (misaligned(x, xDesc->dtype) || misaligned(dy, dyDesc->dtype) || misaligned(dw, dwDesc->dtype) || misaligned(dbias, IGC_DATA_FLOAT))
         return IGC_STATUS_BAD_PARAM;
-    LinearArgs a{};
+    LinearArgs a = backward_filter_sizes(mx, mdy, *dwDesc);
     a.alpha = *static_cast<const float *>(alpha);
     a.beta = *static_cast<const float *>(beta);
-    a.a = dy; a.am = 1; a.ak = mdy.stride;
-    a.b = x; a.bn = 1; a.bk = mx.stride;
-    a.M = dwDesc->k; a.N = dwDesc->c; a.K = (int)mx.rows;
+    a.a = dy;
+    a.b = x;
     a.act = IGC_ACTIVATION_IDENTITY;
     a.r = dw; a.rs = dwDesc->c;
     a.y = dw; a.ys = dwDesc->c;
-    const igcStatus rc = run_product(handle, xDesc->dtype, dwDesc->dtype, a);
+    const igcStatus rc = run_product(handle, xDesc->dtype, dwDesc->dtype, a, workSpace, workSpaceSizeInBytes);
     if (rc != IGC_STATUS_SUCCESS || !dbias) return rc;
     ColumnArgs c{dy, mdy.stride, (int)mdy.rows, dwDesc->k, a.alpha, a.beta, static_cast<float *>(dbias)};
     const dim3 grid((unsigned)(c.K + 63) / 64u);

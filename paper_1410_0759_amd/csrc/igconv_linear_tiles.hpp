@@ -1,0 +1,312 @@
+// Products of bfloat16 matrices whose rows lie on 16-byte boundaries (igconv_linear.h; the float ones run over bfloat16 parts).
+//
+// A workgroup computes a BM x BN tile in steps of 64 of the reduction; a wavefront of it WM x WN results with
+// v_mfma_f32_16x16x32_bf16.  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), one step
+// into each of two stages.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
+// read 16 bytes per lane; one whose reduction index runs along the rows (w for backward data, x and dy for backward filter)
+// lies there as it is, k by k, and is read with the transposing 8-byte reads - no operand is transposed in memory.  In both cases
+// the 16-byte (32-byte) pieces of a row are permuted by an exclusive or with the row's number so that the lanes of a read lie
+// in different banks; the permutation is made on the global side of the copy, whose LDS side is fixed.
+//
+// A step is 2 x FM slots of FN matrix instructions.  Fragments of the first operand are read two slots ahead, those of the
+// second half a step ahead.  Two slots before the end every read of the stage has been requested: the wavefronts meet at
+// the step's only barrier, the stage is given to the copies of the step after next, and the remaining matrix instructions cover
+// the first reads of the other stage.
+#ifndef IGCONV_LINEAR_TILES_HPP_
+#define IGCONV_LINEAR_TILES_HPP_
+
+#include "igconv_linear.h"
+
+namespace igc {
+
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using i16x4 = short __attribute__((ext_vector_type(4)));
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kNowhere = 0x80000000u;        // an offset outside every buffer: the load brings zeros
+
+// One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand.
+// STRIDED: the reduction index runs along the rows of the matrix in memory (`stride` elements apart), the tile's rows are adjacent.
+template <int ROWS, int WAVES, bool STRIDED>
+struct OperandCopy {
+    static constexpr int REQUESTS = ROWS / 8 / WAVES;      // of 1 KB per wavefront and step
+    static constexpr int PIECES = ROWS / 8;                // (strided) 16-byte pieces of a k row
+    static constexpr int KROWS = 64 / PIECES;              // (strided) k rows per request
+    const uint16_t *base;
+    long long left;             // elements from `base` to the end of the operand
+    uint32_t stride_bytes, first;
+    int k_piece;                // (not strided) the lane's first reduction index within a step
+
+    // (strided) the exclusive or of the 32-byte blocks of k row k
+    static __device__ __forceinline__ int twist(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
+
+    __device__ __forceinline__ void init(const void *matrix, long long row_stride, long long k_stride, int row0, int rows, int K, int lane, int wave) {
+        if constexpr (STRIDED) {
+            base = static_cast<const uint16_t *>(matrix) + row0;
+            left = (K - 1) * k_stride + (rows - row0);
+            stride_bytes = (uint32_t)k_stride * 2u;
+            const int k = lane / PIECES, at = lane % PIECES;
+            k_piece = wave * REQUESTS * KROWS + k;       // (the k row of the first request)
+            first = at;
+        } else {
+            base = static_cast<const uint16_t *>(matrix) + row0 * row_stride;
+            left = (rows - row0 - 1) * row_stride + K;
+            stride_bytes = (uint32_t)row_stride * 2u;
+            const int row = lane >> 3, piece = (lane & 7) ^ row;
+            first = (uint32_t)(wave * REQUESTS * 8 + row) * stride_bytes + piece * 16u;
+            k_piece = piece * 8;
+        }
+    }
+
+    // requests the step that begins at reduction index k (of K) of the part `plane` elements further on
+    __device__ __forceinline__ void request(uint8_t *stage, int wave, int k, int K, long long plane) const {
+        const long long skip = plane + (STRIDED ? (long long)k * (stride_bytes / 2u) : 0);
+        const long long bytes = (left - (skip - plane)) * 2;
+        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + skip), 0,
+                                                                            (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll), 0x00020000u);
+        uint8_t *to = stage + wave * REQUESTS * 1024;
+#pragma unroll
+        for (int i = 0; i < REQUESTS; ++i) {
+            uint32_t off;
+            if constexpr (STRIDED) {
+                const int kr = k_piece + i * KROWS;
+                off = (uint32_t)kr * stride_bytes + (first ^ (uint32_t)(twist(kr) << 1)) * 16u;
+            } else {
+                off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * 2u : kNowhere;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(to + i * 1024), 16, off, 0, 0, 0);
+        }
+    }
+};
+
+// One operand's fragments: F of them, 16 rows each, from row `row0` of the tile on.
+template <int ROWS, int F, bool STRIDED>
+struct OperandReads {
+    uint32_t at[STRIDED ? F : 2];
+    __device__ __forceinline__ void init(int row0, int lane) {
+        const int l16 = lane & 15, g = lane >> 4;
+        if constexpr (STRIDED) {
+            const int r = l16 >> 2, twist = r | (g & 1) << 2;
+#pragma unroll
+            for (int i = 0; i < F; ++i) at[i] = (uint32_t)((8 * g + r) * ROWS * 2 + (((row0 >> 4) + i) ^ twist) * 32 + (l16 & 3) * 8);
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) at[kk] = (uint32_t)((row0 + l16) * 128 + ((g + 4 * kk) ^ (l16 & 7)) * 16);
+        }
+    }
+    // fragment i of the step's half kk
+    __device__ __forceinline__ bf16x8 read(const uint8_t *stage, int kk, int i) const {
+        if constexpr (STRIDED) {
+            typedef __attribute__((address_space(3))) i16x4 *lds4;
+            const uint8_t *p = stage + at[i] + kk * 32 * ROWS * 2;
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p);
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * ROWS * 2));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *reinterpret_cast<const bf16x8 *>(stage + at[kk] + i * 2048);
+        }
+    }
+};
+
+// eight neighbours of a row
+struct Eight {
+    float v[8];
+};
+template <class TO>
+__device__ __forceinline__ Eight load8(const void *p, long long at) {
+    Eight r;
+    if constexpr (sizeof(TO) == 4) {
+        const f32x4 *q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at);
+        const f32x4 lo = q[0], hi = q[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = lo[e], r.v[4 + e] = hi[e];
+    } else {
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[2 * e] = bf16_bits_to_float(q[e]), r.v[2 * e + 1] = __builtin_bit_cast(float, q[e] & 0xFFFF0000u);
+    }
+    return r;
+}
+template <class TO>
+__device__ __forceinline__ void store8(void *p, long long at, const Eight &r) {
+    if constexpr (sizeof(TO) == 4) {
+        f32x4 *q = reinterpret_cast<f32x4 *>(static_cast<float *>(p) + at);
+        q[0] = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+        q[1] = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+    } else {
+        u32x4 q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = to_bf16_bits(r.v[2 * e]) | (uint32_t)to_bf16_bits(r.v[2 * e + 1]) << 16;
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = q;
+    }
+}
+// finish_element for eight results at once; the matrices allow 16-byte accesses there
+template <class TO>
+__device__ __forceinline__ void finish8(const LinearArgs &a, int m, int n, Eight d, const Eight &bias) {
+    constexpr bool FINE = sizeof(TO) == 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d.v[e] = a.alpha * d.v[e] + bias.v[e];
+    if (a.z) store8<TO>(a.z, m * a.zs + n, d);
+    if (a.zin) {
+        const Eight z = load8<TO>(a.zin, m * a.zs + n);
+        by_activation(a.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d.v[e] *= activation_slope<FINE>(decltype(act)::value, z.v[e]);
+        });
+    } else {
+        by_activation(a.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d.v[e] = activation<FINE>(decltype(act)::value, d.v[e]);
+        });
+    }
+    if (a.beta != 0.f) {
+        const Eight r = load8<TO>(a.r, m * a.rs + n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d.v[e] += a.beta * r.v[e];
+    }
+    store8<TO>(a.y, m * a.ys + n, d);
+}
+
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool SA_, bool SB_>
+struct TileConfig {
+    static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N;
+    static constexpr bool SA = SA_, SB = SB_;
+    static constexpr int FM = BM / WAVES_M / 16, FN = BN / WAVES_N / 16;
+    static constexpr int STAGE_BYTES = (BM + BN) * kTileStep * 2, LDS_BYTES = 2 * STAGE_BYTES;
+    static constexpr int THREADS = 64 * WAVES;
+};
+
+__device__ __forceinline__ bool tile_of(const TileArgs &p, int *tm, int *tn, int *split) {
+    const int tiles = p.tilesM * p.tilesN, unit = (int)(blockIdx.x & 7u) * p.tilesPerXcd + (int)(blockIdx.x >> 3);
+    if (unit >= tiles * p.splits) return false;
+    *split = unit / tiles;
+    const int t = unit - *split * tiles, width = p.group * p.tilesN, g = t / width, first = g * p.group;
+    const int rows = p.tilesM - first < p.group ? p.tilesM - first : p.group, in = t - g * width;
+    *tm = first + in % rows;
+    *tn = in / rows;
+    return true;
+}
+
+template <class Cfg, class TO>
+__global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const TileArgs p) {
+    constexpr int BM = Cfg::BM, BN = Cfg::BN, FM = Cfg::FM, FN = Cfg::FN, SLOTS = 2 * FM;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[Cfg::LDS_BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / Cfg::WAVES_N, wn = wave % Cfg::WAVES_N;
+    int tm, tn, split;
+    if (!tile_of(p, &tm, &tn, &split)) return;
+    const int m0 = tm * BM, n0 = tn * BN;
+    OperandCopy<BM, Cfg::WAVES, Cfg::SA> copyA;
+    OperandCopy<BN, Cfg::WAVES, Cfg::SB> copyB;
+    copyA.init(p.a, p.am, p.ak, m0, p.M, p.K, lane, wave);
+    copyB.init(p.b, p.bn, p.bk, n0, p.N, p.K, lane, wave);
+    OperandReads<BM, FM, Cfg::SA> readA;
+    OperandReads<BN, FN, Cfg::SB> readB;
+    readA.init(wm * FM * 16, lane);
+    readB.init(wn * FN * 16, lane);
+
+    const int kBegin = split * p.stepsPerSplit * kTileStep;
+    const int kEnd = min(p.K, kBegin + p.stepsPerSplit * kTileStep);
+    const int steps = p.pairs * ((kEnd - kBegin + kTileStep - 1) / kTileStep);
+    int k = kBegin, pair = 0;       // of the next request
+    long long planeA = p.planeA[0], planeB = p.planeB[0];
+    auto request = [&](int stage) __attribute__((always_inline)) {
+        if (pair >= p.pairs) return;
+        uint8_t *to = lds + stage * Cfg::STAGE_BYTES;
+        copyA.request(to, wave, k, kEnd, planeA);
+        copyB.request(to + BM * 128, wave, k, kEnd, planeB);
+        k += kTileStep;
+        if (k >= kEnd) {
+            k = kBegin;
+            if (++pair < p.pairs) {
+                planeA = p.planeA[pair];
+                planeB = p.planeB[pair];
+            }
+        }
+    };
+    auto arrived = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);      // the copies have landed
+        asm volatile("s_barrier" ::: "memory");
+    };
+
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    request(0);
+    arrived();
+    request(1);
+    bf16x8 a[4], b[2][FN];
+    a[0] = readA.read(lds, 0, 0);
+    a[1] = readA.read(lds, 0, 1);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) b[0][j] = readB.read(lds + BM * 128, 0, j);
+
+    int cur = 0;
+    for (int s = 0; s < steps; ++s) {
+        const uint8_t *stage = lds + cur * Cfg::STAGE_BYTES, *next = lds + (cur ^ 1) * Cfg::STAGE_BYTES;
+#pragma unroll
+        for (int t = 0; t < SLOTS; ++t) {
+            if (t == SLOTS - 2) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);   // this wavefront's reads of the stage are done
+                arrived();
+                request(cur);
+            }
+            if (t + 2 < SLOTS) a[(t + 2) % 4] = readA.read(stage, (t + 2) / FM, (t + 2) % FM);
+            else a[(t + 2) % 4] = readA.read(next, 0, t + 2 - SLOTS);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                if (t < FM && t >= FM - FN && j == t - (FM - FN)) b[1][j] = readB.read(stage + BM * 128, 1, j);
+                if (t >= SLOTS - 2 && j / ((FN + 1) / 2) == t - (SLOTS - 2)) b[0][j] = readB.read(next + BM * 128, 0, j);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[t % FM][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[t / FM][j], a[t % 4], acc[t % FM][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        cur ^= 1;
+    }
+
+    // Lane l holds row 16 i + l % 16, columns 16 j + 4 (l / 16) + 0..3 of the wavefront's results.  They go through the wavefront's share of
+    // the LDS (its 16-byte pieces permuted within a row by the row's number), PASS_ROWS rows at a time, so that eight lanes write 128 or 256
+    // adjacent bytes of a row of y.
+    __syncthreads();   // (every read and every copy is done: the last request was waited for)
+    constexpr int WN = FN * 16, PIECES = WN / 4;
+    constexpr int PASS_FRAGS = Cfg::LDS_BYTES / Cfg::WAVES / (16 * WN * 4) < FM ? Cfg::LDS_BYTES / Cfg::WAVES / (16 * WN * 4) : FM;
+    constexpr int PASSES = FM / PASS_FRAGS, LANES = WN / 8, AT_ONCE = 64 / LANES;
+    static_assert(PASSES * PASS_FRAGS == FM, "whole passes");
+    f32x4 *mine = reinterpret_cast<f32x4 *>(lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES));
+    const int l16 = lane & 15, g = lane >> 4, c8 = lane % LANES, n = n0 + wn * WN + c8 * 8;
+    Eight bias;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias.v[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.f;
+    for (int pass = 0; pass < PASSES; ++pass) {
+        // (which accumulators is known at compile time: an index into registers)
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q)
+            if (pass == q)
+#pragma unroll
+                for (int i = 0; i < PASS_FRAGS; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) mine[(i * 16 + l16) * PIECES + ((j * 4 + g) ^ (l16 & (PIECES - 1)))] = acc[q * PASS_FRAGS + i][j];
+        __builtin_amdgcn_wave_barrier();
+        for (int r = lane / LANES; r < PASS_FRAGS * 16; r += AT_ONCE) {
+            const int m = m0 + (wm * FM + pass * PASS_FRAGS) * 16 + r;
+            const f32x4 lo = mine[r * PIECES + ((2 * c8) ^ (r & 15 & (PIECES - 1)))], hi = mine[r * PIECES + ((2 * c8 + 1) ^ (r & 15 & (PIECES - 1)))];
+            if (m >= p.M || n >= p.N) continue;
+            const Eight d = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (p.splits > 1) store8<float>(p.parts, ((long long)split * p.M + m) * p.partsRow + n, d);
+            else if (p.vec && n + 8 <= p.N) finish8<TO>(p, m, n, d, bias);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < p.N) finish_element<TO>(p, m, n + e, d.v[e]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+}  // namespace igc
+#endif
