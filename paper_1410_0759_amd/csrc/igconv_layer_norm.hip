@@ -9,6 +9,8 @@
 //
 // The deviations are taken from the finished mean (a difference of a sum of squares and a squared sum would lose the digits of
 // rows whose mean is large against their spread).  Sums are held in float, in double for double tensors, in a fixed order.
+#include <type_traits>
+
 #include "igconv_rows.h"
 
 namespace igc {
@@ -20,7 +22,7 @@ struct NormArgs {
     void *y;
     W *mean, *invstd;
     long long xs, ys;   // elements between rows
-    int C;
+    int M, C;
     W alpha, beta, epsilon;
 };
 
@@ -36,17 +38,10 @@ struct NormBackwardArgs {
     W alpha, beta, paramBeta;
 };
 
-template <class W>
-__device__ __forceinline__ W wave_sum(W v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-
 // sum over a workgroup of 256 threads, given to all; `slots`: four entries that nothing else uses until the next barrier
 template <class W>
 __device__ __forceinline__ W group_sum(W v, W *slots) {
-    v = wave_sum(v);
+    v = lanes_sum<64>(v);
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
     return (slots[0] + slots[1]) + (slots[2] + slots[3]);
@@ -133,21 +128,24 @@ __global__ __launch_bounds__(256) void layer_norm_params_kernel(const NormBackwa
     }
 }
 
-// adds the ranges' sums in order; without ranges takes the sums over all rows itself
+// Adds the ranges' sums in order; without ranges takes the sums over all rows itself: lanes along 32 feature maps, 32 rows at a time (a range per
+// line and round: with eight lines the 188 ranges of 3001 x 777 were six rounds of waits, 14.2 us in all, so 13.7).
 template <class TX, class TY>
-__global__ __launch_bounds__(256) void layer_norm_params_sum_kernel(const NormBackwardArgs<typename Stored<TX>::wide_t> a) {
+__global__ __launch_bounds__(1024) void layer_norm_params_sum_kernel(const NormBackwardArgs<typename Stored<TX>::wide_t> a) {
     typedef typename Stored<TX>::wide_t W;
-    __shared__ W sums[2][4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
+    constexpr int LINES = 32;
+    __shared__ W sums[2][LINES][32];
+    const int lane = threadIdx.x & 31, line = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + lane;
     W scale = W(0), shift = W(0);
     if (c < a.C) {
         if (a.parts) {
-            for (int r = wave; r < a.ranges; r += 4) {
+#pragma unroll 4
+            for (int r = line; r < a.ranges; r += LINES) {
                 scale += a.parts[(size_t)r * 2 * a.C + c];
                 shift += a.parts[((size_t)r * 2 + 1) * a.C + c];
             }
         } else {
-            for (int i = wave; i < a.M; i += 4) {
+            for (int i = line; i < a.M; i += LINES) {
                 const W dy = Stored<TY>::widen(static_cast<const TY *>(a.dy)[i * a.dys + c]);
                 const W h = (Stored<TX>::widen(static_cast<const TX *>(a.x)[i * a.xs + c]) - a.mean[i]) * a.invstd[i];
                 shift += dy;
@@ -155,15 +153,311 @@ __global__ __launch_bounds__(256) void layer_norm_params_sum_kernel(const NormBa
             }
         }
     }
-    sums[0][wave][lane] = scale;
-    sums[1][wave][lane] = shift;
+    sums[0][line][lane] = scale;
+    sums[1][line][lane] = shift;
     __syncthreads();
-    W *out = wave == 0 ? a.dscale : a.dshift;
-    if (wave < 2 && c < a.C && out) {
-        const W *s = &sums[wave][0][lane];
-        W v = a.alpha * ((s[0] + s[64]) + (s[128] + s[192]));
+    W *out = line == 0 ? a.dscale : a.dshift;
+    if (line < 2 && c < a.C && out) {
+        W v = W(0);
+#pragma unroll
+        for (int i = 0; i < LINES; ++i) v += sums[line][i][lane];
+        v *= a.alpha;
         if (a.paramBeta != W(0)) v += a.paramBeta * out[c];
         out[c] = v;
+    }
+}
+
+// ---- rows that fit into registers ---------------------------------------------------------------------------------------
+// LANES threads (a wavefront or a workgroup) share a row: thread t holds the chunks t, t + LANES, ... of E neighbours, CHUNKS of them at
+// most, so that a row is read once and its deviations are taken in registers.  Workgroups walk down the rows (every gridDim-th group
+// of rows), the loads of the next row under way while the present one is summed; scale and shift stay in registers as well.
+// WHOLE: C is a number of whole chunks.  Else the last chunk is moved back to end with the row; the elements it shares with the chunk
+// before (`skip` of them) are computed, and stored, twice, but counted once.  (Tested and moved element by element that chunk cost as much
+// as the rest of the row: 40000 x 1001 float forward 89 us, 40000 x 1000 61.  Rows off 16-byte boundaries cost next to nothing.)
+template <class T> constexpr int kChunk = sizeof(T) == 8 ? 4 : 8;
+
+// E neighbours as they are stored; rows need not begin on 16-byte boundaries (the wide loads of this machine do not ask for it)
+template <class T, int E>
+struct __attribute__((packed, aligned(sizeof(T)))) Chunk {
+    T v[E];
+};
+template <class T, int E>
+__device__ __forceinline__ void load_chunk(Chunk<T, E> &r, const T *p) {
+    r = *reinterpret_cast<const Chunk<T, E> *>(p);
+}
+template <class T, class W, int E>
+__device__ __forceinline__ void store_chunk(T *p, const W (&v)[E]) {
+    Chunk<T, E> r;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t pair[E / 2];
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) pair[e] = to_bf16_pair(v[2 * e], v[2 * e + 1]);
+        __builtin_memcpy(&r, pair, sizeof(r));
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) r.v[e] = v[e];
+    }
+    *reinterpret_cast<Chunk<T, E> *>(p) = r;
+}
+
+// where a thread's chunks begin
+template <int LANES, int CHUNKS, int E, bool WHOLE>
+struct Place {
+    int c[CHUNKS], skip_[CHUNKS];
+    bool live[CHUNKS];
+    __device__ __forceinline__ Place(int t, int C) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int at = (t + j * LANES) * E;
+            live[j] = at < C;
+            c[j] = WHOLE ? at : min(at, C - E);
+            skip_[j] = at - c[j];
+        }
+    }
+    __device__ __forceinline__ int skip(int j) const { return WHOLE ? 0 : skip_[j]; }
+    __device__ __forceinline__ bool counts(int j, int e) const { return WHOLE || e >= skip_[j]; }
+};
+
+// the sum over the LANES threads of a row; `slots`: LANES / 64 entries that nothing else uses until the next barrier but one
+template <int LANES, class W>
+__device__ __forceinline__ W row_sum(W a, W *slots) {
+    a = lanes_sum<(LANES < 64 ? LANES : 64)>(a);
+    if constexpr (LANES > 64) {
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = W(0);
+#pragma unroll
+        for (int i = 0; i < LANES / 64; ++i) a += slots[i];
+    }
+    return a;
+}
+template <int LANES, class W>
+__device__ __forceinline__ void row_sums(W &a, W &b, W *slots) {   // (two at once: twice the entries, one barrier)
+    a = lanes_sum<(LANES < 64 ? LANES : 64)>(a);
+    b = lanes_sum<(LANES < 64 ? LANES : 64)>(b);
+    if constexpr (LANES > 64) {
+        constexpr int N = LANES / 64;
+        if ((threadIdx.x & 63) == 0) {
+            slots[threadIdx.x >> 6] = a;
+            slots[N + (threadIdx.x >> 6)] = b;
+        }
+        __syncthreads();
+        a = b = W(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            a += slots[i];
+            b += slots[N + i];
+        }
+    }
+}
+
+constexpr int norm_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+template <class TX, class TY, int LANES, int CHUNKS, bool WHOLE>
+__global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(const NormArgs<typename Stored<TX>::wide_t> a) {
+    typedef typename Stored<TX>::wide_t W;
+    constexpr int E = kChunk<TX>, ROWS = norm_threads(LANES) / LANES;
+    __shared__ W slots[2][2][norm_threads(LANES) / 64];
+    const int t = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const W *scale_p = static_cast<const W *>(a.scale), *shift_p = static_cast<const W *>(a.shift);
+    W scale[CHUNKS][E], shift[CHUNKS][E];   // alpha times
+    const Place<LANES, CHUNKS, E, WHOLE> at(t, a.C);
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+        Chunk<W, E> sc, sh;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sc.v[e] = W(1), sh.v[e] = W(0);
+        if (scale_p && at.live[j]) load_chunk(sc, scale_p + at.c[j]);
+        if (shift_p && at.live[j]) load_chunk(sh, shift_p + at.c[j]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) scale[j][e] = a.alpha * sc.v[e], shift[j][e] = a.alpha * sh.v[e];
+    }
+    const int stride = (int)gridDim.x * ROWS;
+    int row = (int)blockIdx.x * ROWS + sub;
+    Chunk<TX, E> raw[CHUNKS];
+    auto load = [&](int r) __attribute__((always_inline)) {
+        const TX *x = static_cast<const TX *>(a.x) + r * a.xs;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+            if (at.live[j]) load_chunk(raw[j], x + at.c[j]);
+    };
+    if (row < a.M) load(row);
+    // (the rows of a workgroup's wavefronts end together but for the last round: with LANES = 64 there is no barrier in the loop)
+    for (int parity = 0; row < a.M; row += stride, parity ^= 1) {
+        W x[CHUNKS][E];
+        W sum = W(0);
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[j][e] = Stored<TX>::widen(raw[j].v[e]);
+                if (at.counts(j, e)) sum += x[j][e];
+            }
+        }
+        TY *y = static_cast<TY *>(a.y) + row * a.ys;
+        Chunk<TY, E> old[CHUNKS];
+        if (a.beta != W(0))   // (all of the row, before any of it is written)
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+                if (at.live[j]) load_chunk(old[j], y + at.c[j]);
+        if (row + stride < a.M) load(row + stride);
+        const W mean = row_sum<LANES>(sum, slots[parity][0]) / W(a.C);
+        W squares = W(0);
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[j][e] -= mean;
+                if (at.counts(j, e)) squares += x[j][e] * x[j][e];
+            }
+        }
+        const W s = W(1) / sqrt(row_sum<LANES>(squares, slots[parity][1]) / W(a.C) + a.epsilon);
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            W out[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[e] = x[j][e] * s * scale[j][e] + shift[j][e];
+            if (a.beta != W(0))
+#pragma unroll
+                for (int e = 0; e < E; ++e) out[e] += a.beta * Stored<TY>::widen(old[j].v[e]);
+            store_chunk(y + at.c[j], out);
+        }
+        if (t == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.invstd) a.invstd[row] = s;
+        }
+    }
+}
+
+// dx of every row, and dscale's and dshift's sums over the workgroup's rows in registers (parts[workgroup]).  With 1024 threads to a
+// row their 128 registers hold the row and the sums only: scale comes from the cache, the next row's loads are not made ahead.
+template <class TX, class TY, int LANES, int CHUNKS, bool WHOLE>
+__global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_kernel(const NormBackwardArgs<typename Stored<TX>::wide_t> a) {
+    typedef typename Stored<TX>::wide_t W;
+    constexpr int E = kChunk<TX>, THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
+    __shared__ W slots[2][2 * THREADS / 64];
+    const int t = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    constexpr bool ROOM = LANES < 1024;
+    W scale[CHUNKS][E], ds[CHUNKS][E], db[CHUNKS][E];
+    const Place<LANES, CHUNKS, E, WHOLE> at(t, a.C);
+    auto load_scale = [&](int j) __attribute__((always_inline)) {
+        Chunk<W, E> sc;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sc.v[e] = W(1);
+        if (a.scale && at.live[j]) load_chunk(sc, a.scale + at.c[j]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) scale[j][e] = sc.v[e];
+    };
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+        if (ROOM) load_scale(j);
+#pragma unroll
+        for (int e = 0; e < E; ++e) ds[j][e] = db[j][e] = W(0);
+    }
+    const int stride = (int)gridDim.x * ROWS;
+    int row = (int)blockIdx.x * ROWS + sub;
+    Chunk<TX, E> rx[CHUNKS], rr[CHUNKS];
+    Chunk<TY, E> rdy[CHUNKS];
+    W mean, s;
+    auto load = [&](int r) __attribute__((always_inline)) {
+        const TX *x = static_cast<const TX *>(a.x) + r * a.xs;
+        const TY *dy = static_cast<const TY *>(a.dy) + r * a.dys;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            load_chunk(rx[j], x + at.c[j]);
+            load_chunk(rdy[j], dy + at.c[j]);
+        }
+        mean = a.mean[r];
+        s = a.invstd[r];
+    };
+    if (ROOM && row < a.M) load(row);
+    for (int parity = 0; row < a.M; row += stride, parity ^= 1) {
+        if (!ROOM) load(row);
+        if (a.beta != W(0)) {
+            const TX *p = static_cast<const TX *>(a.r) + row * a.rs;
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+                if (at.live[j]) load_chunk(rr[j], p + at.c[j]);
+        }
+        W h[CHUNKS][E], q[CHUNKS][E];
+        W sum = W(0), along = W(0);
+        const W inv = s;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            if (!ROOM) load_scale(j);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const W dy = Stored<TY>::widen(rdy[j].v[e]);
+                h[j][e] = (Stored<TX>::widen(rx[j].v[e]) - mean) * inv;
+                q[j][e] = dy * scale[j][e];
+                if (at.counts(j, e)) {
+                    db[j][e] += dy;
+                    ds[j][e] += dy * h[j][e];
+                    sum += q[j][e];
+                    along += q[j][e] * h[j][e];
+                }
+            }
+        }
+        if (ROOM && row + stride < a.M) load(row + stride);
+        row_sums<LANES>(sum, along, slots[parity]);
+        sum /= W(a.C);
+        along /= W(a.C);
+        const W f = a.alpha * inv;
+        TX *dx = static_cast<TX *>(a.dx) + row * a.dxs;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            W out[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[e] = f * (q[j][e] - sum - h[j][e] * along);
+            if (a.beta != W(0))
+#pragma unroll
+                for (int e = 0; e < E; ++e) out[e] += a.beta * Stored<TX>::widen(rr[j].v[e]);
+            store_chunk(dx + at.c[j], out);
+        }
+    }
+    if (!a.parts) return;
+    W *parts = a.parts + (size_t)blockIdx.x * 2 * a.C;
+    if constexpr (ROWS == 1) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            if (at.skip(j) == 0) {
+                store_chunk(parts + at.c[j], ds[j]);
+                store_chunk(parts + a.C + at.c[j], db[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (at.counts(j, e)) {
+                        parts[at.c[j] + e] = ds[j][e];
+                        parts[a.C + at.c[j] + e] = db[j][e];
+                    }
+            }
+        }
+    } else {   // the wavefronts' sums, added in their order
+        __shared__ W sums[ROWS][LANES * E];
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (at.counts(j, e)) sums[sub][(e - at.skip(j)) * LANES + t] = which ? db[j][e] : ds[j][e];
+                __syncthreads();
+                for (int i = threadIdx.x; i < LANES * E; i += THREADS) {
+                    const int c = j * LANES * E + i, at = (i % E) * LANES + i / E;
+                    W v = sums[0][at];
+#pragma unroll
+                    for (int r = 1; r < ROWS; ++r) v += sums[r][at];
+                    if (c < a.C) parts[(which ? a.C : 0) + c] = v;
+                }
+            }
     }
 }
 
@@ -206,8 +500,34 @@ igcStatus check_norm_backward(igcTensorDescriptor_t xDesc, igcTensorDescriptor_t
     return IGC_STATUS_SUCCESS;
 }
 
+// f(LANES, CHUNKS) of the smallest shape that holds a row of C values of `elem` bytes computed with; false: none does
+template <int L, int N> struct Shape {
+    static constexpr int LANES = L, CHUNKS = N;
+};
+template <bool BACKWARD, class F>
+bool by_shape(int C, bool f64, F f) {
+    const int chunks = f64 ? (C + 3) / 4 : (C + 7) / 8;
+    if (C < (f64 ? 4 : 8)) return false;
+    if (chunks <= 16) return f(Shape<16, 1>()), true;
+    if (chunks <= 32) return f(Shape<32, 1>()), true;
+    if (chunks <= 64) return f(Shape<64, 1>()), true;
+    if (chunks <= 128) return f(Shape<64, 2>()), true;
+    if (chunks <= 256) return f(Shape<256, 1>()), true;
+    if (chunks <= 512) return f(Shape<256, 2>()), true;
+    if (chunks <= 1024) return f(Shape<512, 2>()), true;
+    if (chunks <= 2048) return f(typename std::conditional<BACKWARD, Shape<1024, 2>, Shape<512, 4>>::type()), true;
+    return false;
+}
+
 // ranges of rows whose sums are taken side by side
-int param_ranges(const igcContext *h, const Matrix &x) {
+int param_ranges(const igcContext *h, const Matrix &x, bool f64) {
+    int held = 0;
+    if (by_shape<true>(x.cols, f64, [&](auto shape) {
+            constexpr int rows = norm_threads(decltype(shape)::LANES) / decltype(shape)::LANES;
+            const long long wanted = (long long)h->computeUnits * (decltype(shape)::LANES >= 512 ? 1 : 2);
+            held = (int)std::max(1ll, std::min(wanted, (x.rows + 2 * rows - 1) / (2 * rows)));
+        }))
+        return held;
     const long long groups = (x.cols + 63) / 64;
     const long long most = (x.rows + 31) / 32, wanted = (4ll * h->computeUnits + groups - 1) / groups;
     return (int)std::max(1ll, std::min(most, wanted));
@@ -240,8 +560,17 @@ igcStatus igcLayerNormForward(igcHandle_t handle, const void *alpha, igcTensorDe
         NormArgs<W> a{};
         a.x = x; a.scale = scale; a.shift = shift; a.y = y;
         a.mean = static_cast<W *>(mean); a.invstd = static_cast<W *>(invStd);
-        a.xs = p.x.stride; a.ys = p.y.stride; a.C = p.x.cols;
+        a.xs = p.x.stride; a.ys = p.y.stride; a.M = (int)p.x.rows; a.C = p.x.cols;
         a.alpha = (W)host_scalar(alpha, f64); a.beta = (W)host_scalar(beta, f64); a.epsilon = (W)epsilon;
+        igcStatus rc = IGC_STATUS_SUCCESS;
+        if (by_shape<false>(a.C, f64, [&](auto shape) {
+                constexpr int LANES = decltype(shape)::LANES, THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
+                const long long groups = (p.x.rows + ROWS - 1) / ROWS, most = (long long)handle->computeUnits * (LANES >= 512 ? 4 : 8);
+                rc = launch_kernel(a.C % kChunk<TX> == 0 ? reinterpret_cast<const void *>(&layer_norm_held_kernel<TX, TY, LANES, decltype(shape)::CHUNKS, true>)
+                                                     : reinterpret_cast<const void *>(&layer_norm_held_kernel<TX, TY, LANES, decltype(shape)::CHUNKS, false>), a,
+                                   dim3((unsigned)std::min(groups, most)), THREADS, handle->stream);
+            }))
+            return rc;
         return launch_kernel(reinterpret_cast<const void *>(&layer_norm_rows_kernel<TX, TY>), a, dim3((unsigned)p.x.rows), 256, handle->stream);
     });
 }
@@ -252,8 +581,8 @@ igcStatus igcGetLayerNormBackwardWorkspaceSize(igcHandle_t handle, igcTensorDesc
     NormProblem p;
     const igcStatus st = check_norm_backward(xDesc, dyDesc, dxDesc, &p);
     if (st != IGC_STATUS_SUCCESS) return st;
-    const int ranges = param_ranges(handle, p.x);
-    *sizeInBytes = ranges > 1 ? (size_t)ranges * 2 * p.x.cols * (xDesc->dtype == IGC_DATA_DOUBLE ? 8 : 4) : 0;
+    const int ranges = param_ranges(handle, p.x, xDesc->dtype == IGC_DATA_DOUBLE);
+    *sizeInBytes = (size_t)ranges * 2 * p.x.cols * (xDesc->dtype == IGC_DATA_DOUBLE ? 8 : 4);
     return IGC_STATUS_SUCCESS;
 }
 
@@ -289,19 +618,30 @@ igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha, igcTensorD
         a.xs = p.x.stride; a.dys = p.y.stride; a.rs = p.r.stride; a.dxs = p.dx.stride;
         a.M = (int)p.x.rows; a.C = p.x.cols;
         a.alpha = (W)host_scalar(alpha, f64); a.beta = (W)b; a.paramBeta = (W)host_scalar(paramBeta, f64);
-        igcStatus rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_backward_rows_kernel<TX, TY>), a, dim3((unsigned)a.M), 256, handle->stream);
-        if (rc != IGC_STATUS_SUCCESS || (!dscale && !dshift)) return rc;
-        const unsigned groups = (unsigned)(a.C + 63) / 64u;
-        a.ranges = param_ranges(handle, p.x);
+        a.ranges = param_ranges(handle, p.x, f64);
+        const bool params = dscale || dshift;
         const size_t need = (size_t)a.ranges * 2 * (size_t)a.C * sizeof(W);
-        if (a.ranges > 1 && workSpace && workSpaceSizeInBytes >= need && (uintptr_t)workSpace % sizeof(W) == 0) {
-            a.parts = static_cast<W *>(workSpace);
-            a.per = (a.M + a.ranges - 1) / a.ranges;
-            a.ranges = (a.M + a.per - 1) / a.per;
-            rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_params_kernel<TX, TY>), a, dim3(groups, (unsigned)a.ranges), 256, handle->stream);
-            if (rc != IGC_STATUS_SUCCESS) return rc;
+        if (params && workSpace && workSpaceSizeInBytes >= need && (uintptr_t)workSpace % sizeof(W) == 0) a.parts = static_cast<W *>(workSpace);
+        igcStatus rc = IGC_STATUS_SUCCESS;
+        if (by_shape<true>(a.C, f64, [&](auto shape) {
+                constexpr int LANES = decltype(shape)::LANES, THREADS = norm_threads(LANES);
+                rc = launch_kernel(a.C % kChunk<TX> == 0 ? reinterpret_cast<const void *>(&layer_norm_backward_held_kernel<TX, TY, LANES, decltype(shape)::CHUNKS, true>)
+                                                     : reinterpret_cast<const void *>(&layer_norm_backward_held_kernel<TX, TY, LANES, decltype(shape)::CHUNKS, false>), a,
+                                   dim3((unsigned)a.ranges), THREADS, handle->stream);
+            })) {
+            if (rc != IGC_STATUS_SUCCESS || !params) return rc;
+        } else {
+            rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_backward_rows_kernel<TX, TY>), a, dim3((unsigned)a.M), 256, handle->stream);
+            if (rc != IGC_STATUS_SUCCESS || !params) return rc;
+            if (a.parts) {
+                a.per = (a.M + a.ranges - 1) / a.ranges;
+                a.ranges = (a.M + a.per - 1) / a.per;
+                rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_params_kernel<TX, TY>), a, dim3((unsigned)(a.C + 63) / 64u, (unsigned)a.ranges), 256,
+                                   handle->stream);
+                if (rc != IGC_STATUS_SUCCESS) return rc;
+            }
         }
-        return launch_kernel(reinterpret_cast<const void *>(&layer_norm_params_sum_kernel<TX, TY>), a, dim3(groups), 256, handle->stream);
+        return launch_kernel(reinterpret_cast<const void *>(&layer_norm_params_sum_kernel<TX, TY>), a, dim3((unsigned)(a.C + 31) / 32u), 1024, handle->stream);
     });
 }
 

@@ -48,6 +48,40 @@ struct bf16_t {
 __device__ __forceinline__ uint16_t to_bf16_bits(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ float bf16_bits_to_float(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
 
+template <int C> struct DppControl {
+    static constexpr int value = C;
+};
+
+// two of them side by side, the first in the low half: one conversion instruction
+__device__ __forceinline__ uint32_t to_bf16_pair(float lo, float hi) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+
+// sum over each 16, 32 or all 64 lanes, the same in all of them: neighbours, pairs, quads and eights inside a row of 16 lanes, then the rows
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+    auto with = [&](auto control) {
+        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    v = with(DppControl<0xB1>());    // quad_perm 1 0 3 2
+    v = with(DppControl<0x4E>());    // quad_perm 2 3 0 1
+    v = with(DppControl<0x141>());   // mirrored within eight lanes
+    v = with(DppControl<0x140>());   // mirrored within sixteen
+    if constexpr (LANES == 16) return v;
+    if constexpr (LANES == 32) return v + __shfl_xor(v, 16);
+    const int i = __builtin_bit_cast(int, v);
+    return (__builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 0)) + __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 16))) +
+           (__builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 32)) + __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 48)));
+}
+template <int LANES>
+__device__ __forceinline__ double lanes_sum(double v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
 template <class T> struct Stored;   // wide_t: what is computed with
 template <> struct Stored<float> {
     typedef float wide_t;
@@ -70,10 +104,10 @@ template <> struct Stored<double> {
 
 // (the launch call's own return value, not the thread's last-error state, which other users of the runtime may have set)
 template <class Args>
-igcStatus launch_kernel(const void *kernel, const Args &args, dim3 grid, int threads, void *stream, size_t lds_bytes = 0) {
+igcStatus launch_kernel(const void *kernel, const Args &args, dim3 grid, int threads, void *stream) {
     Args copy = args;
     void *argv[] = {&copy};
-    return hipLaunchKernel(kernel, grid, dim3(threads), argv, lds_bytes, static_cast<hipStream_t>(stream)) == hipSuccess ? IGC_STATUS_SUCCESS
+    return hipLaunchKernel(kernel, grid, dim3(threads), argv, 0, static_cast<hipStream_t>(stream)) == hipSuccess ? IGC_STATUS_SUCCESS
                                                                                                                      : IGC_STATUS_EXECUTION_FAILED;
 }
 
