@@ -44,9 +44,9 @@ struct TileArgs : LinearArgs {
 // Tile shapes of linear_tiles_kernel (igconv_linear_tiles.hpp).  sa, sb: the operand's reduction index runs along its rows.
 struct TileKernel {
     int bm, bn, threads;
-    const void *kernel;
+    const void *kernel;   // null: not offered
 };
-constexpr int kTileShapes = 2;
+constexpr int kTileShapes = 3;
 TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent
 TileKernel tile_kernel_rows_columns(int shape, bool f32_out);  // backward data: B strided
 TileKernel tile_kernel_columns(int shape, bool f32_out);       // backward filter: both strided

@@ -188,12 +188,85 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
     }
 }
 
+// ---- operands that are not laid out for the tiles --------------------------------------------------------------------------
+// A matrix copied into rows on 16-byte boundaries, zeros up to the next eighth column.  Float: as bfloat16 parts h + m + l = x (8 bits of
+// the mantissa each, exact), and h once more with zeros in place of infinities and NaN: a product is then the sum of six products of parts,
+// smallest first - l h', h' l, m m, m h', h' m, h h - off by less than 2^-23 of itself (m l, l m and l l are left out), and an
+// infinite or undefined element meets the other operand once, as it does in one product.
+struct PackArgs {
+    const void *from[2];
+    uint16_t *to[2];
+    long long stride[2], toRow[2];     // elements
+    long long rows[2];
+    int cols[2], groups[2];            // groups of eight columns
+    long long plane[2];                // elements from part to part
+    long long blocks0;                 // workgroups of the first matrix
+};
+constexpr int kParts = 4;              // h, m, l, h'
+
+template <class T>
+__global__ __launch_bounds__(256) void linear_pack_kernel(const PackArgs p) {
+    const int w = (long long)blockIdx.x >= p.blocks0 ? 1 : 0;
+    const long long id = ((long long)blockIdx.x - (w ? p.blocks0 : 0)) * 256 + threadIdx.x;
+    const long long row = id / p.groups[w];
+    const int c = (int)(id % p.groups[w]) * 8;
+    if (row >= p.rows[w]) return;
+    const T *from = static_cast<const T *>(p.from[w]) + row * p.stride[w] + c;
+    struct __attribute__((packed, aligned(sizeof(T)))) Raw {
+        T v[8];
+    } raw;
+    const int left = p.cols[w] - c;
+    if (left >= 8) {
+        raw = *reinterpret_cast<const Raw *>(from);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            raw.v[e] = T{};
+            if (e < left) raw.v[e] = from[e];
+        }
+    }
+    uint16_t *to = p.to[w] + row * p.toRow[w] + c;
+    if constexpr (sizeof(T) == 2) {
+        u32x4 q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[e] = raw.v[2 * e].bits | (uint32_t)raw.v[2 * e + 1].bits << 16;
+        *reinterpret_cast<u32x4 *>(to) = q;
+    } else {
+        u32x4 part[kParts];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t bits[kParts][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = raw.v[2 * e + i];
+                const bool finite = __builtin_fabsf(x) < __builtin_inff();
+                uint32_t h = to_bf16_bits(x);
+                if (finite && (h & 0x7FFFu) == 0x7F80u) --h;   // (rounded up to infinity: the value below)
+                const float r = finite ? x - bf16_bits_to_float(h) : 0.f;
+                const uint32_t m = to_bf16_bits(r), l = to_bf16_bits(r - bf16_bits_to_float(m));
+                bits[0][i] = h; bits[1][i] = m; bits[2][i] = l; bits[3][i] = finite ? h : 0u;
+            }
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) part[q][e] = bits[q][0] | bits[q][1] << 16;
+        }
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * p.plane[w]) = part[q];
+    }
+}
+
 // ---- the choice of a tile and of the ranges -------------------------------------------------------------------------------
+struct OperandPlan {
+    bool pack = false;
+    long long rows = 0, stride = 0, toRow = 0, plane = 0;   // of the matrix in memory
+    int cols = 0;
+    size_t at = 0;           // where its copy lies in the workspace
+};
 struct TilePlan {
     bool tiles = false;      // (else the kernel for any layout)
     TileKernel k{};
     int tilesM = 0, tilesN = 0, splits = 1, stepsPerSplit = 0;
-    size_t bytes = 0;        // of workspace: the ranges' parts
+    OperandPlan a, b;
+    size_t partsAt = 0, bytes = 0;   // of workspace
 };
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -202,64 +275,127 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
     return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
 }
 
-// rows on 16-byte boundaries, whole 16-byte pieces, a tile's or step's reach within 31 bits
-bool tile_operand(long long rows, long long cols, long long stride) {
-    return cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride >= cols)) && stride < (1ll << 22);
+// The matrix of an operand, and whether it has to be copied: rows on 16-byte boundaries, whole 16-byte pieces, no row inside another.
+// (A tile's or a step's reach stays within 31 bits: rows of less than 2^22 elements.)
+OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
+    OperandPlan o;
+    o.rows = strided ? K : n;
+    o.cols = (int)(strided ? n : K);
+    o.stride = strided ? ks : ns;
+    o.pack = f32 || !aligned || o.cols % 8 != 0 || (o.rows > 1 && (o.stride % 8 != 0 || o.stride < o.cols));
+    o.toRow = round_up(o.cols, 8);
+    o.plane = o.rows * o.toRow;
+    return o;
 }
 
-TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, size_t room) {
-    TilePlan best;
-    if (in != IGC_DATA_BFLOAT16) return best;
-    const bool sa = a.ak != 1, sb = a.bk != 1;
-    if (!(sa ? tile_operand(a.K, a.M, a.ak) : tile_operand(a.M, a.K, a.am)) || !(sb ? tile_operand(a.K, a.N, a.bk) : tile_operand(a.N, a.K, a.bn))) return best;
-    const int steps = (a.K + kTileStep - 1) / kTileStep;
-    double cost = 1e300;
+// us of a step on one compute unit, that of two workgroups side by side where a compute unit holds two; measured on 8192^3
+struct ShapeCost {
+    int per_cu;
+    double alone, full, ends;   // ends: start and epilogue of a tile
+};
+constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.72, 1.72, 7.0}, {2, 0.60, 1.03, 5.0}, {2, 0.60, 1.03, 5.0}};
+
+TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool aligned_a, bool aligned_b, size_t room) {
+    TilePlan pl;
+    const bool f32 = in == IGC_DATA_FLOAT, sa = a.ak != 1, sb = a.bk != 1;
+    pl.a = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, aligned_a);
+    pl.b = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, aligned_b);
+    size_t at = 0;
+    for (OperandPlan *o : {&pl.a, &pl.b}) {
+        if ((o->pack ? o->toRow : o->stride) >= (1ll << 22)) return pl;
+        if (!o->pack) continue;
+        o->at = at;
+        at += (size_t)round_up(o->plane * 2 * (f32 ? kParts : 1), 256);
+    }
+    if (at > room) return pl;
+    pl.partsAt = at;
+    const int steps = (a.K + kTileStep - 1) / kTileStep, pairs = f32 ? kMaxPairs : 1;
+    double best = 1e300;
     for (int shape = 0; shape < kTileShapes; ++shape) {
         const TileKernel k = tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT);
-        const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn, at_once = h->computeUnits * (shape == 0 ? 1 : 2);
-        for (int splits = 1; splits <= 32 && splits * 4 <= std::max(steps, 4); ++splits) {
+        if (!k.kernel) continue;
+        const ShapeCost &sc = kShapeCost[shape];
+        const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn;
+        for (int splits = 1; splits <= 64 && splits <= steps; ++splits) {
             const int per = (steps + splits - 1) / splits;
             if ((steps + per - 1) / per != splits) continue;
-            const size_t bytes = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0;
-            if (bytes > room) break;
-            const double rounds = (double)((tm * tn * splits + at_once - 1) / at_once);
-            const double c = rounds * (per + 6) * (shape == 0 ? 1.0 : 0.62) + (splits > 1 ? 4.0 + (double)bytes * 2 / 4e6 : 0.0);
-            if (c < cost) {
-                cost = c;
-                best.tiles = true;
-                best.k = k;
-                best.tilesM = (int)tm; best.tilesN = (int)tn; best.splits = splits; best.stepsPerSplit = per; best.bytes = bytes;
+            const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0;
+            if (at + parts > room) break;
+            const long long units = tm * tn * splits;
+            if (units >= (1ll << 27)) break;
+            const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
+            const double full = per * pairs * sc.full + sc.ends, one = per * pairs * sc.alone + sc.ends;
+            const double us = whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)) + (splits > 1 ? 4.0 + (double)parts * 2 / 4e6 : 0.0);
+            if (us < best) {
+                best = us;
+                pl.tiles = true;
+                pl.k = k;
+                pl.tilesM = (int)tm; pl.tilesN = (int)tn; pl.splits = splits; pl.stepsPerSplit = per;
+                pl.bytes = at + parts;
             }
         }
     }
-    return best;
+    return pl;
 }
 
 bool on16(const void *p) { return (uintptr_t)p % 16 == 0; }
 
+// the copies that the plan asks for; the tiles' operands
+igcStatus pack_operands(const TilePlan &pl, bool f32, const LinearArgs &a, TileArgs &t, uint8_t *workSpace, void *stream) {
+    PackArgs p{};
+    long long blocks = 0;
+    int n = 0;
+    for (int i = 0; i < 2; ++i) {
+        const OperandPlan &o = i ? pl.b : pl.a;
+        if (!o.pack) continue;
+        uint16_t *to = reinterpret_cast<uint16_t *>(workSpace + o.at);
+        p.from[n] = i ? a.b : a.a;
+        p.to[n] = to;
+        p.stride[n] = o.stride; p.toRow[n] = o.toRow; p.rows[n] = o.rows; p.cols[n] = o.cols; p.groups[n] = (int)(o.toRow / 8); p.plane[n] = o.plane;
+        const long long own = (o.rows * p.groups[n] + 255) / 256;
+        if (n == 0) p.blocks0 = own;
+        blocks += own;
+        ++n;
+        const bool strided = i ? a.bk != 1 : a.ak != 1;
+        (i ? t.b : t.a) = to;
+        (i ? t.bn : t.am) = strided ? 1 : o.toRow;
+        (i ? t.bk : t.ak) = strided ? o.toRow : 1;
+    }
+    if (n == 0) return IGC_STATUS_SUCCESS;
+    if (blocks >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
+    return launch_kernel(f32 ? reinterpret_cast<const void *>(&linear_pack_kernel<float>) : reinterpret_cast<const void *>(&linear_pack_kernel<bf16_t>), p,
+                         dim3((unsigned)blocks), 256, stream);
+}
+
 igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes) {
-    if (on16(a.a) && on16(a.b)) {
-        const TilePlan pl = plan_tiles(handle, in, out, a, workSpace && on16(workSpace) ? bytes : 0);
-        if (pl.tiles) {
-            TileArgs t{};
-            static_cast<LinearArgs &>(t) = a;
-            t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
-            t.group = std::min(pl.tilesM, 4);
-            t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
-            const long long units = (long long)pl.tilesM * pl.tilesN * pl.splits;
-            t.tilesPerXcd = (int)((units + 7) / 8);
-            t.parts = static_cast<float *>(workSpace);
-            t.partsRow = round_up(a.N, 8);
-            const long long per16 = 16 / elem_size(out);
-            t.vec = on16(a.y) && a.ys % per16 == 0 && (!a.z || on16(a.z)) && (!a.zin || (on16(a.zin) && a.zs % per16 == 0)) &&
-                    (a.beta == 0.f || (on16(a.r) && a.rs % per16 == 0));
-            t.pairs = 1;
-            const igcStatus rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
-            if (rc != IGC_STATUS_SUCCESS || pl.splits == 1) return rc;
-            const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
-                                                    : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
-            return launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
+    const TilePlan pl = plan_tiles(handle, in, out, a, on16(a.a), on16(a.b), workSpace && on16(workSpace) ? bytes : 0);
+    if (pl.tiles) {
+        const bool f32 = in == IGC_DATA_FLOAT;
+        TileArgs t{};
+        static_cast<LinearArgs &>(t) = a;
+        igcStatus rc = pack_operands(pl, f32, a, t, static_cast<uint8_t *>(workSpace), handle->stream);
+        if (rc != IGC_STATUS_SUCCESS) return rc;
+        t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
+        t.group = std::min(pl.tilesM, 4);
+        t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
+        const long long units = (long long)pl.tilesM * pl.tilesN * pl.splits;
+        t.tilesPerXcd = (int)((units + 7) / 8);
+        t.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workSpace) + pl.partsAt);
+        t.partsRow = round_up(a.N, 8);
+        const long long per16 = 16 / elem_size(out);
+        t.vec = on16(a.y) && a.ys % per16 == 0 && (!a.z || on16(a.z)) && (!a.zin || (on16(a.zin) && a.zs % per16 == 0)) &&
+                (a.beta == 0.f || (on16(a.r) && a.rs % per16 == 0));
+        t.pairs = 1;
+        if (f32) {
+            static const int part_a[kMaxPairs] = {2, 3, 1, 1, 3, 0}, part_b[kMaxPairs] = {3, 2, 1, 3, 1, 0};
+            t.pairs = kMaxPairs;
+            for (int i = 0; i < kMaxPairs; ++i) t.planeA[i] = part_a[i] * pl.a.plane, t.planeB[i] = part_b[i] * pl.b.plane;
         }
+        rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+        if (rc != IGC_STATUS_SUCCESS || pl.splits == 1) return rc;
+        const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
+                                                : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
+        return launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
     }
     const long long tiles = (long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile);
     if (tiles >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
@@ -302,7 +438,7 @@ igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescript
     Matrix x, y;
     const igcStatus st = check_linear(xDesc, wDesc, yDesc, false, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -336,7 +472,7 @@ igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDes
     Matrix dy, dx;
     const igcStatus st = check_linear(dyDesc, wDesc, dxDesc, true, &dy, &dx);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -370,7 +506,7 @@ igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorD
     Matrix x, dy;
     const igcStatus st = check_linear_filter(xDesc, dyDesc, dwDesc, &x, &dy);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 

@@ -45,14 +45,14 @@ struct OperandCopy {
     __device__ __forceinline__ void init(const void *matrix, long long row_stride, long long k_stride, int row0, int rows, int K, int lane, int wave) {
         if constexpr (STRIDED) {
             base = static_cast<const uint16_t *>(matrix) + row0;
-            left = (K - 1) * k_stride + (rows - row0);
+            left = (K - 1) * k_stride + ((rows + 7) & ~7) - row0;   // (whole pieces: a matrix whose rows do not end with one is a copy that does)
             stride_bytes = (uint32_t)k_stride * 2u;
             const int k = lane / PIECES, at = lane % PIECES;
             k_piece = wave * REQUESTS * KROWS + k;       // (the k row of the first request)
             first = at;
         } else {
             base = static_cast<const uint16_t *>(matrix) + row0 * row_stride;
-            left = (rows - row0 - 1) * row_stride + K;
+            left = (rows - row0 - 1) * row_stride + ((K + 7) & ~7);
             stride_bytes = (uint32_t)row_stride * 2u;
             const int row = lane >> 3, piece = (lane & 7) ^ row;
             first = (uint32_t)(wave * REQUESTS * 8 + row) * stride_bytes + piece * 16u;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
             else a[(t + 2) % 4] = readA.read(next, 0, t + 2 - SLOTS);
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                if (t < FM && t >= FM - FN && j == t - (FM - FN)) b[1][j] = readB.read(stage + BM * 128, 1, j);
+                if (t == (FM >= FN ? FM - FN + j : j * FM / FN)) b[1][j] = readB.read(stage + BM * 128, 1, j);
                 if (t >= SLOTS - 2 && j / ((FN + 1) / 2) == t - (SLOTS - 2)) b[0][j] = readB.read(next + BM * 128, 0, j);
             }
 #pragma unroll
