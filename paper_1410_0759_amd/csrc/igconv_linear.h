@@ -13,6 +13,7 @@ namespace igc {
 struct LinearArgs {
     const void *a, *b;
     long long am, ak, bn, bk;
+    bool strided_a, strided_b;   // the reduction index runs along the rows in memory (am, bn are 1)
     int M, N, K;
     // after the product: t = alpha D + bias[n]; z[m][n] = t where z is kept; t = f(t) (forward) or t f'(zin[m][n]) (backward
     // data); y[m][n] = t + beta r[m][n]
@@ -26,8 +27,7 @@ struct LinearArgs {
     long long zs, rs, ys;   // elements between rows (z is laid out as y is)
 };
 
-constexpr int kTileStep = 64;                     // reduction indices per step
-constexpr int kMaxPairs = 6;
+constexpr int kTileStep = 64, kFloatStep = 32;   // reduction indices per step (float: in parts)
 
 struct TileArgs : LinearArgs {
     int tilesM, tilesN, group;     // tiles are taken `group` rows of tiles at a time
@@ -36,9 +36,8 @@ struct TileArgs : LinearArgs {
     float *parts;                  // [split][M][partsRow] (partsRow: N rounded up to 8), where splits > 1
     long long partsRow;
     int vec;                       // the epilogue's matrices allow 16-byte accesses at every eighth column
-    // the operands' parts: the products of a pair of parts are summed one after the other
-    int pairs;
-    long long planeA[kMaxPairs], planeB[kMaxPairs];   // elements
+    float *columnParts;            // [split][tile column][M]: sums of the first operand's rows, or null
+    int blocksA, blocksB;          // (float) blocks of 16 rows of the operands
 };
 
 // Tile shapes of linear_tiles_kernel (igconv_linear_tiles.hpp).  sa, sb: the operand's reduction index runs along its rows.
@@ -47,6 +46,7 @@ struct TileKernel {
     const void *kernel;   // null: not offered
 };
 constexpr int kTileShapes = 3;
+TileKernel float_kernel();                                     // any pass, operands in parts (igconv_linear_float.hpp)
 TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent
 TileKernel tile_kernel_rows_columns(int shape, bool f32_out);  // backward data: B strided
 TileKernel tile_kernel_columns(int shape, bool f32_out);       // backward filter: both strided

@@ -5,7 +5,7 @@
 //   backward filter  dw = alpha dy^T x + beta dw,  dbias = alpha (column sums of dy) + beta dbias
 //
 // Products of bfloat16 are accumulated in fp32 by the matrix instructions, in a fixed order.
-#include "igconv_linear_tiles.hpp"
+#include "igconv_linear_float.hpp"
 
 namespace igc {
 namespace {
@@ -189,84 +189,141 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
 }
 
 // ---- operands that are not laid out for the tiles --------------------------------------------------------------------------
-// A matrix copied into rows on 16-byte boundaries, zeros up to the next eighth column.  Float: as bfloat16 parts h + m + l = x (8 bits of
-// the mantissa each, exact), and h once more with zeros in place of infinities and NaN: a product is then the sum of six products of parts,
-// smallest first - l h', h' l, m m, m h', h' m, h h - off by less than 2^-23 of itself (m l, l m and l l are left out), and an
-// infinite or undefined element meets the other operand once, as it does in one product.
-struct PackArgs {
-    const void *from[2];
-    uint16_t *to[2];
-    long long stride[2], toRow[2];     // elements
-    long long rows[2];
-    int cols[2], groups[2];            // groups of eight columns
-    long long plane[2];                // elements from part to part
-    long long blocks0;                 // workgroups of the first matrix
+struct PackOperand {
+    const void *from;
+    uint16_t *to;
+    long long rows, stride, toRow;     // of the matrix in memory, elements
+    int cols, groups;                  // (rows on 16-byte boundaries) groups of eight columns
+    int strided, blocks;               // (parts) whether the reduction index runs along the rows; blocks of 16 of the other index
+    long long workgroups;
 };
-constexpr int kParts = 4;              // h, m, l, h'
-
+struct PackArgs {
+    PackOperand o[2];
+};
 template <class T>
-__global__ __launch_bounds__(256) void linear_pack_kernel(const PackArgs p) {
-    const int w = (long long)blockIdx.x >= p.blocks0 ? 1 : 0;
-    const long long id = ((long long)blockIdx.x - (w ? p.blocks0 : 0)) * 256 + threadIdx.x;
-    const long long row = id / p.groups[w];
-    const int c = (int)(id % p.groups[w]) * 8;
-    if (row >= p.rows[w]) return;
-    const T *from = static_cast<const T *>(p.from[w]) + row * p.stride[w] + c;
-    struct __attribute__((packed, aligned(sizeof(T)))) Raw {
-        T v[8];
-    } raw;
-    const int left = p.cols[w] - c;
+struct __attribute__((packed, aligned(sizeof(T)))) EightStored {
+    T v[8];
+};
+
+// a matrix copied into rows on 16-byte boundaries, zeros up to the next eighth column
+__global__ __launch_bounds__(256) void linear_pack_kernel(const PackArgs args) {
+    const bool second = (long long)blockIdx.x >= args.o[0].workgroups;
+    const PackOperand &p = args.o[second ? 1 : 0];
+    const long long id = ((long long)blockIdx.x - (second ? args.o[0].workgroups : 0)) * 256 + threadIdx.x;
+    const long long row = id / p.groups;
+    const int c = (int)(id % p.groups) * 8, left = p.cols - c;
+    if (row >= p.rows) return;
+    const uint16_t *from = static_cast<const uint16_t *>(p.from) + row * p.stride + c;
+    EightStored<uint16_t> raw;
     if (left >= 8) {
-        raw = *reinterpret_cast<const Raw *>(from);
+        raw = *reinterpret_cast<const EightStored<uint16_t> *>(from);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            raw.v[e] = T{};
+            raw.v[e] = 0;
             if (e < left) raw.v[e] = from[e];
         }
     }
-    uint16_t *to = p.to[w] + row * p.toRow[w] + c;
-    if constexpr (sizeof(T) == 2) {
-        u32x4 q;
+    u32x4 q;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = raw.v[2 * e].bits | (uint32_t)raw.v[2 * e + 1].bits << 16;
-        *reinterpret_cast<u32x4 *>(to) = q;
-    } else {
-        u32x4 part[kParts];
+    for (int e = 0; e < 4; ++e) q[e] = raw.v[2 * e] | (uint32_t)raw.v[2 * e + 1] << 16;
+    *reinterpret_cast<u32x4 *>(p.to + row * p.toRow + c) = q;
+}
+
+// Eight neighbours along the reduction index as parts (igconv_linear_float.hpp): by truncation, so that all parts have x's sign.
+__device__ __forceinline__ void store_parts(uint16_t *unit, int slot, const float (&x)[8]) {
+    u32x4 part[kFloatParts];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t bits[kParts][2];
+    for (int e = 0; e < 4; ++e) {
+        uint32_t bits[kFloatParts][2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float x = raw.v[2 * e + i];
-                const bool finite = __builtin_fabsf(x) < __builtin_inff();
-                uint32_t h = to_bf16_bits(x);
-                if (finite && (h & 0x7FFFu) == 0x7F80u) --h;   // (rounded up to infinity: the value below)
-                const float r = finite ? x - bf16_bits_to_float(h) : 0.f;
-                const uint32_t m = to_bf16_bits(r), l = to_bf16_bits(r - bf16_bits_to_float(m));
-                bits[0][i] = h; bits[1][i] = m; bits[2][i] = l; bits[3][i] = finite ? h : 0u;
+        for (int i = 0; i < 2; ++i) {
+            const float v = x[2 * e + i];
+            const uint32_t all = __builtin_bit_cast(uint32_t, v), sign = all & 0x80000000u;
+            const bool finite = (all & 0x7F800000u) != 0x7F800000u;
+            const uint32_t h = finite ? all & 0xFFFF0000u : (all & 0x007FFFFFu ? 0x7FC00000u : all);   // (an undefined value must not become an infinity)
+            const float r = finite ? v - __builtin_bit_cast(float, h) : 0.f;
+            uint32_t m = __builtin_bit_cast(uint32_t, r) & 0xFFFF0000u;
+            uint32_t l = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, m)) & 0xFFFF0000u;
+            if ((all & 0x7F800000u) >= 0x0D800000u) {   // from 2^-100 on
+                if ((m & 0x7FFFFFFFu) == 0u) m = sign | 0x00800000u;
+                if ((l & 0x7FFFFFFFu) == 0u) l = sign | 0x00800000u;
             }
-#pragma unroll
-            for (int q = 0; q < kParts; ++q) part[q][e] = bits[q][0] | bits[q][1] << 16;
+            bits[0][i] = h >> 16; bits[1][i] = m >> 16; bits[2][i] = l >> 16;
         }
 #pragma unroll
-        for (int q = 0; q < kParts; ++q) *reinterpret_cast<u32x4 *>(to + q * p.plane[w]) = part[q];
+        for (int q = 0; q < kFloatParts; ++q) part[q][e] = bits[q][0] | bits[q][1] << 16;
     }
+#pragma unroll
+    for (int q = 0; q < kFloatParts; ++q) *reinterpret_cast<u32x4 *>(unit + (q * kUnitBytes + slot * 16) / 2) = part[q];
+}
+
+// A float operand as units of parts.  Reduction index adjacent: a wavefront makes the units of 16 rows by 32 indices, a lane 8 of a row.
+// Else a wavefront's lanes take 64 adjacent rows of the operand (columns of the matrix), 8 indices at a time.
+__global__ __launch_bounds__(256) void linear_parts_pack_kernel(const PackArgs args) {
+    const bool second = (long long)blockIdx.x >= args.o[0].workgroups;
+    const PackOperand &p = args.o[second ? 1 : 0];
+    const long long task = ((long long)blockIdx.x - (second ? args.o[0].workgroups : 0)) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    const float *from = static_cast<const float *>(p.from);
+    if (!p.strided) {
+        const int steps = (p.cols + kFloatStep - 1) / kFloatStep;
+        const long long block = task / steps, row = block * 16 + l16;
+        const int step = (int)(task % steps), k = step * kFloatStep + g * 8, left = p.cols - k;
+        if (block >= p.blocks) return;
+        float x[8];
+        if (row < p.rows && left >= 8) {
+            const EightStored<float> raw = *reinterpret_cast<const EightStored<float> *>(from + row * p.stride + k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = raw.v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = 0.f;
+                if (row < p.rows && e < left) x[e] = from[row * p.stride + k + e];
+            }
+        }
+        store_parts(p.to + ((long long)step * p.blocks + block) * (kFloatParts * kUnitBytes / 2), lane, x);
+    } else {
+        const int groups = (p.blocks + 3) / 4;
+        const int step = (int)(task / groups), block = (int)(task % groups) * 4 + g, col = block * 16 + l16;
+        if ((long long)step * kFloatStep >= p.rows) return;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const long long k = (long long)step * kFloatStep + c * 8;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = k + e < p.rows && col < p.cols ? from[(k + e) * p.stride + col] : 0.f;
+            if (block < p.blocks) store_parts(p.to + ((long long)step * p.blocks + block) * (kFloatParts * kUnitBytes / 2), c * 16 + l16, x);
+        }
+    }
+}
+
+// ---- the sums of the first operand's rows (bias gradient) over ranges and tiles --------------------------------------------------
+__global__ __launch_bounds__(256) void linear_sums_kernel(const float *parts, int count, int M, float alpha, float beta, float *out) {
+    const int m = (int)blockIdx.x * 256 + threadIdx.x;
+    if (m >= M) return;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < count; ++i) sum += parts[(long long)i * M + m];
+    float v = alpha * sum;
+    if (beta != 0.f) v += beta * out[m];
+    out[m] = v;
 }
 
 // ---- the choice of a tile and of the ranges -------------------------------------------------------------------------------
 struct OperandPlan {
     bool pack = false;
-    long long rows = 0, stride = 0, toRow = 0, plane = 0;   // of the matrix in memory
-    int cols = 0;
-    size_t at = 0;           // where its copy lies in the workspace
+    long long rows = 0, stride = 0, toRow = 0;   // of the matrix in memory
+    int cols = 0, blocks = 0;
+    size_t at = 0, bytes = 0;                    // its copy in the workspace
 };
 struct TilePlan {
     bool tiles = false;      // (else the kernel for any layout)
     TileKernel k{};
     int tilesM = 0, tilesN = 0, splits = 1, stepsPerSplit = 0;
     OperandPlan a, b;
-    size_t partsAt = 0, bytes = 0;   // of workspace
+    size_t partsAt = 0, sumsAt = 0, bytes = 0;   // of workspace
 };
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -275,8 +332,7 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
     return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
 }
 
-// The matrix of an operand, and whether it has to be copied: rows on 16-byte boundaries, whole 16-byte pieces, no row inside another.
-// (A tile's or a step's reach stays within 31 bits: rows of less than 2^22 elements.)
+// The matrix of an operand, and whether it has to be copied: bfloat16 rows on 16-byte boundaries, whole 16-byte pieces, no row inside another.
 OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
     OperandPlan o;
     o.rows = strided ? K : n;
@@ -284,57 +340,56 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
     o.stride = strided ? ks : ns;
     o.pack = f32 || !aligned || o.cols % 8 != 0 || (o.rows > 1 && (o.stride % 8 != 0 || o.stride < o.cols));
     o.toRow = round_up(o.cols, 8);
-    o.plane = o.rows * o.toRow;
+    o.blocks = (int)((n + 15) / 16);
+    if (o.pack)
+        o.bytes = f32 ? (size_t)((K + kFloatStep - 1) / kFloatStep) * o.blocks * (kFloatParts * kUnitBytes) : (size_t)round_up(o.rows * o.toRow * 2, 256);
     return o;
 }
 
-// us of a step on one compute unit, that of two workgroups side by side where a compute unit holds two; measured on 8192^3
+// us of a step on one compute unit, that of two workgroups side by side where a compute unit holds two; measured on 8192^3 (float: 4096^3)
 struct ShapeCost {
     int per_cu;
     double alone, full, ends;   // ends: start and epilogue of a tile
 };
 constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.72, 1.72, 7.0}, {2, 0.60, 1.03, 5.0}, {2, 0.60, 1.03, 5.0}};
+constexpr ShapeCost kFloatCost = {1, 1.0, 1.0, 6.0};
 
-TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool aligned_a, bool aligned_b, size_t room) {
+TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, bool aligned_a, bool aligned_b, size_t room) {
     TilePlan pl;
-    const bool f32 = in == IGC_DATA_FLOAT, sa = a.ak != 1, sb = a.bk != 1;
+    const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
     pl.a = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, aligned_a);
     pl.b = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, aligned_b);
     size_t at = 0;
     for (OperandPlan *o : {&pl.a, &pl.b}) {
-        if ((o->pack ? o->toRow : o->stride) >= (1ll << 22)) return pl;
-        if (!o->pack) continue;
+        if (!f32 && (o->pack ? o->toRow : o->stride) >= (1ll << 22)) return pl;   // (a tile's reach stays within 31 bits)
         o->at = at;
-        at += (size_t)round_up(o->plane * 2 * (f32 ? kParts : 1), 256);
+        at += o->bytes;
     }
     if (at > room) return pl;
-    pl.partsAt = at;
-    const int steps = (a.K + kTileStep - 1) / kTileStep, pairs = f32 ? kMaxPairs : 1;
+    const int step = f32 ? kFloatStep : kTileStep, steps = (a.K + step - 1) / step;
     double best = 1e300;
-    for (int shape = 0; shape < kTileShapes; ++shape) {
-        const TileKernel k = tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT);
-        if (!k.kernel) continue;
-        const ShapeCost &sc = kShapeCost[shape];
-        const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn;
-        for (int splits = 1; splits <= 64 && splits <= steps; ++splits) {
-            const int per = (steps + splits - 1) / splits;
-            if ((steps + per - 1) / per != splits) continue;
-            const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0;
-            if (at + parts > room) break;
-            const long long units = tm * tn * splits;
-            if (units >= (1ll << 27)) break;
-            const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
-            const double full = per * pairs * sc.full + sc.ends, one = per * pairs * sc.alone + sc.ends;
-            const double us = whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)) + (splits > 1 ? 4.0 + (double)parts * 2 / 4e6 : 0.0);
-            if (us < best) {
-                best = us;
-                pl.tiles = true;
-                pl.k = k;
-                pl.tilesM = (int)tm; pl.tilesN = (int)tn; pl.splits = splits; pl.stepsPerSplit = per;
-                pl.bytes = at + parts;
-            }
-        }
-    }
+    auto consider = [&](int shape, int splits) {
+        const TileKernel k = f32 ? float_kernel() : tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT);
+        const int per = (steps + splits - 1) / splits;
+        if (!k.kernel || (steps + per - 1) / per != splits) return;
+        const ShapeCost &sc = f32 ? kFloatCost : kShapeCost[shape];
+        const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn, units = tm * tn * splits;
+        const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0, sum_bytes = sums ? (size_t)(splits * tn) * a.M * 4 : 0;
+        if (at + parts + sum_bytes > room || units >= (1ll << 27)) return;
+        const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
+        const double full = per * sc.full + sc.ends, one = per * sc.alone + sc.ends;
+        const double us = whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)) + (splits > 1 ? 4.0 + (double)parts * 2 / 4e6 : 0.0);
+        if (us >= best) return;
+        best = us;
+        pl.tiles = true;
+        pl.k = k;
+        pl.tilesM = (int)tm; pl.tilesN = (int)tn; pl.splits = splits; pl.stepsPerSplit = per;
+        pl.partsAt = at;
+        pl.sumsAt = at + parts;
+        pl.bytes = at + parts + sum_bytes;
+    };
+    for (int shape = 0; shape < (f32 ? 1 : kTileShapes); ++shape)
+        for (int splits = 1; splits <= 64 && splits <= steps; ++splits) consider(shape, splits);
     return pl;
 }
 
@@ -343,59 +398,74 @@ bool on16(const void *p) { return (uintptr_t)p % 16 == 0; }
 // the copies that the plan asks for; the tiles' operands
 igcStatus pack_operands(const TilePlan &pl, bool f32, const LinearArgs &a, TileArgs &t, uint8_t *workSpace, void *stream) {
     PackArgs p{};
-    long long blocks = 0;
+    long long workgroups = 0;
     int n = 0;
     for (int i = 0; i < 2; ++i) {
         const OperandPlan &o = i ? pl.b : pl.a;
         if (!o.pack) continue;
-        uint16_t *to = reinterpret_cast<uint16_t *>(workSpace + o.at);
-        p.from[n] = i ? a.b : a.a;
-        p.to[n] = to;
-        p.stride[n] = o.stride; p.toRow[n] = o.toRow; p.rows[n] = o.rows; p.cols[n] = o.cols; p.groups[n] = (int)(o.toRow / 8); p.plane[n] = o.plane;
-        const long long own = (o.rows * p.groups[n] + 255) / 256;
-        if (n == 0) p.blocks0 = own;
-        blocks += own;
-        ++n;
-        const bool strided = i ? a.bk != 1 : a.ak != 1;
-        (i ? t.b : t.a) = to;
+        const bool strided = i ? a.strided_b : a.strided_a;
+        PackOperand &q = p.o[n++];
+        q.from = i ? a.b : a.a;
+        q.to = reinterpret_cast<uint16_t *>(workSpace + o.at);
+        q.rows = o.rows; q.stride = o.stride; q.toRow = o.toRow; q.cols = o.cols; q.groups = (int)(o.toRow / 8);
+        q.strided = strided ? 1 : 0; q.blocks = o.blocks;
+        const long long steps = (a.K + kFloatStep - 1) / kFloatStep;
+        q.workgroups = f32 ? (steps * (strided ? (o.blocks + 3) / 4 : o.blocks) + 3) / 4 : (o.rows * q.groups + 255) / 256;
+        workgroups += q.workgroups;
+        (i ? t.b : t.a) = q.to;
         (i ? t.bn : t.am) = strided ? 1 : o.toRow;
         (i ? t.bk : t.ak) = strided ? o.toRow : 1;
+        (i ? t.blocksB : t.blocksA) = o.blocks;
     }
     if (n == 0) return IGC_STATUS_SUCCESS;
-    if (blocks >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
-    return launch_kernel(f32 ? reinterpret_cast<const void *>(&linear_pack_kernel<float>) : reinterpret_cast<const void *>(&linear_pack_kernel<bf16_t>), p,
-                         dim3((unsigned)blocks), 256, stream);
+    if (workgroups >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
+    return launch_kernel(f32 ? reinterpret_cast<const void *>(&linear_parts_pack_kernel) : reinterpret_cast<const void *>(&linear_pack_kernel), p,
+                         dim3((unsigned)workgroups), 256, stream);
 }
 
-igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes) {
-    const TilePlan pl = plan_tiles(handle, in, out, a, on16(a.a), on16(a.b), workSpace && on16(workSpace) ? bytes : 0);
+// column sums of dy, [M of the product], beside backward filter
+struct SumsOut {
+    float *out = nullptr;
+    float alpha = 1.f, beta = 0.f;
+};
+
+igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes, const SumsOut &sums = SumsOut(),
+                      bool *summed = nullptr) {
+    const TilePlan pl = plan_tiles(handle, in, out, a, sums.out != nullptr, on16(a.a), on16(a.b), workSpace && on16(workSpace) ? bytes : 0);
     if (pl.tiles) {
-        const bool f32 = in == IGC_DATA_FLOAT;
         TileArgs t{};
         static_cast<LinearArgs &>(t) = a;
-        igcStatus rc = pack_operands(pl, f32, a, t, static_cast<uint8_t *>(workSpace), handle->stream);
+        uint8_t *ws = static_cast<uint8_t *>(workSpace);
+        igcStatus rc = pack_operands(pl, in == IGC_DATA_FLOAT, a, t, ws, handle->stream);
         if (rc != IGC_STATUS_SUCCESS) return rc;
         t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
         t.group = std::min(pl.tilesM, 4);
         t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
         const long long units = (long long)pl.tilesM * pl.tilesN * pl.splits;
         t.tilesPerXcd = (int)((units + 7) / 8);
-        t.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workSpace) + pl.partsAt);
+        t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
         t.partsRow = round_up(a.N, 8);
+        t.columnParts = sums.out ? reinterpret_cast<float *>(ws + pl.sumsAt) : nullptr;
         const long long per16 = 16 / elem_size(out);
         t.vec = on16(a.y) && a.ys % per16 == 0 && (!a.z || on16(a.z)) && (!a.zin || (on16(a.zin) && a.zs % per16 == 0)) &&
                 (a.beta == 0.f || (on16(a.r) && a.rs % per16 == 0));
-        t.pairs = 1;
-        if (f32) {
-            static const int part_a[kMaxPairs] = {2, 3, 1, 1, 3, 0}, part_b[kMaxPairs] = {3, 2, 1, 3, 1, 0};
-            t.pairs = kMaxPairs;
-            for (int i = 0; i < kMaxPairs; ++i) t.planeA[i] = part_a[i] * pl.a.plane, t.planeB[i] = part_b[i] * pl.b.plane;
-        }
         rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
-        if (rc != IGC_STATUS_SUCCESS || pl.splits == 1) return rc;
-        const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
-                                                : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
-        return launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
+        if (rc == IGC_STATUS_SUCCESS && pl.splits > 1) {
+            const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
+                                                    : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
+            rc = launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
+        }
+        if (rc == IGC_STATUS_SUCCESS && sums.out) {
+            const float *parts = t.columnParts;
+            int count = pl.splits * pl.tilesN, M = a.M;
+            SumsOut o = sums;
+            void *argv[] = {&parts, &count, &M, &o.alpha, &o.beta, &o.out};
+            *summed = true;
+            if (hipLaunchKernel(reinterpret_cast<const void *>(&linear_sums_kernel), dim3((unsigned)(M + 255) / 256u), dim3(256), argv, 0,
+                                static_cast<hipStream_t>(handle->stream)) != hipSuccess)
+                rc = IGC_STATUS_EXECUTION_FAILED;
+        }
+        return rc;
     }
     const long long tiles = (long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile);
     if (tiles >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
@@ -413,13 +483,13 @@ LinearArgs forward_sizes(const Matrix &x, const igcFilterStruct &w) {
 }
 LinearArgs backward_data_sizes(const Matrix &dy, const igcFilterStruct &w) {
     LinearArgs a{};
-    a.am = dy.stride; a.ak = 1; a.bn = 1; a.bk = w.c;
+    a.am = dy.stride; a.ak = 1; a.bn = 1; a.bk = w.c; a.strided_b = true;
     a.M = (int)dy.rows; a.N = w.c; a.K = w.k;
     return a;
 }
 LinearArgs backward_filter_sizes(const Matrix &x, const Matrix &dy, const igcFilterStruct &dw) {
     LinearArgs a{};
-    a.am = 1; a.ak = dy.stride; a.bn = 1; a.bk = x.stride;
+    a.am = 1; a.ak = dy.stride; a.bn = 1; a.bk = x.stride; a.strided_a = a.strided_b = true;
     a.M = dw.k; a.N = dw.c; a.K = (int)x.rows;
     return a;
 }
@@ -438,7 +508,7 @@ igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescript
     Matrix x, y;
     const igcStatus st = check_linear(xDesc, wDesc, yDesc, false, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), false, true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -472,7 +542,7 @@ igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDes
     Matrix dy, dx;
     const igcStatus st = check_linear(dyDesc, wDesc, dxDesc, true, &dy, &dx);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), false, true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -506,7 +576,7 @@ igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorD
     Matrix x, dy;
     const igcStatus st = check_linear_filter(xDesc, dyDesc, dwDesc, &x, &dy);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), true, true, true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -527,8 +597,13 @@ igcStatus igcLinearBackwardFilter(igcHandle_t handle, const void *alpha, igcTens
     a.act = IGC_ACTIVATION_IDENTITY;
     a.r = dw; a.rs = dwDesc->c;
     a.y = dw; a.ys = dwDesc->c;
-    const igcStatus rc = run_product(handle, xDesc->dtype, dwDesc->dtype, a, workSpace, workSpaceSizeInBytes);
-    if (rc != IGC_STATUS_SUCCESS || !dbias) return rc;
+    SumsOut sums;
+    sums.out = static_cast<float *>(dbias);
+    sums.alpha = a.alpha;
+    sums.beta = a.beta;
+    bool summed = false;
+    const igcStatus rc = run_product(handle, xDesc->dtype, dwDesc->dtype, a, workSpace, workSpaceSizeInBytes, sums, &summed);
+    if (rc != IGC_STATUS_SUCCESS || !dbias || summed) return rc;
     ColumnArgs c{dy, mdy.stride, (int)mdy.rows, dwDesc->k, a.alpha, a.beta, static_cast<float *>(dbias)};
     const dim3 grid((unsigned)(c.K + 63) / 64u);
     return dyDesc->dtype == IGC_DATA_FLOAT ? launch_kernel(reinterpret_cast<const void *>(&column_sum_kernel<float>), c, grid, 256, handle->stream)

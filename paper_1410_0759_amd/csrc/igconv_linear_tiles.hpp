@@ -1,4 +1,4 @@
-// Products of bfloat16 matrices whose rows lie on 16-byte boundaries (igconv_linear.h; the float ones run over bfloat16 parts).
+// Products of bfloat16 matrices whose rows lie on 16-byte boundaries (float ones: igconv_linear_float.hpp).
 //
 // A workgroup computes a BM x BN tile in steps of 64 of the reduction; a wavefront of it WM x WN results with
 // v_mfma_f32_16x16x32_bf16.  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), one step
@@ -60,10 +60,10 @@ struct OperandCopy {
         }
     }
 
-    // requests the step that begins at reduction index k (of K) of the part `plane` elements further on
-    __device__ __forceinline__ void request(uint8_t *stage, int wave, int k, int K, long long plane) const {
-        const long long skip = plane + (STRIDED ? (long long)k * (stride_bytes / 2u) : 0);
-        const long long bytes = (left - (skip - plane)) * 2;
+    // requests the step that begins at reduction index k (of K)
+    __device__ __forceinline__ void request(uint8_t *stage, int wave, int k, int K) const {
+        const long long skip = STRIDED ? (long long)k * (stride_bytes / 2u) : 0;
+        const long long bytes = (left - skip) * 2;
         const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + skip), 0,
                                                                             (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll), 0x00020000u);
         uint8_t *to = stage + wave * REQUESTS * 1024;
@@ -189,6 +189,46 @@ __device__ __forceinline__ bool tile_of(const TileArgs &p, int *tm, int *tn, int
     return true;
 }
 
+// A wavefront's results, FM x FN blocks of 16 x 16 from row m0, column n0 on: lane l holds row 16 i + l % 16, columns 16 j + 4 (l / 16) + 0..3.
+// They go through the wavefront's share of the LDS (its 16-byte pieces permuted within a row by the row's number), as many rows at a time as
+// it has room for, so that eight lanes write 128 or 256 adjacent bytes of a row of y.
+template <int FM, int FN, int SHARE, class TO>
+__device__ __forceinline__ void write_results(const TileArgs &p, uint8_t *share, int lane, int split, int m0, int n0, const f32x4 (&acc)[FM][FN]) {
+    constexpr int WN = FN * 16, PIECES = WN / 4;
+    constexpr int PASS_FRAGS = SHARE / (16 * WN * 4) < FM ? SHARE / (16 * WN * 4) : FM;
+    constexpr int PASSES = FM / PASS_FRAGS, LANES = WN / 8, AT_ONCE = 64 / LANES;
+    static_assert(PASSES * PASS_FRAGS == FM, "whole passes");
+    f32x4 *mine = reinterpret_cast<f32x4 *>(share);
+    const int l16 = lane & 15, g = lane >> 4, c8 = lane % LANES, n = n0 + c8 * 8;
+    Eight bias;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias.v[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.f;
+    for (int pass = 0; pass < PASSES; ++pass) {
+        // (which accumulators is known at compile time: an index into registers)
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q)
+            if (pass == q)
+#pragma unroll
+                for (int i = 0; i < PASS_FRAGS; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) mine[(i * 16 + l16) * PIECES + ((j * 4 + g) ^ (l16 & (PIECES - 1)))] = acc[q * PASS_FRAGS + i][j];
+        __builtin_amdgcn_wave_barrier();
+        for (int r = lane / LANES; r < PASS_FRAGS * 16; r += AT_ONCE) {
+            const int m = m0 + pass * PASS_FRAGS * 16 + r;
+            const f32x4 lo = mine[r * PIECES + ((2 * c8) ^ (r & 15 & (PIECES - 1)))], hi = mine[r * PIECES + ((2 * c8 + 1) ^ (r & 15 & (PIECES - 1)))];
+            if (m >= p.M || n >= p.N) continue;
+            const Eight d = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (p.splits > 1) store8<float>(p.parts, ((long long)split * p.M + m) * p.partsRow + n, d);
+            else if (p.vec && n + 8 <= p.N) finish8<TO>(p, m, n, d, bias);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < p.N) finish_element<TO>(p, m, n + e, d.v[e]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 template <class Cfg, class TO>
 __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const TileArgs p) {
     constexpr int BM = Cfg::BM, BN = Cfg::BN, FM = Cfg::FM, FN = Cfg::FN, SLOTS = 2 * FM;
@@ -209,22 +249,14 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
 
     const int kBegin = split * p.stepsPerSplit * kTileStep;
     const int kEnd = min(p.K, kBegin + p.stepsPerSplit * kTileStep);
-    const int steps = p.pairs * ((kEnd - kBegin + kTileStep - 1) / kTileStep);
-    int k = kBegin, pair = 0;       // of the next request
-    long long planeA = p.planeA[0], planeB = p.planeB[0];
+    const int steps = (kEnd - kBegin + kTileStep - 1) / kTileStep;
+    int k = kBegin;       // of the next request
     auto request = [&](int stage) __attribute__((always_inline)) {
-        if (pair >= p.pairs) return;
+        if (k >= kEnd) return;
         uint8_t *to = lds + stage * Cfg::STAGE_BYTES;
-        copyA.request(to, wave, k, kEnd, planeA);
-        copyB.request(to + BM * 128, wave, k, kEnd, planeB);
+        copyA.request(to, wave, k, kEnd);
+        copyB.request(to + BM * 128, wave, k, kEnd);
         k += kTileStep;
-        if (k >= kEnd) {
-            k = kBegin;
-            if (++pair < p.pairs) {
-                planeA = p.planeA[pair];
-                planeB = p.planeB[pair];
-            }
-        }
     };
     auto arrived = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_s_waitcnt(0x0F70);      // the copies have landed
@@ -245,9 +277,26 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
 #pragma unroll
     for (int j = 0; j < FN; ++j) b[0][j] = readB.read(lds + BM * 128, 0, j);
 
+    // (backward filter) The sums of the first operand's rows over the reduction: the tiles of a row of tiles, which share these rows, take them
+    // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every sixteenth k row, which hold the same
+    // eight rows of the operand.  (A second body of the step with products with ones among the others spilled registers.  So the sums cost nothing
+    // that shows: 8192 x 4096 -> 4096, 252 us with them and 253 without, and the sum over the tiles 4 us.)
+    Eight sum = {};
+    int turn = Cfg::SA && p.columnParts ? tn : -1;   // steps until the next one whose sums are this tile's
+
     int cur = 0;
     for (int s = 0; s < steps; ++s) {
         const uint8_t *stage = lds + cur * Cfg::STAGE_BYTES, *next = lds + (cur ^ 1) * Cfg::STAGE_BYTES;
+        if constexpr (Cfg::SA) {
+            if (turn == 0)
+#pragma unroll
+                for (int i = 0; i < kTileStep / 16; ++i) {
+                    const Eight q = load8<bf16_t>(stage, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
+                }
+            turn = turn == 0 ? p.tilesN - 1 : turn - 1;
+        }
 #pragma unroll
         for (int t = 0; t < SLOTS; ++t) {
             if (t == SLOTS - 2) {
@@ -269,42 +318,25 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         cur ^= 1;
     }
 
-    // Lane l holds row 16 i + l % 16, columns 16 j + 4 (l / 16) + 0..3 of the wavefront's results.  They go through the wavefront's share of
-    // the LDS (its 16-byte pieces permuted within a row by the row's number), PASS_ROWS rows at a time, so that eight lanes write 128 or 256
-    // adjacent bytes of a row of y.
     __syncthreads();   // (every read and every copy is done: the last request was waited for)
-    constexpr int WN = FN * 16, PIECES = WN / 4;
-    constexpr int PASS_FRAGS = Cfg::LDS_BYTES / Cfg::WAVES / (16 * WN * 4) < FM ? Cfg::LDS_BYTES / Cfg::WAVES / (16 * WN * 4) : FM;
-    constexpr int PASSES = FM / PASS_FRAGS, LANES = WN / 8, AT_ONCE = 64 / LANES;
-    static_assert(PASSES * PASS_FRAGS == FM, "whole passes");
-    f32x4 *mine = reinterpret_cast<f32x4 *>(lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES));
-    const int l16 = lane & 15, g = lane >> 4, c8 = lane % LANES, n = n0 + wn * WN + c8 * 8;
-    Eight bias;
+    write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0 + wm * FM * 16, n0 + wn * FN * 16, acc);
+    if constexpr (Cfg::SA) {
+        if (p.columnParts) {
+            typedef OperandCopy<BM, Cfg::WAVES, true> Copy;
+            static_assert(Cfg::THREADS == 16 * Copy::PIECES, "16 k rows at a time");
+            float *sums = reinterpret_cast<float *>(lds);   // [16][BM]
+            const int kr = (int)threadIdx.x / Copy::PIECES, piece = ((int)threadIdx.x % Copy::PIECES) ^ (Copy::twist(kr) << 1);
+            __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) bias.v[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.f;
-    for (int pass = 0; pass < PASSES; ++pass) {
-        // (which accumulators is known at compile time: an index into registers)
+            for (int e = 0; e < 8; ++e) sums[kr * BM + piece * 8 + e] = sum.v[e];
+            __syncthreads();
+            for (int m = threadIdx.x; m < BM && m0 + m < p.M; m += Cfg::THREADS) {
+                float v = 0.f;
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q)
-            if (pass == q)
-#pragma unroll
-                for (int i = 0; i < PASS_FRAGS; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) mine[(i * 16 + l16) * PIECES + ((j * 4 + g) ^ (l16 & (PIECES - 1)))] = acc[q * PASS_FRAGS + i][j];
-        __builtin_amdgcn_wave_barrier();
-        for (int r = lane / LANES; r < PASS_FRAGS * 16; r += AT_ONCE) {
-            const int m = m0 + (wm * FM + pass * PASS_FRAGS) * 16 + r;
-            const f32x4 lo = mine[r * PIECES + ((2 * c8) ^ (r & 15 & (PIECES - 1)))], hi = mine[r * PIECES + ((2 * c8 + 1) ^ (r & 15 & (PIECES - 1)))];
-            if (m >= p.M || n >= p.N) continue;
-            const Eight d = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (p.splits > 1) store8<float>(p.parts, ((long long)split * p.M + m) * p.partsRow + n, d);
-            else if (p.vec && n + 8 <= p.N) finish8<TO>(p, m, n, d, bias);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + e < p.N) finish_element<TO>(p, m, n + e, d.v[e]);
+                for (int i = 0; i < 16; ++i) v += sums[i * BM + m];
+                p.columnParts[(long long)(split * p.tilesN + tn) * p.M + m0 + m] = v;
+            }
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 

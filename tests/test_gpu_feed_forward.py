@@ -1,7 +1,8 @@
 """Layer norm and the matrix products with their epilogues on the GPU, element by element against the formulas in 64 bits.
 
 Tolerances.  u: half a step of the result's type; e = 2^-24 (2^-53 for double).  A sum of n products in any order is off by at
-most (n + 4) e times the sum of the products' magnitudes; float products taken in three parts add 2^-22 of a product.  What
+most (n + 4) e times the sum of the products' magnitudes; float products taken in three parts (8 bits of the
+significand each, m < 2^-7 and l < 2^-15 of the number) leave out m l + l m + l l, less than 2^-21 + 2^-30 of a product.  What
 follows the sum has slopes of at most 1.13 (GELU), 1.1 (SiLU) or 1; the activations computed for bfloat16 results are off by up
 to 4e-7 (1 + |z|) (the polynomial's 1.5e-7, the exponential, the reciprocal), those for float results by 4e (1 + |z|)."""
 import numpy as np
@@ -194,7 +195,7 @@ def linear_case(types, M, C, K):
 
 
 def sum_error(n, magnitude, dtype):
-    return ((n + 4) * 2.0 ** -24 + (2.0 ** -22 if dtype == "f32" else 0)) * magnitude
+    return ((n + 4) * 2.0 ** -24 + (2.0 ** -21 + 2.0 ** -30 if dtype == "f32" else 0)) * magnitude
 
 
 @pytest.mark.parametrize("lend", [True, False], ids=["workspace", "alone"])
@@ -265,7 +266,7 @@ def test_linear_backward_filter(types, layout, lend):
     u, ig = _u(), _u().ig
     dtype, out = types
     h, half = u.handle(), u.HALF_STEP[out]
-    for M, C, K in LINEAR_SHAPES + [(2000, 64, 72), (1111, 65, 33)]:
+    for M, C, K in LINEAR_SHAPES + [(2000, 64, 72), (1111, 65, 33), (1, 600, 520), (4000, 8, 300)]:
         rng, x, _, dy = linear_case(types, M, C, K)
         old, oldb = rounded(normal(rng, K, C), out), rounded(normal(rng, K), "f32")
         X, DY = u.Rows(x, dtype, *layout), u.Rows(dy, dtype, *layout)
@@ -283,6 +284,38 @@ def test_linear_backward_filter(types, layout, lend):
             u.close(DW.numpy(), ww, tol + 1.01 * half * np.abs(ww) + 1e-30, "dw")
             if with_bias:
                 u.close(DB.double().cpu().numpy(), wb, (M + 8) * 2.0 ** -24 * (np.abs(dy).sum(0) + np.abs(beta * oldb)) + 1e-30, "dbias")
+
+
+@pytest.mark.parametrize("lend", [True, False], ids=["workspace", "alone"])
+@pytest.mark.parametrize("types", LINEAR_TYPES, ids="-".join)
+def test_products_with_infinities_and_nan(types, lend):
+    """An infinite factor makes its row of results infinite (of the other factor's sign) or, against an infinity of the other sign or a
+    zero, undefined, as a sum of products is; every other row stays as it was.  Large and small finite numbers keep their products."""
+    u, ig = _u(), _u().ig
+    dtype, out = types
+    h = u.handle()
+    M, C, K = 40, 100, 72
+    rng, x, w, _ = linear_case(types, M, C, K)
+    x[3, 7], x[5, 9], x[8, 11], x[9, 99] = np.inf, -np.inf, np.nan, 3.0e38
+    x[20] *= 2.0 ** -90
+    x[11, 4], x[11, 60] = np.inf, -np.inf
+    w[6, 7], w[7, 9] = 0.0, 2.0 ** -60
+    w[:, 99] = np.sign(w[:, 99]) * 0.25
+    w[30, 7] = 1.0
+    x, w = rounded(x, dtype), rounded(w, dtype)
+    X, W, WD, Y = u.Rows(x, dtype), u.vector(w, dtype), u.filter_desc(dtype, K, C), u.Rows((M, K), out)
+    size = ig.get_linear_forward_workspace_size(h, X.desc, WD, Y.desc) if lend else 0
+    ws = u.Workspace(size)
+    ig.check(ig.linear_forward(h, 1.0, X.desc, X.ptr, WD, W.data_ptr(), ws.buf.data_ptr() if lend else 0, size, 0, -1, 0.0, None, 0, Y.desc, 0, Y.ptr))
+    got = Y.view.double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = (x[:, None, :] * w[None, :, :]).sum(2)
+        scale = (np.abs(x)[:, None, :] * np.abs(w)[None, :, :]).sum(2)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.isinf(got), np.isinf(want)) and np.array_equal(got[np.isinf(got)], want[np.isinf(want)])
+    fin = np.isfinite(want)
+    tol = sum_error(C, scale[fin], dtype) + 1.01 * u.HALF_STEP[out] * np.abs(want[fin])
+    assert np.all(np.abs(got[fin] - want[fin]) <= tol)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
