@@ -62,17 +62,22 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Til
     const uint8_t *from = static_cast<const uint8_t *>(of_a ? p.a : p.b) + skip;
     long long left = steps_all * step_bytes - skip;      // bytes from there to the operand's end (past it: zeros)
     int to_request = steps, request_stage = 0;
-    auto request = [&]() __attribute__((always_inline)) {
-        const uint32_t bytes = to_request > 0 && left > 0 ? (uint32_t)(left < 0x7FFFFFFFll ? left : 0x7FFFFFFFll) : 0u;   // (past the last step: nothing is read, the counts stay alike)
-        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(from), 0, bytes, 0x00020000u);
-        uint8_t *to = lds + request_stage * Cfg::STAGE_BYTES + wave * R * kUnitBytes;
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(to + i * kUnitBytes), 16, (uint32_t)(i * kUnitBytes + lane * 16), 0, 0, 0);
+    u32x4 buf;
+    uint32_t to;
+    auto begin_requests = [&]() __attribute__((always_inline)) {
+        // (past the last step: nothing is read, the counts stay alike)
+        buf = raw_buffer(from, to_request > 0 && left > 0 ? (uint32_t)(left < 0x7FFFFFFFll ? left : 0x7FFFFFFFll) : 0u);
+        to = lds_address(lds) + request_stage * Cfg::STAGE_BYTES + wave * R * kUnitBytes;
         --to_request;
         from += step_bytes;
         left -= step_bytes;
         request_stage = request_stage == Cfg::STAGES - 1 ? 0 : request_stage + 1;
+    };
+    // third g of a step's requests (a few to a slot: eight wavefronts with all of theirs at once wait for each other's)
+    auto request = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i * 3 / R == g) copy_to_lds(buf, to + i * kUnitBytes, (uint32_t)(i * kUnitBytes + lane * 16));
     };
     constexpr int kAllButOneStep = 0x0F70 | (R & 15) | ((R >> 4) << 14);
 
@@ -94,11 +99,17 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Til
     // the sums of the first operand's rows are products with ones, the tiles of a row of tiles in turns, a step each
     int turn = p.columnParts ? tn : -1;
 
-    request();
-    request();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        begin_requests();
+        request(0);
+        request(1);
+        request(2);
+    }
     __builtin_amdgcn_s_waitcnt(kAllButOneStep);
     asm volatile("s_barrier" ::: "memory");
-    request();
+    begin_requests();
+    request(0);
     bf16x8 a[2][kFloatParts], b[2][FN][kFloatParts];
     read(a[0], lds + at_a);
 #pragma unroll
@@ -116,13 +127,15 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Til
                 __builtin_amdgcn_s_waitcnt(0xC07F);            // this wavefront's reads of the stage are done
                 __builtin_amdgcn_s_waitcnt(kAllButOneStep);    // its copies into the next one have landed
                 asm volatile("s_barrier" ::: "memory");
-                request();
+                begin_requests();
+                request(0);
                 read(a[(t + 1) & 1], next + at_a);
 #pragma unroll
                 for (int j = 0; j < FN; ++j) read(b[P ^ 1][j], next + at_b + j * kFloatParts * kUnitBytes);
             } else {
                 read(a[(t + 1) & 1], here + at_a + (t + 1) * kFloatParts * kUnitBytes);
             }
+            if (t < 2) request(t + 1);   // (of the step that the barrier before gave its place)
             constexpr int part_a[6] = {2, 0, 1, 1, 0, 0}, part_b[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
             for (int q = 0; q < 6; ++q)
@@ -140,7 +153,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Til
         else step(parity, Constant<0>());
         turn = turn == 0 ? p.tilesN - 1 : turn - 1;
     };
-    static_assert(FM % 2 == 0, "a step leaves the fragments where the next expects them");
+    static_assert(FM % 2 == 0 && FM > 2, "a step leaves the fragments where the next expects them");
     int s = 0;
     for (; s + 1 < steps; s += 2) {
         either(Constant<0>());

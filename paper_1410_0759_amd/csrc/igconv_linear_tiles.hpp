@@ -1,17 +1,17 @@
 // Products of bfloat16 matrices whose rows lie on 16-byte boundaries (float ones: igconv_linear_float.hpp).
 //
 // A workgroup computes a BM x BN tile in steps of 64 of the reduction; a wavefront of it WM x WN results with
-// v_mfma_f32_16x16x32_bf16.  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), one step
-// into each of two stages.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
+// v_mfma_f32_16x16x32_bf16.  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), two steps
+// ahead.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
 // read 16 bytes per lane; one whose reduction index runs along the rows (w for backward data, x and dy for backward filter)
 // lies there as it is, k by k, and is read with the transposing 8-byte reads - no operand is transposed in memory.  In both cases
 // the 16-byte (32-byte) pieces of a row are permuted by an exclusive or with the row's number so that the lanes of a read lie
 // in different banks; the permutation is made on the global side of the copy, whose LDS side is fixed.
 //
-// A step is 2 x FM slots of FN matrix instructions.  Fragments of the first operand are read two slots ahead, those of the
-// second half a step ahead.  Two slots before the end every read of the stage has been requested: the wavefronts meet at
-// the step's only barrier, the stage is given to the copies of the step after next, and the remaining matrix instructions cover
-// the first reads of the other stage.
+// A step is 2 x FM slots of FN matrix instructions.  Fragments of the first operand are read two slots ahead; those of the second operand's
+// second half in the first quarter of the step, after which its place in LDS is free: there, at a first barrier, the step after next is
+// requested (three places for the first operand, two for the second: all of the LDS with 256 x 256).  Two slots before the end, at a second
+// barrier, the next step has to be there; the remaining matrix instructions cover its first reads.
 #ifndef IGCONV_LINEAR_TILES_HPP_
 #define IGCONV_LINEAR_TILES_HPP_
 
@@ -26,6 +26,19 @@ using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kNowhere = 0x80000000u;        // an offset outside every buffer: the load brings zeros
+
+// 16 bytes per lane from global memory into LDS at `to`, lane after lane; past the buffer's end: zeros.  In assembly (there is no register that
+// it writes) because the compiler puts a wait for every such copy under way before each transposing read, which no alias information keeps
+// it from: 8192^3 by backward filter 1060 us as against 796.  The waits are the kernels' own: `arrived`.
+__device__ __forceinline__ void copy_to_lds(const u32x4 &buffer, uint32_t to, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buffer) : "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t *)p; }
+// the words of a raw buffer descriptor
+__device__ __forceinline__ u32x4 raw_buffer(const void *base, uint32_t bytes) {
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+}
 
 // One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand.
 // STRIDED: the reduction index runs along the rows of the matrix in memory (`stride` elements apart), the tile's rows are adjacent.
@@ -60,24 +73,27 @@ struct OperandCopy {
         }
     }
 
-    // requests the step that begins at reduction index k (of K)
-    __device__ __forceinline__ void request(uint8_t *stage, int wave, int k, int K) const {
-        const long long skip = STRIDED ? (long long)k * (stride_bytes / 2u) : 0;
+    // the step that begins at reduction index k (of K), to be copied to `to`; not live: reads nothing, the counts of requests stay alike
+    u32x4 buf;
+    uint32_t to;
+    int k, K;
+    __device__ __forceinline__ void begin(uint8_t *stage, int wave, int k_, int K_, bool live) {
+        const long long skip = STRIDED ? (long long)k_ * (stride_bytes / 2u) : 0;
         const long long bytes = (left - skip) * 2;
-        const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(base + skip), 0,
-                                                                            (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll), 0x00020000u);
-        uint8_t *to = stage + wave * REQUESTS * 1024;
-#pragma unroll
-        for (int i = 0; i < REQUESTS; ++i) {
-            uint32_t off;
-            if constexpr (STRIDED) {
-                const int kr = k_piece + i * KROWS;
-                off = (uint32_t)kr * stride_bytes + (first ^ (uint32_t)(twist(kr) << 1)) * 16u;
-            } else {
-                off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * 2u : kNowhere;
-            }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(to + i * 1024), 16, off, 0, 0, 0);
+        buf = raw_buffer(base + skip, live ? (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll) : 0u);
+        to = lds_address(stage) + wave * REQUESTS * 1024;
+        k = k_;
+        K = K_;
+    }
+    __device__ __forceinline__ void request(int i) const {
+        uint32_t off;
+        if constexpr (STRIDED) {
+            const int kr = k_piece + i * KROWS;
+            off = (uint32_t)kr * stride_bytes + (first ^ (uint32_t)(twist(kr) << 1)) * 16u;
+        } else {
+            off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * 2u : kNowhere;
         }
+        copy_to_lds(buf, to + i * 1024, off);
     }
 };
 
@@ -174,7 +190,10 @@ struct TileConfig {
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N;
     static constexpr bool SA = SA_, SB = SB_;
     static constexpr int FM = BM / WAVES_M / 16, FN = BN / WAVES_N / 16;
-    static constexpr int STAGE_BYTES = (BM + BN) * kTileStep * 2, LDS_BYTES = 2 * STAGE_BYTES;
+    // slots of the rings of both operands' steps: a step of B is free again within its own step, one of A after it
+    static constexpr int SLOTS_A = 3, SLOTS_B = 2, BYTES_A = BM * kTileStep * 2, BYTES_B = BN * kTileStep * 2;
+    static constexpr int LDS_BYTES = SLOTS_A * BYTES_A + SLOTS_B * BYTES_B;
+    static_assert(LDS_BYTES <= 160 * 1024, "");
     static constexpr int THREADS = 64 * WAVES;
 };
 
@@ -195,7 +214,7 @@ __device__ __forceinline__ bool tile_of(const TileArgs &p, int *tm, int *tn, int
 template <int FM, int FN, int SHARE, class TO>
 __device__ __forceinline__ void write_results(const TileArgs &p, uint8_t *share, int lane, int split, int m0, int n0, const f32x4 (&acc)[FM][FN]) {
     constexpr int WN = FN * 16, PIECES = WN / 4;
-    constexpr int PASS_FRAGS = SHARE / (16 * WN * 4) < FM ? SHARE / (16 * WN * 4) : FM;
+    constexpr int ROOM = SHARE / (16 * WN * 4), PASS_FRAGS = ROOM >= FM ? FM : (ROOM >= 4 ? 4 : (ROOM >= 2 ? 2 : 1));
     constexpr int PASSES = FM / PASS_FRAGS, LANES = WN / 8, AT_ONCE = 64 / LANES;
     static_assert(PASSES * PASS_FRAGS == FM, "whole passes");
     f32x4 *mine = reinterpret_cast<f32x4 *>(share);
@@ -231,7 +250,7 @@ __device__ __forceinline__ void write_results(const TileArgs &p, uint8_t *share,
 
 template <class Cfg, class TO>
 __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const TileArgs p) {
-    constexpr int BM = Cfg::BM, BN = Cfg::BN, FM = Cfg::FM, FN = Cfg::FN, SLOTS = 2 * FM;
+    constexpr int BM = Cfg::BM, BN = Cfg::BN, FM = Cfg::FM, FN = Cfg::FN, SLOTS = 2 * FM, FREE = FM / 2;
     __shared__ __attribute__((aligned(16))) uint8_t lds[Cfg::LDS_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / Cfg::WAVES_N, wn = wave % Cfg::WAVES_N;
@@ -250,16 +269,23 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     const int kBegin = split * p.stepsPerSplit * kTileStep;
     const int kEnd = min(p.K, kBegin + p.stepsPerSplit * kTileStep);
     const int steps = (kEnd - kBegin + kTileStep - 1) / kTileStep;
-    int k = kBegin;       // of the next request
-    auto request = [&](int stage) __attribute__((always_inline)) {
-        if (k >= kEnd) return;
-        uint8_t *to = lds + stage * Cfg::STAGE_BYTES;
-        copyA.request(to, wave, k, kEnd);
-        copyB.request(to + BM * 128, wave, k, kEnd);
+    int k = kBegin, slotA = 0, slotB = 0;       // of the next request
+    uint8_t *const ldsB = lds + Cfg::SLOTS_A * Cfg::BYTES_A;
+    constexpr int RA = OperandCopy<BM, Cfg::WAVES, Cfg::SA>::REQUESTS, RB = OperandCopy<BN, Cfg::WAVES, Cfg::SB>::REQUESTS, R = RA + RB;
+    auto begin_requests = [&]() __attribute__((always_inline)) {
+        const bool live = k < kEnd;
+        copyA.begin(lds + slotA * Cfg::BYTES_A, wave, k, kEnd, live);
+        copyB.begin(ldsB + slotB * Cfg::BYTES_B, wave, k, kEnd, live);
         k += kTileStep;
+        slotA = slotA == Cfg::SLOTS_A - 1 ? 0 : slotA + 1;
+        slotB ^= 1;
     };
-    auto arrived = [&]() __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);      // the copies have landed
+    auto request = [&](int i) __attribute__((always_inline)) {
+        if (i < RA) copyA.request(i);
+        else copyB.request(i - RA);
+    };
+    auto arrived = [&]() __attribute__((always_inline)) {     // all but the last step requested
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (R & 15) | ((R >> 4) << 14));
         asm volatile("s_barrier" ::: "memory");
     };
 
@@ -268,14 +294,18 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    request(0);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        begin_requests();
+#pragma unroll
+        for (int i = 0; i < R; ++i) request(i);
+    }
     arrived();
-    request(1);
     bf16x8 a[4], b[2][FN];
     a[0] = readA.read(lds, 0, 0);
     a[1] = readA.read(lds, 0, 1);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) b[0][j] = readB.read(lds + BM * 128, 0, j);
+    for (int j = 0; j < FN; ++j) b[0][j] = readB.read(ldsB, 0, j);
 
     // (backward filter) The sums of the first operand's rows over the reduction: the tiles of a row of tiles, which share these rows, take them
     // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every sixteenth k row, which hold the same
@@ -284,14 +314,18 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     Eight sum = {};
     int turn = Cfg::SA && p.columnParts ? tn : -1;   // steps until the next one whose sums are this tile's
 
-    int cur = 0;
+    constexpr int PER_SLOT = (R + SLOTS - 2 - FREE - 1) / (SLOTS - 2 - FREE);
+    int atA = 0, atB = 0;
     for (int s = 0; s < steps; ++s) {
-        const uint8_t *stage = lds + cur * Cfg::STAGE_BYTES, *next = lds + (cur ^ 1) * Cfg::STAGE_BYTES;
+        const uint8_t *hereA = lds + atA * Cfg::BYTES_A, *hereB = ldsB + atB * Cfg::BYTES_B;
+        atA = atA == Cfg::SLOTS_A - 1 ? 0 : atA + 1;
+        atB ^= 1;
+        const uint8_t *nextA = lds + atA * Cfg::BYTES_A, *nextB = ldsB + atB * Cfg::BYTES_B;
         if constexpr (Cfg::SA) {
             if (turn == 0)
 #pragma unroll
                 for (int i = 0; i < kTileStep / 16; ++i) {
-                    const Eight q = load8<bf16_t>(stage, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
+                    const Eight q = load8<bf16_t>(hereA, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
                 }
@@ -299,26 +333,31 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         }
 #pragma unroll
         for (int t = 0; t < SLOTS; ++t) {
-            if (t == SLOTS - 2) {
-                __builtin_amdgcn_s_waitcnt(0xC07F);   // this wavefront's reads of the stage are done
-                arrived();
-                request(cur);
+            if (t == FREE) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);   // this wavefront's reads of B's step, and of A's step before, are done
+                asm volatile("s_barrier" ::: "memory");
+                begin_requests();
             }
-            if (t + 2 < SLOTS) a[(t + 2) % 4] = readA.read(stage, (t + 2) / FM, (t + 2) % FM);
-            else a[(t + 2) % 4] = readA.read(next, 0, t + 2 - SLOTS);
+            if (t == SLOTS - 2) arrived();
+            // (a few to a slot: eight wavefronts with eight requests each at once wait for each other's)
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (t == FREE + i / PER_SLOT) request(i);
+            if (t + 2 < SLOTS) a[(t + 2) % 4] = readA.read(hereA, (t + 2) / FM, (t + 2) % FM);
+            else a[(t + 2) % 4] = readA.read(nextA, 0, t + 2 - SLOTS);
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                if (t == (FM >= FN ? FM - FN + j : j * FM / FN)) b[1][j] = readB.read(stage + BM * 128, 1, j);
-                if (t >= SLOTS - 2 && j / ((FN + 1) / 2) == t - (SLOTS - 2)) b[0][j] = readB.read(next + BM * 128, 0, j);
+                if (t == j * FREE / FN) b[1][j] = readB.read(hereB, 1, j);
+                if (t >= SLOTS - 2 && j / ((FN + 1) / 2) == t - (SLOTS - 2)) b[0][j] = readB.read(nextB, 0, j);
             }
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[t % FM][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[t / FM][j], a[t % 4], acc[t % FM][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
-        cur ^= 1;
     }
 
-    __syncthreads();   // (every read and every copy is done: the last request was waited for)
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // (nothing may be on its way into LDS)
+    __syncthreads();
     write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0 + wm * FM * 16, n0 + wn * FN * 16, acc);
     if constexpr (Cfg::SA) {
         if (p.columnParts) {
