@@ -260,10 +260,10 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
     __shared__ W slots[2][2][norm_threads(LANES) / 64];
     const int t = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     const W *scale_p = static_cast<const W *>(a.scale), *shift_p = static_cast<const W *>(a.shift);
+    constexpr bool ROOM = LANES < 1024;     // (1024 threads of 128 registers hold the row only)
     W scale[CHUNKS][E], shift[CHUNKS][E];   // alpha times
     const Place<LANES, CHUNKS, E, WHOLE> at(t, a.C);
-#pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) {
+    auto load_params = [&](int j) __attribute__((always_inline)) {
         Chunk<W, E> sc, sh;
 #pragma unroll
         for (int e = 0; e < E; ++e) sc.v[e] = W(1), sh.v[e] = W(0);
@@ -271,7 +271,10 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
         if (shift_p && at.live[j]) load_chunk(sh, shift_p + at.c[j]);
 #pragma unroll
         for (int e = 0; e < E; ++e) scale[j][e] = a.alpha * sc.v[e], shift[j][e] = a.alpha * sh.v[e];
-    }
+    };
+    if (ROOM)
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) load_params(j);
     const int stride = (int)gridDim.x * ROWS;
     int row = (int)blockIdx.x * ROWS + sub;
     Chunk<TX, E> raw[CHUNKS];
@@ -281,9 +284,10 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
         for (int j = 0; j < CHUNKS; ++j)
             if (at.live[j]) load_chunk(raw[j], x + at.c[j]);
     };
-    if (row < a.M) load(row);
+    if (ROOM && row < a.M) load(row);
     // (the rows of a workgroup's wavefronts end together but for the last round: with LANES = 64 there is no barrier in the loop)
     for (int parity = 0; row < a.M; row += stride, parity ^= 1) {
+        if (!ROOM) load(row);
         W x[CHUNKS][E];
         W sum = W(0);
 #pragma unroll
@@ -301,7 +305,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) load_chunk(old[j], y + at.c[j]);
-        if (row + stride < a.M) load(row + stride);
+        if (ROOM && row + stride < a.M) load(row + stride);
         const W mean = row_sum<LANES>(sum, slots[parity][0]) / W(a.C);
         W squares = W(0);
 #pragma unroll
@@ -317,6 +321,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (!at.live[j]) continue;
+            if (!ROOM) load_params(j);
             W out[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) out[e] = x[j][e] * s * scale[j][e] + shift[j][e];
@@ -516,6 +521,8 @@ bool by_shape(int C, bool f64, F f) {
     if (chunks <= 512) return f(Shape<256, 2>()), true;
     if (chunks <= 1024) return f(Shape<512, 2>()), true;
     if (chunks <= 2048) return f(typename std::conditional<BACKWARD, Shape<1024, 2>, Shape<512, 4>>::type()), true;
+    if constexpr (!BACKWARD)
+        if (chunks <= 4096) return f(Shape<1024, 4>()), true;
     return false;
 }
 

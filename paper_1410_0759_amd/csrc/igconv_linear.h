@@ -35,7 +35,6 @@ struct TileArgs : LinearArgs {
     int splits, stepsPerSplit;     // the reduction in ranges of steps
     float *parts;                  // [split][M][partsRow] (partsRow: N rounded up to 8), where splits > 1
     long long partsRow;
-    int vec;                       // the epilogue's matrices allow 16-byte accesses at every eighth column
     float *columnParts;            // [split][tile column][M]: sums of the first operand's rows, or null
     int blocksA, blocksB;          // (float) blocks of 16 rows of the operands
 };
@@ -46,7 +45,7 @@ struct TileKernel {
     const void *kernel;   // null: not offered
 };
 constexpr int kTileShapes = 3;
-TileKernel float_kernel();                                     // any pass, operands in parts (igconv_linear_float.hpp)
+TileKernel float_kernel();                                           // any pass, operands in parts (igconv_linear_float.hpp)
 TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent
 TileKernel tile_kernel_rows_columns(int shape, bool f32_out);  // backward data: B strided
 TileKernel tile_kernel_columns(int shape, bool f32_out);       // backward filter: both strided

@@ -171,6 +171,7 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
     const int m = (int)(id / groups), n = (int)(id % groups) * 8;
     if (m >= p.M) return;
     Eight d = load8<float>(p.parts, (long long)m * p.partsRow + n);
+#pragma unroll 4
     for (int s = 1; s < p.splits; ++s) {
         const Eight q = load8<float>(p.parts, ((long long)s * p.M + m) * p.partsRow + n);
 #pragma unroll
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
     Eight bias;
 #pragma unroll
     for (int e = 0; e < 8; ++e) bias.v[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.f;
-    if (p.vec && n + 8 <= p.N) {
+    if (n + 8 <= p.N) {
         finish8<TO>(p, m, n, d, bias);
     } else {
 #pragma unroll
@@ -346,13 +347,17 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
     return o;
 }
 
-// us of a step on one compute unit, that of two workgroups side by side where a compute unit holds two; measured on 8192^3 (float: 4096^3)
+// us of a step of a workgroup alone on its compute unit and with another beside it, and of a tile's start and epilogue.  Measured: forward 8192^3 is 512
+// steps of 256 x 256, 786 us, or 1024 of 128 x 128 two by two, 1003; 2048^3 32 steps, 44, 21.4 (alone) and, 64 x 128 two by two, 24.7;
+// 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.
 struct ShapeCost {
     int per_cu;
-    double alone, full, ends;   // ends: start and epilogue of a tile
+    double alone, full, ends, bytes;   // bytes: what it reads from memory per us (8 x 4096 -> 16384: 128 workgroups 26.5 us, 256 23.8)
 };
-constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.72, 1.72, 7.0}, {2, 0.60, 1.03, 5.0}, {2, 0.60, 1.03, 5.0}};
-constexpr ShapeCost kFloatCost = {1, 1.0, 1.0, 6.0};
+constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0, 90e3}, {2, 0.45, 0.98, 2.5, 45e3}, {2, 0.42, 0.60, 2.0, 30e3}};
+constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0, 90e3};
+// The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory.
+constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6;
 
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, bool aligned_a, bool aligned_b, size_t room) {
     TilePlan pl;
@@ -378,7 +383,9 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         if (at + parts + sum_bytes > room || units >= (1ll << 27)) return;
         const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
         const double full = per * sc.full + sc.ends, one = per * sc.alone + sc.ends;
-        const double us = whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)) + (splits > 1 ? 4.0 + (double)parts * 2 / 4e6 : 0.0);
+        const double memory = (double)(a.K * ((long long)a.M + a.N) * elem_size(in)) / std::min(kMemoryBytes, units * sc.bytes);
+        const double us = std::max(whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)), memory) +
+                          (splits > 1 ? kPartsLaunch + (double)parts * 2 / kPartsBytes : 0.0);
         if (us >= best) return;
         best = us;
         pl.tiles = true;
@@ -446,9 +453,6 @@ igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const
         t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
         t.partsRow = round_up(a.N, 8);
         t.columnParts = sums.out ? reinterpret_cast<float *>(ws + pl.sumsAt) : nullptr;
-        const long long per16 = 16 / elem_size(out);
-        t.vec = on16(a.y) && a.ys % per16 == 0 && (!a.z || on16(a.z)) && (!a.zin || (on16(a.zin) && a.zs % per16 == 0)) &&
-                (a.beta == 0.f || (on16(a.r) && a.rs % per16 == 0));
         rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
         if (rc == IGC_STATUS_SUCCESS && pl.splits > 1) {
             const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)

@@ -126,20 +126,24 @@ struct OperandReads {
     }
 };
 
-// eight neighbours of a row
+// eight neighbours of a row (which need not lie on a 16-byte boundary)
 struct Eight {
     float v[8];
+};
+template <class T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Adjacent {
+    T v[N];
 };
 template <class TO>
 __device__ __forceinline__ Eight load8(const void *p, long long at) {
     Eight r;
     if constexpr (sizeof(TO) == 4) {
-        const f32x4 *q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at);
-        const f32x4 lo = q[0], hi = q[1];
+        const Adjacent<float, 8> q = *reinterpret_cast<const Adjacent<float, 8> *>(static_cast<const float *>(p) + at);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r.v[e] = lo[e], r.v[4 + e] = hi[e];
+        for (int e = 0; e < 8; ++e) r.v[e] = q.v[e];
     } else {
-        const u32x4 q = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at);
+        const Adjacent<uint16_t, 8> a = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(static_cast<const uint16_t *>(p) + at);
+        const u32x4 q = __builtin_bit_cast(u32x4, a);
 #pragma unroll
         for (int e = 0; e < 4; ++e) r.v[2 * e] = bf16_bits_to_float(q[e]), r.v[2 * e + 1] = __builtin_bit_cast(float, q[e] & 0xFFFF0000u);
     }
@@ -148,17 +152,15 @@ __device__ __forceinline__ Eight load8(const void *p, long long at) {
 template <class TO>
 __device__ __forceinline__ void store8(void *p, long long at, const Eight &r) {
     if constexpr (sizeof(TO) == 4) {
-        f32x4 *q = reinterpret_cast<f32x4 *>(static_cast<float *>(p) + at);
-        q[0] = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
-        q[1] = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+        *reinterpret_cast<Adjacent<float, 8> *>(static_cast<float *>(p) + at) = __builtin_bit_cast(Adjacent<float, 8>, r);
     } else {
         u32x4 q;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = to_bf16_bits(r.v[2 * e]) | (uint32_t)to_bf16_bits(r.v[2 * e + 1]) << 16;
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = q;
+        for (int e = 0; e < 4; ++e) q[e] = to_bf16_pair(r.v[2 * e], r.v[2 * e + 1]);
+        *reinterpret_cast<Adjacent<uint16_t, 8> *>(static_cast<uint16_t *>(p) + at) = __builtin_bit_cast(Adjacent<uint16_t, 8>, q);
     }
 }
-// finish_element for eight results at once; the matrices allow 16-byte accesses there
+// finish_element for eight results at once
 template <class TO>
 __device__ __forceinline__ void finish8(const LinearArgs &a, int m, int n, Eight d, const Eight &bias) {
     constexpr bool FINE = sizeof(TO) == 4;
@@ -190,11 +192,12 @@ struct TileConfig {
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N;
     static constexpr bool SA = SA_, SB = SB_;
     static constexpr int FM = BM / WAVES_M / 16, FN = BN / WAVES_N / 16;
-    // slots of the rings of both operands' steps: a step of B is free again within its own step, one of A after it
-    static constexpr int SLOTS_A = 3, SLOTS_B = 2, BYTES_A = BM * kTileStep * 2, BYTES_B = BN * kTileStep * 2;
+    // Steps requested ahead, and the places of both operands' rings: a step of B is free again within its own step, one of A after it.  (Four ahead, for
+    // 128 x 128 tiles that leave room: 1000^3 17 us, two ahead 13.)
+    static constexpr int AHEAD = 2, SLOTS_A = AHEAD + 1, SLOTS_B = AHEAD, BYTES_A = BM * kTileStep * 2, BYTES_B = BN * kTileStep * 2;
     static constexpr int LDS_BYTES = SLOTS_A * BYTES_A + SLOTS_B * BYTES_B;
     static_assert(LDS_BYTES <= 160 * 1024, "");
-    static constexpr int THREADS = 64 * WAVES;
+    static constexpr int THREADS = 64 * WAVES, SUM_ROWS = THREADS / (BM / 8);
 };
 
 __device__ __forceinline__ bool tile_of(const TileArgs &p, int *tm, int *tn, int *split) {
@@ -238,7 +241,7 @@ __device__ __forceinline__ void write_results(const TileArgs &p, uint8_t *share,
             if (m >= p.M || n >= p.N) continue;
             const Eight d = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (p.splits > 1) store8<float>(p.parts, ((long long)split * p.M + m) * p.partsRow + n, d);
-            else if (p.vec && n + 8 <= p.N) finish8<TO>(p, m, n, d, bias);
+            else if (n + 8 <= p.N) finish8<TO>(p, m, n, d, bias);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -278,14 +281,15 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         copyB.begin(ldsB + slotB * Cfg::BYTES_B, wave, k, kEnd, live);
         k += kTileStep;
         slotA = slotA == Cfg::SLOTS_A - 1 ? 0 : slotA + 1;
-        slotB ^= 1;
+        slotB = slotB == Cfg::SLOTS_B - 1 ? 0 : slotB + 1;
     };
     auto request = [&](int i) __attribute__((always_inline)) {
         if (i < RA) copyA.request(i);
         else copyB.request(i - RA);
     };
-    auto arrived = [&]() __attribute__((always_inline)) {     // all but the last step requested
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (R & 15) | ((R >> 4) << 14));
+    constexpr int LATER = (Cfg::AHEAD - 1) * R;
+    auto arrived = [&]() __attribute__((always_inline)) {     // all but the steps after the next
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (LATER & 15) | ((LATER >> 4) << 14));
         asm volatile("s_barrier" ::: "memory");
     };
 
@@ -295,7 +299,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < Cfg::AHEAD; ++n) {
         begin_requests();
 #pragma unroll
         for (int i = 0; i < R; ++i) request(i);
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     for (int j = 0; j < FN; ++j) b[0][j] = readB.read(ldsB, 0, j);
 
     // (backward filter) The sums of the first operand's rows over the reduction: the tiles of a row of tiles, which share these rows, take them
-    // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every sixteenth k row, which hold the same
+    // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every sixteenth (32nd) k row, which hold the same
     // eight rows of the operand.  (A second body of the step with products with ones among the others spilled registers.  So the sums cost nothing
     // that shows: 8192 x 4096 -> 4096, 252 us with them and 253 without, and the sum over the tiles 4 us.)
     Eight sum = {};
@@ -319,12 +323,12 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     for (int s = 0; s < steps; ++s) {
         const uint8_t *hereA = lds + atA * Cfg::BYTES_A, *hereB = ldsB + atB * Cfg::BYTES_B;
         atA = atA == Cfg::SLOTS_A - 1 ? 0 : atA + 1;
-        atB ^= 1;
+        atB = atB == Cfg::SLOTS_B - 1 ? 0 : atB + 1;
         const uint8_t *nextA = lds + atA * Cfg::BYTES_A, *nextB = ldsB + atB * Cfg::BYTES_B;
         if constexpr (Cfg::SA) {
             if (turn == 0)
 #pragma unroll
-                for (int i = 0; i < kTileStep / 16; ++i) {
+                for (int i = 0; i < kTileStep / Cfg::SUM_ROWS; ++i) {
                     const Eight q = load8<bf16_t>(hereA, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
@@ -362,8 +366,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     if constexpr (Cfg::SA) {
         if (p.columnParts) {
             typedef OperandCopy<BM, Cfg::WAVES, true> Copy;
-            static_assert(Cfg::THREADS == 16 * Copy::PIECES, "16 k rows at a time");
-            float *sums = reinterpret_cast<float *>(lds);   // [16][BM]
+            static_assert(Cfg::SUM_ROWS % 16 == 0 && Cfg::SUM_ROWS * BM * 4 <= Cfg::LDS_BYTES, "");
+            float *sums = reinterpret_cast<float *>(lds);   // [SUM_ROWS][BM]
             const int kr = (int)threadIdx.x / Copy::PIECES, piece = ((int)threadIdx.x % Copy::PIECES) ^ (Copy::twist(kr) << 1);
             __syncthreads();
 #pragma unroll
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
             for (int m = threadIdx.x; m < BM && m0 + m < p.M; m += Cfg::THREADS) {
                 float v = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v += sums[i * BM + m];
+                for (int i = 0; i < Cfg::SUM_ROWS; ++i) v += sums[i * BM + m];
                 p.columnParts[(long long)(split * p.tilesN + tn) * p.M + m0 + m] = v;
             }
         }

@@ -11,7 +11,7 @@ static TileKernel entry(bool f32_out) {
 
 TileKernel tile_kernel_columns(int shape, bool f32_out) {
     if (shape == 0) return entry<TileConfig<256, 256, 2, 4, true, true>>(f32_out);
-    if (shape == 1) return entry<TileConfig<128, 128, 2, 2, true, true>>(f32_out);
+    if (shape == 1) return entry<TileConfig<128, 128, 2, 4, true, true>>(f32_out);
     return {};   // (a gradient of few features out is short anyway)
 }
 

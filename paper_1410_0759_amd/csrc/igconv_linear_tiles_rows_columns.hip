@@ -11,7 +11,7 @@ static TileKernel entry(bool f32_out) {
 
 TileKernel tile_kernel_rows_columns(int shape, bool f32_out) {
     if (shape == 0) return entry<TileConfig<256, 256, 2, 4, false, true>>(f32_out);
-    if (shape == 1) return entry<TileConfig<128, 128, 2, 2, false, true>>(f32_out);
+    if (shape == 1) return entry<TileConfig<128, 128, 2, 4, false, true>>(f32_out);
     if (shape == 2) return entry<TileConfig<64, 128, 1, 4, false, true>>(f32_out);   // few tokens
     return {};
 }
