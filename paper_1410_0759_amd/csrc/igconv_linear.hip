@@ -333,13 +333,16 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
     return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
 }
 
-// The matrix of an operand, and whether it has to be copied: bfloat16 rows on 16-byte boundaries, whole 16-byte pieces, no row inside another.
+// Rows of whole 16-byte pieces (of n elements) on 16-byte boundaries, if the first is, no row inside another; a tile's reach below 2^31 bytes.
+bool fits(const OperandPlan &o, int n) { return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && o.stride < (1ll << 22); }
+
+// The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
 OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
     OperandPlan o;
     o.rows = strided ? K : n;
     o.cols = (int)(strided ? n : K);
     o.stride = strided ? ks : ns;
-    o.pack = f32 || !aligned || o.cols % 8 != 0 || (o.rows > 1 && (o.stride % 8 != 0 || o.stride < o.cols));
+    o.pack = f32 || !aligned || !fits(o, 8);
     o.toRow = round_up(o.cols, 8);
     o.blocks = (int)((n + 15) / 16);
     if (o.pack)
@@ -355,29 +358,20 @@ struct ShapeCost {
     double alone, full, ends, bytes;   // bytes: what it reads from memory per us (8 x 4096 -> 16384: 128 workgroups 26.5 us, 256 23.8)
 };
 constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0, 90e3}, {2, 0.45, 0.98, 2.5, 45e3}, {2, 0.42, 0.60, 2.0, 30e3}};
-constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0, 90e3};
+constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0, 90e3}, kFewFloatCost = {2, 0.60, 0.95, 2.0, 30e3};
 // The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory.
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6;
 
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, bool aligned_a, bool aligned_b, size_t room) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
-    pl.a = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, aligned_a);
-    pl.b = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, aligned_b);
-    size_t at = 0;
-    for (OperandPlan *o : {&pl.a, &pl.b}) {
-        if (!f32 && (o->pack ? o->toRow : o->stride) >= (1ll << 22)) return pl;   // (a tile's reach stays within 31 bits)
-        o->at = at;
-        at += o->bytes;
-    }
-    if (at > room) return pl;
-    const int step = f32 ? kFloatStep : kTileStep, steps = (a.K + step - 1) / step;
+    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, aligned_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, aligned_b);
     double best = 1e300;
-    auto consider = [&](int shape, int splits) {
-        const TileKernel k = f32 ? float_kernel() : tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT);
-        const int per = (steps + splits - 1) / splits;
-        if (!k.kernel || (steps + per - 1) / per != splits) return;
-        const ShapeCost &sc = f32 ? kFloatCost : kShapeCost[shape];
+    // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
+    auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
+        const int steps = (a.K + step - 1) / step, per = (steps + splits - 1) / splits;
+        if (!k.kernel || splits > steps || (steps + per - 1) / per != splits) return;
+        const size_t at_b = copied ? oa.bytes : 0, at = copied ? oa.bytes + ob.bytes : 0;
         const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn, units = tm * tn * splits;
         const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0, sum_bytes = sums ? (size_t)(splits * tn) * a.M * 4 : 0;
         if (at + parts + sum_bytes > room || units >= (1ll << 27)) return;
@@ -385,18 +379,33 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         const double full = per * sc.full + sc.ends, one = per * sc.alone + sc.ends;
         const double memory = (double)(a.K * ((long long)a.M + a.N) * elem_size(in)) / std::min(kMemoryBytes, units * sc.bytes);
         const double us = std::max(whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)), memory) +
-                          (splits > 1 ? kPartsLaunch + (double)parts * 2 / kPartsBytes : 0.0);
+                          (splits > 1 ? kPartsLaunch + (double)parts * 2 / kPartsBytes : 0.0) + (at > 0 ? kPartsLaunch + (double)at * 2 / kMemoryBytes : 0.0);
         if (us >= best) return;
         best = us;
         pl.tiles = true;
         pl.k = k;
         pl.tilesM = (int)tm; pl.tilesN = (int)tn; pl.splits = splits; pl.stepsPerSplit = per;
+        pl.a = oa;
+        pl.b = ob;
+        pl.a.pack = oa.pack && copied;
+        pl.b.pack = ob.pack && copied;
+        pl.b.at = at_b;
         pl.partsAt = at;
         pl.sumsAt = at + parts;
         pl.bytes = at + parts + sum_bytes;
     };
-    for (int shape = 0; shape < (f32 ? 1 : kTileShapes); ++shape)
-        for (int splits = 1; splits <= 64 && splits <= steps; ++splits) consider(shape, splits);
+    constexpr int kMostSplits = 64;
+    if (f32) {
+        if (!sa && fits(oa, 4) && fits(ob, 4) && aligned_a && aligned_b)
+            for (int splits = 1; splits <= kMostSplits; ++splits) consider(few_float_kernel(sb), kFewFloatCost, kFloatStep, splits, false);
+        for (int splits = 1; splits <= kMostSplits; ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
+        return pl;
+    }
+    // (a tile's reach stays within 31 bits)
+    if ((oa.pack ? oa.toRow : oa.stride) >= (1ll << 22) || (ob.pack ? ob.toRow : ob.stride) >= (1ll << 22)) return pl;
+    for (int shape = 0; shape < kTileShapes; ++shape)
+        for (int splits = 1; splits <= kMostSplits; ++splits)
+            consider(tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), kShapeCost[shape], kTileStep, splits, true);
     return pl;
 }
 

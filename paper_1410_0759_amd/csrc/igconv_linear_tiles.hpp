@@ -1,11 +1,12 @@
-// Products of bfloat16 matrices whose rows lie on 16-byte boundaries (float ones: igconv_linear_float.hpp).
+// Products of matrices whose rows lie on 16-byte boundaries: bfloat16, and float with few tokens, where reading the filter is what takes the
+// time (more of them: igconv_linear_float.hpp).
 //
-// A workgroup computes a BM x BN tile in steps of 64 of the reduction; a wavefront of it WM x WN results with
-// v_mfma_f32_16x16x32_bf16.  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), two steps
+// A workgroup computes a BM x BN tile in steps of 128 bytes of the reduction, a wavefront of it FM x FN blocks of 16 x 16 with
+// v_mfma_f32_16x16x32_bf16 or v_mfma_f32_16x16x4_f32.  (Blocks of 32 x 32 are slower: 8192^3 814 us instead of 754.)  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), two steps
 // ahead.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
 // read 16 bytes per lane; one whose reduction index runs along the rows (w for backward data, x and dy for backward filter)
-// lies there as it is, k by k, and is read with the transposing 8-byte reads - no operand is transposed in memory.  In both cases
-// the 16-byte (32-byte) pieces of a row are permuted by an exclusive or with the row's number so that the lanes of a read lie
+// lies there as it is, k by k, and is read with the transposing 8-byte reads (float: 4 bytes at a time) - no operand is transposed in memory.  In both cases
+// the 16-byte (32-, 64-byte) pieces of a row are permuted by an exclusive or with the row's number so that the lanes of a read lie
 // in different banks; the permutation is made on the global side of the copy, whose LDS side is fixed.
 //
 // A step is 2 x FM slots of FN matrix instructions.  Fragments of the first operand are read two slots ahead; those of the second operand's
@@ -40,36 +41,38 @@ __device__ __forceinline__ u32x4 raw_buffer(const void *base, uint32_t bytes) {
     return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
 }
 
-// One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand.
+// One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand; elements of ELEM bytes.
 // STRIDED: the reduction index runs along the rows of the matrix in memory (`stride` elements apart), the tile's rows are adjacent.
-template <int ROWS, int WAVES, bool STRIDED>
+template <int ROWS, int WAVES, bool STRIDED, int ELEM>
 struct OperandCopy {
     static constexpr int REQUESTS = ROWS / 8 / WAVES;      // of 1 KB per wavefront and step
-    static constexpr int PIECES = ROWS / 8;                // (strided) 16-byte pieces of a k row
+    static constexpr int PIECES = ROWS * ELEM / 16;        // (strided) 16-byte pieces of a k row
     static constexpr int KROWS = 64 / PIECES;              // (strided) k rows per request
-    const uint16_t *base;
-    long long left;             // elements from `base` to the end of the operand
+    static constexpr int IN_PIECE = 16 / ELEM;
+    const uint8_t *base;
+    long long left;             // bytes from `base` to the end of the operand
     uint32_t stride_bytes, first;
     int k_piece;                // (not strided) the lane's first reduction index within a step
 
-    // (strided) the exclusive or of the 32-byte blocks of k row k
-    static __device__ __forceinline__ int twist(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
+    // (strided) the exclusive or of the pieces of k row k: the rows that a read takes at once lie in different banks
+    static __device__ __forceinline__ int twist(int k) { return ELEM == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2; }
 
     __device__ __forceinline__ void init(const void *matrix, long long row_stride, long long k_stride, int row0, int rows, int K, int lane, int wave) {
+        // (whole pieces: a matrix whose rows do not end with one is a copy that does)
         if constexpr (STRIDED) {
-            base = static_cast<const uint16_t *>(matrix) + row0;
-            left = (K - 1) * k_stride + ((rows + 7) & ~7) - row0;   // (whole pieces: a matrix whose rows do not end with one is a copy that does)
-            stride_bytes = (uint32_t)k_stride * 2u;
+            base = static_cast<const uint8_t *>(matrix) + (long long)row0 * ELEM;
+            left = ((K - 1) * k_stride + (rows + IN_PIECE - 1) / IN_PIECE * IN_PIECE - row0) * ELEM;
+            stride_bytes = (uint32_t)k_stride * ELEM;
             const int k = lane / PIECES, at = lane % PIECES;
             k_piece = wave * REQUESTS * KROWS + k;       // (the k row of the first request)
             first = at;
         } else {
-            base = static_cast<const uint16_t *>(matrix) + row0 * row_stride;
-            left = (rows - row0 - 1) * row_stride + ((K + 7) & ~7);
-            stride_bytes = (uint32_t)row_stride * 2u;
+            base = static_cast<const uint8_t *>(matrix) + row0 * row_stride * ELEM;
+            left = ((rows - row0 - 1) * row_stride + (K + IN_PIECE - 1) / IN_PIECE * IN_PIECE) * ELEM;
+            stride_bytes = (uint32_t)row_stride * ELEM;
             const int row = lane >> 3, piece = (lane & 7) ^ row;
             first = (uint32_t)(wave * REQUESTS * 8 + row) * stride_bytes + piece * 16u;
-            k_piece = piece * 8;
+            k_piece = piece * IN_PIECE;
         }
     }
 
@@ -78,8 +81,7 @@ struct OperandCopy {
     uint32_t to;
     int k, K;
     __device__ __forceinline__ void begin(uint8_t *stage, int wave, int k_, int K_, bool live) {
-        const long long skip = STRIDED ? (long long)k_ * (stride_bytes / 2u) : 0;
-        const long long bytes = (left - skip) * 2;
+        const long long skip = STRIDED ? (long long)k_ * stride_bytes : 0, bytes = left - skip;
         buf = raw_buffer(base + skip, live ? (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll) : 0u);
         to = lds_address(stage) + wave * REQUESTS * 1024;
         k = k_;
@@ -89,39 +91,64 @@ struct OperandCopy {
         uint32_t off;
         if constexpr (STRIDED) {
             const int kr = k_piece + i * KROWS;
-            off = (uint32_t)kr * stride_bytes + (first ^ (uint32_t)(twist(kr) << 1)) * 16u;
+            off = (uint32_t)kr * stride_bytes + (first ^ (uint32_t)twist(kr)) * 16u;
         } else {
-            off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * 2u : kNowhere;
+            off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * ELEM : kNowhere;
         }
         copy_to_lds(buf, to + i * 1024, off);
     }
 };
 
+// Fragments: eight bfloat16 or four float reduction indices of a row per lane.  Products of a block of 16 x 16 with half a step's indices (float: four
+// instructions, each taking one of every lane's four).
+template <int ELEM> struct Fragment;
+template <> struct Fragment<2> {
+    typedef bf16x8 type;
+    static __device__ __forceinline__ f32x4 multiply(bf16x8 b, bf16x8 a, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0); }
+};
+template <> struct Fragment<4> {
+    typedef f32x4 type;
+    static __device__ __forceinline__ f32x4 multiply(f32x4 b, f32x4 a, f32x4 c) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[q], a[q], c, 0, 0, 0);
+        return c;
+    }
+};
+
 // One operand's fragments: F of them, 16 rows each, from row `row0` of the tile on.
-template <int ROWS, int F, bool STRIDED>
+template <int ROWS, int F, bool STRIDED, int ELEM>
 struct OperandReads {
+    typedef typename Fragment<ELEM>::type fragment_t;
     uint32_t at[STRIDED ? F : 2];
     __device__ __forceinline__ void init(int row0, int lane) {
         const int l16 = lane & 15, g = lane >> 4;
-        if constexpr (STRIDED) {
+        if constexpr (STRIDED && ELEM == 2) {
             const int r = l16 >> 2, twist = r | (g & 1) << 2;
 #pragma unroll
             for (int i = 0; i < F; ++i) at[i] = (uint32_t)((8 * g + r) * ROWS * 2 + (((row0 >> 4) + i) ^ twist) * 32 + (l16 & 3) * 8);
+        } else if constexpr (STRIDED) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) at[i] = (uint32_t)(4 * g * ROWS * 4 + (((row0 >> 4) + i) ^ g) * 64 + l16 * 4);
         } else {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) at[kk] = (uint32_t)((row0 + l16) * 128 + ((g + 4 * kk) ^ (l16 & 7)) * 16);
         }
     }
     // fragment i of the step's half kk
-    __device__ __forceinline__ bf16x8 read(const uint8_t *stage, int kk, int i) const {
-        if constexpr (STRIDED) {
+    __device__ __forceinline__ fragment_t read(const uint8_t *stage, int kk, int i) const {
+        if constexpr (STRIDED && ELEM == 2) {
             typedef __attribute__((address_space(3))) i16x4 *lds4;
             const uint8_t *p = stage + at[i] + kk * 32 * ROWS * 2;
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)p);
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * ROWS * 2));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else if constexpr (STRIDED) {
+            f32x4 r;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) r[q] = *reinterpret_cast<const float *>(stage + at[i] + (kk * 16 + q) * ROWS * 4);
+            return r;
         } else {
-            return *reinterpret_cast<const bf16x8 *>(stage + at[kk] + i * 2048);
+            return *reinterpret_cast<const fragment_t *>(stage + at[kk] + i * 2048);
         }
     }
 };
@@ -187,14 +214,15 @@ __device__ __forceinline__ void finish8(const LinearArgs &a, int m, int n, Eight
     store8<TO>(a.y, m * a.ys + n, d);
 }
 
-template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool SA_, bool SB_>
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool SA_, bool SB_, int ELEM_ = 2>
 struct TileConfig {
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N;
     static constexpr bool SA = SA_, SB = SB_;
+    static constexpr int ELEM = ELEM_, STEP = 128 / ELEM;   // bytes of the operands' elements, reduction indices per step
     static constexpr int FM = BM / WAVES_M / 16, FN = BN / WAVES_N / 16;
     // Steps requested ahead, and the places of both operands' rings: a step of B is free again within its own step, one of A after it.  (Four ahead, for
     // 128 x 128 tiles that leave room: 1000^3 17 us, two ahead 13.)
-    static constexpr int AHEAD = 2, SLOTS_A = AHEAD + 1, SLOTS_B = AHEAD, BYTES_A = BM * kTileStep * 2, BYTES_B = BN * kTileStep * 2;
+    static constexpr int AHEAD = 2, SLOTS_A = AHEAD + 1, SLOTS_B = AHEAD, BYTES_A = BM * 128, BYTES_B = BN * 128;
     static constexpr int LDS_BYTES = SLOTS_A * BYTES_A + SLOTS_B * BYTES_B;
     static_assert(LDS_BYTES <= 160 * 1024, "");
     static constexpr int THREADS = 64 * WAVES, SUM_ROWS = THREADS / (BM / 8);
@@ -260,26 +288,26 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     int tm, tn, split;
     if (!tile_of(p, &tm, &tn, &split)) return;
     const int m0 = tm * BM, n0 = tn * BN;
-    OperandCopy<BM, Cfg::WAVES, Cfg::SA> copyA;
-    OperandCopy<BN, Cfg::WAVES, Cfg::SB> copyB;
+    OperandCopy<BM, Cfg::WAVES, Cfg::SA, Cfg::ELEM> copyA;
+    OperandCopy<BN, Cfg::WAVES, Cfg::SB, Cfg::ELEM> copyB;
     copyA.init(p.a, p.am, p.ak, m0, p.M, p.K, lane, wave);
     copyB.init(p.b, p.bn, p.bk, n0, p.N, p.K, lane, wave);
-    OperandReads<BM, FM, Cfg::SA> readA;
-    OperandReads<BN, FN, Cfg::SB> readB;
+    OperandReads<BM, FM, Cfg::SA, Cfg::ELEM> readA;
+    OperandReads<BN, FN, Cfg::SB, Cfg::ELEM> readB;
     readA.init(wm * FM * 16, lane);
     readB.init(wn * FN * 16, lane);
 
-    const int kBegin = split * p.stepsPerSplit * kTileStep;
-    const int kEnd = min(p.K, kBegin + p.stepsPerSplit * kTileStep);
-    const int steps = (kEnd - kBegin + kTileStep - 1) / kTileStep;
+    const int kBegin = split * p.stepsPerSplit * Cfg::STEP;
+    const int kEnd = min(p.K, kBegin + p.stepsPerSplit * Cfg::STEP);
+    const int steps = (kEnd - kBegin + Cfg::STEP - 1) / Cfg::STEP;
     int k = kBegin, slotA = 0, slotB = 0;       // of the next request
     uint8_t *const ldsB = lds + Cfg::SLOTS_A * Cfg::BYTES_A;
-    constexpr int RA = OperandCopy<BM, Cfg::WAVES, Cfg::SA>::REQUESTS, RB = OperandCopy<BN, Cfg::WAVES, Cfg::SB>::REQUESTS, R = RA + RB;
+    constexpr int RA = decltype(copyA)::REQUESTS, RB = decltype(copyB)::REQUESTS, R = RA + RB;
     auto begin_requests = [&]() __attribute__((always_inline)) {
         const bool live = k < kEnd;
         copyA.begin(lds + slotA * Cfg::BYTES_A, wave, k, kEnd, live);
         copyB.begin(ldsB + slotB * Cfg::BYTES_B, wave, k, kEnd, live);
-        k += kTileStep;
+        k += Cfg::STEP;
         slotA = slotA == Cfg::SLOTS_A - 1 ? 0 : slotA + 1;
         slotB = slotB == Cfg::SLOTS_B - 1 ? 0 : slotB + 1;
     };
@@ -305,7 +333,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         for (int i = 0; i < R; ++i) request(i);
     }
     arrived();
-    bf16x8 a[4], b[2][FN];
+    typename Fragment<Cfg::ELEM>::type a[4], b[2][FN];
     a[0] = readA.read(lds, 0, 0);
     a[1] = readA.read(lds, 0, 1);
 #pragma unroll
@@ -328,7 +356,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         if constexpr (Cfg::SA) {
             if (turn == 0)
 #pragma unroll
-                for (int i = 0; i < kTileStep / Cfg::SUM_ROWS; ++i) {
+                for (int i = 0; i < Cfg::STEP / Cfg::SUM_ROWS; ++i) {
                     const Eight q = load8<bf16_t>(hereA, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
@@ -355,7 +383,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
                 if (t >= SLOTS - 2 && j / ((FN + 1) / 2) == t - (SLOTS - 2)) b[0][j] = readB.read(nextB, 0, j);
             }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[t % FM][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[t / FM][j], a[t % 4], acc[t % FM][j], 0, 0, 0);
+            for (int j = 0; j < FN; ++j) acc[t % FM][j] = Fragment<Cfg::ELEM>::multiply(b[t / FM][j], a[t % 4], acc[t % FM][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -365,10 +393,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0 + wm * FM * 16, n0 + wn * FN * 16, acc);
     if constexpr (Cfg::SA) {
         if (p.columnParts) {
-            typedef OperandCopy<BM, Cfg::WAVES, true> Copy;
+            typedef decltype(copyA) Copy;
             static_assert(Cfg::SUM_ROWS % 16 == 0 && Cfg::SUM_ROWS * BM * 4 <= Cfg::LDS_BYTES, "");
             float *sums = reinterpret_cast<float *>(lds);   // [SUM_ROWS][BM]
-            const int kr = (int)threadIdx.x / Copy::PIECES, piece = ((int)threadIdx.x % Copy::PIECES) ^ (Copy::twist(kr) << 1);
+            const int kr = (int)threadIdx.x / Copy::PIECES, piece = ((int)threadIdx.x % Copy::PIECES) ^ Copy::twist(kr);
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 8; ++e) sums[kr * BM + piece * 8 + e] = sum.v[e];
