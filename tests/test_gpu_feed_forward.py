@@ -286,6 +286,77 @@ def test_linear_backward_filter(types, layout, lend):
                 u.close(DB.double().cpu().numpy(), wb, (M + 8) * 2.0 ** -24 * (np.abs(dy).sum(0) + np.abs(beta * oldb)) + 1e-30, "dbias")
 
 
+# sizes at which the large tiles, the ranges of the reduction and the kernels for few tokens run, none a multiple of theirs
+LARGE_SHAPES = [(4000, 4104, 4040), (1023, 2050, 1000), (3, 9000, 520), (40, 5000, 300), (600, 776, 640), (1, 640, 9003)]
+
+
+@pytest.mark.parametrize("pad", [0, 1, 8])
+@pytest.mark.parametrize("types", LINEAR_TYPES, ids="-".join)
+def test_large_products(types, pad):
+    """Forward with residual and kept z, backward data through SiLU, backward filter with the bias, against products in 64 bits on the GPU."""
+    import torch
+    u, ig = _u(), _u().ig
+    dtype, out = types
+    h, half = u.handle(), u.HALF_STEP[out]
+    e = 2.0 ** -24
+
+    def matrix(rows, cols, t, fill=None):
+        wide = torch.full((rows, cols + pad), u.GUARD, dtype=u.DTYPES[t], device="cuda")
+        view = wide[:, :cols]
+        view.copy_(torch.randn(rows, cols, device="cuda", generator=g)) if fill is None else view.fill_(fill)
+        return wide, view, ig.TensorDescriptor().set(u.DATA[t], rows, cols, 1, 1, (cols + pad, 1, 1, 1))
+
+    def near(got, want, tol, what):
+        bad = ~((got.double() - want).abs() <= tol + 1e-30)
+        assert not bool(bad.any()), (what, int(bad.sum()), float(((got.double() - want).abs() / (tol + 1e-30)).max()))
+
+    def product_error(n, a, b, scale=1.0):
+        return scale * ((n + 4) * e + (2.0 ** -21 + 2.0 ** -30 if dtype == "f32" else 0)) * (a.abs() @ b.abs())
+
+    for M, C, K in LARGE_SHAPES:
+        g = torch.Generator(device="cuda").manual_seed(M + C + K)
+        print("large", types, pad, M, C, K, flush=True)
+        _, x, xd = matrix(M, C, dtype)
+        _, dy, dyd = matrix(M, K, dtype)
+        w, wd = torch.randn(K, C, device="cuda", generator=g).to(u.DTYPES[dtype]), u.filter_desc(dtype, K, C)
+        bias = torch.randn(K, device="cuda", generator=g)
+        X, W, DY = x.double(), w.double(), dy.double()
+        # forward
+        _, r, rd = matrix(M, K, out)
+        yw, y, yd = matrix(M, K, out, float("nan"))
+        zw, z, _ = matrix(M, K, out, float("nan"))
+        ws = u.Workspace(ig.get_linear_forward_workspace_size(h, xd, wd, yd))
+        ig.check(ig.linear_forward(h, 0.5, xd, x.data_ptr(), wd, w.data_ptr(), ws.buf.data_ptr(), ws.size, bias.data_ptr(), ig.IGC_ACTIVATION_GELU, 2.0, rd,
+                                   r.data_ptr(), yd, z.data_ptr(), y.data_ptr()))
+        ws.check()
+        wz = 0.5 * (X @ W.t()) + bias.double()
+        ez = product_error(C, X, W.t(), 0.5) + 3 * e * wz.abs()
+        wy = 0.5 * wz * torch.special.erfc(-wz / 2 ** 0.5) + 2 * r.double()
+        near(z, wz, ez + 1.01 * half * wz.abs(), "z")
+        near(y, wy, 1.13 * ez + (4e-7 if out == "bf16" else 4 * e) * (1 + wz.abs()) + 4 * e * r.double().abs() + 1.01 * half * wy.abs(), "y")
+        assert pad == 0 or (bool((yw[:, K:] == u.GUARD).all()) and bool((zw[:, K:] == u.GUARD).all()))
+        # backward data
+        _, zi, zid = matrix(M, C, out)
+        dw_, dx, dxd = matrix(M, C, out, float("nan"))
+        ws = u.Workspace(ig.get_linear_backward_data_workspace_size(h, wd, dyd, dxd))
+        ig.check(ig.linear_backward_data(h, 1.0, wd, w.data_ptr(), dyd, dy.data_ptr(), ws.buf.data_ptr(), ws.size, ig.IGC_ACTIVATION_SILU, zid, zi.data_ptr(), 0.0,
+                                         None, 0, dxd, dx.data_ptr()))
+        ws.check()
+        G, Z = DY @ W, zi.double()
+        s = torch.sigmoid(Z)
+        want = G * (s + Z * s * (1 - s))
+        near(dx, want, 1.1 * product_error(K, DY, W) + G.abs() * ((4e-7 if out == "bf16" else 4 * e) * (1 + Z.abs()) + 4 * e) + 1.01 * half * want.abs(), "dx")
+        assert pad == 0 or bool((dw_[:, C:] == u.GUARD).all())
+        # backward filter
+        dw, db, dwd = torch.full((K, C), float("nan"), dtype=u.DTYPES[out], device="cuda"), torch.full((K,), float("nan"), device="cuda"), u.filter_desc(out, K, C)
+        ws = u.Workspace(ig.get_linear_backward_filter_workspace_size(h, xd, dyd, dwd))
+        ig.check(ig.linear_backward_filter(h, 1.0, xd, x.data_ptr(), dyd, dy.data_ptr(), ws.buf.data_ptr(), ws.size, 0.0, dwd, dw.data_ptr(), db.data_ptr()))
+        ws.check()
+        want = DY.t() @ X
+        near(dw, want, product_error(M, DY.t(), X) + 1.01 * half * want.abs(), "dw")
+        near(db, DY.sum(0), (M + 8) * e * DY.abs().sum(0), "dbias")
+
+
 @pytest.mark.parametrize("lend", [True, False], ids=["workspace", "alone"])
 @pytest.mark.parametrize("types", LINEAR_TYPES, ids="-".join)
 def test_products_with_infinities_and_nan(types, lend):
