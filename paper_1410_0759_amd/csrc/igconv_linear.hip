@@ -336,6 +336,8 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
 // Rows of whole 16-byte pieces (of n elements) on 16-byte boundaries, if the first is, no row inside another; a tile's reach below 2^31 bytes.
 bool fits(const OperandPlan &o, int n) { return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && o.stride < (1ll << 22); }
 
+bool whole_pieces(const OperandPlan &o) { return o.cols % 4 == 0 && (o.rows == 1 || o.stride >= o.cols) && o.stride < (1ll << 21); }
+
 // The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
 OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
     OperandPlan o;
@@ -355,12 +357,13 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
 // 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.
 struct ShapeCost {
     int per_cu;
-    double alone, full, ends, bytes;   // bytes: what it reads from memory per us (8 x 4096 -> 16384: 128 workgroups 26.5 us, 256 23.8)
+    double alone, full, ends;
 };
-constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0, 90e3}, {2, 0.45, 0.98, 2.5, 45e3}, {2, 0.42, 0.60, 2.0, 30e3}};
-constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0, 90e3}, kFewFloatCost = {2, 0.60, 0.95, 2.0, 30e3};
-// The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory.
-constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6;
+constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0.98, 2.5}, {2, 0.42, 0.60, 2.0}};
+constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.10, 2.00, 2.5}, {2, 0.60, 1.00, 2.0}};
+// The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory, and what one
+// workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
+constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;
 
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, bool aligned_a, bool aligned_b, size_t room) {
     TilePlan pl;
@@ -376,10 +379,11 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0, sum_bytes = sums ? (size_t)(splits * tn) * a.M * 4 : 0;
         if (at + parts + sum_bytes > room || units >= (1ll << 27)) return;
         const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
-        const double full = per * sc.full + sc.ends, one = per * sc.alone + sc.ends;
-        const double memory = (double)(a.K * ((long long)a.M + a.N) * elem_size(in)) / std::min(kMemoryBytes, units * sc.bytes);
-        const double us = std::max(whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)), memory) +
-                          (splits > 1 ? kPartsLaunch + (double)parts * 2 / kPartsBytes : 0.0) + (at > 0 ? kPartsLaunch + (double)at * 2 / kMemoryBytes : 0.0);
+        // what a unit, two side by side and one alone, takes: its steps, or what it reads from memory
+        const double read = (double)(a.K * ((long long)a.M + a.N) * elem_size(in)) / (double)units;
+        const double full = std::max(per * sc.full + sc.ends, read * sc.per_cu * h->computeUnits / kMemoryBytes), one = std::max(per * sc.alone + sc.ends, read / kWorkgroupBytes);
+        const double us = whole * full + (rest == 0 ? 0.0 : (rest <= h->computeUnits ? one : full)) + (splits > 1 ? kPartsLaunch + (double)parts * 2 / kPartsBytes : 0.0) +
+                          (at > 0 ? kPartsLaunch + (double)at * 2 / kMemoryBytes : 0.0);
         if (us >= best) return;
         best = us;
         pl.tiles = true;
@@ -396,8 +400,11 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     };
     constexpr int kMostSplits = 64;
     if (f32) {
-        if (!sa && fits(oa, 4) && fits(ob, 4) && aligned_a && aligned_b)
-            for (int splits = 1; splits <= kMostSplits; ++splits) consider(few_float_kernel(sb), kFewFloatCost, kFloatStep, splits, false);
+        // (float rows need not begin on 16-byte boundaries: the copies into LDS ask for 4)
+        if (whole_pieces(oa) && whole_pieces(ob))
+            for (int shape = 0; shape < kDirectShapes; ++shape)
+                for (int splits = 1; splits <= kMostSplits; ++splits)
+                    consider(direct_float_kernel(sa, sb, shape), kDirectCost[shape], kFloatStep, splits, false);
         for (int splits = 1; splits <= kMostSplits; ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
         return pl;
     }

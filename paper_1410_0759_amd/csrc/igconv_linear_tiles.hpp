@@ -225,7 +225,7 @@ struct TileConfig {
     static constexpr int AHEAD = 2, SLOTS_A = AHEAD + 1, SLOTS_B = AHEAD, BYTES_A = BM * 128, BYTES_B = BN * 128;
     static constexpr int LDS_BYTES = SLOTS_A * BYTES_A + SLOTS_B * BYTES_B;
     static_assert(LDS_BYTES <= 160 * 1024, "");
-    static constexpr int THREADS = 64 * WAVES, SUM_ROWS = THREADS / (BM / 8);
+    static constexpr int THREADS = 64 * WAVES, SUM_ROWS = THREADS / (BM * ELEM / 16);   // k rows that the threads cover, a piece each
 };
 
 __device__ __forceinline__ bool tile_of(const TileArgs &p, int *tm, int *tn, int *split) {
@@ -340,8 +340,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     for (int j = 0; j < FN; ++j) b[0][j] = readB.read(ldsB, 0, j);
 
     // (backward filter) The sums of the first operand's rows over the reduction: the tiles of a row of tiles, which share these rows, take them
-    // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every sixteenth (32nd) k row, which hold the same
-    // eight rows of the operand.  (A second body of the step with products with ones among the others spilled registers.  So the sums cost nothing
+    // in turns, a step each, from the step's stage: a thread the 16-byte pieces of one place of every SUM_ROWS-th k row, which hold the same
+    // rows of the operand.  (A second body of the step with products with ones among the others spilled registers.  So the sums cost nothing
     // that shows: 8192 x 4096 -> 4096, 252 us with them and 253 without, and the sum over the tiles 4 us.)
     Eight sum = {};
     int turn = Cfg::SA && p.columnParts ? tn : -1;   // steps until the next one whose sums are this tile's
@@ -357,9 +357,16 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
             if (turn == 0)
 #pragma unroll
                 for (int i = 0; i < Cfg::STEP / Cfg::SUM_ROWS; ++i) {
-                    const Eight q = load8<bf16_t>(hereA, (int)threadIdx.x * 8 + i * Cfg::THREADS * 8);
+                    const uint8_t *piece = hereA + ((int)threadIdx.x + i * Cfg::THREADS) * 16;
+                    if constexpr (Cfg::ELEM == 2) {
+                        const Eight q = load8<bf16_t>(piece, 0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
+                        for (int e = 0; e < 8; ++e) sum.v[e] += q.v[e];
+                    } else {
+                        const f32x4 q = *reinterpret_cast<const f32x4 *>(piece);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum.v[e] += q[e];
+                    }
                 }
             turn = turn == 0 ? p.tilesN - 1 : turn - 1;
         }
@@ -394,12 +401,12 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     if constexpr (Cfg::SA) {
         if (p.columnParts) {
             typedef decltype(copyA) Copy;
-            static_assert(Cfg::SUM_ROWS % 16 == 0 && Cfg::SUM_ROWS * BM * 4 <= Cfg::LDS_BYTES, "");
+            static_assert(Cfg::SUM_ROWS % 16 == 0 && Cfg::STEP % Cfg::SUM_ROWS == 0 && Cfg::SUM_ROWS * BM * 4 <= Cfg::LDS_BYTES, "");
             float *sums = reinterpret_cast<float *>(lds);   // [SUM_ROWS][BM]
             const int kr = (int)threadIdx.x / Copy::PIECES, piece = ((int)threadIdx.x % Copy::PIECES) ^ Copy::twist(kr);
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[kr * BM + piece * 8 + e] = sum.v[e];
+            for (int e = 0; e < Copy::IN_PIECE; ++e) sums[kr * BM + piece * Copy::IN_PIECE + e] = sum.v[e];
             __syncthreads();
             for (int m = threadIdx.x; m < BM && m0 + m < p.M; m += Cfg::THREADS) {
                 float v = 0.f;
