@@ -354,12 +354,13 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
 
 // us of a step of a workgroup alone on its compute unit and with another beside it, and of a tile's start and epilogue.  Measured: forward 8192^3 is 512
 // steps of 256 x 256, 786 us, or 1024 of 128 x 128 two by two, 1003; 2048^3 32 steps, 44, 21.4 (alone) and, 64 x 128 two by two, 24.7;
-// 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.
+// 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.  With the pieces through registers a step waits for memory: 8 x 4097 ->
+// 8000, 252 workgroups of 17 steps, 34 us, 504 of 9, 24 - with copies first 41; 1000 x 1001 -> 1001, 16 steps, 28, with copies first 16.
 struct ShapeCost {
     int per_cu;
     double alone, full, ends;
 };
-constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0.98, 2.5}, {2, 0.42, 0.60, 2.0}};
+constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0.98, 2.5}, {2, 0.42, 0.60, 2.0}, {2, 1.65, 2.00, 2.0}};
 constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.10, 2.00, 2.5}, {2, 0.60, 1.00, 2.0}};
 // The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory, and what one
 // workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
@@ -410,9 +411,9 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     }
     // (a tile's reach stays within 31 bits)
     if ((oa.pack ? oa.toRow : oa.stride) >= (1ll << 22) || (ob.pack ? ob.toRow : ob.stride) >= (1ll << 22)) return pl;
-    for (int shape = 0; shape < kTileShapes; ++shape)
+    for (int shape = 0; shape < (oa.pack || ob.pack ? kTileShapes : kStagedShape); ++shape)
         for (int splits = 1; splits <= kMostSplits; ++splits)
-            consider(tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), kShapeCost[shape], kTileStep, splits, true);
+            consider(tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), kShapeCost[shape], kTileStep, splits, shape < kStagedShape);
     return pl;
 }
 

@@ -28,6 +28,12 @@ using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kNowhere = 0x80000000u;        // an offset outside every buffer: the load brings zeros
 
+// neighbours in memory, on no boundary but their own
+template <class T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Adjacent {
+    T v[N];
+};
+
 // 16 bytes per lane from global memory into LDS at `to`, lane after lane; past the buffer's end: zeros.  In assembly (there is no register that
 // it writes) because the compiler puts a wait for every such copy under way before each transposing read, which no alias information keeps
 // it from: 8192^3 by backward filter 1060 us as against 796.  The waits are the kernels' own: `arrived`.
@@ -43,7 +49,9 @@ __device__ __forceinline__ u32x4 raw_buffer(const void *base, uint32_t bytes) {
 
 // One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand; elements of ELEM bytes.
 // STRIDED: the reduction index runs along the rows of the matrix in memory (`stride` elements apart), the tile's rows are adjacent.
-template <int ROWS, int WAVES, bool STRIDED, int ELEM>
+// STAGED (bfloat16): the rows begin or end off 16-byte boundaries, which copies straight into LDS do not serve; the lanes load the same pieces into
+// registers, element by element where one is cut by the matrix's end, and write them to LDS a step later.
+template <int ROWS, int WAVES, bool STRIDED, int ELEM, bool STAGED>
 struct OperandCopy {
     static constexpr int REQUESTS = ROWS / 8 / WAVES;      // of 1 KB per wavefront and step
     static constexpr int PIECES = ROWS * ELEM / 16;        // (strided) 16-byte pieces of a k row
@@ -52,12 +60,15 @@ struct OperandCopy {
     const uint8_t *base;
     long long left;             // bytes from `base` to the end of the operand
     uint32_t stride_bytes, first;
-    int k_piece;                // (not strided) the lane's first reduction index within a step
+    int k_piece, k_row;         // (not strided) the lane's first reduction index within a step, and its first row
 
     // (strided) the exclusive or of the pieces of k row k: the rows that a read takes at once lie in different banks
     static __device__ __forceinline__ int twist(int k) { return ELEM == 2 ? ((k & 3) | ((k >> 3) & 1) << 2) << 1 : ((k >> 2) & 3) << 2; }
 
     __device__ __forceinline__ void init(const void *matrix, long long row_stride, long long k_stride, int row0, int rows, int K, int lane, int wave) {
+        rows_left = rows - row0;
+        cols_left = rows - row0;
+        k_row = wave * REQUESTS * 8 + (lane >> 3);
         // (whole pieces: a matrix whose rows do not end with one is a copy that does)
         if constexpr (STRIDED) {
             base = static_cast<const uint8_t *>(matrix) + (long long)row0 * ELEM;
@@ -80,14 +91,43 @@ struct OperandCopy {
     u32x4 buf;
     uint32_t to;
     int k, K;
+    // (staged) rows and columns of the matrix from the tile's first on, the pieces in registers and where they go
+    int rows_left, cols_left;
+    u32x4 held[STAGED ? REQUESTS : 1];
+    uint8_t *held_to, *next_to;
     __device__ __forceinline__ void begin(uint8_t *stage, int wave, int k_, int K_, bool live) {
+        if constexpr (STAGED) {
+            held_to = next_to;
+            next_to = stage + wave * REQUESTS * 1024 + (threadIdx.x & 63) * 16;
+            k = k_;
+            K = live ? K_ : 0;
+            return;
+        }
         const long long skip = STRIDED ? (long long)k_ * stride_bytes : 0, bytes = left - skip;
         buf = raw_buffer(base + skip, live ? (uint32_t)(bytes < 0x7FFFFFFFll ? bytes : 0x7FFFFFFFll) : 0u);
         to = lds_address(stage) + wave * REQUESTS * 1024;
         k = k_;
         K = K_;
     }
-    __device__ __forceinline__ void request(int i) const {
+    __device__ __forceinline__ void store(int i) { *reinterpret_cast<u32x4 *>(held_to + i * 1024) = held[i]; }
+    __device__ __forceinline__ void request(int i) {
+        if constexpr (STAGED) {
+            const int row = STRIDED ? k + k_piece + i * KROWS : k_row + i * 8, col = STRIDED ? (int)(first ^ (uint32_t)twist(k_piece + i * KROWS)) * IN_PIECE : k + k_piece;
+            const int there = row < (STRIDED ? K : rows_left) ? (STRIDED ? cols_left : K) - col : 0;   // elements
+            const uint16_t *from = reinterpret_cast<const uint16_t *>(base + (long long)row * stride_bytes) + col;
+            if (there >= 8) {
+                held[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Adjacent<uint16_t, 8> *>(from));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t lo = 0, hi = 0;
+                    if (2 * e < there) lo = from[2 * e];
+                    if (2 * e + 1 < there) hi = from[2 * e + 1];
+                    held[i][e] = lo | hi << 16;
+                }
+            }
+            return;
+        }
         uint32_t off;
         if constexpr (STRIDED) {
             const int kr = k_piece + i * KROWS;
@@ -157,10 +197,6 @@ struct OperandReads {
 struct Eight {
     float v[8];
 };
-template <class T, int N>
-struct __attribute__((packed, aligned(sizeof(T)))) Adjacent {
-    T v[N];
-};
 template <class TO>
 __device__ __forceinline__ Eight load8(const void *p, long long at) {
     Eight r;
@@ -214,8 +250,9 @@ __device__ __forceinline__ void finish8(const LinearArgs &a, int m, int n, Eight
     store8<TO>(a.y, m * a.ys + n, d);
 }
 
-template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool SA_, bool SB_, int ELEM_ = 2>
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, bool SA_, bool SB_, int ELEM_ = 2, bool STAGED_ = false>
 struct TileConfig {
+    static constexpr bool STAGED = STAGED_;
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, WAVES = WAVES_M * WAVES_N;
     static constexpr bool SA = SA_, SB = SB_;
     static constexpr int ELEM = ELEM_, STEP = 128 / ELEM;   // bytes of the operands' elements, reduction indices per step
@@ -288,8 +325,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     int tm, tn, split;
     if (!tile_of(p, &tm, &tn, &split)) return;
     const int m0 = tm * BM, n0 = tn * BN;
-    OperandCopy<BM, Cfg::WAVES, Cfg::SA, Cfg::ELEM> copyA;
-    OperandCopy<BN, Cfg::WAVES, Cfg::SB, Cfg::ELEM> copyB;
+    OperandCopy<BM, Cfg::WAVES, Cfg::SA, Cfg::ELEM, Cfg::STAGED> copyA;
+    OperandCopy<BN, Cfg::WAVES, Cfg::SB, Cfg::ELEM, Cfg::STAGED> copyB;
     copyA.init(p.a, p.am, p.ak, m0, p.M, p.K, lane, wave);
     copyB.init(p.b, p.bn, p.bk, n0, p.N, p.K, lane, wave);
     OperandReads<BM, FM, Cfg::SA, Cfg::ELEM> readA;
@@ -315,9 +352,14 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         if (i < RA) copyA.request(i);
         else copyB.request(i - RA);
     };
+    auto store = [&](int i) __attribute__((always_inline)) {
+        if (i < RA) copyA.store(i);
+        else copyB.store(i - RA);
+    };
     constexpr int LATER = (Cfg::AHEAD - 1) * R;
     auto arrived = [&]() __attribute__((always_inline)) {     // all but the steps after the next
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (LATER & 15) | ((LATER >> 4) << 14));
+        if (Cfg::STAGED) __builtin_amdgcn_s_waitcnt(0xC07F);   // (this wavefront's writes)
+        else __builtin_amdgcn_s_waitcnt(0x0F70 | (LATER & 15) | ((LATER >> 4) << 14));
         asm volatile("s_barrier" ::: "memory");
     };
 
@@ -330,7 +372,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
     for (int n = 0; n < Cfg::AHEAD; ++n) {
         begin_requests();
 #pragma unroll
-        for (int i = 0; i < R; ++i) request(i);
+        for (int i = 0; i < R; ++i) {
+            if (Cfg::STAGED && n > 0) store(i);
+            request(i);
+        }
     }
     arrived();
     typename Fragment<Cfg::ELEM>::type a[4], b[2][FN];
@@ -381,7 +426,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
             // (a few to a slot: eight wavefronts with eight requests each at once wait for each other's)
 #pragma unroll
             for (int i = 0; i < R; ++i)
-                if (t == FREE + i / PER_SLOT) request(i);
+                if (t == FREE + i / PER_SLOT) {
+                    if (Cfg::STAGED) store(i);
+                    request(i);
+                }
             if (t + 2 < SLOTS) a[(t + 2) % 4] = readA.read(hereA, (t + 2) / FM, (t + 2) % FM);
             else a[(t + 2) % 4] = readA.read(nextA, 0, t + 2 - SLOTS);
 #pragma unroll
