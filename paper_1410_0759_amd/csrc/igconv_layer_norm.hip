@@ -200,6 +200,17 @@ __device__ __forceinline__ void store_chunk(T *p, const W (&v)[E]) {
     *reinterpret_cast<Chunk<T, E> *>(p) = r;
 }
 
+// The chunk has arrived from here on.  (A row may be written in place, and a chunk that was moved back shares elements with another thread's: all of a
+// row is read before the barrier after which any of it is written.)
+template <class T, int E>
+__device__ __forceinline__ void arrive(Chunk<T, E> &r) {
+    uint32_t words[sizeof(r) / 4];
+    __builtin_memcpy(words, &r, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r) / 4); ++i) asm volatile("" : "+v"(words[i]));
+    __builtin_memcpy(&r, words, sizeof(r));
+}
+
 // where a thread's chunks begin
 template <int LANES, int CHUNKS, int E, bool WHOLE>
 struct Place {
@@ -306,6 +317,10 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) load_chunk(old[j], y + at.c[j]);
         if (ROOM && row + stride < a.M) load(row + stride);
+        if (a.beta != W(0))
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+                if (at.live[j]) arrive(old[j]);
         const W mean = row_sum<LANES>(sum, slots[parity][0]) / W(a.C);
         W squares = W(0);
 #pragma unroll
@@ -338,7 +353,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
 }
 
 // dx of every row, and dscale's and dshift's sums over the workgroup's rows in registers (parts[workgroup]).  With 1024 threads to a
-// row their 128 registers hold the row and the sums only: scale comes from the cache, the next row's loads are not made ahead.
+// row their 128 registers hold the row as it is stored and the sums only: scale comes from the cache, the next row's loads are not made ahead.
 template <class TX, class TY, int LANES, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_kernel(const NormBackwardArgs<typename Stored<TX>::wide_t> a) {
     typedef typename Stored<TX>::wide_t W;
@@ -346,7 +361,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
     __shared__ W slots[2][2 * THREADS / 64];
     const int t = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     constexpr bool ROOM = LANES < 1024;
-    W scale[CHUNKS][E], ds[CHUNKS][E], db[CHUNKS][E];
+    W scale[CHUNKS][E], ds[CHUNKS][E], db[CHUNKS][E];   // (without room one chunk's scale is alive at a time)
     const Place<LANES, CHUNKS, E, WHOLE> at(t, a.C);
     auto load_scale = [&](int j) __attribute__((always_inline)) {
         Chunk<W, E> sc;
@@ -364,7 +379,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
     }
     const int stride = (int)gridDim.x * ROWS;
     int row = (int)blockIdx.x * ROWS + sub;
-    Chunk<TX, E> rx[CHUNKS], rr[CHUNKS];
+    Chunk<TX, E> rx[CHUNKS], rr[CHUNKS], next_r[CHUNKS];
     Chunk<TY, E> rdy[CHUNKS];
     W mean, s;
     auto load = [&](int r) __attribute__((always_inline)) {
@@ -375,6 +390,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
             if (!at.live[j]) continue;
             load_chunk(rx[j], x + at.c[j]);
             load_chunk(rdy[j], dy + at.c[j]);
+            if (a.beta != W(0)) load_chunk(next_r[j], static_cast<const TX *>(a.r) + r * a.rs + at.c[j]);
         }
         mean = a.mean[r];
         s = a.invstd[r];
@@ -382,33 +398,45 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
     if (ROOM && row < a.M) load(row);
     for (int parity = 0; row < a.M; row += stride, parity ^= 1) {
         if (!ROOM) load(row);
-        if (a.beta != W(0)) {
-            const TX *p = static_cast<const TX *>(a.r) + row * a.rs;
+        // h and q of the row's elements; without room for them they are taken from the row again when dx is written
+        W h[ROOM ? CHUNKS : 1][E], q[ROOM ? CHUNKS : 1][E];
+        W sum = W(0), along = W(0);
+        const W inv = s, average = mean;
+        if (ROOM && a.beta != W(0))
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
-                if (at.live[j]) load_chunk(rr[j], p + at.c[j]);
-        }
-        W h[CHUNKS][E], q[CHUNKS][E];
-        W sum = W(0), along = W(0);
-        const W inv = s;
-#pragma unroll
-        for (int j = 0; j < CHUNKS; ++j) {
-            if (!at.live[j]) continue;
+                if (at.live[j]) {
+                    arrive(next_r[j]);
+                    rr[j] = next_r[j];
+                }
+        auto take = [&](int j, int to) __attribute__((always_inline)) {
             if (!ROOM) load_scale(j);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const W dy = Stored<TY>::widen(rdy[j].v[e]);
-                h[j][e] = (Stored<TX>::widen(rx[j].v[e]) - mean) * inv;
-                q[j][e] = dy * scale[j][e];
-                if (at.counts(j, e)) {
-                    db[j][e] += dy;
-                    ds[j][e] += dy * h[j][e];
-                    sum += q[j][e];
-                    along += q[j][e] * h[j][e];
-                }
+                h[to][e] = (Stored<TX>::widen(rx[j].v[e]) - average) * inv;
+                q[to][e] = Stored<TY>::widen(rdy[j].v[e]) * scale[j][e];
             }
+        };
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (!at.live[j]) continue;
+            const int to = ROOM ? j : 0;
+            take(j, to);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (at.counts(j, e)) {
+                    const W dy = Stored<TY>::widen(rdy[j].v[e]);
+                    db[j][e] += dy;
+                    ds[j][e] += dy * h[to][e];
+                    sum += q[to][e];
+                    along += q[to][e] * h[to][e];
+                }
         }
         if (ROOM && row + stride < a.M) load(row + stride);
+        if (!ROOM && a.beta != W(0))
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j)
+                if (at.live[j]) arrive(next_r[j]);
         row_sums<LANES>(sum, along, slots[parity]);
         sum /= W(a.C);
         along /= W(a.C);
@@ -417,12 +445,14 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (!at.live[j]) continue;
+            const int to = ROOM ? j : 0;
+            if (!ROOM) take(j, 0);
             W out[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) out[e] = f * (q[j][e] - sum - h[j][e] * along);
+            for (int e = 0; e < E; ++e) out[e] = f * (q[to][e] - sum - h[to][e] * along);
             if (a.beta != W(0))
 #pragma unroll
-                for (int e = 0; e < E; ++e) out[e] += a.beta * Stored<TX>::widen(rr[j].v[e]);
+                for (int e = 0; e < E; ++e) out[e] += a.beta * Stored<TX>::widen((ROOM ? rr[j] : next_r[j]).v[e]);
             store_chunk(dx + at.c[j], out);
         }
     }
