@@ -47,34 +47,37 @@ __device__ __forceinline__ W group_sum(W v, W *slots) {
     return (slots[0] + slots[1]) + (slots[2] + slots[3]);
 }
 
-// ---- any row length: a workgroup per row, the row read once per pass ------------------------------------------------
+// ---- any row length: a workgroup per row at a time, the row read once per pass ------------------------------------------
+constexpr int kMostRowGroups = 1 << 20;   // (workgroups times threads is a 32-bit number)
 template <class TX, class TY>
 __global__ __launch_bounds__(256) void layer_norm_rows_kernel(const NormArgs<typename Stored<TX>::wide_t> a) {
     typedef typename Stored<TX>::wide_t W;
     __shared__ W slots[8];
-    const TX *x = static_cast<const TX *>(a.x) + (long long)blockIdx.x * a.xs;
-    TY *y = static_cast<TY *>(a.y) + (long long)blockIdx.x * a.ys;
-    W sum = W(0);
-    for (int c = threadIdx.x; c < a.C; c += 256) sum += Stored<TX>::widen(x[c]);
-    const W mean = group_sum(sum, slots) / W(a.C);
-    W squares = W(0);
-    for (int c = threadIdx.x; c < a.C; c += 256) {
-        const W d = Stored<TX>::widen(x[c]) - mean;
-        squares += d * d;
-    }
-    const W s = W(1) / sqrt(group_sum(squares, slots + 4) / W(a.C) + a.epsilon);
-    const W *scale = static_cast<const W *>(a.scale), *shift = static_cast<const W *>(a.shift);
-    for (int c = threadIdx.x; c < a.C; c += 256) {
-        W v = (Stored<TX>::widen(x[c]) - mean) * s;
-        if (scale) v *= scale[c];
-        if (shift) v += shift[c];
-        v *= a.alpha;
-        if (a.beta != W(0)) v += a.beta * Stored<TY>::widen(y[c]);
-        y[c] = Stored<TY>::narrow(v);
-    }
-    if (threadIdx.x == 0) {
-        if (a.mean) a.mean[blockIdx.x] = mean;
-        if (a.invstd) a.invstd[blockIdx.x] = s;
+    for (int i = blockIdx.x; i < a.M; i += (int)gridDim.x) {
+        const TX *x = static_cast<const TX *>(a.x) + i * a.xs;
+        TY *y = static_cast<TY *>(a.y) + i * a.ys;
+        W sum = W(0);
+        for (int c = threadIdx.x; c < a.C; c += 256) sum += Stored<TX>::widen(x[c]);
+        const W mean = group_sum(sum, slots) / W(a.C);
+        W squares = W(0);
+        for (int c = threadIdx.x; c < a.C; c += 256) {
+            const W d = Stored<TX>::widen(x[c]) - mean;
+            squares += d * d;
+        }
+        const W s = W(1) / sqrt(group_sum(squares, slots + 4) / W(a.C) + a.epsilon);
+        const W *scale = static_cast<const W *>(a.scale), *shift = static_cast<const W *>(a.shift);
+        for (int c = threadIdx.x; c < a.C; c += 256) {
+            W v = (Stored<TX>::widen(x[c]) - mean) * s;
+            if (scale) v *= scale[c];
+            if (shift) v += shift[c];
+            v *= a.alpha;
+            if (a.beta != W(0)) v += a.beta * Stored<TY>::widen(y[c]);
+            y[c] = Stored<TY>::narrow(v);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[i] = mean;
+            if (a.invstd) a.invstd[i] = s;
+        }
     }
 }
 
@@ -82,25 +85,26 @@ template <class TX, class TY>
 __global__ __launch_bounds__(256) void layer_norm_backward_rows_kernel(const NormBackwardArgs<typename Stored<TX>::wide_t> a) {
     typedef typename Stored<TX>::wide_t W;
     __shared__ W slots[8];
-    const long long i = blockIdx.x;
-    const TX *x = static_cast<const TX *>(a.x) + i * a.xs;
-    const TY *dy = static_cast<const TY *>(a.dy) + i * a.dys;
-    const W mean = a.mean[i], s = a.invstd[i];
-    W sum = W(0), along = W(0);
-    for (int c = threadIdx.x; c < a.C; c += 256) {
-        const W q = Stored<TY>::widen(dy[c]) * (a.scale ? a.scale[c] : W(1));
-        sum += q;
-        along += q * ((Stored<TX>::widen(x[c]) - mean) * s);
-    }
-    sum = group_sum(sum, slots) / W(a.C);
-    along = group_sum(along, slots + 4) / W(a.C);
-    const TX *r = static_cast<const TX *>(a.r) + i * a.rs;
-    TX *dx = static_cast<TX *>(a.dx) + i * a.dxs;
-    for (int c = threadIdx.x; c < a.C; c += 256) {
-        const W q = Stored<TY>::widen(dy[c]) * (a.scale ? a.scale[c] : W(1)), h = (Stored<TX>::widen(x[c]) - mean) * s;
-        W v = a.alpha * (s * (q - sum - h * along));
-        if (a.beta != W(0)) v += a.beta * Stored<TX>::widen(r[c]);
-        dx[c] = Stored<TX>::narrow(v);
+    for (int i = blockIdx.x; i < a.M; i += (int)gridDim.x) {
+        const TX *x = static_cast<const TX *>(a.x) + i * a.xs;
+        const TY *dy = static_cast<const TY *>(a.dy) + i * a.dys;
+        const W mean = a.mean[i], s = a.invstd[i];
+        W sum = W(0), along = W(0);
+        for (int c = threadIdx.x; c < a.C; c += 256) {
+            const W q = Stored<TY>::widen(dy[c]) * (a.scale ? a.scale[c] : W(1));
+            sum += q;
+            along += q * ((Stored<TX>::widen(x[c]) - mean) * s);
+        }
+        sum = group_sum(sum, slots) / W(a.C);
+        along = group_sum(along, slots + 4) / W(a.C);
+        const TX *r = static_cast<const TX *>(a.r) + i * a.rs;
+        TX *dx = static_cast<TX *>(a.dx) + i * a.dxs;
+        for (int c = threadIdx.x; c < a.C; c += 256) {
+            const W q = Stored<TY>::widen(dy[c]) * (a.scale ? a.scale[c] : W(1)), h = (Stored<TX>::widen(x[c]) - mean) * s;
+            W v = a.alpha * (s * (q - sum - h * along));
+            if (a.beta != W(0)) v += a.beta * Stored<TX>::widen(r[c]);
+            dx[c] = Stored<TX>::narrow(v);
+        }
     }
 }
 
@@ -304,6 +308,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (!at.live[j]) continue;
+            if (!WHOLE) arrive(raw[j]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 x[j][e] = Stored<TX>::widen(raw[j].v[e]);
@@ -317,7 +322,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) load_chunk(old[j], y + at.c[j]);
         if (ROOM && row + stride < a.M) load(row + stride);
-        if (a.beta != W(0))
+        if (!WHOLE && a.beta != W(0))
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) arrive(old[j]);
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) {
-                    arrive(next_r[j]);
+                    if (!WHOLE) arrive(next_r[j]);
                     rr[j] = next_r[j];
                 }
         auto take = [&](int j, int to) __attribute__((always_inline)) {
@@ -433,7 +438,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
                 }
         }
         if (ROOM && row + stride < a.M) load(row + stride);
-        if (!ROOM && a.beta != W(0))
+        if (!ROOM && !WHOLE && a.beta != W(0))
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) arrive(next_r[j]);
@@ -608,7 +613,7 @@ igcStatus igcLayerNormForward(igcHandle_t handle, const void *alpha, igcTensorDe
                                    dim3((unsigned)std::min(groups, most)), THREADS, handle->stream);
             }))
             return rc;
-        return launch_kernel(reinterpret_cast<const void *>(&layer_norm_rows_kernel<TX, TY>), a, dim3((unsigned)p.x.rows), 256, handle->stream);
+        return launch_kernel(reinterpret_cast<const void *>(&layer_norm_rows_kernel<TX, TY>), a, dim3((unsigned)std::min(a.M, kMostRowGroups)), 256, handle->stream);
     });
 }
 
@@ -668,7 +673,7 @@ igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha, igcTensorD
             })) {
             if (rc != IGC_STATUS_SUCCESS || !params) return rc;
         } else {
-            rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_backward_rows_kernel<TX, TY>), a, dim3((unsigned)a.M), 256, handle->stream);
+            rc = launch_kernel(reinterpret_cast<const void *>(&layer_norm_backward_rows_kernel<TX, TY>), a, dim3((unsigned)std::min(a.M, kMostRowGroups)), 256, handle->stream);
             if (rc != IGC_STATUS_SUCCESS || !params) return rc;
             if (a.parts) {
                 a.per = (a.M + a.ranges - 1) / a.ranges;

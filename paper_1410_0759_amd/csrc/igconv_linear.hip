@@ -10,6 +10,8 @@
 namespace igc {
 namespace {
 
+constexpr long long kMostGroups = 1ll << 22;   // of a launch, to be safe with 512 threads each: their product is a 32-bit number
+
 // ---- any strides, any alignment, no workspace -------------------------------------------------------------------------
 // A workgroup computes 64 x 64 results, its four wavefronts 32 x 32 each, in steps of 32 of the reduction that go element by
 // element through LDS, k innermost; the lanes of a load run along whichever index is adjacent in memory.
@@ -69,24 +71,27 @@ __global__ __launch_bounds__(256) void linear_any_kernel(const LinearArgs p) {
     __shared__ __attribute__((aligned(16))) typename Tile::lds_t la[kAnyTile * Tile::ROW], lb[kAnyTile * Tile::ROW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
     const int tilesM = (p.M + kAnyTile - 1) / kAnyTile;
-    const int m0 = (int)(blockIdx.x % (unsigned)tilesM) * kAnyTile, n0 = (int)(blockIdx.x / (unsigned)tilesM) * kAnyTile;
     const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    f32x16 acc;
+    const long long tiles = (long long)tilesM * ((p.N + kAnyTile - 1) / kAnyTile);
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int m0 = (int)(tile % tilesM) * kAnyTile, n0 = (int)(tile / tilesM) * kAnyTile;
+        f32x16 acc;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
-    for (int k0 = 0; k0 < p.K; k0 += kAnyStep) {
-        load_any<T>(p.a, p.am, p.ak, m0, p.M, k0, p.K, la);
-        load_any<T>(p.b, p.bn, p.bk, n0, p.N, k0, p.K, lb);
-        __syncthreads();
-        Tile::multiply(la + (wm + l32) * Tile::ROW, lb + (wn + l32) * Tile::ROW, half, acc);
-        __syncthreads();
-    }
-    // (the second operand's index runs along the lanes, the first's along the registers: 8 (v / 4) + 4 half + v % 4)
-    const int m = m0 + wm + l32;
+        for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+        for (int k0 = 0; k0 < p.K; k0 += kAnyStep) {
+            load_any<T>(p.a, p.am, p.ak, m0, p.M, k0, p.K, la);
+            load_any<T>(p.b, p.bn, p.bk, n0, p.N, k0, p.K, lb);
+            __syncthreads();
+            Tile::multiply(la + (wm + l32) * Tile::ROW, lb + (wn + l32) * Tile::ROW, half, acc);
+            __syncthreads();
+        }
+        // (the second operand's index runs along the lanes, the first's along the registers: 8 (v / 4) + 4 half + v % 4)
+        const int m = m0 + wm + l32;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const int n = n0 + wn + 8 * (v >> 2) + 4 * half + (v & 3);
-        if (m < p.M && n < p.N) finish_element<TO>(p, m, n, acc[v]);
+        for (int v = 0; v < 16; ++v) {
+            const int n = n0 + wn + 8 * (v >> 2) + 4 * half + (v & 3);
+            if (m < p.M && n < p.N) finish_element<TO>(p, m, n, acc[v]);
+        }
     }
 }
 
@@ -168,8 +173,9 @@ igcStatus check_beside(igcTensorDescriptor_t out, igcTensorDescriptor_t d, const
 template <class TO>
 __global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
     const long long groups = p.partsRow / 8, id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int m = (int)(id / groups), n = (int)(id % groups) * 8;
-    if (m >= p.M) return;
+    const int n = (int)(id % groups) * 8;
+    if (id / groups >= p.M) return;
+    const int m = (int)(id / groups);
     Eight d = load8<float>(p.parts, (long long)m * p.partsRow + n);
 #pragma unroll 4
     for (int s = 1; s < p.splits; ++s) {
@@ -334,9 +340,13 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
 }
 
 // Rows of whole 16-byte pieces (of n elements) on 16-byte boundaries, if the first is, no row inside another; a tile's reach below 2^31 bytes.
-bool fits(const OperandPlan &o, int n) { return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && o.stride < (1ll << 22); }
+bool fits(const OperandPlan &o, int n) {
+    return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && std::max(o.stride, (long long)o.cols) < (1ll << 22);
+}
 
-bool whole_pieces(const OperandPlan &o) { return o.cols % 4 == 0 && (o.rows == 1 || o.stride >= o.cols) && o.stride < (1ll << 21); }
+bool whole_pieces(const OperandPlan &o) {
+    return o.cols % 4 == 0 && (o.rows == 1 || o.stride >= o.cols) && std::max(o.stride, (long long)o.cols) < (1ll << 21);
+}
 
 // The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
 OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
@@ -374,11 +384,12 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
     auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
         const int steps = (a.K + step - 1) / step, per = (steps + splits - 1) / splits;
-        if (!k.kernel || splits > steps || (steps + per - 1) / per != splits) return;
+        if (!k.kernel || (steps + per - 1) / per != splits) return;
         const size_t at_b = copied ? oa.bytes : 0, at = copied ? oa.bytes + ob.bytes : 0;
         const long long tm = (a.M + k.bm - 1) / k.bm, tn = (a.N + k.bn - 1) / k.bn, units = tm * tn * splits;
         const size_t parts = splits > 1 ? (size_t)splits * a.M * round_up(a.N, 8) * 4 : 0, sum_bytes = sums ? (size_t)(splits * tn) * a.M * 4 : 0;
-        if (at + parts + sum_bytes > room || units >= (1ll << 27)) return;
+        // (a launch holds 2^32 threads: of the sum over the ranges one to 32 bytes, of the copies 256 to 4 KB of bfloat16 or 12 KB of parts)
+        if (at + parts + sum_bytes > room || units > kMostGroups || parts / splits >= (1ull << 36) || at >= (1ull << 35)) return;
         const long long slots = (long long)h->computeUnits * sc.per_cu, whole = units / slots, rest = units % slots;
         // what a unit, two side by side and one alone, takes: its steps, or what it reads from memory
         const double read = (double)(a.K * ((long long)a.M + a.N) * elem_size(in)) / (double)units;
@@ -399,20 +410,21 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         pl.sumsAt = at + parts;
         pl.bytes = at + parts + sum_bytes;
     };
-    constexpr int kMostSplits = 64;
+    // (no range without a step)
+    auto most_splits = [&](int step) { return std::min(64, (a.K + step - 1) / step); };
     if (f32) {
         // (float rows need not begin on 16-byte boundaries: the copies into LDS ask for 4)
         if (whole_pieces(oa) && whole_pieces(ob))
             for (int shape = 0; shape < kDirectShapes; ++shape)
-                for (int splits = 1; splits <= kMostSplits; ++splits)
+                for (int splits = 1; splits <= most_splits(kFloatStep); ++splits)
                     consider(direct_float_kernel(sa, sb, shape), kDirectCost[shape], kFloatStep, splits, false);
-        for (int splits = 1; splits <= kMostSplits; ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
+        for (int splits = 1; splits <= most_splits(kFloatStep); ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
         return pl;
     }
     // (a tile's reach stays within 31 bits)
     if ((oa.pack ? oa.toRow : oa.stride) >= (1ll << 22) || (ob.pack ? ob.toRow : ob.stride) >= (1ll << 22)) return pl;
     for (int shape = 0; shape < (oa.pack || ob.pack ? kTileShapes : kStagedShape); ++shape)
-        for (int splits = 1; splits <= kMostSplits; ++splits)
+        for (int splits = 1; splits <= most_splits(kTileStep); ++splits)
             consider(tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), kShapeCost[shape], kTileStep, splits, shape < kStagedShape);
     return pl;
 }
@@ -442,7 +454,6 @@ igcStatus pack_operands(const TilePlan &pl, bool f32, const LinearArgs &a, TileA
         (i ? t.blocksB : t.blocksA) = o.blocks;
     }
     if (n == 0) return IGC_STATUS_SUCCESS;
-    if (workgroups >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
     return launch_kernel(f32 ? reinterpret_cast<const void *>(&linear_parts_pack_kernel) : reinterpret_cast<const void *>(&linear_pack_kernel), p,
                          dim3((unsigned)workgroups), 256, stream);
 }
@@ -489,9 +500,9 @@ igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const
         return rc;
     }
     const long long tiles = (long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile);
-    if (tiles >= (1ll << 31)) return IGC_STATUS_NOT_SUPPORTED;
     return by_types(in, out, [&](auto ti, auto to) {
-        return launch_kernel(reinterpret_cast<const void *>(&linear_any_kernel<decltype(ti), decltype(to)>), a, dim3((unsigned)tiles), 256, handle->stream);
+        return launch_kernel(reinterpret_cast<const void *>(&linear_any_kernel<decltype(ti), decltype(to)>), a, dim3((unsigned)std::min(tiles, kMostGroups)), 256,
+                             handle->stream);
     });
 }
 

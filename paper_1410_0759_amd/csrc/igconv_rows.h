@@ -18,9 +18,11 @@ struct Matrix {
 };
 
 // The descriptor's tensor as rows of adjacent feature maps; false where its feature maps do not lie next to each other or
-// its positions are not evenly spaced in the order n, h, w.
+// its positions are not evenly spaced in the order n, h, w, or where there are more than 2^30 rows or 2^26 columns (the
+// kernels' indexes are 32 bits and step past the end before they stop; so are workgroups times threads).
+constexpr long long kMostRows = 1ll << 30, kMostColumns = 1ll << 26;
 inline bool matrix_of(const igcTensorStruct &t, Matrix *m) {
-    if (t.dim[1] > 1 && t.stride[1] != 1) return false;
+    if ((t.dim[1] > 1 && t.stride[1] != 1) || t.dim[1] > kMostColumns) return false;
     const int order[3] = {3, 2, 0};   // from the innermost position outwards
     long long rows = 1, step = 0;
     for (int d : order) {
@@ -28,8 +30,8 @@ inline bool matrix_of(const igcTensorStruct &t, Matrix *m) {
         if (rows == 1) step = t.stride[d];
         else if (t.stride[d] != rows * step) return false;
         rows *= t.dim[d];
+        if (rows > kMostRows) return false;
     }
-    if (rows >= (1ll << 31)) return false;
     m->rows = rows;
     m->stride = rows == 1 ? t.dim[1] : step;
     m->cols = t.dim[1];
