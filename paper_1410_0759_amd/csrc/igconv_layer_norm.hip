@@ -275,15 +275,17 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
     __shared__ W slots[2][2][norm_threads(LANES) / 64];
     const int t = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     const W *scale_p = static_cast<const W *>(a.scale), *shift_p = static_cast<const W *>(a.shift);
-    constexpr bool ROOM = LANES < 1024;     // (1024 threads of 128 registers hold the row only)
+    constexpr bool ROOM = LANES < 1024;     // (1024 threads of 128 registers hold this row and the next only)
     W scale[CHUNKS][E], shift[CHUNKS][E];   // alpha times
     const Place<LANES, CHUNKS, E, WHOLE> at(t, a.C);
     auto load_params = [&](int j) __attribute__((always_inline)) {
         Chunk<W, E> sc, sh;
+        int c = at.c[j];
+        if (!ROOM) asm volatile("" : "+v"(c));   // (row by row, not all of them from before the rows on)
 #pragma unroll
         for (int e = 0; e < E; ++e) sc.v[e] = W(1), sh.v[e] = W(0);
-        if (scale_p && at.live[j]) load_chunk(sc, scale_p + at.c[j]);
-        if (shift_p && at.live[j]) load_chunk(sh, shift_p + at.c[j]);
+        if (scale_p && at.live[j]) load_chunk(sc, scale_p + c);
+        if (shift_p && at.live[j]) load_chunk(sh, shift_p + c);
 #pragma unroll
         for (int e = 0; e < E; ++e) scale[j][e] = a.alpha * sc.v[e], shift[j][e] = a.alpha * sh.v[e];
     };
@@ -299,10 +301,9 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
         for (int j = 0; j < CHUNKS; ++j)
             if (at.live[j]) load_chunk(raw[j], x + at.c[j]);
     };
-    if (ROOM && row < a.M) load(row);
+    if (row < a.M) load(row);
     // (the rows of a workgroup's wavefronts end together but for the last round: with LANES = 64 there is no barrier in the loop)
     for (int parity = 0; row < a.M; row += stride, parity ^= 1) {
-        if (!ROOM) load(row);
         W x[CHUNKS][E];
         W sum = W(0);
 #pragma unroll
@@ -317,11 +318,11 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
         }
         TY *y = static_cast<TY *>(a.y) + row * a.ys;
         Chunk<TY, E> old[CHUNKS];
-        if (a.beta != W(0))   // (all of the row, before any of it is written)
+        if ((ROOM || !WHOLE) && a.beta != W(0))   // (all of the row, before any of it is written)
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
                 if (at.live[j]) load_chunk(old[j], y + at.c[j]);
-        if (ROOM && row + stride < a.M) load(row + stride);
+        if (row + stride < a.M) load(row + stride);
         if (!WHOLE && a.beta != W(0))
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j)
@@ -341,7 +342,11 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_held_kernel(co
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (!at.live[j]) continue;
-            if (!ROOM) load_params(j);
+            if (!ROOM) {
+                __builtin_amdgcn_sched_barrier(0);   // (one chunk's at a time)
+                load_params(j);
+                if (WHOLE && a.beta != W(0)) load_chunk(old[j], y + at.c[j]);
+            }
             W out[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) out[e] = x[j][e] * s * scale[j][e] + shift[j][e];
@@ -372,7 +377,9 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_held_
         Chunk<W, E> sc;
 #pragma unroll
         for (int e = 0; e < E; ++e) sc.v[e] = W(1);
-        if (a.scale && at.live[j]) load_chunk(sc, a.scale + at.c[j]);
+        int c = at.c[j];
+        if (!ROOM) asm volatile("" : "+v"(c));   // (as above)
+        if (a.scale && at.live[j]) load_chunk(sc, a.scale + c);
 #pragma unroll
         for (int e = 0; e < E; ++e) scale[j][e] = sc.v[e];
     };
