@@ -4,7 +4,16 @@
 //   backward data    dx = alpha (dy w) f'(z) + beta r
 //   backward filter  dw = alpha dy^T x + beta dw,  dbias = alpha (column sums of dy) + beta dbias
 //
-// Products of bfloat16 are accumulated in fp32 by the matrix instructions, in a fixed order.
+// Accumulated in fp32 by the matrix instructions, in a fixed order.  Four kernels, the choice by what their steps were measured to take
+// (`plan_tiles`): bfloat16 tiles of 256 x 256, 128 x 128 or 64 x 128, straight from memory or, where rows lie off 16-byte boundaries, from copies
+// or through registers (igconv_linear_tiles.hpp); float as it is where the filter's reading or the launch is what takes the time (the same file);
+// float in bfloat16 parts (igconv_linear_float.hpp); and the one below for anything.  Few tiles: the reduction is cut into ranges, whose
+// sums a second kernel adds in their order with the epilogue.
+//
+// Large products are bound by the matrix instructions under the card's power (zeros for numbers: 580 us for 770 in one run): 8192^3 forward 736 us, 1493 TFLOP/s,
+// backward data 756, backward filter 796.  Their epilogue has no matrix instructions beside it: 8192 x 4096 -> 16384 775 us, with z kept 797, with
+// GELU 844; the gradient back through GELU 789 -> 921, of which the vector instructions of f' alone (two transcendental ones and about sixteen
+// others an element) are 80.  Few tokens are bound by the filter's bytes: 8 x 4096 -> 16384 26 us, 5.1 TB/s.
 #include "igconv_linear_float.hpp"
 
 namespace igc {
@@ -168,10 +177,30 @@ igcStatus check_beside(igcTensorDescriptor_t out, igcTensorDescriptor_t d, const
     return IGC_STATUS_SUCCESS;
 }
 
-// ---- the sum of the ranges' parts, with the epilogue --------------------------------------------------------------------
-// a thread per eight neighbours of a row
+// ---- the sum of the ranges' parts, with the epilogue; the bias gradient ----------------------------------------------------
+struct FinishArgs : TileArgs {
+    long long partsGroups;         // workgroups of the first kind (0: one range, nothing to add)
+    // the sums of the first operand's rows over ranges and columns of tiles: sums[i][M], i < sumsCount
+    int sumsCount;
+    float sumsAlpha, sumsBeta;
+    float *sums;
+};
+
+// A thread per eight neighbours of a row; the workgroups behind them a thread per row's sum.  (One launch for both: 3333 x 1001 x 1503 backward filter
+// 34.3 us for 36.1 with two.)
 template <class TO>
-__global__ __launch_bounds__(256) void linear_parts_kernel(const TileArgs p) {
+__global__ __launch_bounds__(256) void linear_finish_kernel(const FinishArgs p) {
+    if (blockIdx.x >= p.partsGroups) {
+        const long long m = (blockIdx.x - p.partsGroups) * 256 + threadIdx.x;
+        if (m >= p.M) return;
+        float sum = 0.f;
+#pragma unroll 8
+        for (int i = 0; i < p.sumsCount; ++i) sum += p.columnParts[(long long)i * p.M + m];
+        float v = p.sumsAlpha * sum;
+        if (p.sumsBeta != 0.f) v += p.sumsBeta * p.sums[m];
+        p.sums[m] = v;
+        return;
+    }
     const long long groups = p.partsRow / 8, id = (long long)blockIdx.x * 256 + threadIdx.x;
     const int n = (int)(id % groups) * 8;
     if (id / groups >= p.M) return;
@@ -304,18 +333,6 @@ __global__ __launch_bounds__(256) void linear_parts_pack_kernel(const PackArgs a
             if (block < p.blocks) store_parts(p.to + ((long long)step * p.blocks + block) * (kFloatParts * kUnitBytes / 2), c * 16 + l16, x);
         }
     }
-}
-
-// ---- the sums of the first operand's rows (bias gradient) over ranges and tiles --------------------------------------------------
-__global__ __launch_bounds__(256) void linear_sums_kernel(const float *parts, int count, int M, float alpha, float beta, float *out) {
-    const int m = (int)blockIdx.x * 256 + threadIdx.x;
-    if (m >= M) return;
-    float sum = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < count; ++i) sum += parts[(long long)i * M + m];
-    float v = alpha * sum;
-    if (beta != 0.f) v += beta * out[m];
-    out[m] = v;
 }
 
 // ---- the choice of a tile and of the ranges -------------------------------------------------------------------------------
@@ -482,20 +499,17 @@ igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const
         t.partsRow = round_up(a.N, 8);
         t.columnParts = sums.out ? reinterpret_cast<float *>(ws + pl.sumsAt) : nullptr;
         rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
-        if (rc == IGC_STATUS_SUCCESS && pl.splits > 1) {
-            const void *sum = out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_parts_kernel<float>)
-                                                    : reinterpret_cast<const void *>(&linear_parts_kernel<bf16_t>);
-            rc = launch_kernel(sum, t, dim3((unsigned)((a.M * (t.partsRow / 8) + 255) / 256)), 256, handle->stream);
-        }
-        if (rc == IGC_STATUS_SUCCESS && sums.out) {
-            const float *parts = t.columnParts;
-            int count = pl.splits * pl.tilesN, M = a.M;
-            SumsOut o = sums;
-            void *argv[] = {&parts, &count, &M, &o.alpha, &o.beta, &o.out};
-            *summed = true;
-            if (hipLaunchKernel(reinterpret_cast<const void *>(&linear_sums_kernel), dim3((unsigned)(M + 255) / 256u), dim3(256), argv, 0,
-                                static_cast<hipStream_t>(handle->stream)) != hipSuccess)
-                rc = IGC_STATUS_EXECUTION_FAILED;
+        if (rc == IGC_STATUS_SUCCESS && (pl.splits > 1 || sums.out)) {
+            FinishArgs f{};
+            static_cast<TileArgs &>(f) = t;
+            f.partsGroups = pl.splits > 1 ? (a.M * (t.partsRow / 8) + 255) / 256 : 0;
+            f.sumsCount = pl.splits * pl.tilesN;
+            f.sums = sums.out; f.sumsAlpha = sums.alpha; f.sumsBeta = sums.beta;
+            const long long sum_groups = sums.out ? (a.M + 255) / 256 : 0;
+            rc = launch_kernel(out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_finish_kernel<float>)
+                                                     : reinterpret_cast<const void *>(&linear_finish_kernel<bf16_t>),
+                               f, dim3((unsigned)(f.partsGroups + sum_groups)), 256, handle->stream);
+            if (summed) *summed = sums.out != nullptr;
         }
         return rc;
     }
