@@ -452,20 +452,23 @@ igcStatus igcPoolingBackward(igcHandle_t handle, igcPoolingDescriptor_t poolDesc
  * The functions below see a tensor as a matrix: every position (n,h,w) is a row, its feature
  * maps are the columns.  Feature maps must lie next to each other (stride 1) and the positions
  * be evenly spaced in the order n, h, w, with any distance between rows (tokens (M,C,1,1), a
- * slice of a wider buffer, N,H,W,C images); anything else is NOT_SUPPORTED.  A tensor may
- * exceed 2 GiB.  alpha, beta and paramBeta are HOST floats (doubles for double tensors).
+ * slice of a wider buffer, N,H,W,C images); anything else is NOT_SUPPORTED, and so are more
+ * than 2^30 rows or 2^26 feature maps.  A tensor may exceed 2 GiB.  alpha, beta and paramBeta are HOST floats (doubles for double tensors).
  * Sums are accumulated in fp32 (fp64 for double tensors) in a fixed order: results are
  * bitwise repeatable.  Outputs must not overlap inputs or each other except where said;
  * an output is read only where its factor is not 0.  Errors as for the other functions:
  * BAD_PARAM for null pointers, mismatched dimensions, aliasing output strides, misaligned
  * pointers; NOT_INITIALIZED; NOT_SUPPORTED; EXECUTION_FAILED; validation precedes any GPU call.
  *
+ * A row that holds an infinity or NaN has no effect on other rows.
+ *
  * igcLayerNormForward: per row, over its C feature maps,
  *   y = alpha * ((x - mean) * invStd * scale + shift) + beta * y,
  *   mean = sum(x) / C,  invStd = 1 / sqrt(sum((x - mean)^2) / C + epsilon).
  * x and y: float or bfloat16, each its own, or both double.  scale, shift (C values) and mean,
  * invStd (one value per row): packed floats (doubles for double x), each may be NULL: no scale,
- * no shift, not kept.  epsilon >= 0, finite.  y may be x itself (same type, same descriptor). */
+ * no shift, not kept.  epsilon >= 0, finite (0 and a row without spread: 1 / 0).  y may be x
+ * itself (same type, same descriptor). */
 igcStatus igcLayerNormForward(igcHandle_t handle, const void *alpha,
                               igcTensorDescriptor_t xDesc, const void *x,
                               const void *scale, const void *shift, double epsilon,
@@ -501,8 +504,17 @@ igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha,
  * packed floats or NULL; activation: an igcActivationMode or IGC_ACTIVATION_IDENTITY; z: NULL
  * where it is not kept; f is applied before z is rounded.  r is read only where *beta != 0
  * (else rDesc and r may be NULL) and may be y itself (same descriptor).  Double:
- * NOT_SUPPORTED.  workSpace (device, 16-byte aligned, contents mean nothing): as many bytes as
- * the query reports, or NULL / less: same result to rounding, slower. */
+ * NOT_SUPPORTED.
+ * Float products: long ones are taken as bfloat16 ones of three parts of each operand, off by at
+ * most 2^-21 of a product, about 2^-24 on average; infinities and NaN come out as of the floats.
+ * f for bfloat16 results is off by up to 4e-7 (1 + |z|) before it is rounded.
+ * workSpace (device, 16-byte aligned, contents mean nothing) holds the sums of ranges of the
+ * reduction where there are few tiles, copies of bfloat16 operands whose rows do not lie on
+ * 16-byte boundaries, the parts of float ones, and the bias gradient's sums.  The query reports
+ * what the fastest choice takes with x, w, dy and workSpace on 16-byte boundaries.  Any size
+ * will do, NULL too: the call takes the fastest way that fits into it; the order of a sum, so
+ * its rounding, depends on the size lent.  Without any, products with few tiles, of floats and
+ * of rows off 16-byte boundaries are up to 8 times slower, others as fast. */
 igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
                                            igcFilterDescriptor_t wDesc,
                                            igcTensorDescriptor_t yDesc, size_t *sizeInBytes);

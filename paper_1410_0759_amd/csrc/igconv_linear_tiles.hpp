@@ -2,8 +2,9 @@
 // time (more of them: igconv_linear_float.hpp).
 //
 // A workgroup computes a BM x BN tile in steps of 128 bytes of the reduction, a wavefront of it FM x FN blocks of 16 x 16 with
-// v_mfma_f32_16x16x32_bf16 or v_mfma_f32_16x16x4_f32.  (Blocks of 32 x 32 are slower: 8192^3 814 us instead of 754.)  Both operands go from global memory straight into LDS (16 bytes per lane, no registers), two steps
-// ahead.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
+// v_mfma_f32_16x16x32_bf16 or v_mfma_f32_16x16x4_f32.  (Blocks of 32 x 32 were slower: 8192^3
+// 814 us instead of 754 with two places in LDS for each operand; it is 736 now.)  Both operands go from global memory straight into LDS (16 bytes per lane, no
+// registers), two steps ahead.  An operand whose reduction index is adjacent in memory lies in LDS row by row (128 bytes a row) and is
 // read 16 bytes per lane; one whose reduction index runs along the rows (w for backward data, x and dy for backward filter)
 // lies there as it is, k by k, and is read with the transposing 8-byte reads (float: 4 bytes at a time) - no operand is transposed in memory.  In both cases
 // the 16-byte (32-, 64-byte) pieces of a row are permuted by an exclusive or with the row's number so that the lanes of a read lie
@@ -13,6 +14,9 @@
 // second half in the first quarter of the step, after which its place in LDS is free: there, at a first barrier, the step after next is
 // requested (three places for the first operand, two for the second: all of the LDS with 256 x 256).  Two slots before the end, at a second
 // barrier, the next step has to be there; the remaining matrix instructions cover its first reads.
+//
+// Tried at 8192^3 and slower: workgroups that stay and take several tiles (798 us for 743: a store before the next tile's copies holds up their
+// waits), raised priority of the multiplying wavefronts (783 for 761), rings of four places (below).  Tiles taken 4 or 8 rows at a time: alike.
 #ifndef IGCONV_LINEAR_TILES_HPP_
 #define IGCONV_LINEAR_TILES_HPP_
 
