@@ -12,8 +12,8 @@
 //
 // Large products are bound by the matrix instructions under the card's power (zeros for numbers: 580 us for 770 in one run): 8192^3 forward 736 us, 1493 TFLOP/s,
 // backward data 756, backward filter 796.  Their epilogue has no matrix instructions beside it: 8192 x 4096 -> 16384 775 us, with z kept 797, with
-// GELU 844; the gradient back through GELU 789 -> 921, of which the vector instructions of f' alone (two transcendental ones and about sixteen
-// others an element) are 80.  Few tokens are bound by the filter's bytes: 8 x 4096 -> 16384 26 us, 5.1 TB/s.
+// GELU 844; the gradient back through GELU 789 -> 912, for 268 MB of z (55 us at a copy's rate, asked for by all compute units at once) and f'.
+// Neither a quarter fewer vector instructions in f and f' nor z loaded before the last products made a difference: not kept.  Few tokens are bound by the filter's bytes: 8 x 4096 -> 16384 26 us, 5.1 TB/s.
 #include "igconv_linear_float.hpp"
 
 namespace igc {
