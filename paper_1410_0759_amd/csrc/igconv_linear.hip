@@ -361,8 +361,9 @@ bool fits(const OperandPlan &o, int n) {
     return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && std::max(o.stride, (long long)o.cols) < (1ll << 22);
 }
 
-bool whole_pieces(const OperandPlan &o) {
-    return o.cols % 4 == 0 && (o.rows == 1 || o.stride >= o.cols) && std::max(o.stride, (long long)o.cols) < (1ll << 21);
+// Float: whole pieces along the reduction index; across it none are needed.
+bool whole_pieces(const OperandPlan &o, bool strided) {
+    return (strided || o.cols % 4 == 0) && (o.rows == 1 || o.stride >= o.cols) && std::max(o.stride, (long long)o.cols) < (1ll << 21);
 }
 
 // The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
@@ -431,7 +432,7 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     auto most_splits = [&](int step) { return std::min(64, (a.K + step - 1) / step); };
     if (f32) {
         // (float rows need not begin on 16-byte boundaries: the copies into LDS ask for 4)
-        if (whole_pieces(oa) && whole_pieces(ob))
+        if (whole_pieces(oa, sa) && whole_pieces(ob, sb))
             for (int shape = 0; shape < kDirectShapes; ++shape)
                 for (int splits = 1; splits <= most_splits(kFloatStep); ++splits)
                     consider(direct_float_kernel(sa, sb, shape), kDirectCost[shape], kFloatStep, splits, false);

@@ -73,10 +73,12 @@ struct OperandCopy {
         rows_left = rows - row0;
         cols_left = rows - row0;
         k_row = wave * REQUESTS * 8 + (lane >> 3);
-        // (whole pieces: a matrix whose rows do not end with one is a copy that does)
+        // (Whole pieces: a bfloat16 matrix whose rows do not end with one is a copy that does.  Float and strided: the last piece of a row may hold
+        // what follows the row, which only reaches results outside the product; of a piece across the end of the buffer the words inside it are
+        // read, the others are zeros, as was measured.)
         if constexpr (STRIDED) {
             base = static_cast<const uint8_t *>(matrix) + (long long)row0 * ELEM;
-            left = ((K - 1) * k_stride + (rows + IN_PIECE - 1) / IN_PIECE * IN_PIECE - row0) * ELEM;
+            left = ((K - 1) * k_stride + (ELEM == 4 ? rows : (rows + IN_PIECE - 1) / IN_PIECE * IN_PIECE) - row0) * ELEM;
             stride_bytes = (uint32_t)k_stride * ELEM;
             const int k = lane / PIECES, at = lane % PIECES;
             k_piece = wave * REQUESTS * KROWS + k;       // (the k row of the first request)
