@@ -510,11 +510,12 @@ igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha,
  * f for bfloat16 results is off by up to 4e-7 (1 + |z|) before it is rounded.
  * workSpace (device, 16-byte aligned, contents mean nothing) holds the sums of ranges of the
  * reduction where there are few tiles, copies of bfloat16 operands whose rows do not lie on
- * 16-byte boundaries, the parts of float ones, and the bias gradient's sums.  The query reports
- * what the fastest choice takes with x, w, dy and workSpace on 16-byte boundaries.  Any size
+ * 4-byte boundaries or have, along the reduction index, a length that is no multiple of 8,
+ * the parts of float ones, and the bias gradient's sums.  The query reports what the fastest
+ * choice takes with x, w and dy on 4-byte boundaries.  Any size
  * will do, NULL too: the call takes the fastest way that fits into it; the order of a sum, so
  * its rounding, depends on the size lent.  Without any, products with few tiles, of floats and
- * of rows off 16-byte boundaries are up to 8 times slower, others as fast. */
+ * of operands that would be copied are up to 8 times slower, others as fast. */
 igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
                                            igcFilterDescriptor_t wDesc,
                                            igcTensorDescriptor_t yDesc, size_t *sizeInBytes);

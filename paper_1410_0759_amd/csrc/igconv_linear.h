@@ -44,7 +44,7 @@ struct TileKernel {
     int bm, bn, threads;
     const void *kernel;   // null: not offered
 };
-constexpr int kTileShapes = 4, kStagedShape = 3 /* rows off 16-byte boundaries */, kDirectShapes = 2;
+constexpr int kTileShapes = 4, kStagedShape = 3 /* operands that the others have copied first */, kDirectShapes = 2;
 TileKernel direct_float_kernel(bool sa, bool sb, int shape);   // float operands as they are: few tokens, small products
 TileKernel float_kernel();                                           // any pass, operands in parts (igconv_linear_float.hpp)
 TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent

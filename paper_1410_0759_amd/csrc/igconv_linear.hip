@@ -5,8 +5,8 @@
 //   backward filter  dw = alpha dy^T x + beta dw,  dbias = alpha (column sums of dy) + beta dbias
 //
 // Accumulated in fp32 by the matrix instructions, in a fixed order.  Four kernels, the choice by what their steps were measured to take
-// (`plan_tiles`): bfloat16 tiles of 256 x 256, 128 x 128 or 64 x 128, straight from memory or, where rows lie off 16-byte boundaries, from copies
-// or through registers (igconv_linear_tiles.hpp); float as it is where the filter's reading or the launch is what takes the time (the same file);
+// (`plan_tiles`): bfloat16 tiles of 256 x 256, 128 x 128 or 64 x 128, straight from memory or, where rows lie off 4-byte boundaries or end inside
+// 16 bytes of the reduction, from copies or through registers (igconv_linear_tiles.hpp); float as it is where the filter's reading or the launch is what takes the time (the same file);
 // float in bfloat16 parts (igconv_linear_float.hpp); and the one below for anything.  Few tiles: the reduction is cut into ranges, whose
 // sums a second kernel adds in their order with the epilogue.
 //
@@ -356,23 +356,22 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
     return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
 }
 
-// Rows of whole 16-byte pieces (of n elements) on 16-byte boundaries, if the first is, no row inside another; a tile's reach below 2^31 bytes.
-bool fits(const OperandPlan &o, int n) {
-    return o.cols % n == 0 && (o.rows == 1 || (o.stride % n == 0 && o.stride >= o.cols)) && std::max(o.stride, (long long)o.cols) < (1ll << 22);
-}
-
-// Float: whole pieces along the reduction index; across it none are needed.
-bool whole_pieces(const OperandPlan &o, bool strided) {
-    return (strided || o.cols % 4 == 0) && (o.rows == 1 || o.stride >= o.cols) && std::max(o.stride, (long long)o.cols) < (1ll << 21);
+// Whether the tiles take an operand as it lies: rows on boundaries of 4 bytes, of whole pieces of 16 along the reduction index, of whole words across
+// it; no row inside another; a tile's reach below 2^31 bytes.  (Rows on 4-byte boundaries as against copies on 16: forward 1000^3 9.6 us for 13.5,
+// 8192 x 4096 x 4096 212 for 221, filter gradient 208 for 248; on 16-byte boundaries 9.5, 201 and 207.)
+bool fits(const OperandPlan &o, bool strided, int elem, const void *p) {
+    const int words = 4 / elem, most = (1 << 23) / elem;
+    return o.cols % (strided ? words : 16 / elem) == 0 && (o.rows == 1 || (o.stride % words == 0 && o.stride >= o.cols)) &&
+           std::max(o.stride, (long long)o.cols) < most && (uintptr_t)p % 4 == 0;
 }
 
 // The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
-OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, bool aligned) {
+OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, const void *p) {
     OperandPlan o;
     o.rows = strided ? K : n;
     o.cols = (int)(strided ? n : K);
     o.stride = strided ? ks : ns;
-    o.pack = f32 || !aligned || !fits(o, 8);
+    o.pack = f32 || !fits(o, strided, 2, p);
     o.toRow = round_up(o.cols, 8);
     o.blocks = (int)((n + 15) / 16);
     if (o.pack)
@@ -394,10 +393,10 @@ constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes
 // workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;
 
-TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, bool aligned_a, bool aligned_b, size_t room) {
+TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
-    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, aligned_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, aligned_b);
+    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b);
     double best = 1e300;
     // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
     auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
@@ -431,8 +430,7 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     // (no range without a step)
     auto most_splits = [&](int step) { return std::min(64, (a.K + step - 1) / step); };
     if (f32) {
-        // (float rows need not begin on 16-byte boundaries: the copies into LDS ask for 4)
-        if (whole_pieces(oa, sa) && whole_pieces(ob, sb))
+        if (fits(oa, sa, 4, a.a) && fits(ob, sb, 4, a.b))
             for (int shape = 0; shape < kDirectShapes; ++shape)
                 for (int splits = 1; splits <= most_splits(kFloatStep); ++splits)
                     consider(direct_float_kernel(sa, sb, shape), kDirectCost[shape], kFloatStep, splits, false);
@@ -484,7 +482,7 @@ struct SumsOut {
 
 igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes, const SumsOut &sums = SumsOut(),
                       bool *summed = nullptr) {
-    const TilePlan pl = plan_tiles(handle, in, out, a, sums.out != nullptr, on16(a.a), on16(a.b), workSpace && on16(workSpace) ? bytes : 0);
+    const TilePlan pl = plan_tiles(handle, in, out, a, sums.out != nullptr, workSpace && on16(workSpace) ? bytes : 0);
     if (pl.tiles) {
         TileArgs t{};
         static_cast<LinearArgs &>(t) = a;
@@ -555,7 +553,7 @@ igcStatus igcGetLinearForwardWorkspaceSize(igcHandle_t handle, igcTensorDescript
     Matrix x, y;
     const igcStatus st = check_linear(xDesc, wDesc, yDesc, false, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), false, true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, yDesc->dtype, forward_sizes(x, *wDesc), false, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -589,7 +587,7 @@ igcStatus igcGetLinearBackwardDataWorkspaceSize(igcHandle_t handle, igcFilterDes
     Matrix dy, dx;
     const igcStatus st = check_linear(dyDesc, wDesc, dxDesc, true, &dy, &dx);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), false, true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, dyDesc->dtype, dxDesc->dtype, backward_data_sizes(dy, *wDesc), false, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -623,7 +621,7 @@ igcStatus igcGetLinearBackwardFilterWorkspaceSize(igcHandle_t handle, igcTensorD
     Matrix x, dy;
     const igcStatus st = check_linear_filter(xDesc, dyDesc, dwDesc, &x, &dy);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), true, true, true, kNoLimit).bytes;
+    *sizeInBytes = plan_tiles(handle, xDesc->dtype, dwDesc->dtype, backward_filter_sizes(x, dy, *dwDesc), true, kNoLimit).bytes;
     return IGC_STATUS_SUCCESS;
 }
 

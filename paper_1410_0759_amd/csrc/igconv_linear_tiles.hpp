@@ -1,4 +1,4 @@
-// Products of matrices whose rows lie on 16-byte boundaries: bfloat16, and float with few tokens, where reading the filter is what takes the
+// Products of matrices whose rows lie on 4-byte boundaries: bfloat16, and float with few tokens, where reading the filter is what takes the
 // time (more of them: igconv_linear_float.hpp).
 //
 // A workgroup computes a BM x BN tile in steps of 128 bytes of the reduction, a wavefront of it FM x FN blocks of 16 x 16 with
@@ -53,7 +53,7 @@ __device__ __forceinline__ u32x4 raw_buffer(const void *base, uint32_t bytes) {
 
 // One operand's copies into a stage: ROWS rows of the tile, from row `row0` of the operand; elements of ELEM bytes.
 // STRIDED: the reduction index runs along the rows of the matrix in memory (`stride` elements apart), the tile's rows are adjacent.
-// STAGED (bfloat16): the rows begin or end off 16-byte boundaries, which copies straight into LDS do not serve; the lanes load the same pieces into
+// STAGED (bfloat16): the rows begin off 4-byte boundaries or end inside a piece, which copies straight into LDS do not serve; the lanes load the same pieces into
 // registers, element by element where one is cut by the matrix's end, and write them to LDS a step later.
 template <int ROWS, int WAVES, bool STRIDED, int ELEM, bool STAGED>
 struct OperandCopy {
@@ -73,12 +73,12 @@ struct OperandCopy {
         rows_left = rows - row0;
         cols_left = rows - row0;
         k_row = wave * REQUESTS * 8 + (lane >> 3);
-        // (Whole pieces: a bfloat16 matrix whose rows do not end with one is a copy that does.  Float and strided: the last piece of a row may hold
-        // what follows the row, which only reaches results outside the product; of a piece across the end of the buffer the words inside it are
-        // read, the others are zeros, as was measured.)
+        // (Rows end with a whole piece along the reduction index.  Strided, with a whole word of 4 bytes: the last piece of a row may hold what follows the
+        // row, which only reaches results outside the product; of a piece across the end of the buffer the words inside it are read, the
+        // others are zeros, as was measured.)
         if constexpr (STRIDED) {
             base = static_cast<const uint8_t *>(matrix) + (long long)row0 * ELEM;
-            left = ((K - 1) * k_stride + (ELEM == 4 ? rows : (rows + IN_PIECE - 1) / IN_PIECE * IN_PIECE) - row0) * ELEM;
+            left = ((K - 1) * k_stride + (rows + IN_PIECE / 4 - 1) / (IN_PIECE / 4) * (IN_PIECE / 4) - row0) * ELEM;
             stride_bytes = (uint32_t)k_stride * ELEM;
             const int k = lane / PIECES, at = lane % PIECES;
             k_piece = wave * REQUESTS * KROWS + k;       // (the k row of the first request)
