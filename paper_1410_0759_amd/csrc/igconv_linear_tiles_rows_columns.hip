@@ -13,7 +13,7 @@ TileKernel tile_kernel_rows_columns(int shape, bool f32_out) {
     if (shape == 0) return entry<TileConfig<256, 256, 2, 4, false, true>>(f32_out);
     if (shape == 1) return entry<TileConfig<128, 128, 2, 4, false, true>>(f32_out);
     if (shape == 2) return entry<TileConfig<64, 128, 1, 4, false, true>>(f32_out);   // few tokens
-    if (shape == 3) return entry<TileConfig<64, 128, 1, 4, false, true, 2, true>>(f32_out);   // the same, rows off 16-byte boundaries
+    if (shape == 3) return entry<TileConfig<64, 128, 1, 4, false, true, 2, true>>(f32_out);   // the same, operands through registers
     return {};
 }
 
