@@ -63,7 +63,7 @@ struct OperandCopy {
     static constexpr int IN_PIECE = 16 / ELEM;
     const uint8_t *base;
     long long left;             // bytes from `base` to the end of the operand
-    uint32_t stride_bytes, first;
+    uint32_t stride_bytes, first;   // (descriptors hold strides below 2^31 elements: below 2^32 bytes where rows are read through registers)
     int k_piece, k_row;         // (not strided) the lane's first reduction index within a step, and its first row
 
     // (strided) the exclusive or of the pieces of k row k: the rows that a read takes at once lie in different banks
