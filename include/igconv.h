@@ -505,8 +505,9 @@ igcStatus igcLayerNormBackward(igcHandle_t handle, const void *alpha,
  * where it is not kept; f is applied before z is rounded.  r is read only where *beta != 0
  * (else rDesc and r may be NULL) and may be y itself (same descriptor).  Double:
  * NOT_SUPPORTED.
- * Float products: long ones are taken as bfloat16 ones of three parts of each operand, off by at
- * most 2^-21 of a product, about 2^-24 on average; infinities and NaN come out as of the floats.
+ * Float products: long ones are taken as bfloat16 ones of three parts of each operand.  A product
+ * a b is then off by at most 2^-21 of itself, about 2^-24 on average, and 2^-131 (|a| + |b|), which
+ * counts where a factor is below 2^-110; infinities and NaN come out as of the floats.
  * f for bfloat16 results is off by up to 4e-7 (1 + |z|) before it is rounded.
  * workSpace (device, 16-byte aligned, contents mean nothing) holds the sums of ranges of the
  * reduction where there are few tiles, copies of bfloat16 operands whose rows do not lie on

@@ -277,14 +277,14 @@ __device__ __forceinline__ void store_parts(uint16_t *unit, int slot, const floa
             const float v = x[2 * e + i];
             const uint32_t all = __builtin_bit_cast(uint32_t, v), sign = all & 0x80000000u;
             const bool finite = (all & 0x7F800000u) != 0x7F800000u;
-            const uint32_t h = finite ? all & 0xFFFF0000u : (all & 0x007FFFFFu ? 0x7FC00000u : all);   // (an undefined value must not become an infinity)
+            uint32_t h = finite ? all & 0xFFFF0000u : (all & 0x007FFFFFu ? 0x7FC00000u : all);   // (an undefined value must not become an infinity)
             const float r = finite ? v - __builtin_bit_cast(float, h) : 0.f;
             uint32_t m = __builtin_bit_cast(uint32_t, r) & 0xFFFF0000u;
             uint32_t l = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, m)) & 0xFFFF0000u;
-            if ((all & 0x7F800000u) >= 0x0D800000u) {   // from 2^-100 on
-                if ((m & 0x7FFFFFFFu) == 0u) m = sign | 0x00800000u;
-                if ((l & 0x7FFFFFFFu) == 0u) l = sign | 0x00800000u;
-            }
+            const uint32_t least = (all & 0x7FFFFFFFu) != 0u ? sign | 0x00010000u : 0u;   // in place of a part that is zero though x is not
+            if ((h & 0x7FFFFFFFu) == 0u) h = least;
+            if ((m & 0x7FFFFFFFu) == 0u) m = least;
+            if ((l & 0x7FFFFFFFu) == 0u) l = least;
             bits[0][i] = h >> 16; bits[1][i] = m >> 16; bits[2][i] = l >> 16;
         }
 #pragma unroll

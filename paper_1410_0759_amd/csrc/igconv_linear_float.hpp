@@ -4,9 +4,10 @@
 //   l h + h l + m m + m h + h m + h h
 // summed in that order (smallest first) in fp32; m l, l m and l l, below 2^-21 of the product together and about 2^-24 of it on average, are
 // left out.  The matrix instructions do 16 times as many bfloat16 products as float ones in a cycle, so that six of them take a third
-// of the time of one.  Parts have x's sign, and where a part would be zero though x is not it is the smallest normal number of
-// that sign (left as it is below 2^-100, where that number would count): an infinite factor then meets no zero but in a product with
-// zero itself.
+// of the time of one.  Parts have x's sign, and where a part would be zero though x is not it is the smallest subnormal number of
+// that sign, 2^-133, which the matrix instructions take as it is: an infinite factor then meets no zero but in a product with zero itself.
+// Parts end at 2^-133 too, so that of a number below 2^-110 the last bits are lost: x is off by less than 2^-131 in all (a float unit that flushes
+// subnormal operands: 2^-126), which for a product a b comes to less than 2^-131 (|a| + |b|) beside what is left out.
 //
 // The parts lie in memory as they are wanted in LDS (linear_parts_pack_kernel): units of 1 KB, 16 rows by 32 reduction indices of one
 // part, 16 bytes for each lane of a fragment in turn; the three parts of a block of rows next to each other, block after block of rows,
