@@ -356,12 +356,12 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
     return sa ? tile_kernel_columns(shape, f32_out) : (sb ? tile_kernel_rows_columns(shape, f32_out) : tile_kernel_rows(shape, f32_out));
 }
 
-// Whether the tiles take an operand as it lies: rows on boundaries of 4 bytes, of whole pieces of 16 along the reduction index, of whole words across
-// it; no row inside another; a tile's reach below 2^31 bytes.  (Rows on 4-byte boundaries as against copies on 16: forward 1000^3 9.6 us for 13.5,
+// Whether the tiles take an operand as it lies: rows on boundaries of 4 bytes, of whole pieces of 16 along the reduction index (float: of any length), of
+// whole words across it; no row inside another; a tile's reach below 2^31 bytes.  (Rows on 4-byte boundaries as against copies on 16: forward 1000^3 9.6 us for 13.5,
 // 8192 x 4096 x 4096 212 for 221, filter gradient 208 for 248; on 16-byte boundaries 9.5, 201 and 207.)
 bool fits(const OperandPlan &o, bool strided, int elem, const void *p) {
     const int words = 4 / elem, most = (1 << 23) / elem;
-    return o.cols % (strided ? words : 16 / elem) == 0 && (o.rows == 1 || (o.stride % words == 0 && o.stride >= o.cols)) &&
+    return o.cols % (strided || elem == 4 ? words : 16 / elem) == 0 && (o.rows == 1 || (o.stride % words == 0 && o.stride >= o.cols)) &&
            std::max(o.stride, (long long)o.cols) < most && (uintptr_t)p % 4 == 0;
 }
 
@@ -383,12 +383,14 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
 // steps of 256 x 256, 786 us, or 1024 of 128 x 128 two by two, 1003; 2048^3 32 steps, 44, 21.4 (alone) and, 64 x 128 two by two, 24.7;
 // 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.  With the pieces through registers a step waits for memory: 8 x 4097 ->
 // 8000, 252 workgroups of 17 steps, 34 us, 504 of 9, 24 - with copies first 41; 1000 x 1001 -> 1001, 16 steps, 28, with copies first 16.
+// Float as it is: 512 x 4096 -> 4096 in 128 steps, 64 x 128 alone 147, 32 x 128 two by two 145 (in parts 124), 348 x 8083 -> 5280 in 127 steps, 64 x 128
+// two by two 268 (in parts 242).
 struct ShapeCost {
     int per_cu;
     double alone, full, ends;
 };
 constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0.98, 2.5}, {2, 0.42, 0.60, 2.0}, {2, 1.65, 2.00, 2.0}};
-constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.10, 2.00, 2.5}, {2, 0.60, 1.00, 2.0}};
+constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.12, 2.10, 2.5}, {2, 0.60, 1.12, 2.0}};
 // The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory, and what one
 // workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;

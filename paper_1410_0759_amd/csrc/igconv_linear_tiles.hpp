@@ -73,8 +73,9 @@ struct OperandCopy {
         rows_left = rows - row0;
         cols_left = rows - row0;
         k_row = wave * REQUESTS * 8 + (lane >> 3);
-        // (Rows end with a whole piece along the reduction index.  Strided, with a whole word of 4 bytes: the last piece of a row may hold what follows the
-        // row, which only reaches results outside the product; of a piece across the end of the buffer the words inside it are read, the
+        // (Rows of bfloat16 end with a whole piece along the reduction index, of float anywhere: what follows the row in its last piece is cleared in LDS
+        // (`cut`).  Strided, rows end with a whole word of 4 bytes: the last piece of a row may hold what follows the
+        // row, which only reaches results outside the product.  Of a piece across the end of the buffer the words inside it are read, the
         // others are zeros, as was measured.)
         if constexpr (STRIDED) {
             base = static_cast<const uint8_t *>(matrix) + (long long)row0 * ELEM;
@@ -85,7 +86,7 @@ struct OperandCopy {
             first = at;
         } else {
             base = static_cast<const uint8_t *>(matrix) + row0 * row_stride * ELEM;
-            left = ((rows - row0 - 1) * row_stride + (K + IN_PIECE - 1) / IN_PIECE * IN_PIECE) * ELEM;
+            left = ((rows - row0 - 1) * row_stride + (ELEM == 4 ? K : (K + IN_PIECE - 1) / IN_PIECE * IN_PIECE)) * ELEM;
             stride_bytes = (uint32_t)row_stride * ELEM;
             const int row = lane >> 3, piece = (lane & 7) ^ row;
             first = (uint32_t)(wave * REQUESTS * 8 + row) * stride_bytes + piece * 16u;
@@ -142,6 +143,15 @@ struct OperandCopy {
             off = k + k_piece < K ? first + (uint32_t)i * 8u * stride_bytes + (uint32_t)k * ELEM : kNowhere;
         }
         copy_to_lds(buf, to + i * 1024, off);
+    }
+
+    // (float, not strided) The tile's rows end with index `end` of the step in `stage`: zeros in the rest of that index's piece, by all of the workgroup.
+    static __device__ __forceinline__ void cut(uint8_t *stage, int end) {
+        if constexpr (!STRIDED)
+            for (int row = threadIdx.x; row < ROWS; row += 64 * WAVES) {
+                float *piece = reinterpret_cast<float *>(stage + row * 128 + (((end / IN_PIECE) ^ (row & 7)) * 16));
+                for (int e = end % IN_PIECE; e < IN_PIECE; ++e) piece[e] = 0.f;
+            }
     }
 };
 
@@ -368,6 +378,16 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         else __builtin_amdgcn_s_waitcnt(0x0F70 | (LATER & 15) | ((LATER >> 4) << 14));
         asm volatile("s_barrier" ::: "memory");
     };
+    // The last step of float rows that end inside a piece, once it has arrived: the rest of the piece may be anything, the next row's infinities too.
+    constexpr bool CUT = Cfg::ELEM == 4 && !(Cfg::SA && Cfg::SB);
+    const int tail = CUT && kEnd % 4 != 0 ? kEnd - kBegin - (steps - 1) * Cfg::STEP : 0;
+    auto cut = [&](int step, uint8_t *stageA, uint8_t *stageB) __attribute__((always_inline)) {
+        if (!CUT || tail == 0 || step != steps - 1) return;
+        decltype(copyA)::cut(stageA, tail);
+        decltype(copyB)::cut(stageB, tail);
+        __builtin_amdgcn_s_waitcnt(0xC07F);
+        asm volatile("s_barrier" ::: "memory");
+    };
 
     f32x4 acc[FM][FN];
 #pragma unroll
@@ -384,6 +404,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         }
     }
     arrived();
+    cut(0, lds, ldsB);
     typename Fragment<Cfg::ELEM>::type a[4], b[2][FN];
     a[0] = readA.read(lds, 0, 0);
     a[1] = readA.read(lds, 0, 1);
@@ -403,7 +424,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
         const uint8_t *hereA = lds + atA * Cfg::BYTES_A, *hereB = ldsB + atB * Cfg::BYTES_B;
         atA = atA == Cfg::SLOTS_A - 1 ? 0 : atA + 1;
         atB = atB == Cfg::SLOTS_B - 1 ? 0 : atB + 1;
-        const uint8_t *nextA = lds + atA * Cfg::BYTES_A, *nextB = ldsB + atB * Cfg::BYTES_B;
+        uint8_t *nextA = lds + atA * Cfg::BYTES_A, *nextB = ldsB + atB * Cfg::BYTES_B;
         if constexpr (Cfg::SA) {
             if (turn == 0)
 #pragma unroll
@@ -428,7 +449,10 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
                 asm volatile("s_barrier" ::: "memory");
                 begin_requests();
             }
-            if (t == SLOTS - 2) arrived();
+            if (t == SLOTS - 2) {
+                arrived();
+                cut(s + 1, nextA, nextB);
+            }
             // (a few to a slot: eight wavefronts with eight requests each at once wait for each other's)
 #pragma unroll
             for (int i = 0; i < R; ++i)
