@@ -59,9 +59,19 @@ class FeedForward:
         self.grads = {n: like(getattr(self, n)) for n in ("w1", "b1", "w2", "b2", "scale", "shift")}
         self._buffers = {}
 
-    def _use(self, x):
-        if x.dtype != self.dtype or x.dim() != 2 or x.shape[1] != self.width or x.stride(1) != 1:
-            raise ValueError("x: rows of %d adjacent features of type %s" % (self.width, self.dtype))
+    def _check(self, name, t, rows=None):
+        """Rows as the library's functions read them; they are not told more than the distance between rows."""
+        if t.dim() != 2 or t.shape[1] != self.width or t.stride(1) != 1 or t.dtype != self.dtype or rows not in (None, t.shape[0]):
+            raise ValueError("%s: %srows of %d adjacent features of type %s" % (name, "" if rows is None else "%d " % rows, self.width, self.dtype))
+        if t.device != self.w1.device:
+            raise ValueError("%s: on the weights' device, %s" % (name, self.w1.device))
+
+    def _use(self, x, dy=None):
+        self._check("x", x)
+        if dy is not None:
+            self._check("dy", dy, x.shape[0])
+        if not self.w1.is_cuda:
+            raise ValueError("the block's calls need its weights on a GPU")
         self.handle.set_stream(torch.cuda.current_stream().cuda_stream)
         if x.shape[0] not in self._buffers:
             self._buffers[x.shape[0]] = _Buffers(self, x.shape[0])
@@ -79,9 +89,9 @@ class FeedForward:
         return b.y
 
     def backward(self, x, dy, accumulate=False):
-        """Gradient with respect to x of the forward pass that ran last on x, given that with respect to its result; ``grads`` receives
-        (accumulate: is increased by) the parameters' gradients."""
-        b, hd, xd, dyd = self._use(x), self.handle, _desc(x), _desc(dy)
+        """Gradient with respect to x of the forward pass that ran last on x, given that with respect to its result (dy: laid out in rows as
+        x is, any distance apart); ``grads`` receives (accumulate: is increased by) the parameters' gradients."""
+        b, hd, xd, dyd = self._use(x, dy), self.handle, _desc(x), _desc(dy)
         g, keep = {n: t.data_ptr() for n, t in self.grads.items()}, 1.0 if accumulate else 0.0
         ws, room = b.ws.data_ptr(), b.room
         ig.check(ig.linear_backward_filter(hd, 1.0, b.wide, b.a.data_ptr(), dyd, dy.data_ptr(), ws, room, keep, self.dw2_desc, g["w2"], g["b2"]),
