@@ -18,23 +18,25 @@ def _desc(t):
 
 
 class _Buffers:
-    """What a batch of M tokens needs: the forward pass's results that the backward pass reads, gradients, workspaces."""
+    """What a batch of M tokens needs.  keep: also the forward pass's results that the backward pass reads, and the gradients."""
 
-    def __init__(self, block, M):
+    def __init__(self, block, M, keep):
         D, H, dt, dev = block.width, block.hidden, block.dtype, block.w1.device
         new = lambda n, dtype=dt: torch.empty(M, n, dtype=dtype, device=dev)
-        self.h, self.z, self.a, self.y = new(D), new(H), new(H), new(D)
-        self.mean, self.invstd = (torch.empty(M, device=dev) for _ in range(2))
-        self.dz, self.dh, self.dx = new(H), new(D), new(D)
-        self.narrow, self.wide = _desc(self.h), _desc(self.z)         # rows of D, rows of H
+        self.h, self.a, self.y = new(D), new(H), new(D)
+        self.narrow, self.wide = _desc(self.h), _desc(self.a)         # rows of D, rows of H
         hd, w1, w2 = block.handle, block.w1_desc, block.w2_desc
         sizes = [ig.get_linear_forward_workspace_size(hd, self.narrow, w1, self.wide),
-                 ig.get_linear_forward_workspace_size(hd, self.wide, w2, self.narrow),
-                 ig.get_linear_backward_data_workspace_size(hd, w2, self.narrow, self.wide),
-                 ig.get_linear_backward_data_workspace_size(hd, w1, self.wide, self.narrow),
-                 ig.get_linear_backward_filter_workspace_size(hd, self.narrow, self.wide, block.dw1_desc),
-                 ig.get_linear_backward_filter_workspace_size(hd, self.wide, self.narrow, block.dw2_desc),
-                 ig.get_layer_norm_backward_workspace_size(hd, self.narrow, self.narrow, self.narrow)]
+                 ig.get_linear_forward_workspace_size(hd, self.wide, w2, self.narrow)]
+        if keep:
+            self.x = None                                               # the rows that the results are of
+            self.z, self.dz, self.dh, self.dx = new(H), new(H), new(D), new(D)
+            self.mean, self.invstd = (torch.empty(M, device=dev) for _ in range(2))
+            sizes += [ig.get_linear_backward_data_workspace_size(hd, w2, self.narrow, self.wide),
+                      ig.get_linear_backward_data_workspace_size(hd, w1, self.wide, self.narrow),
+                      ig.get_linear_backward_filter_workspace_size(hd, self.narrow, self.wide, block.dw1_desc),
+                      ig.get_linear_backward_filter_workspace_size(hd, self.wide, self.narrow, block.dw2_desc),
+                      ig.get_layer_norm_backward_workspace_size(hd, self.narrow, self.narrow, self.narrow)]
         self.room = max(sizes)                                          # (calls of one stream follow each other: one workspace for all)
         self.ws = torch.empty(max(self.room, 16), dtype=torch.uint8, device=dev)
 
@@ -66,32 +68,44 @@ class FeedForward:
         if t.device != self.w1.device:
             raise ValueError("%s: on the weights' device, %s" % (name, self.w1.device))
 
-    def _use(self, x, dy=None):
+    def _use(self, x, dy=None, keep=True):
         self._check("x", x)
         if dy is not None:
             self._check("dy", dy, x.shape[0])
         if not self.w1.is_cuda:
             raise ValueError("the block's calls need its weights on a GPU")
         self.handle.set_stream(torch.cuda.current_stream().cuda_stream)
-        if x.shape[0] not in self._buffers:
-            self._buffers[x.shape[0]] = _Buffers(self, x.shape[0])
-        return self._buffers[x.shape[0]]
+        size = x.shape[0], keep
+        if size not in self._buffers:
+            self._buffers[size] = _Buffers(self, *size)
+        return self._buffers[size]
 
     def forward(self, x, keep=True):
-        """The block's result (a buffer of the block, overwritten by the next call with as many tokens).  keep: for ``backward``."""
-        b, hd, xd = self._use(x), self.handle, _desc(x)
+        """The block's result (a buffer of the block, overwritten by the next call with as many tokens and the same ``keep``).  keep: for ``backward``; x
+        is held until the next such call and has to stay as it is until then.  Without, nothing that ``backward`` reads is touched."""
+        b, hd, xd = self._use(x, keep=keep), self.handle, _desc(x)
+        mean, invstd, z = (t.data_ptr() for t in (b.mean, b.invstd, b.z)) if keep else (0, 0, 0)
+        if keep:
+            if x.untyped_storage().data_ptr() == b.y.untyped_storage().data_ptr():
+                raise ValueError("x: the block's own result buffer, which this pass would overwrite, and backward reads x; clone it")
+            b.x = None
         ig.check(ig.layer_norm_forward(hd, 1.0, xd, x.data_ptr(), self.scale.data_ptr(), self.shift.data_ptr(), self.EPS, 0.0, b.narrow,
-                                       b.h.data_ptr(), b.mean.data_ptr() if keep else 0, b.invstd.data_ptr() if keep else 0), "igcLayerNormForward")
+                                       b.h.data_ptr(), mean, invstd), "igcLayerNormForward")
         ig.check(ig.linear_forward(hd, 1.0, b.narrow, b.h.data_ptr(), self.w1_desc, self.w1.data_ptr(), b.ws.data_ptr(), b.room, self.b1.data_ptr(),
-                                   ig.IGC_ACTIVATION_GELU, 0.0, None, 0, b.wide, b.z.data_ptr() if keep else 0, b.a.data_ptr()), "igcLinearForward")
+                                   ig.IGC_ACTIVATION_GELU, 0.0, None, 0, b.wide, z, b.a.data_ptr()), "igcLinearForward")
         ig.check(ig.linear_forward(hd, 1.0, b.wide, b.a.data_ptr(), self.w2_desc, self.w2.data_ptr(), b.ws.data_ptr(), b.room, self.b2.data_ptr(),
                                    ig.IGC_ACTIVATION_IDENTITY, 1.0, xd, x.data_ptr(), b.narrow, 0, b.y.data_ptr()), "igcLinearForward")
+        if keep:
+            b.x = x
         return b.y
 
     def backward(self, x, dy, accumulate=False):
-        """Gradient with respect to x of the forward pass that ran last on x, given that with respect to its result (dy: laid out in rows as
-        x is, any distance apart); ``grads`` receives (accumulate: is increased by) the parameters' gradients."""
+        """Gradient with respect to x, given that with respect to the result (dy: laid out in rows as x is, any distance apart) of the last forward pass
+        that kept its results for as many tokens, which has to have been of these rows, in this place; ``grads`` receives (accumulate: is
+        increased by) the parameters' gradients."""
         b, hd, xd, dyd = self._use(x, dy), self.handle, _desc(x), _desc(dy)
+        if b.x is None or (b.x.data_ptr(), b.x.stride()) != (x.data_ptr(), x.stride()):
+            raise ValueError("backward: the last forward pass of %d tokens that kept its results was not of these rows" % x.shape[0])
         g, keep = {n: t.data_ptr() for n, t in self.grads.items()}, 1.0 if accumulate else 0.0
         ws, room = b.ws.data_ptr(), b.room
         ig.check(ig.linear_backward_filter(hd, 1.0, b.wide, b.a.data_ptr(), dyd, dy.data_ptr(), ws, room, keep, self.dw2_desc, g["w2"], g["b2"]),
