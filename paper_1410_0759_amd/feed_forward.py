@@ -6,6 +6,9 @@ PyTorch serves for device memory and streams only.  A block keeps its descriptor
 step makes no allocation after the first of its size and can be captured into a graph.  ``python -m paper_1410_0759_amd.feed_forward`` trains one
 on a fixed random batch for a few steps and then runs single tokens through it.
 """
+import contextlib
+import threading
+
 import torch
 
 from . import binding as ig
@@ -39,10 +42,17 @@ class _Buffers:
                       ig.get_layer_norm_backward_workspace_size(hd, self.narrow, self.narrow, self.narrow)]
         self.room = max(sizes)                                          # (calls of one stream follow each other: one workspace for all)
         self.ws = torch.empty(max(self.room, 16), dtype=torch.uint8, device=dev)
+        self.tensors = [t for t in vars(self).values() if isinstance(t, torch.Tensor)]
+        self.stream = torch.cuda.current_stream()                       # that they are allocated on
 
 
 class FeedForward:
-    """Weights of the compute type, float master gradients.  All calls run on ``torch.cuda.current_stream()``."""
+    """Weights of the compute type, float master gradients.
+
+    Calls run on the current stream of the weights' device.  Buffers, workspace and gradients are shared: a call on another stream than the call
+    before first waits for what that stream holds by then, its reads of results included.  (Not while a graph is captured: its replays among
+    other calls are the caller's to order.)  Calls from several threads are made one after the other; a result is the next call's to overwrite
+    all the same, and a backward pass belongs to the last forward pass, whoever made it."""
 
     EPS = 1e-5
 
@@ -59,7 +69,8 @@ class FeedForward:
         self.dw1_desc, self.dw2_desc = filt(self.w1, ig.IGC_DATA_FLOAT), filt(self.w2, ig.IGC_DATA_FLOAT)
         like = lambda t: torch.zeros(t.shape, device=device)
         self.grads = {n: like(getattr(self, n)) for n in ("w1", "b1", "w2", "b2", "scale", "shift")}
-        self._buffers = {}
+        self._buffers, self._lock = {}, threading.RLock()
+        self._stream = torch.cuda.current_stream(self.w1.device) if self.w1.is_cuda else None      # of the last call; the weights are made on it
 
     def _check(self, name, t, rows=None):
         """Rows as the library's functions read them; they are not told more than the distance between rows."""
@@ -68,21 +79,42 @@ class FeedForward:
         if t.device != self.w1.device:
             raise ValueError("%s: on the weights' device, %s" % (name, self.w1.device))
 
-    def _use(self, x, dy=None, keep=True):
+    @contextlib.contextmanager
+    def _call(self, x, dy=None):
+        """The arguments checked; the block for one call at a time, on its device."""
         self._check("x", x)
         if dy is not None:
             self._check("dy", dy, x.shape[0])
         if not self.w1.is_cuda:
             raise ValueError("the block's calls need its weights on a GPU")
-        self.handle.set_stream(torch.cuda.current_stream().cuda_stream)
+        with self._lock, torch.cuda.device(self.w1.device):
+            yield
+
+    def _use(self, x, keep=True):
+        """The buffers for x, with the handle on the current stream and that behind the calls before."""
+        stream = torch.cuda.current_stream()
+        captured = torch.cuda.is_current_stream_capturing()
+        if not captured:
+            if stream != self._stream:
+                stream.wait_stream(self._stream)
+            self._stream = stream
+        self.handle.set_stream(stream.cuda_stream)
         size = x.shape[0], keep
         if size not in self._buffers:
             self._buffers[size] = _Buffers(self, *size)
-        return self._buffers[size]
+        b = self._buffers[size]
+        if not captured and stream != b.stream:
+            for t in b.tensors:
+                t.record_stream(stream)      # (memory of another stream's: not given away before this one is done with it)
+        return b
 
     def forward(self, x, keep=True):
         """The block's result (a buffer of the block, overwritten by the next call with as many tokens and the same ``keep``).  keep: for ``backward``; x
         is held until the next such call and has to stay as it is until then.  Without, nothing that ``backward`` reads is touched."""
+        with self._call(x):
+            return self._forward(x, keep)
+
+    def _forward(self, x, keep):
         b, hd, xd = self._use(x, keep=keep), self.handle, _desc(x)
         mean, invstd, z = (t.data_ptr() for t in (b.mean, b.invstd, b.z)) if keep else (0, 0, 0)
         if keep:
@@ -103,7 +135,11 @@ class FeedForward:
         """Gradient with respect to x, given that with respect to the result (dy: laid out in rows as x is, any distance apart) of the last forward pass
         that kept its results for as many tokens, which has to have been of these rows, in this place; ``grads`` receives (accumulate: is
         increased by) the parameters' gradients."""
-        b, hd, xd, dyd = self._use(x, dy), self.handle, _desc(x), _desc(dy)
+        with self._call(x, dy):
+            return self._backward(x, dy, accumulate)
+
+    def _backward(self, x, dy, accumulate):
+        b, hd, xd, dyd = self._use(x), self.handle, _desc(x), _desc(dy)
         if b.x is None or (b.x.data_ptr(), b.x.stride()) != (x.data_ptr(), x.stride()):
             raise ValueError("backward: the last forward pass of %d tokens that kept its results was not of these rows" % x.shape[0])
         g, keep = {n: t.data_ptr() for n, t in self.grads.items()}, 1.0 if accumulate else 0.0

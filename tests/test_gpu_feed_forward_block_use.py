@@ -1,4 +1,4 @@
-"""A feed-forward block between several uses: passes without a gradient among passes with one."""
+"""A feed-forward block between several uses: passes without a gradient among passes with one, streams, threads."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +62,62 @@ def test_the_result_as_the_next_input():
     assert torch.equal(block.forward(block.forward(x, keep=False), keep=False), want)
     block.forward(once)
     block.backward(once, dy)
+
+
+def test_two_streams_in_turn():
+    """Passes of as many tokens on two streams, nothing synchronised between them but by the block: what each gives alone, bit for bit."""
+    torch, ff = _modules()
+    block = ff.FeedForward(1024, 4096)
+    data = _data(torch, block, 2000, 4)
+    want = []
+    for x, dy in (data[:2], data[2:]):
+        want.append([block.forward(x).clone(), block.backward(x, dy).clone()] + [t.clone() for t in block.grads.values()])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(6):
+        for s, (x, dy) in zip(streams, (data[:2], data[2:])):
+            with torch.cuda.stream(s):
+                y = block.forward(x).clone()
+                got.append([y, block.backward(x, dy).clone()] + [t.clone() for t in block.grads.values()])
+    torch.cuda.synchronize()
+    for i, results in enumerate(got):
+        assert all(torch.equal(p, q) for p, q in zip(results, want[i % 2])), i
+
+
+def test_the_first_call_on_another_stream():
+    torch, ff = _modules()
+    x = torch.randn(64, 2048, device="cuda").to(torch.bfloat16)
+    torch.cuda.synchronize()
+    block = ff.FeedForward(2048, 8192)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = block.forward(x).clone()            # (behind the weights, which are still being made)
+    torch.cuda.synchronize()
+    assert torch.equal(got, block.forward(x))
+
+
+def test_threads():
+    """Passes without a gradient from several threads, each on its own stream, with its own number of tokens."""
+    import threading
+    torch, ff = _modules()
+    block = ff.FeedForward(256, 1024)
+    sizes = (5, 64, 300)
+    xs = [_data(torch, block, M, 1, seed=M)[0] for M in sizes]
+    want = [block.forward(x, keep=False).clone() for x in xs]
+    torch.cuda.synchronize()
+    results, errors = {}, []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                results[i] = [block.forward(xs[i], keep=False).clone() for _ in range(30)]
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sizes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    assert not errors and len(results) == len(sizes)
+    assert all(torch.equal(y, want[i]) for i in results for y in results[i])
