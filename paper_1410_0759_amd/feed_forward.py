@@ -2,9 +2,9 @@
 
     h = layer_norm(x);  z = h w1^T + b1;  y = gelu(z) w2^T + b2 + x
 
-PyTorch serves for device memory and streams only.  A block keeps its descriptors, output buffers and workspaces per number of tokens, so that a
-step makes no allocation after the first of its size and can be captured into a graph.  ``python -m paper_1410_0759_amd.feed_forward`` trains one
-on a fixed random batch for a few steps and then runs single tokens through it.
+PyTorch serves for device memory and streams only.  A block keeps its descriptors, output buffers and workspaces for the numbers of tokens that it met
+last, so that a step makes no allocation after the first of its size and can be captured into a graph.  ``python -m paper_1410_0759_amd.feed_forward``
+trains one on a fixed random batch for a few steps and then runs single tokens through it.
 """
 import contextlib
 import threading
@@ -44,6 +44,7 @@ class _Buffers:
         self.ws = torch.empty(max(self.room, 16), dtype=torch.uint8, device=dev)
         self.tensors = [t for t in vars(self).values() if isinstance(t, torch.Tensor)]
         self.stream = torch.cuda.current_stream()                       # that they are allocated on
+        self.captured = False                                           # a graph may read and write them at any time
 
 
 class FeedForward:
@@ -52,14 +53,17 @@ class FeedForward:
     Calls run on the current stream of the weights' device.  Buffers, workspace and gradients are shared: a call on another stream than the call
     before first waits for what that stream holds by then, its reads of results included.  (Not while a graph is captured: its replays among
     other calls are the caller's to order.)  Calls from several threads are made one after the other; a result is the next call's to overwrite
-    all the same, and a backward pass belongs to the last forward pass, whoever made it."""
+    all the same, and a backward pass belongs to the last forward pass, whoever made it.
+
+    sizes: buffers are kept for so many numbers of tokens, passes with and without gradient counted apart; those not used for longest go, a pending
+    backward pass with them.  Buffers that were used while a graph was captured stay for the block's life, which has to be the graph's."""
 
     EPS = 1e-5
 
-    def __init__(self, width, hidden, dtype=torch.bfloat16, device="cuda", seed=0):
+    def __init__(self, width, hidden, dtype=torch.bfloat16, device="cuda", seed=0, sizes=16):
         g = torch.Generator(device=device).manual_seed(seed)
         rand = lambda k, c: (torch.randn(k, c, generator=g, device=device) / c ** 0.5).to(dtype)
-        self.width, self.hidden, self.dtype = width, hidden, dtype
+        self.width, self.hidden, self.dtype, self.sizes = width, hidden, dtype, max(1, sizes)
         self.w1, self.w2 = rand(hidden, width), rand(width, hidden)
         self.b1, self.b2 = torch.zeros(hidden, device=device), torch.zeros(width, device=device)
         self.scale, self.shift = torch.ones(width, device=device), torch.zeros(width, device=device)
@@ -100,9 +104,14 @@ class FeedForward:
             self._stream = stream
         self.handle.set_stream(stream.cuda_stream)
         size = x.shape[0], keep
-        if size not in self._buffers:
-            self._buffers[size] = _Buffers(self, *size)
-        b = self._buffers[size]
+        b = self._buffers.pop(size, None) or _Buffers(self, *size)
+        self._buffers[size] = b                  # (the last one used at the end)
+        if captured:
+            b.captured = True
+        else:
+            others = [k for k, v in self._buffers.items() if not v.captured]
+            for k in others[:max(0, len(others) - self.sizes)]:
+                del self._buffers[k]
         if not captured and stream != b.stream:
             for t in b.tensors:
                 t.record_stream(stream)      # (memory of another stream's: not given away before this one is done with it)

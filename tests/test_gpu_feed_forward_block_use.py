@@ -1,4 +1,5 @@
-"""A feed-forward block between several uses: passes without a gradient among passes with one, streams, threads."""
+"""A feed-forward block between several uses: passes without a gradient among passes with one, streams, threads, many
+numbers of tokens."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -121,3 +122,30 @@ def test_threads():
         t.join(60)
     assert not errors and len(results) == len(sizes)
     assert all(torch.equal(y, want[i]) for i in results for y in results[i])
+
+
+def test_many_numbers_of_tokens():
+    """Buffers are kept for the last few sizes only, and for what a graph holds."""
+    torch, ff = _modules()
+    block = ff.FeedForward(64, 256, sizes=3)
+    data = {M: _data(torch, block, M, 2, seed=M) for M in range(1, 41)}
+    x, dy = data[7]
+    want = [block.forward(x).clone(), block.backward(x, dy).clone()] + [t.clone() for t in block.grads.values()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = [block.forward(x), block.backward(x, dy)]
+    y = {}
+    for M in (*range(1, 7), *range(8, 41), 3):
+        y[M] = block.forward(data[M][0], keep=M % 2 == 0).clone()
+        assert len(block._buffers) <= 4 and all(size[0] in (7, M, *y) for size in block._buffers)
+    for M in (4, 40, 3):
+        assert torch.equal(block.forward(data[M][0]), y[M])
+    block.backward(*data[4])
+    with pytest.raises(ValueError, match="forward"):
+        block.backward(*data[6])                                   # (its buffers are gone)
+    for t in captured + list(block.grads.values()):
+        t.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(captured + list(block.grads.values()), want))
