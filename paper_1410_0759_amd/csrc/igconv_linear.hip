@@ -383,14 +383,12 @@ OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, l
 // steps of 256 x 256, 786 us, or 1024 of 128 x 128 two by two, 1003; 2048^3 32 steps, 44, 21.4 (alone) and, 64 x 128 two by two, 24.7;
 // 2048 x 1024 -> 1024 16 steps of 64 x 128 alone, 9.7.  Float 4096^3: 512 steps, 560.  With the pieces through registers a step waits for memory: 8 x 4097 ->
 // 8000, 252 workgroups of 17 steps, 34 us, 504 of 9, 24 - with copies first 41; 1000 x 1001 -> 1001, 16 steps, 28, with copies first 16.
-// Float as it is: 512 x 4096 -> 4096 in 128 steps, 64 x 128 alone 147, 32 x 128 two by two 145 (in parts 124), 348 x 8083 -> 5280 in 127 steps, 64 x 128
-// two by two 268 (in parts 242).
 struct ShapeCost {
     int per_cu;
     double alone, full, ends;
 };
 constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0.98, 2.5}, {2, 0.42, 0.60, 2.0}, {2, 1.65, 2.00, 2.0}};
-constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.12, 2.10, 2.5}, {2, 0.60, 1.12, 2.0}};
+constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.10, 2.00, 2.5}, {2, 0.60, 1.00, 2.0}};
 // The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory, and what one
 // workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;
@@ -432,10 +430,15 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     // (no range without a step)
     auto most_splits = [&](int step) { return std::min(64, (a.K + step - 1) / step); };
     if (f32) {
+        // (rows that end inside a piece begin off 16-byte boundaries as well: 1024 x 2050 -> 1000 65 steps of 32 x 128 49 us, 1024 x 2048 -> 1000 64 steps 45;
+        // in parts both 42)
+        const double steps = a.K % 4 != 0 && !(sa && sb) ? 1.1 : 1.0;
         if (fits(oa, sa, 4, a.a) && fits(ob, sb, 4, a.b))
-            for (int shape = 0; shape < kDirectShapes; ++shape)
+            for (int shape = 0; shape < kDirectShapes; ++shape) {
+                const ShapeCost sc = kDirectCost[shape];
                 for (int splits = 1; splits <= most_splits(kFloatStep); ++splits)
-                    consider(direct_float_kernel(sa, sb, shape), kDirectCost[shape], kFloatStep, splits, false);
+                    consider(direct_float_kernel(sa, sb, shape), {sc.per_cu, sc.alone * steps, sc.full * steps, sc.ends}, kFloatStep, splits, false);
+            }
         for (int splits = 1; splits <= most_splits(kFloatStep); ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
         return pl;
     }
