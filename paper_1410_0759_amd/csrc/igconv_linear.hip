@@ -10,10 +10,13 @@
 // float in bfloat16 parts (igconv_linear_float.hpp); and the one below for anything.  Few tiles: the reduction is cut into ranges, whose
 // sums a second kernel adds in their order with the epilogue.
 //
-// Large products are bound by the matrix instructions under the card's power (zeros for numbers: 580 us for 770 in one run): 8192^3 forward 736 us, 1493 TFLOP/s,
+// Large products are bound by the matrix instructions under the card's power (zeros for numbers: 580 us for 770 in one run; 8192 x 4096 -> 16384 with
+// GELU runs at 1.90 GHz, the matrix units busy for 64 % of that): 8192^3 forward 736 us, 1493 TFLOP/s,
 // backward data 756, backward filter 796.  Their epilogue has no matrix instructions beside it: 8192 x 4096 -> 16384 775 us, with z kept 797, with
-// GELU 844; the gradient back through GELU 789 -> 912, for 268 MB of z (55 us at a copy's rate, asked for by all compute units at once) and f'.
-// Neither a quarter fewer vector instructions in f and f' nor z loaded before the last products made a difference: not kept.  Few tokens are bound by the filter's bytes: 8 x 4096 -> 16384 26 us, 5.1 TB/s.
+// GELU 844 to 867; the gradient back through GELU 789 -> 912 to 922, for 268 MB of z (55 us at a copy's rate, asked for by all compute units at once) and f'.
+// Neither a quarter fewer vector instructions in f and f' nor z loaded before the last products made a difference: not kept.  Few
+// tokens are bound by the filter's bytes: 8 x 4096 -> 16384 bfloat16 23 us for the tiles, 4.5 for the sum of four ranges, 31.7 the call with the filter in no
+// cache; float 42 and 4.9 warm, 71 the call, 8 x 4001 -> 16384 45, 4.8 and 61.
 #include "igconv_linear_float.hpp"
 
 namespace igc {

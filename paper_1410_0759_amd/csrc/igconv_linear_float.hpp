@@ -17,7 +17,7 @@
 // ahead into a ring of three stages.  A wavefront's slot is a block of 16 rows: 6 FN matrix instructions, with the next block's
 // fragments on their way; before the last one the wavefronts meet, the stage after is complete and the one read is given to the copies.
 //
-// Bound by the matrix instructions: 4096^3 608 us, of them 51 for the parts, 226 TFLOP/s or 1.36 PFLOP/s in bfloat16 products (the float instruction's
+// Bound by the matrix instructions: 4096^3 608 to 614 us, of them 51 for the parts, 226 TFLOP/s or 1.36 PFLOP/s in bfloat16 products (the float instruction's
 // own tiles: 999 us).  1023 x 2050 -> 1000 takes 41 us: 9 for the parts, 27 for 256 workgroups of 17 steps, 6.6 for the sum of their ranges.
 // 256 x 128 tiles (719 us for 656 at the time) and fragments taken column by column (651 for 626) were slower.
 #ifndef IGCONV_LINEAR_FLOAT_HPP_

@@ -27,7 +27,7 @@ def _product(u, kind, a, b, lend):
     (m, n), (k, _) = a.shape, b.shape
     out = torch.full((m, k), float("nan"), device="cuda")
     desc = lambda t: ig.TensorDescriptor().set(ig.IGC_DATA_FLOAT, t.shape[0], t.shape[1], 1, 1, (t.stride(0), 1, 1, 1))
-    parts = sum(-(-r // 16) * -(-n // 32) * 3072 for r in (m, k))
+    parts = sum(-(-r // 16) * -(-n // 32) * 3 * 1024 for r in (m, k))
 
     def workspace(size):
         assert parts <= size < parts + 4 * m * k, "not taken in parts"
