@@ -566,6 +566,44 @@ igcStatus igcLinearBackwardFilter(igcHandle_t handle, const void *alpha,
                                   const void *beta, igcFilterDescriptor_t dwDesc, void *dw,
                                   void *dbias);
 
+/* ---- training and serving such blocks ---------------------------------------------------------
+ * igcAdamWStep: one step of AdamW over any number of tensors.  With g = gradientScale * grad and t = step:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   param = param (1 - rate weightDecay) - rate (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + epsilon)
+ * in fp32 for every element, whatever its types; the update takes m and v before they are rounded.  0 <= beta < 1, epsilon > 0, step >= 1; finite numbers.
+ * deviceLearningRate, deviceGradientScale, deviceStep: device pointers or NULL, read when the step runs (so that a captured one
+ * can be replayed): the rate in place of learningRate, a factor beside gradientScale, the step in place of step (below 1: 1).
+ *
+ * A tensor: count elements next to each other (0: nothing is done; pointers may then be NULL).  param and grad: float or
+ * bfloat16, each its own; copy: NULL, or bfloat16, where a float param's new value is put rounded.  stateBits 32: m and v
+ * are floats.  stateBits 8: m is e4m3 and v is e5m2 (the OCP formats), a byte an element, in units of a float for each 256
+ * elements, mScale and vScale (ceil(count / 256) of them; all zero: no steps taken yet): the largest finite magnitude of the 256
+ * divided by the format's largest number (448, 57344), 0 where that is below 2^-100.  An element y (in those units) is rounded to 3 (v: 2)
+ * bits behind the leading one, up where the bits that go, as a fraction, and r / 2^16 reach one, then (below the smallest normal
+ * number) to the format's nearest; a v above zero stays above zero.  r: the low (v: the high) half of
+ * h(i ^ h(seed ^ h(step))), i: the element's index, its upper 32 bits times 0x9E3779B9 exclusive-or'ed to the lower ones, with
+ * h(x): x ^= x >> 16, x *= 0x7FEB352D, x ^= x >> 15, x *= 0x846CA68B, x ^= x >> 16.  Elements that are infinite or undefined become the
+ * format's NaN and touch no others.  Results repeat bit by bit.
+ * No two arrays of a list may overlap, but tensors may lie at any element boundary and behind each other.  At most 48 tensors are taken by a launch. */
+typedef struct {
+    double learningRate, beta1, beta2, epsilon, gradientScale;
+    int step;
+    unsigned int seed;
+    const float *deviceLearningRate, *deviceGradientScale;
+    const int *deviceStep;
+} igcAdamWParameters;
+typedef struct {
+    void *param;
+    const void *grad;
+    void *copy, *m, *v;
+    float *mScale, *vScale;
+    long long count;
+    double weightDecay;
+    igcDataType paramType, gradType;
+    int stateBits;
+} igcAdamWTensor;
+igcStatus igcAdamWStep(igcHandle_t handle, const igcAdamWParameters *parameters, int tensors, const igcAdamWTensor *list);
+
 /* ---- introspection and tuning (host only; no GPU call) ----------------------------
  * The launch plan the library derives for a problem: the tile of the lowered
  * product O_m (K x NPQ) = F_m (K x CRS) . D_m (CRS x NPQ) each workgroup computes,

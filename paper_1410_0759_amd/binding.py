@@ -27,6 +27,7 @@ __all__ = [
     "layer_norm_forward", "get_layer_norm_backward_workspace_size", "layer_norm_backward",
     "get_linear_forward_workspace_size", "linear_forward", "get_linear_backward_data_workspace_size", "linear_backward_data",
     "get_linear_backward_filter_workspace_size", "linear_backward_filter",
+    "AdamWParameters", "AdamWTensor", "adamw_step",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -51,6 +52,34 @@ class igcConvolutionForwardPlan(ctypes.Structure):
 
 _vp, _i, _ll, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
 _P = ctypes.POINTER
+
+
+class _Filled(ctypes.Structure):
+    """Fields by keyword, in the library's order; an unknown name is an error, for attributes too."""
+
+    def __init__(self, **fields):
+        unknown = set(fields) - {n for n, _ in self._fields_}
+        if unknown:
+            raise TypeError("no field %s" % ", ".join(sorted(unknown)))
+        super().__init__(**fields)
+
+    def __setattr__(self, name, value):
+        if name not in {n for n, _ in self._fields_}:
+            raise AttributeError("no field %s" % name)
+        super().__setattr__(name, value)
+
+
+class AdamWParameters(_Filled):
+    """igcAdamWParameters; the device pointers are integers, 0 for none."""
+    _fields_ = [(n, ctypes.c_double) for n in ("learning_rate", "beta1", "beta2", "epsilon", "gradient_scale")] + [
+        ("step", _i), ("seed", ctypes.c_uint), ("device_learning_rate", _vp), ("device_gradient_scale", _vp), ("device_step", _vp)]
+
+
+class AdamWTensor(_Filled):
+    """igcAdamWTensor; pointers are integers, 0 for none."""
+    _fields_ = [(n, _vp) for n in ("param", "grad", "copy", "m", "v", "m_scale", "v_scale")] + [
+        ("count", _ll), ("weight_decay", ctypes.c_double), ("param_type", _i), ("grad_type", _i), ("state_bits", _i)]
+
 
 # name -> (restype, argtypes): every symbol include/igconv.h declares
 DECLARED_SYMBOLS = {
@@ -105,6 +134,7 @@ DECLARED_SYMBOLS = {
     "igcLinearBackwardData": (_i, [_vp] * 7 + [_sz, _i] + [_vp] * 7),
     "igcGetLinearBackwardFilterWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
     "igcLinearBackwardFilter": (_i, [_vp] * 7 + [_sz] + [_vp] * 4),
+    "igcAdamWStep": (_i, [_vp, _P(AdamWParameters), _i, _P(AdamWTensor)]),
     "igcGetConvolutionForwardPlan": (_i, [_vp, _vp, _vp, _vp, _vp, _P(igcConvolutionForwardPlan)]),
     "igcGetKernelCount": (_i, []),
     "igcGetKernelName": (ctypes.c_char_p, [_i]),
@@ -496,6 +526,11 @@ def linear_backward_filter(handle, alpha, xdesc, x_ptr, dydesc, dy_ptr, workspac
     a, b = _scalars(dwdesc, alpha, beta)
     return lib().igcLinearBackwardFilter(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), dydesc.ptr, _vp(dy_ptr), _vp(workspace_ptr),
                                          workspace_bytes, ctypes.byref(b), dwdesc.ptr, _vp(dw_ptr), _vp(dbias_ptr))
+
+
+def adamw_step(handle, parameters, tensors):
+    """igcAdamWStep; ``tensors``: a ctypes array of AdamWTensor (kept by the caller from step to step)."""
+    return lib().igcAdamWStep(handle.ptr, ctypes.byref(parameters), len(tensors), tensors)
 
 
 def kernel_names():
