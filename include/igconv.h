@@ -604,6 +604,35 @@ typedef struct {
 } igcAdamWTensor;
 igcStatus igcAdamWStep(igcHandle_t handle, const igcAdamWParameters *parameters, int tensors, const igcAdamWTensor *list);
 
+/* Filters in four bits for serving: W[k][c] = scale[c / group][k] * q[k][c] for K x C filters (r = s = 1), groups of 32, 64 or 128
+ * features of a row (the last one may be shorter), q of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7) and their negatives (codes 8
+ * to 15).  codes: K rows of ceil(C / 128) blocks of 64 bytes, 16-byte aligned; of a block's 16 words (32 bits, little-endian), word
+ * 4 g + i holds the codes of features 32 i + 8 g to 32 i + 8 g + 7 of the block, the first in the lowest four bits (g, i: 0 to 3); codes behind
+ * feature C have to be 0.  scales: bfloat16, ceil(C / group) rows of K.  The query reports both arrays' bytes (host only).
+ *
+ * igcQuantizeFilter4: the scale of a group is the smallest bfloat16 number not below a sixth of its largest magnitude, a code the nearest to
+ * w / scale, of two as near the even one; exactly so, for float and bfloat16 w.  (A group that holds an infinity or NaN gets the scale NaN.)
+ * igcDequantizeFilter4: w (float or bfloat16) = the numbers that codes and scales stand for, exact in float, rounded to bfloat16. */
+igcStatus igcGetFilter4Size(igcFilterDescriptor_t wDesc, int group, size_t *codeBytes, size_t *scaleBytes);
+igcStatus igcQuantizeFilter4(igcHandle_t handle, igcFilterDescriptor_t wDesc, const void *w, int group, void *codes, void *scales);
+igcStatus igcDequantizeFilter4(igcHandle_t handle, int group, const void *codes, const void *scales, igcFilterDescriptor_t wDesc, void *w);
+
+/* Matrix product with such a filter:  y = f(alpha * x W^T + bias) + beta * r
+ * as igcLinearForward has it: x M rows of C, y and r M rows of K.  x bfloat16 with y bfloat16 or float, or both float; of wDesc the sizes count (its type:
+ * float or bfloat16).  The weights are not rounded on the way: products with q are exact, a group's sum is multiplied by its scale in
+ * fp32 (sums of x q have to stay within float's range).  workSpace (device, 16-byte aligned, contents mean nothing): the query's bytes make long
+ * prompts fast; any size will do, NULL too. */
+igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                            igcFilterDescriptor_t wDesc, int group,
+                                            igcTensorDescriptor_t yDesc, size_t *sizeInBytes);
+igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha,
+                            igcTensorDescriptor_t xDesc, const void *x,
+                            igcFilterDescriptor_t wDesc, int group, const void *codes, const void *scales,
+                            void *workSpace, size_t workSpaceSizeInBytes,
+                            const void *bias, int activation, const void *beta,
+                            igcTensorDescriptor_t rDesc, const void *r,
+                            igcTensorDescriptor_t yDesc, void *y);
+
 /* ---- introspection and tuning (host only; no GPU call) ----------------------------
  * The launch plan the library derives for a problem: the tile of the lowered
  * product O_m (K x NPQ) = F_m (K x CRS) . D_m (CRS x NPQ) each workgroup computes,

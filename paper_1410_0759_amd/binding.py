@@ -28,6 +28,7 @@ __all__ = [
     "get_linear_forward_workspace_size", "linear_forward", "get_linear_backward_data_workspace_size", "linear_backward_data",
     "get_linear_backward_filter_workspace_size", "linear_backward_filter",
     "AdamWParameters", "AdamWTensor", "adamw_step",
+    "get_filter4_size", "quantize_filter4", "dequantize_filter4", "get_linear4_forward_workspace_size", "linear4_forward",
 ]
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -135,6 +136,11 @@ DECLARED_SYMBOLS = {
     "igcGetLinearBackwardFilterWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
     "igcLinearBackwardFilter": (_i, [_vp] * 7 + [_sz] + [_vp] * 4),
     "igcAdamWStep": (_i, [_vp, _P(AdamWParameters), _i, _P(AdamWTensor)]),
+    "igcGetFilter4Size": (_i, [_vp, _i, _P(_sz), _P(_sz)]),
+    "igcQuantizeFilter4": (_i, [_vp, _vp, _vp, _i, _vp, _vp]),
+    "igcDequantizeFilter4": (_i, [_vp, _i] + [_vp] * 4),
+    "igcGetLinear4ForwardWorkspaceSize": (_i, [_vp, _vp, _vp, _i, _vp, _P(_sz)]),
+    "igcLinear4Forward": (_i, [_vp] * 5 + [_i] + [_vp] * 3 + [_sz, _vp, _i] + [_vp] * 5),
     "igcGetConvolutionForwardPlan": (_i, [_vp, _vp, _vp, _vp, _vp, _P(igcConvolutionForwardPlan)]),
     "igcGetKernelCount": (_i, []),
     "igcGetKernelName": (ctypes.c_char_p, [_i]),
@@ -531,6 +537,37 @@ def linear_backward_filter(handle, alpha, xdesc, x_ptr, dydesc, dy_ptr, workspac
 def adamw_step(handle, parameters, tensors):
     """igcAdamWStep; ``tensors``: a ctypes array of AdamWTensor (kept by the caller from step to step)."""
     return lib().igcAdamWStep(handle.ptr, ctypes.byref(parameters), len(tensors), tensors)
+
+
+def get_filter4_size(wdesc, group):
+    """(bytes of the codes, bytes of the scales)."""
+    codes, scales = _sz(), _sz()
+    check(lib().igcGetFilter4Size(wdesc.ptr, group, ctypes.byref(codes), ctypes.byref(scales)), "igcGetFilter4Size")
+    return codes.value, scales.value
+
+
+def quantize_filter4(handle, wdesc, w_ptr, group, codes_ptr, scales_ptr):
+    """igcQuantizeFilter4."""
+    return lib().igcQuantizeFilter4(handle.ptr, wdesc.ptr, _vp(w_ptr), group, _vp(codes_ptr), _vp(scales_ptr))
+
+
+def dequantize_filter4(handle, group, codes_ptr, scales_ptr, wdesc, w_ptr):
+    """igcDequantizeFilter4."""
+    return lib().igcDequantizeFilter4(handle.ptr, group, _vp(codes_ptr), _vp(scales_ptr), wdesc.ptr, _vp(w_ptr))
+
+
+def get_linear4_forward_workspace_size(handle, xdesc, wdesc, group, ydesc):
+    out = _sz()
+    check(lib().igcGetLinear4ForwardWorkspaceSize(handle.ptr, xdesc.ptr, wdesc.ptr, group, ydesc.ptr, ctypes.byref(out)), "igcGetLinear4ForwardWorkspaceSize")
+    return out.value
+
+
+def linear4_forward(handle, alpha, xdesc, x_ptr, wdesc, group, codes_ptr, scales_ptr, workspace_ptr, workspace_bytes, bias_ptr, activation, beta, rdesc,
+                    r_ptr, ydesc, y_ptr):
+    """igcLinear4Forward; rdesc may be None where beta is 0, the bias pointer 0, activation -1 for none."""
+    a, b = _scalars(ydesc, alpha, beta)
+    return lib().igcLinear4Forward(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), wdesc.ptr, group, _vp(codes_ptr), _vp(scales_ptr), _vp(workspace_ptr),
+                                   workspace_bytes, _vp(bias_ptr), activation, ctypes.byref(b), _desc_ptr(rdesc), _vp(r_ptr), ydesc.ptr, _vp(y_ptr))
 
 
 def kernel_names():

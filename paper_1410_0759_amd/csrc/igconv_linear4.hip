@@ -1,0 +1,426 @@
+// Filters held in four bits, and products with them:
+//
+//   y = f(alpha x W^T + bias) + beta r,   W[k][c] = scale[c / group][k] q[k][c],  q of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (e2m1)
+//
+// The q are bfloat16 numbers, and one instruction makes two of them: the products x q are exact in the matrix instructions, and a group's sum is
+// multiplied by its scale in fp32.  A scaled weight, which has up to eleven bits, is never rounded.  Float x goes in as three bfloat16 parts
+// of eight bits, whose products are exact too.
+//
+// Layout.  A row of W is cut into blocks of 128 features in 64 bytes; word 4 g + i of a block holds features 32 i + 8 g to + 7, the first in the lowest bits.
+// So the 16 bytes that lane group g of a wavefront (16 lanes each) loads are its share of four matrix instructions of 32 features each, and every instruction's features
+// lie in one group of any size.  Scales are kept with the rows next to each other: a lane's four results have theirs in 8 bytes.
+#include "igconv_linear_tiles.hpp"
+
+namespace igc {
+namespace {
+
+constexpr int kBlock = 128, kBlockBytes = 64;
+
+using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+
+__host__ __device__ inline long long code_row(int C) { return (long long)((C + kBlock - 1) / kBlock) * kBlockBytes; }
+
+// eight codes as bfloat16 numbers
+__device__ __forceinline__ bf16x8 widen8(uint32_t codes) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 1);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// ---- into four bits and back --------------------------------------------------------------------------------------------
+struct StoreArgs {
+    const void *w;
+    void *out;            // (back)
+    uint8_t *codes;
+    uint16_t *scales;
+    int K, C, group;
+    long long tiles;
+};
+
+// A workgroup takes 64 rows of a block: a lane one word of it, sixteen lanes a row, so that a group's largest is found among 4, 8 or 16 lanes
+// and 64 rows' scales of a group go out next to each other.  All in exact arithmetic: the scale is the smallest bfloat16 number not below
+// a sixth of the largest, the borders between codes are products of eight bits by three.
+template <class T>
+__global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
+    const int lane = threadIdx.x & 63, word = lane & 15;
+    const int blocks = (p.C + kBlock - 1) / kBlock;
+    // (lane j of the sixteen: features 8 j to 8 j + 7, which word 4 (j % 4) + j / 4 holds)
+    const int at = 4 * (word & 3) + (word >> 2);
+    for (long long tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+        const int block = (int)(tile % blocks), c = block * kBlock + word * 8;
+        const long long k0 = tile / blocks * 64 + (threadIdx.x >> 4);
+        float w[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long k = k0 + 16 * i;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[i][e] = 0.f;
+            if (k >= p.K) continue;
+            const T *from = static_cast<const T *>(p.w) + k * p.C + c;
+            if (c + 8 <= p.C) {
+                const Adjacent<T, 8> q = *reinterpret_cast<const Adjacent<T, 8> *>(from);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[i][e] = Stored<T>::widen(q.v[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < p.C) w[i][e] = Stored<T>::widen(from[e]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long k = k0 + 16 * i;
+            uint32_t most = 0;      // (magnitudes as whole numbers: what is infinite or undefined lies above all others)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, __builtin_bit_cast(uint32_t, w[i][e]) & 0x7FFFFFFFu);
+            for (int d = 1; d < p.group / 8; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+            uint32_t scale = 0x7FC00000u;
+            if (most < 0x7F800000u) {
+                const double want = (double)__builtin_bit_cast(float, most) / 6.0;
+                scale = __builtin_bit_cast(uint32_t, (float)want) & 0xFFFF0000u;
+                if ((double)__builtin_bit_cast(float, scale) < want) scale += 0x10000u;
+            }
+            const float s = __builtin_bit_cast(float, scale);
+            uint32_t codes = 0;
+            if (scale != 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = __builtin_fabsf(w[i][e]);
+                    // the even code of two as near
+                    const uint32_t q = (v > 0.25f * s) + (v >= 0.75f * s) + (v > 1.25f * s) + (v >= 1.75f * s) + (v > 2.5f * s) + (v >= 3.5f * s) + (v > 5.f * s);
+                    codes |= (q | (w[i][e] < 0.f && q ? 8u : 0u)) << (4 * e);
+                }
+            }
+            if (k >= p.K) continue;
+            *reinterpret_cast<uint32_t *>(p.codes + k * code_row(p.C) + block * kBlockBytes + at * 4) = codes;
+            if (word % (p.group / 8) == 0 && c < p.C) p.scales[(long long)(c / p.group) * p.K + k] = (uint16_t)(scale >> 16);
+        }
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) {
+    const int lane = threadIdx.x & 63, word = lane & 15, at = 4 * (word & 3) + (word >> 2);
+    const int blocks = (p.C + kBlock - 1) / kBlock;
+    for (long long tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+        const int block = (int)(tile % blocks), c = block * kBlock + word * 8;
+        const long long k0 = tile / blocks * 64 + (threadIdx.x >> 4);
+        if (c >= p.C) continue;
+        uint32_t codes[4];
+        float scale[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long k = k0 + 16 * i < p.K ? k0 + 16 * i : p.K - 1;
+            codes[i] = *reinterpret_cast<const uint32_t *>(p.codes + k * code_row(p.C) + block * kBlockBytes + at * 4);
+            scale[i] = bf16_bits_to_float(p.scales[(long long)(c / p.group) * p.K + k]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long k = k0 + 16 * i;
+            if (k >= p.K) continue;
+            const bf16x8 q = widen8(codes[i]);
+            Adjacent<T, 8> v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v.v[e] = Stored<T>::narrow((float)q[e] * scale[i]);
+            T *to = static_cast<T *>(p.out) + k * p.C + c;
+            if (c + 8 <= p.C) {
+                *reinterpret_cast<Adjacent<T, 8> *>(to) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < p.C) to[e] = v.v[e];
+            }
+        }
+    }
+}
+
+// ---- products -----------------------------------------------------------------------------------------------------------
+struct Linear4Args : LinearArgs {      // a: x; M tokens, N rows of W, K features
+    const uint8_t *codes;
+    const uint16_t *scales;
+    int group;
+    long long tilesM, tilesN;
+};
+
+// A lane's eight features of a token, in bfloat16 parts.
+template <class T> struct Parts;
+template <> struct Parts<bf16_t> {
+    static constexpr int N = 1;
+    static __device__ __forceinline__ void split(const Adjacent<bf16_t, 8> &x, bf16x8 (&p)[1]) { p[0] = __builtin_bit_cast(bf16x8, x); }
+};
+template <> struct Parts<float> {
+    static constexpr int N = 3;
+    // by truncation: 24 bits are three times eight.  (An infinity has no rest; an undefined number must not become one.)
+    static __device__ __forceinline__ void split(const Adjacent<float, 8> &x, bf16x8 (&p)[3]) {
+        u32x4 h, m, l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t hb[2], mb[2], lb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float v = x.v[2 * e + i];
+                const uint32_t all = __builtin_bit_cast(uint32_t, v);
+                const bool finite = (all & 0x7F800000u) != 0x7F800000u;
+                hb[i] = (!finite && (all & 0x007FFFFFu)) ? 0x7FC00000u : all & 0xFFFF0000u;
+                const float r = finite ? v - __builtin_bit_cast(float, hb[i]) : 0.f;
+                mb[i] = __builtin_bit_cast(uint32_t, r) & 0xFFFF0000u;
+                lb[i] = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, mb[i]));
+            }
+            h[e] = __builtin_amdgcn_perm(hb[1], hb[0], 0x07060302u);
+            m[e] = __builtin_amdgcn_perm(mb[1], mb[0], 0x07060302u);
+            l[e] = __builtin_amdgcn_perm(lb[1], lb[0], 0x07060302u);
+        }
+        p[0] = __builtin_bit_cast(bf16x8, h);
+        p[1] = __builtin_bit_cast(bf16x8, m);
+        p[2] = __builtin_bit_cast(bf16x8, l);
+    }
+};
+
+// Any number of tokens.  A workgroup computes 16 TB tokens x 16 KB rows of W; its wavefronts take the blocks of 128 features in turns and add their sums at
+// the end, so that a few rows of W keep a compute unit's loads under way.
+template <int KB, int TB, int WAVES, class TX, class TO>
+__global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p) {
+    constexpr int N = Parts<TX>::N;
+    __shared__ f32x4 sums[WAVES][KB * TB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group - 1) / p.group;
+    const long long row_bytes = code_row(p.K);
+    const uint32_t last_of_group = p.group == 32 ? 0xFu : (p.group == 64 ? 0xAu : 0x8u);
+    for (long long tile = blockIdx.x; tile < p.tilesM * p.tilesN; tile += gridDim.x) {
+        const int n0 = (int)(tile % p.tilesN) * (16 * KB);
+        const long long m0 = tile / p.tilesN * (16 * TB);
+        const uint8_t *row[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) row[kb] = p.codes + (long long)min(n0 + 16 * kb + l16, p.N - 1) * row_bytes + g * 16;
+        const TX *token[TB];
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) token[tb] = static_cast<const TX *>(p.a) + min(m0 + 16 * tb + l16, (long long)p.M - 1) * p.am + 8 * g;
+        f32x4 total[KB][TB], part[KB][TB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) total[kb][tb] = part[kb][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        u32x4 codes[KB], next[KB];
+        auto load = [&](int s, u32x4 (&to)[KB]) __attribute__((always_inline)) {
+            if (s < blocks)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) to[kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
+        };
+        load(wave, next);
+        for (int s = wave; s < blocks; s += WAVES) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) codes[kb] = next[kb];
+            load(s + WAVES, next);
+            const int left = p.K - s * kBlock - 8 * g;      // features from this lane's first on
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bf16x8 x[TB][N];
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb) {
+                    const TX *from = token[tb] + s * kBlock + 32 * i;
+                    Adjacent<TX, 8> v;
+                    if (left - 32 * i >= 8) {
+                        v = *reinterpret_cast<const Adjacent<TX, 8> *>(from);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            v.v[e] = TX{};
+                            if (e < left - 32 * i) v.v[e] = from[e];
+                        }
+                    }
+                    Parts<TX>::split(v, x[tb]);
+                }
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const bf16x8 q = widen8(codes[kb][i]);
+#pragma unroll
+                    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                        for (int n = 0; n < N; ++n) part[kb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, x[tb][n], part[kb][tb], 0, 0, 0);
+                }
+                if (!(last_of_group >> i & 1)) continue;
+                const int group = (s * kBlock + 32 * i) / p.group;
+                if (group >= groups) continue;      // (the last block's codes behind the row are zeros, and so is the part)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const int n = n0 + 16 * kb + 4 * g;
+                    const uint16_t *from = p.scales + (long long)group * p.N + n;
+                    Adjacent<uint16_t, 4> v{};
+                    if (n + 4 <= p.N) {
+                        v = *reinterpret_cast<const Adjacent<uint16_t, 4> *>(from);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (n + e < p.N) v.v[e] = from[e];
+                    }
+#pragma unroll
+                    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            total[kb][tb][e] += bf16_bits_to_float(v.v[e]) * part[kb][tb][e];
+                            part[kb][tb][e] = 0.f;
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) sums[wave][kb * TB + tb][lane] = total[kb][tb];
+        __syncthreads();
+        for (int at = threadIdx.x; at < KB * TB * 64; at += 64 * WAVES) {
+            const int block = at >> 6, l = at & 63;
+            f32x4 d = sums[0][block][l];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) d += sums[w][block][l];
+            const long long m = m0 + 16 * (block % TB) + (l & 15);
+            const int n = n0 + 16 * (block / TB) + 4 * (l >> 4);
+            if (m < p.M)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < p.N) finish_element<TO>(p, (int)m, n + e, d[e]);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+bool off(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
+
+igcStatus check_filter(igcFilterDescriptor_t w, int group) {
+    if (!w) return IGC_STATUS_BAD_PARAM;
+    if (!w->set) return IGC_STATUS_NOT_INITIALIZED;
+    if (w->r != 1 || w->s != 1) return IGC_STATUS_BAD_PARAM;
+    if ((w->dtype != IGC_DATA_FLOAT && w->dtype != IGC_DATA_BFLOAT16) || (group != 32 && group != 64 && group != 128) || w->k > kMostColumns || w->c > kMostColumns)
+        return IGC_STATUS_NOT_SUPPORTED;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus check_product(igcTensorDescriptor_t x, igcFilterDescriptor_t w, int group, igcTensorDescriptor_t y, Matrix *mx, Matrix *my) {
+    if (!x || !w || !y) return IGC_STATUS_BAD_PARAM;
+    if (!x->set || !y->set) return IGC_STATUS_NOT_INITIALIZED;
+    const igcStatus st = check_filter(w, group);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    if (x->dim[1] != w->c || y->dim[1] != w->k || !same_positions(*x, *y) || !non_aliasing(y->dim, y->stride)) return IGC_STATUS_BAD_PARAM;
+    if ((x->dtype != IGC_DATA_BFLOAT16 && x->dtype != IGC_DATA_FLOAT) || (y->dtype != IGC_DATA_FLOAT && !(x->dtype == IGC_DATA_BFLOAT16 && y->dtype == IGC_DATA_BFLOAT16)) ||
+        !matrix_of(*x, mx) || !matrix_of(*y, my))
+        return IGC_STATUS_NOT_SUPPORTED;
+    return IGC_STATUS_SUCCESS;
+}
+
+constexpr long long kMostGroups = 1ll << 21;   // workgroups of a launch (times 1024 threads: a 32-bit number); more tiles are taken in turns
+
+template <class F>
+igcStatus with_types(igcDataType in, igcDataType out, F f) {
+    if (in == IGC_DATA_FLOAT) return f(float(), float());
+    return out == IGC_DATA_FLOAT ? f(bf16_t(), float()) : f(bf16_t(), bf16_t());
+}
+
+template <int KB, int TB, class TX, class TO>
+igcStatus launch_linear4(Linear4Args a, void *stream) {
+    constexpr int WAVES = KB * TB > 4 ? 8 : 16;
+    a.tilesM = ((long long)a.M + 16 * TB - 1) / (16 * TB);
+    a.tilesN = (a.N + 16 * KB - 1) / (16 * KB);
+    return launch_kernel(reinterpret_cast<const void *>(&linear4_kernel<KB, TB, WAVES, TX, TO>), a, dim3((unsigned)std::min(a.tilesM * a.tilesN, kMostGroups)), 64 * WAVES, stream);
+}
+
+template <class TX, class TO>
+igcStatus run_linear4(igcHandle_t handle, const Linear4Args &a) {
+    const int tb = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
+    const long long tm = ((long long)a.M + 16 * tb - 1) / (16 * tb);
+    auto enough = [&](int kb) { return tm * ((a.N + 16 * kb - 1) / (16 * kb)) >= handle->computeUnits; };
+    const int kb = enough(4) ? 4 : (enough(2) ? 2 : 1);
+    auto with_kb = [&](auto t) {
+        constexpr int TB = decltype(t)::value;
+        if (kb == 4) return launch_linear4<4, TB, TX, TO>(a, handle->stream);
+        return kb == 2 ? launch_linear4<2, TB, TX, TO>(a, handle->stream) : launch_linear4<1, TB, TX, TO>(a, handle->stream);
+    };
+    return tb == 1 ? with_kb(Constant<1>()) : (tb == 2 ? with_kb(Constant<2>()) : with_kb(Constant<4>()));
+}
+
+}  // namespace
+}  // namespace igc
+
+using namespace igc;
+
+extern "C" {
+
+igcStatus igcGetFilter4Size(igcFilterDescriptor_t wDesc, int group, size_t *codeBytes, size_t *scaleBytes) {
+    if (!codeBytes || !scaleBytes) return IGC_STATUS_BAD_PARAM;
+    const igcStatus st = check_filter(wDesc, group);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    *codeBytes = (size_t)(wDesc->k * code_row(wDesc->c));
+    *scaleBytes = (size_t)((wDesc->c + group - 1) / group) * wDesc->k * 2;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus igcQuantizeFilter4(igcHandle_t handle, igcFilterDescriptor_t wDesc, const void *w, int group, void *codes, void *scales) {
+    if (!handle || !w || !codes || !scales) return IGC_STATUS_BAD_PARAM;
+    const igcStatus st = check_filter(wDesc, group);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    if (off(w, elem_size(wDesc->dtype)) || off(codes, 16) || off(scales, 2)) return IGC_STATUS_BAD_PARAM;
+    StoreArgs a{};
+    a.w = w;
+    a.codes = static_cast<uint8_t *>(codes);
+    a.scales = static_cast<uint16_t *>(scales);
+    a.K = wDesc->k; a.C = wDesc->c; a.group = group;
+    a.tiles = (long long)((a.C + kBlock - 1) / kBlock) * ((a.K + 63) / 64);
+    const void *kernel = wDesc->dtype == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&to_four_bits_kernel<float>) : reinterpret_cast<const void *>(&to_four_bits_kernel<bf16_t>);
+    return launch_kernel(kernel, a, dim3((unsigned)std::min(a.tiles, kMostGroups)), 256, handle->stream);
+}
+
+igcStatus igcDequantizeFilter4(igcHandle_t handle, int group, const void *codes, const void *scales, igcFilterDescriptor_t wDesc, void *w) {
+    if (!handle || !w || !codes || !scales) return IGC_STATUS_BAD_PARAM;
+    const igcStatus st = check_filter(wDesc, group);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    if (off(w, elem_size(wDesc->dtype)) || off(codes, 16) || off(scales, 2)) return IGC_STATUS_BAD_PARAM;
+    StoreArgs a{};
+    a.out = w;
+    a.codes = const_cast<uint8_t *>(static_cast<const uint8_t *>(codes));
+    a.scales = const_cast<uint16_t *>(static_cast<const uint16_t *>(scales));
+    a.K = wDesc->k; a.C = wDesc->c; a.group = group;
+    a.tiles = (long long)((a.C + kBlock - 1) / kBlock) * ((a.K + 63) / 64);
+    const void *kernel = wDesc->dtype == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&from_four_bits_kernel<float>) : reinterpret_cast<const void *>(&from_four_bits_kernel<bf16_t>);
+    return launch_kernel(kernel, a, dim3((unsigned)std::min(a.tiles, kMostGroups)), 256, handle->stream);
+}
+
+igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc, igcFilterDescriptor_t wDesc, int group, igcTensorDescriptor_t yDesc,
+                                            size_t *sizeInBytes) {
+    if (!handle || !sizeInBytes) return IGC_STATUS_BAD_PARAM;
+    Matrix x, y;
+    const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &x, &y);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    *sizeInBytes = 0;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDescriptor_t xDesc, const void *x, igcFilterDescriptor_t wDesc, int group,
+                            const void *codes, const void *scales, void *workSpace, size_t workSpaceSizeInBytes, const void *bias, int activation, const void *beta,
+                            igcTensorDescriptor_t rDesc, const void *r, igcTensorDescriptor_t yDesc, void *y) {
+    if (!handle || !alpha || !beta || !x || !codes || !scales || !y || activation < IGC_ACTIVATION_IDENTITY || activation > IGC_ACTIVATION_SILU) return IGC_STATUS_BAD_PARAM;
+    Matrix mx, my, mr;
+    const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &mx, &my);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    Linear4Args a{};
+    a.alpha = *static_cast<const float *>(alpha);
+    a.beta = *static_cast<const float *>(beta);
+    if (a.beta != 0.f) {
+        if (!rDesc || !r) return IGC_STATUS_BAD_PARAM;
+        if (!rDesc->set) return IGC_STATUS_NOT_INITIALIZED;
+        if (!same_positions(*yDesc, *rDesc) || yDesc->dim[1] != rDesc->dim[1] || off(r, elem_size(rDesc->dtype))) return IGC_STATUS_BAD_PARAM;
+        if (rDesc->dtype != yDesc->dtype || !matrix_of(*rDesc, &mr)) return IGC_STATUS_NOT_SUPPORTED;
+    }
+    if (off(x, elem_size(xDesc->dtype)) || off(y, elem_size(yDesc->dtype)) || off(bias, 4) || off(codes, 16) || off(scales, 2)) return IGC_STATUS_BAD_PARAM;
+    a.a = x; a.am = mx.stride; a.ak = 1;
+    a.M = (int)mx.rows; a.N = wDesc->k; a.K = wDesc->c;
+    a.bias = static_cast<const float *>(bias);
+    a.act = activation;
+    a.r = r; a.rs = mr.stride;
+    a.y = y; a.ys = my.stride;
+    a.codes = static_cast<const uint8_t *>(codes);
+    a.scales = static_cast<const uint16_t *>(scales);
+    a.group = group;
+    return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_linear4<decltype(tx), decltype(ty)>(handle, a); });
+}
+
+}  // extern "C"
