@@ -604,6 +604,38 @@ typedef struct {
 } igcAdamWTensor;
 igcStatus igcAdamWStep(igcHandle_t handle, const igcAdamWParameters *parameters, int tensors, const igcAdamWTensor *list);
 
+/* Cross entropy over a vocabulary of V entries, from the features in front of the last product, without the logits z (M x V) in
+ * memory: they are made in pieces of the vocabulary.  x: M rows of C, w: filter V x C x 1 x 1, both bfloat16 or both float; bias: V packed floats or NULL (minus
+ * infinity takes an entry out); targets: M packed ints, device; a row whose target is not in 0..V-1 has none.
+ *   z = x w^T + bias,   logSum = log(sum of exp(z) over a row),   loss = logSum - z[target], 0 for a row without target
+ * loss and logSum: M packed floats; logSum (every row's) is what the backward pass reads, NULL: not kept.  A row with an undefined or
+ * positive infinite logit, or all of them minus infinity, comes out undefined; other rows are not touched by it. */
+igcStatus igcGetLinearCrossEntropyForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                                       igcFilterDescriptor_t wDesc, size_t *sizeInBytes);
+igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t xDesc, const void *x,
+                                       igcFilterDescriptor_t wDesc, const void *w, const void *bias, const int *targets,
+                                       void *workSpace, size_t workSpaceSizeInBytes, void *loss, void *logSum);
+
+/* Its gradients.  With dloss: M packed floats (NULL: ones; the gradient that reaches each row's loss),
+ *   dz = alpha * dloss * (exp(z - logSum) - [v is the target]), 0 in a row without target,
+ *   dx = dz w + beta * dx,   dw = dz^T x + paramBeta * dw,   dbias = column sums of dz + paramBeta * dbias
+ * dx: M rows of C, dw: filter V x C x 1 x 1, each float or, for bfloat16 x, bfloat16 too; dbias: V packed floats.  Each may be NULL (its descriptor too): not computed.
+ * For bfloat16 x, dz is rounded to bfloat16 in front of the two products, as their operand (dbias sums it before); the sums over
+ * pieces of the vocabulary are held in floats.  A row without target adds zeros times its x to dw: that x has to be finite.
+ *
+ * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports, about 256 MB to 1 GB for
+ * long batches; less is BAD_PARAM.  Sums in a fixed order: results repeat bit by bit. */
+igcStatus igcGetLinearCrossEntropyBackwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
+                                                        igcFilterDescriptor_t wDesc, igcTensorDescriptor_t dxDesc,
+                                                        igcFilterDescriptor_t dwDesc, size_t *sizeInBytes);
+igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha,
+                                        igcTensorDescriptor_t xDesc, const void *x,
+                                        igcFilterDescriptor_t wDesc, const void *w, const void *bias, const int *targets,
+                                        const void *logSum, const void *dloss,
+                                        void *workSpace, size_t workSpaceSizeInBytes,
+                                        const void *beta, igcTensorDescriptor_t dxDesc, void *dx,
+                                        const void *paramBeta, igcFilterDescriptor_t dwDesc, void *dw, void *dbias);
+
 /* Filters in four bits for serving: W[k][c] = scale[c / group][k] * q[k][c] for K x C filters (r = s = 1), groups of 32, 64 or 128
  * features of a row (the last one may be shorter), q of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 to 7) and their negatives (codes 8
  * to 15).  codes: K rows of ceil(C / 128) blocks of 64 bytes, 16-byte aligned; of a block's 16 words (32 bits, little-endian), word

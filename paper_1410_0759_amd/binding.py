@@ -28,6 +28,8 @@ __all__ = [
     "get_linear_forward_workspace_size", "linear_forward", "get_linear_backward_data_workspace_size", "linear_backward_data",
     "get_linear_backward_filter_workspace_size", "linear_backward_filter",
     "AdamWParameters", "AdamWTensor", "adamw_step",
+    "get_linear_cross_entropy_forward_workspace_size", "linear_cross_entropy_forward", "get_linear_cross_entropy_backward_workspace_size",
+    "linear_cross_entropy_backward",
     "get_filter4_size", "quantize_filter4", "dequantize_filter4", "get_linear4_forward_workspace_size", "linear4_forward",
 ]
 
@@ -136,6 +138,10 @@ DECLARED_SYMBOLS = {
     "igcGetLinearBackwardFilterWorkspaceSize": (_i, [_vp] * 4 + [_P(_sz)]),
     "igcLinearBackwardFilter": (_i, [_vp] * 7 + [_sz] + [_vp] * 4),
     "igcAdamWStep": (_i, [_vp, _P(AdamWParameters), _i, _P(AdamWTensor)]),
+    "igcGetLinearCrossEntropyForwardWorkspaceSize": (_i, [_vp] * 3 + [_P(_sz)]),
+    "igcLinearCrossEntropyForward": (_i, [_vp] * 8 + [_sz, _vp, _vp]),
+    "igcGetLinearCrossEntropyBackwardWorkspaceSize": (_i, [_vp] * 5 + [_P(_sz)]),
+    "igcLinearCrossEntropyBackward": (_i, [_vp] * 11 + [_sz] + [_vp] * 7),
     "igcGetFilter4Size": (_i, [_vp, _i, _P(_sz), _P(_sz)]),
     "igcQuantizeFilter4": (_i, [_vp, _vp, _vp, _i, _vp, _vp]),
     "igcDequantizeFilter4": (_i, [_vp, _i] + [_vp] * 4),
@@ -537,6 +543,35 @@ def linear_backward_filter(handle, alpha, xdesc, x_ptr, dydesc, dy_ptr, workspac
 def adamw_step(handle, parameters, tensors):
     """igcAdamWStep; ``tensors``: a ctypes array of AdamWTensor (kept by the caller from step to step)."""
     return lib().igcAdamWStep(handle.ptr, ctypes.byref(parameters), len(tensors), tensors)
+
+
+def get_linear_cross_entropy_forward_workspace_size(handle, xdesc, wdesc):
+    out = _sz()
+    check(lib().igcGetLinearCrossEntropyForwardWorkspaceSize(handle.ptr, xdesc.ptr, wdesc.ptr, ctypes.byref(out)), "igcGetLinearCrossEntropyForwardWorkspaceSize")
+    return out.value
+
+
+def linear_cross_entropy_forward(handle, xdesc, x_ptr, wdesc, w_ptr, bias_ptr, targets_ptr, workspace_ptr, workspace_bytes, loss_ptr, log_sum_ptr):
+    """igcLinearCrossEntropyForward; the bias and log_sum pointers may be 0.  targets: 32-bit integers."""
+    return lib().igcLinearCrossEntropyForward(handle.ptr, xdesc.ptr, _vp(x_ptr), wdesc.ptr, _vp(w_ptr), _vp(bias_ptr), _vp(targets_ptr), _vp(workspace_ptr),
+                                              workspace_bytes, _vp(loss_ptr), _vp(log_sum_ptr))
+
+
+def get_linear_cross_entropy_backward_workspace_size(handle, xdesc, wdesc, dxdesc, dwdesc):
+    """dxdesc, dwdesc: None where that gradient is not asked for."""
+    out = _sz()
+    check(lib().igcGetLinearCrossEntropyBackwardWorkspaceSize(handle.ptr, xdesc.ptr, wdesc.ptr, _desc_ptr(dxdesc), _desc_ptr(dwdesc), ctypes.byref(out)),
+          "igcGetLinearCrossEntropyBackwardWorkspaceSize")
+    return out.value
+
+
+def linear_cross_entropy_backward(handle, alpha, xdesc, x_ptr, wdesc, w_ptr, bias_ptr, targets_ptr, log_sum_ptr, dloss_ptr, workspace_ptr, workspace_bytes, beta,
+                                  dxdesc, dx_ptr, param_beta, dwdesc, dw_ptr, dbias_ptr=0):
+    """igcLinearCrossEntropyBackward; the bias and dloss pointers may be 0, and those of gradients that are not asked for (their descriptors None)."""
+    a, b, pb = (ctypes.c_float(v) for v in (alpha, beta, param_beta))
+    return lib().igcLinearCrossEntropyBackward(handle.ptr, ctypes.byref(a), xdesc.ptr, _vp(x_ptr), wdesc.ptr, _vp(w_ptr), _vp(bias_ptr), _vp(targets_ptr),
+                                               _vp(log_sum_ptr), _vp(dloss_ptr), _vp(workspace_ptr), workspace_bytes, ctypes.byref(b), _desc_ptr(dxdesc), _vp(dx_ptr),
+                                               ctypes.byref(pb), _desc_ptr(dwdesc), _vp(dw_ptr), _vp(dbias_ptr))
 
 
 def get_filter4_size(wdesc, group):

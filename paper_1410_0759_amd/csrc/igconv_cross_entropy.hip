@@ -1,0 +1,471 @@
+// Cross entropy over a vocabulary, straight from the features in front of the last product:
+//
+//   z = x w^T + bias,  logSum_i = log sum_v exp z_iv,  loss_i = logSum_i - z_it
+//   dz_iv = alpha dloss_i (exp(z_iv - logSum_i) - [v = t]),  dx = dz w + beta dx,  dw = dz^T x + paramBeta dw,  dbias = column sums of dz + paramBeta dbias
+//
+// The logits are never held whole: pieces of the vocabulary are multiplied, taken in and overwritten by the next piece's.  Forward, a piece leaves the largest
+// logit of each row and range of columns and the sum of exp(z - largest); a last kernel joins them.  Backward, the piece's logits are made again, become dz, and go
+// into two products.
+#include "igconv_linear.h"
+
+namespace igc {
+namespace {
+
+constexpr int kRange = 2048;                         // columns of one entry of the row statistics
+constexpr size_t kPieceBytes = (size_t)256 << 20;    // of logits (or dz) at a time
+
+struct RowPart {
+    float most, sum;      // largest logit, sum of exp(z - largest)
+};
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896f); }
+
+// (nothing but minus infinities: a sum of zero, and no difference of infinities)
+__device__ __forceinline__ RowPart joined(RowPart a, RowPart b) {
+    const float most = fmaxf(a.most, b.most);
+    if (most == -INFINITY) return {most, a.sum + b.sum};
+    return {most, a.sum * exp_of(a.most - most) + b.sum * exp_of(b.most - most)};
+}
+
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
+// ---- forward ------------------------------------------------------------------------------------------------------------
+struct RowPartsArgs {
+    const float *logits;        // [M][stride]
+    long long stride;
+    int M, columns, ranges;
+    int first;                  // the piece's first vocabulary entry
+    const int *targets;
+    RowPart *parts;             // [range][M], from the piece's first range on
+    float *picked;              // the targets' logits
+};
+
+// A wavefront takes a row's range of columns.
+__global__ __launch_bounds__(256) void row_parts_kernel(const RowPartsArgs a) {
+    const int lane = threadIdx.x & 63;
+    const long long tasks = (long long)a.M * a.ranges;
+    for (long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); task < tasks; task += (long long)gridDim.x * 4) {
+        const int range = (int)(task / a.M);
+        const long long m = task % a.M;
+        const float *row = a.logits + m * a.stride;
+        float z[kRange / 64];
+#pragma unroll
+        for (int i = 0; i < kRange / 256; ++i) {
+            const int n = range * kRange + i * 256 + lane * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * i + e] = -INFINITY;
+            if (n + 4 <= a.columns) {
+                const float4 q = *reinterpret_cast<const float4 *>(row + n);
+                z[4 * i] = q.x; z[4 * i + 1] = q.y; z[4 * i + 2] = q.z; z[4 * i + 3] = q.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < a.columns) z[4 * i + e] = row[n + e];
+            }
+        }
+        float most = z[0];
+#pragma unroll
+        for (int i = 1; i < kRange / 64; ++i) most = fmaxf(most, z[i]);
+        most = lanes_max(most);
+        float sum = 0.f;
+        if (most > -INFINITY)
+#pragma unroll
+            for (int i = 0; i < kRange / 64; ++i) sum += exp_of(z[i] - most);
+        else
+#pragma unroll
+            for (int i = 0; i < kRange / 64; ++i) sum += z[i] == z[i] ? 0.f : z[i];     // (what is undefined stays so)
+        sum = lanes_sum<64>(sum);
+        if (lane == 0) {
+            a.parts[(long long)range * a.M + m] = {most, sum};
+            const long long t = (long long)a.targets[m] - a.first;
+            if (t >= (long long)range * kRange && t < (long long)(range + 1) * kRange && t < a.columns) a.picked[m] = row[t];
+        }
+    }
+}
+
+struct LossArgs {
+    const RowPart *parts;
+    int M, V, ranges;
+    const int *targets;
+    const float *picked;
+    float *loss, *logSum;
+};
+
+// 64 rows to a workgroup, its sixteen wavefronts on every sixteenth range.
+__global__ __launch_bounds__(1024) void loss_kernel(const LossArgs a) {
+    __shared__ RowPart parts[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (long long first = (long long)blockIdx.x * 64; first < a.M; first += (long long)gridDim.x * 64) {
+        const long long m = first + lane;
+        RowPart mine{-INFINITY, 0.f};
+        if (m < a.M)
+#pragma unroll 4
+            for (int r = wave; r < a.ranges; r += 16) mine = joined(mine, a.parts[(long long)r * a.M + m]);
+        parts[wave][lane] = mine;
+        __syncthreads();
+        if (wave == 0 && m < a.M) {
+#pragma unroll
+            for (int w = 1; w < 16; ++w) mine = joined(mine, parts[w][lane]);
+            const float log_sum = mine.most == -INFINITY ? mine.most + mine.sum : mine.most + logf(mine.sum);
+            const int t = a.targets[m];
+            a.loss[m] = t >= 0 && t < a.V ? log_sum - a.picked[m] : 0.f;
+            if (a.logSum) a.logSum[m] = log_sum;
+        }
+        __syncthreads();
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------------------------------
+struct SlopeArgs {
+    const float *logits;        // [M][stride]
+    void *dz;                   // [M][stride], in place where it is float; zeros from `columns` up to the next eighth column
+    long long stride;
+    int M, columns, first;
+    float alpha;
+    const int *targets;
+    int V;
+    const float *logSum, *dloss;
+    float *sums;                // [rows / kSlopeRows][stride]: column sums, or null
+};
+constexpr int kSlopeRows = 32;
+
+// A thread takes four columns of kSlopeRows rows.
+template <class TZ>
+__global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
+    const int across = (int)((a.stride + 1023) / 1024);
+    const long long tasks = (long long)across * ((a.M + kSlopeRows - 1) / kSlopeRows);
+    for (long long task = blockIdx.x; task < tasks; task += gridDim.x) {
+        const int n = (int)(task % across) * 1024 + (int)threadIdx.x * 4;
+        const long long block = task / across, m0 = block * kSlopeRows;
+        if (n >= a.columns && (n & ~7) >= a.columns) continue;      // (nothing of the last eight)
+        float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int r = 0; r < kSlopeRows; ++r) {
+            const long long m = m0 + r;
+            if (m >= a.M) break;
+            const float4 q = *reinterpret_cast<const float4 *>(a.logits + m * a.stride + n);
+            const float z[4] = {q.x, q.y, q.z, q.w};
+            const int t = a.targets[m];
+            const bool there = t >= 0 && t < a.V;
+            const float slope = a.alpha * (a.dloss ? a.dloss[m] : 1.f), log_sum = a.logSum[m];
+            float d[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = sizeof(TZ) == 4 ? expf(z[e] - log_sum) : exp_of(z[e] - log_sum);
+                d[e] = there && n + e < a.columns ? slope * (t - a.first == n + e ? p - 1.f : p) : 0.f;
+                sums[e] += d[e];
+            }
+            TZ *to = static_cast<TZ *>(a.dz) + m * a.stride + n;
+            if constexpr (sizeof(TZ) == 4) *reinterpret_cast<float4 *>(to) = float4{d[0], d[1], d[2], d[3]};
+            else *reinterpret_cast<uint2 *>(to) = uint2{to_bf16_pair(d[0], d[1]), to_bf16_pair(d[2], d[3])};
+        }
+        if (a.sums) *reinterpret_cast<float4 *>(a.sums + block * a.stride + n) = float4{sums[0], sums[1], sums[2], sums[3]};
+    }
+}
+
+struct BiasGradientArgs {
+    const float *sums;
+    long long stride, blocks;
+    int columns;
+    float beta;
+    float *out;
+};
+// 64 columns to a workgroup, its four wavefronts on every fourth block of rows
+__global__ __launch_bounds__(256) void bias_gradient_kernel(const BiasGradientArgs a) {
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)blockIdx.x * 64 + lane;
+    float sum = 0.f;
+    if (n < a.columns)
+#pragma unroll 4
+        for (long long b = wave; b < a.blocks; b += 4) sum += a.sums[b * a.stride + n];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && n < a.columns) {
+        float v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        if (a.beta != 0.f) v += a.beta * a.out[n];
+        a.out[n] = v;
+    }
+}
+
+struct RoundArgs {
+    const float *from;      // packed
+    bf16_t *to;
+    long long stride;
+    int M, C;
+    float beta;
+};
+// The pieces' sum into bfloat16 rows.
+__global__ __launch_bounds__(256) void round_kernel(const RoundArgs a) {
+    const int groups = (a.C + 3) / 4;
+    const long long tasks = (long long)a.M * groups;
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < tasks; id += (long long)gridDim.x * 256) {
+        const long long m = id / groups;
+        const int c = (int)(id % groups) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.C) {
+                bf16_t *to = a.to + m * a.stride + c + e;
+                float v = a.from[m * a.C + c + e];
+                if (a.beta != 0.f) v += a.beta * Stored<bf16_t>::widen(*to);
+                *to = Stored<bf16_t>::narrow(v);
+            }
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+constexpr long long kMostGroups = 1ll << 20;   // workgroups of a launch; more is taken in turns
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+bool off(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
+unsigned grid_of(long long groups) { return (unsigned)std::min(std::max(groups, 1ll), kMostGroups); }
+
+// The vocabulary in pieces of `size` entries, a multiple of 256 unless it is the whole; `bytes` to an entry of a row.  (Tiles take rows of less than 2^22
+// elements.)
+struct Pieces {
+    int size, count;
+    long long stride;      // of the rows of a piece, elements
+};
+Pieces pieces_of(long long M, int V, size_t bytes) {
+    const long long most = std::min(std::max((long long)(kPieceBytes / bytes) / M / 256 * 256, 256ll), 1ll << 20);
+    Pieces p;
+    if (V <= most) {
+        p.size = V;
+    } else {
+        const long long count = (V + most - 1) / most;
+        p.size = (int)round_up((V + count - 1) / count, 256);
+    }
+    p.count = (V + p.size - 1) / p.size;
+    p.stride = round_up(p.size, 64);
+    return p;
+}
+
+struct Room {
+    size_t total = 0;
+    size_t take(size_t bytes) {
+        const size_t at = total;
+        total += (bytes + 255) / 256 * 256;
+        return at;
+    }
+};
+
+LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns) {
+    LinearArgs a{};
+    a.am = x.stride; a.ak = 1; a.bn = C; a.bk = 1;
+    a.M = (int)x.rows; a.N = columns; a.K = C;
+    a.alpha = 1.f;
+    a.act = IGC_ACTIVATION_IDENTITY;
+    a.ys = p.stride;
+    return a;
+}
+
+struct ForwardPlan {
+    Pieces pieces;
+    int ranges;          // of a whole piece
+    size_t logits, parts, picked, room, total, room_bytes;
+};
+ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
+    ForwardPlan p;
+    p.pieces = pieces_of(x.rows, V, 4);
+    p.ranges = (p.pieces.size + kRange - 1) / kRange;
+    Room r;
+    p.logits = r.take((size_t)x.rows * p.pieces.stride * 4);
+    p.parts = r.take((size_t)x.rows * p.ranges * p.pieces.count * sizeof(RowPart));
+    p.picked = r.take((size_t)x.rows * 4);
+    // (the last piece may be smaller, and then take other tiles)
+    p.room_bytes = std::max(product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, p.pieces.size)),
+                            product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, V - (p.pieces.count - 1) * p.pieces.size)));
+    p.room = r.take(p.room_bytes);
+    p.total = r.total;
+    return p;
+}
+
+struct BackwardPlan {
+    Pieces pieces;
+    bool sum;            // dx of several pieces is summed in floats first
+    size_t logits, dz, dx, sums, room, total, room_bytes;
+};
+LinearArgs data_product(const Matrix &x, int C, const Pieces &p, int columns) {
+    LinearArgs a{};
+    a.am = p.stride; a.ak = 1; a.bn = 1; a.bk = C; a.strided_b = true; a.padded_a = true;
+    a.M = (int)x.rows; a.N = C; a.K = columns;
+    a.alpha = 1.f;
+    a.act = IGC_ACTIVATION_IDENTITY;
+    return a;
+}
+LinearArgs filter_product(const Matrix &x, int C, const Pieces &p, int columns) {
+    LinearArgs a{};
+    a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = x.stride; a.strided_a = a.strided_b = true; a.padded_a = true;
+    a.M = columns; a.N = C; a.K = (int)x.rows;
+    a.alpha = 1.f;
+    a.act = IGC_ACTIVATION_IDENTITY;
+    return a;
+}
+// dx, dw: null where that gradient is not asked for
+BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
+    BackwardPlan p;
+    p.pieces = pieces_of(x.rows, V, 4);
+    p.sum = dx && p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16;
+    Room r;
+    p.logits = r.take((size_t)x.rows * p.pieces.stride * 4);
+    p.dz = t == IGC_DATA_FLOAT ? p.logits : r.take((size_t)x.rows * p.pieces.stride * 2);
+    p.dx = r.take(p.sum ? (size_t)x.rows * C * 4 : 0);
+    p.sums = r.take((size_t)((x.rows + kSlopeRows - 1) / kSlopeRows) * p.pieces.stride * 4);
+    p.room_bytes = 0;
+    for (int columns : {p.pieces.size, V - (p.pieces.count - 1) * p.pieces.size}) {
+        p.room_bytes = std::max(p.room_bytes, product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, columns)));
+        if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(x, C, p.pieces, columns)));
+        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, C, p.pieces, columns)));
+    }
+    p.room = r.take(p.room_bytes);
+    p.total = r.total;
+    return p;
+}
+
+igcStatus check_sizes(igcTensorDescriptor_t x, igcFilterDescriptor_t w, Matrix *mx) {
+    if (!x || !w) return IGC_STATUS_BAD_PARAM;
+    if (!x->set || !w->set) return IGC_STATUS_NOT_INITIALIZED;
+    if (w->r != 1 || w->s != 1 || x->dim[1] != w->c) return IGC_STATUS_BAD_PARAM;
+    if ((x->dtype != IGC_DATA_FLOAT && x->dtype != IGC_DATA_BFLOAT16) || w->dtype != x->dtype || !matrix_of(*x, mx) || w->k > kMostColumns) return IGC_STATUS_NOT_SUPPORTED;
+    return IGC_STATUS_SUCCESS;
+}
+igcStatus check_gradients(igcTensorDescriptor_t x, igcFilterDescriptor_t w, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, Matrix *mdx) {
+    const auto type = [&](igcDataType t) { return t == IGC_DATA_FLOAT || (t == IGC_DATA_BFLOAT16 && x->dtype == IGC_DATA_BFLOAT16); };
+    if ((dx && !dx->set) || (dw && !dw->set)) return IGC_STATUS_NOT_INITIALIZED;
+    if (dx && (!same_positions(*x, *dx) || dx->dim[1] != x->dim[1] || !non_aliasing(dx->dim, dx->stride))) return IGC_STATUS_BAD_PARAM;
+    if (dw && (dw->k != w->k || dw->c != w->c || dw->r != 1 || dw->s != 1)) return IGC_STATUS_BAD_PARAM;
+    if ((dx && (!type(dx->dtype) || !matrix_of(*dx, mdx))) || (dw && !type(dw->dtype))) return IGC_STATUS_NOT_SUPPORTED;
+    return IGC_STATUS_SUCCESS;
+}
+
+}  // namespace
+}  // namespace igc
+
+using namespace igc;
+
+extern "C" {
+
+igcStatus igcGetLinearCrossEntropyForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc, igcFilterDescriptor_t wDesc, size_t *sizeInBytes) {
+    if (!handle || !sizeInBytes) return IGC_STATUS_BAD_PARAM;
+    Matrix x;
+    const igcStatus st = check_sizes(xDesc, wDesc, &x);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    *sizeInBytes = plan_forward(handle, xDesc->dtype, x, wDesc->c, wDesc->k).total;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t xDesc, const void *x, igcFilterDescriptor_t wDesc, const void *w, const void *bias,
+                                       const int *targets, void *workSpace, size_t workSpaceSizeInBytes, void *loss, void *logSum) {
+    if (!handle || !x || !w || !targets || !loss || !workSpace) return IGC_STATUS_BAD_PARAM;
+    Matrix mx;
+    igcStatus st = check_sizes(xDesc, wDesc, &mx);
+    if (st != IGC_STATUS_SUCCESS) return st;
+    const igcDataType t = xDesc->dtype;
+    if (off(x, elem_size(t)) || off(w, elem_size(t)) || off(bias, 4) || off(targets, 4) || off(loss, 4) || off(logSum, 4) || off(workSpace, 16)) return IGC_STATUS_BAD_PARAM;
+    const int C = wDesc->c, V = wDesc->k, M = (int)mx.rows;
+    const ForwardPlan p = plan_forward(handle, t, mx, C, V);
+    if (workSpaceSizeInBytes < p.total) return IGC_STATUS_BAD_PARAM;
+    uint8_t *ws = static_cast<uint8_t *>(workSpace);
+    RowPart *parts = reinterpret_cast<RowPart *>(ws + p.parts);
+    float *picked = reinterpret_cast<float *>(ws + p.picked);
+    int ranges = 0;
+    for (int first = 0; first < V; first += p.pieces.size) {
+        const int columns = std::min(p.pieces.size, V - first);
+        LinearArgs a = logits_product(mx, C, p.pieces, columns);
+        a.a = x;
+        a.b = static_cast<const uint8_t *>(w) + (size_t)first * C * elem_size(t);
+        a.bias = bias ? static_cast<const float *>(bias) + first : nullptr;
+        a.y = ws + p.logits;
+        if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+        const int here = (columns + kRange - 1) / kRange;
+        RowPartsArgs q{reinterpret_cast<const float *>(ws + p.logits), p.pieces.stride, M, columns, here, first, targets, parts + (long long)ranges * M, picked};
+        st = launch_kernel(reinterpret_cast<const void *>(&row_parts_kernel), q, dim3(grid_of(((long long)M * here + 3) / 4)), 256, handle->stream);
+        if (st != IGC_STATUS_SUCCESS) return st;
+        ranges += here;
+    }
+    LossArgs q{parts, M, V, ranges, targets, picked, static_cast<float *>(loss), static_cast<float *>(logSum)};
+    return launch_kernel(reinterpret_cast<const void *>(&loss_kernel), q, dim3(grid_of((M + 63) / 64)), 1024, handle->stream);
+}
+
+igcStatus igcGetLinearCrossEntropyBackwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc, igcFilterDescriptor_t wDesc, igcTensorDescriptor_t dxDesc,
+                                                        igcFilterDescriptor_t dwDesc, size_t *sizeInBytes) {
+    if (!handle || !sizeInBytes) return IGC_STATUS_BAD_PARAM;
+    Matrix x, dx;
+    igcStatus st = check_sizes(xDesc, wDesc, &x);
+    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &dx)) != IGC_STATUS_SUCCESS) return st;
+    *sizeInBytes = plan_backward(handle, xDesc->dtype, dxDesc, dwDesc, x, wDesc->c, wDesc->k).total;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, igcTensorDescriptor_t xDesc, const void *x, igcFilterDescriptor_t wDesc, const void *w,
+                                        const void *bias, const int *targets, const void *logSum, const void *dloss, void *workSpace, size_t workSpaceSizeInBytes,
+                                        const void *beta, igcTensorDescriptor_t dxDesc, void *dx, const void *paramBeta, igcFilterDescriptor_t dwDesc, void *dw, void *dbias) {
+    if (!dx) dxDesc = nullptr;
+    if (!dw) dwDesc = nullptr;
+    if (!handle || !alpha || !beta || !paramBeta || !x || !w || !targets || !logSum || !workSpace || (!dx && !dw && !dbias) || (dx && !dxDesc) || (dw && !dwDesc)) return IGC_STATUS_BAD_PARAM;
+    Matrix mx, mdx;
+    igcStatus st = check_sizes(xDesc, wDesc, &mx);
+    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &mdx)) != IGC_STATUS_SUCCESS) return st;
+    const igcDataType t = xDesc->dtype;
+    if (off(x, elem_size(t)) || off(w, elem_size(t)) || off(bias, 4) || off(targets, 4) || off(logSum, 4) || off(dloss, 4) || off(workSpace, 16) ||
+        (dx && off(dx, elem_size(dxDesc->dtype))) || (dw && off(dw, elem_size(dwDesc->dtype))) || off(dbias, 4))
+        return IGC_STATUS_BAD_PARAM;
+    const int C = wDesc->c, V = wDesc->k, M = (int)mx.rows;
+    const BackwardPlan p = plan_backward(handle, t, dxDesc, dwDesc, mx, C, V);
+    if (workSpaceSizeInBytes < p.total) return IGC_STATUS_BAD_PARAM;
+    const float dx_beta = *static_cast<const float *>(beta), w_beta = *static_cast<const float *>(paramBeta);
+    uint8_t *ws = static_cast<uint8_t *>(workSpace);
+    const long long row_blocks = (M + kSlopeRows - 1) / kSlopeRows;
+    for (int first = 0; first < V; first += p.pieces.size) {
+        const int columns = std::min(p.pieces.size, V - first);
+        const void *piece = static_cast<const uint8_t *>(w) + (size_t)first * C * elem_size(t);
+        LinearArgs a = logits_product(mx, C, p.pieces, columns);
+        a.a = x;
+        a.b = piece;
+        a.bias = bias ? static_cast<const float *>(bias) + first : nullptr;
+        a.y = ws + p.logits;
+        if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+        SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
+                    static_cast<const float *>(logSum), static_cast<const float *>(dloss), dbias ? reinterpret_cast<float *>(ws + p.sums) : nullptr};
+        st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
+                           dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
+        if (st != IGC_STATUS_SUCCESS) return st;
+        if (dbias) {
+            BiasGradientArgs b{q.sums, p.pieces.stride, row_blocks, columns, w_beta, static_cast<float *>(dbias) + first};
+            st = launch_kernel(reinterpret_cast<const void *>(&bias_gradient_kernel), b, dim3((unsigned)(columns + 63) / 64u), 256, handle->stream);
+            if (st != IGC_STATUS_SUCCESS) return st;
+        }
+        if (dx) {
+            LinearArgs d = data_product(mx, C, p.pieces, columns);
+            d.a = ws + p.dz;
+            d.b = piece;
+            d.y = p.sum ? ws + p.dx : dx;
+            d.ys = p.sum ? C : mdx.stride;
+            d.r = d.y;
+            d.rs = d.ys;
+            d.beta = first > 0 ? 1.f : (p.sum ? 0.f : dx_beta);
+            if ((st = product(handle, t, p.sum ? IGC_DATA_FLOAT : dxDesc->dtype, d, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+        }
+        if (dw) {
+            LinearArgs f = filter_product(mx, C, p.pieces, columns);
+            f.a = ws + p.dz;
+            f.b = x;
+            f.y = static_cast<uint8_t *>(dw) + (size_t)first * C * elem_size(dwDesc->dtype);
+            f.ys = C;
+            f.r = f.y;
+            f.rs = C;
+            f.beta = w_beta;
+            if ((st = product(handle, t, dwDesc->dtype, f, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+        }
+    }
+    if (dx && p.sum) {
+        RoundArgs r{reinterpret_cast<const float *>(ws + p.dx), static_cast<bf16_t *>(dx), mdx.stride, M, C, dx_beta};
+        return launch_kernel(reinterpret_cast<const void *>(&round_kernel), r, dim3(grid_of(((long long)M * ((C + 3) / 4) + 255) / 256)), 256, handle->stream);
+    }
+    return IGC_STATUS_SUCCESS;
+}
+
+}  // extern "C"

@@ -14,6 +14,7 @@ struct LinearArgs {
     const void *a, *b;
     long long am, ak, bn, bk;
     bool strided_a, strided_b;   // the reduction index runs along the rows in memory (am, bn are 1)
+    bool padded_a;               // the first operand's rows in memory may be read up to the next eighth element, where zeros lie
     int M, N, K;
     // after the product: t = alpha D + bias[n]; z[m][n] = t where z is kept; t = f(t) (forward) or t f'(zin[m][n]) (backward
     // data); y[m][n] = t + beta r[m][n]
@@ -50,6 +51,10 @@ TileKernel float_kernel();                                           // any pass
 TileKernel tile_kernel_rows(int shape, bool f32_out);          // forward: both operands' reduction indices adjacent
 TileKernel tile_kernel_rows_columns(int shape, bool f32_out);  // backward data: B strided
 TileKernel tile_kernel_columns(int shape, bool f32_out);       // backward filter: both strided
+
+// One product with its epilogue on the handle's stream, by the fastest way that fits into the workspace (igconv_linear.hip), and what the fastest takes.
+igcStatus product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes);
+size_t product_room(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a);
 
 // ---- activations -----------------------------------------------------------------------------------------------------
 // FINE: to float's last digits, for float results.  Otherwise for results that are rounded to bfloat16 (half a step: up to 2^-8 of

@@ -362,19 +362,19 @@ TileKernel tile_kernel(bool sa, bool sb, int shape, bool f32_out) {
 // Whether the tiles take an operand as it lies: rows on boundaries of 4 bytes, of whole pieces of 16 along the reduction index (float: of any length), of
 // whole words across it; no row inside another; a tile's reach below 2^31 bytes.  (Rows on 4-byte boundaries as against copies on 16: forward 1000^3 9.6 us for 13.5,
 // 8192 x 4096 x 4096 212 for 221, filter gradient 208 for 248; on 16-byte boundaries 9.5, 201 and 207.)
-bool fits(const OperandPlan &o, bool strided, int elem, const void *p) {
+bool fits(const OperandPlan &o, bool strided, int elem, const void *p, bool padded = false) {
     const int words = 4 / elem, most = (1 << 23) / elem;
-    return o.cols % (strided || elem == 4 ? words : 16 / elem) == 0 && (o.rows == 1 || (o.stride % words == 0 && o.stride >= o.cols)) &&
+    return (padded || o.cols % (strided || elem == 4 ? words : 16 / elem) == 0) && (o.rows == 1 || (o.stride % words == 0 && o.stride >= o.cols)) &&
            std::max(o.stride, (long long)o.cols) < most && (uintptr_t)p % 4 == 0;
 }
 
 // The matrix of an operand, and whether it has to be copied: a bfloat16 one that does not fit, a float one to have its parts.
-OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, const void *p) {
+OperandPlan operand_plan(bool strided, long long n, long long K, long long ns, long long ks, bool f32, const void *p, bool padded = false) {
     OperandPlan o;
     o.rows = strided ? K : n;
     o.cols = (int)(strided ? n : K);
     o.stride = strided ? ks : ns;
-    o.pack = f32 || !fits(o, strided, 2, p);
+    o.pack = f32 || !fits(o, strided, 2, p, padded);
     o.toRow = round_up(o.cols, 8);
     o.blocks = (int)((n + 15) / 16);
     if (o.pack)
@@ -399,7 +399,7 @@ constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kW
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
-    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b);
+    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a, a.padded_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b);
     double best = 1e300;
     // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
     auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
@@ -549,6 +549,12 @@ LinearArgs backward_filter_sizes(const Matrix &x, const Matrix &dy, const igcFil
 constexpr size_t kNoLimit = ~(size_t)0;
 
 }  // namespace
+
+igcStatus product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes) {
+    return run_product(handle, in, out, a, workSpace, bytes);
+}
+size_t product_room(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a) { return plan_tiles(handle, in, out, a, false, kNoLimit).bytes; }
+
 }  // namespace igc
 
 using namespace igc;
