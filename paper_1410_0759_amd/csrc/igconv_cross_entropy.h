@@ -1,0 +1,54 @@
+// What a tile of logits leaves in place of the logits: statistics of its rows, or its part of the loss's gradient.  Internal.
+#ifndef IGCONV_CROSS_ENTROPY_H_
+#define IGCONV_CROSS_ENTROPY_H_
+
+#include "igconv_linear.h"
+
+namespace igc {
+
+struct RowPart {
+    float most, sum;      // largest logit of some of a row's columns, sum of their exp(z - most)
+};
+
+struct RowStatistics {};               // ends of a tile, in place of the type of stored results
+template <class TZ> struct Slopes {};  // dz stored as TZ
+
+// The product's columns are the vocabulary from entry `first` on.
+struct CrossEnd {
+    const int *targets;
+    int first, V;
+    // RowStatistics
+    RowPart *parts;             // [tile column][M]
+    float *picked;              // [M]: the targets' logits
+    // Slopes: dz goes to LinearArgs::y, with zeros from the last column up to the next eighth
+    float alpha;
+    const float *logSum, *dloss;
+    float *sums;                // column sums of dz over each wavefront's rows, [sumBlocks][sumStride], or null
+    long long sumStride;
+};
+struct CrossArgs : TileArgs {
+    CrossEnd end;
+};
+
+enum CrossKind { kRowStatistics, kSlopes };
+// The kernels with these ends: bfloat16 tiles (as tile_kernel_rows), float operands as they are, float in parts.
+TileKernel cross_tile_kernel(CrossKind kind, int shape);
+TileKernel cross_direct_float_kernel(CrossKind kind, int shape);
+TileKernel cross_float_kernel(CrossKind kind);
+
+// Such a product by the kernels with these ends: us by the figures of the choice (below 0: none of them takes it), columns of a tile, blocks of rows with column sums.
+struct CrossPlan {
+    double us = -1.0;
+    size_t room = 0;
+    int tileColumns = 0, sumBlocks = 0;
+};
+CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);
+igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes,
+                        CrossPlan *taken);
+// what an ordinary product takes, in us by the same figures, with so much room
+double product_us(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, size_t room);
+
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896f); }
+
+}  // namespace igc
+#endif

@@ -6,19 +6,13 @@
 // The logits are never held whole: pieces of the vocabulary are multiplied, taken in and overwritten by the next piece's.  Forward, a piece leaves the largest
 // logit of each row and range of columns and the sum of exp(z - largest); a last kernel joins them.  Backward, the piece's logits are made again, become dz, and go
 // into two products.
-#include "igconv_linear.h"
+#include "igconv_cross_entropy.h"
 
 namespace igc {
 namespace {
 
 constexpr int kRange = 2048;                         // columns of one entry of the row statistics
 constexpr size_t kPieceBytes = (size_t)256 << 20;    // of logits (or dz) at a time
-
-struct RowPart {
-    float most, sum;      // largest logit, sum of exp(z - largest)
-};
-
-__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896f); }
 
 // (nothing but minus infinities: a sum of zero, and no difference of infinities)
 __device__ __forceinline__ RowPart joined(RowPart a, RowPart b) {
@@ -262,32 +256,40 @@ LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns) 
     return a;
 }
 
+// Logits in memory are written and read once more, at bytes per us, by a second launch.
+constexpr double kLogitsBytes = 4.5e6, kLaunch = 3.0;
+double through_memory_us(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V, const Pieces &p, double bytes, size_t room) {
+    return p.count * (product_us(h, t, IGC_DATA_FLOAT, logits_product(x, C, p, p.size), room) + kLaunch) + (double)x.rows * V * bytes / kLogitsBytes;
+}
+constexpr size_t kNoLimit = ~(size_t)0;
+constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a tile's entry in the statistics and the column sums
+
+// (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
 struct ForwardPlan {
+    bool whole;          // the tiles leave the statistics, no logits in memory
     Pieces pieces;
-    int ranges;          // of a whole piece
+    int ranges;          // of all columns
     size_t logits, parts, picked, room, total, room_bytes;
 };
 ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
     ForwardPlan p;
     p.pieces = pieces_of(x.rows, V, 4);
-    p.ranges = (p.pieces.size + kRange - 1) / kRange;
-    Room r;
-    p.logits = r.take((size_t)x.rows * p.pieces.stride * 4);
-    p.parts = r.take((size_t)x.rows * p.ranges * p.pieces.count * sizeof(RowPart));
-    p.picked = r.take((size_t)x.rows * 4);
     // (the last piece may be smaller, and then take other tiles)
     p.room_bytes = std::max(product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, p.pieces.size)),
                             product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, V - (p.pieces.count - 1) * p.pieces.size)));
+    const CrossPlan cross = plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, V), kNoLimit);
+    p.whole = cross.us >= 0.0 && cross.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes);
+    if (p.whole) p.room_bytes = cross.room;
+    p.ranges = p.whole ? (V + kLeastColumns - 1) / kLeastColumns : (p.pieces.size + kRange - 1) / kRange * p.pieces.count;
+    Room r;
+    p.logits = r.take(p.whole ? 0 : (size_t)x.rows * p.pieces.stride * 4);
+    p.parts = r.take((size_t)x.rows * p.ranges * sizeof(RowPart));
+    p.picked = r.take((size_t)x.rows * 4);
     p.room = r.take(p.room_bytes);
     p.total = r.total;
     return p;
 }
 
-struct BackwardPlan {
-    Pieces pieces;
-    bool sum;            // dx of several pieces is summed in floats first
-    size_t logits, dz, dx, sums, room, total, room_bytes;
-};
 LinearArgs data_product(const Matrix &x, int C, const Pieces &p, int columns) {
     LinearArgs a{};
     a.am = p.stride; a.ak = 1; a.bn = 1; a.bk = C; a.strided_b = true; a.padded_a = true;
@@ -304,19 +306,32 @@ LinearArgs filter_product(const Matrix &x, int C, const Pieces &p, int columns) 
     a.act = IGC_ACTIVATION_IDENTITY;
     return a;
 }
+struct BackwardPlan {
+    bool direct;         // the tiles leave dz, no logits in memory
+    Pieces pieces;
+    bool sum;            // dx of several pieces is summed in floats first
+    size_t logits, dz, dx, sums, room, total, room_bytes;
+};
 // dx, dw: null where that gradient is not asked for
 BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
     BackwardPlan p;
-    p.pieces = pieces_of(x.rows, V, 4);
+    const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
+    p.pieces = pieces_of(x.rows, V, elem);
+    const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size), kNoLimit);
+    const Pieces wide = pieces_of(x.rows, V, 4);
+    p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit);
+    p.room_bytes = p.direct ? cross.room : 0;
+    if (!p.direct) p.pieces = wide;
     p.sum = dx && p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16;
     Room r;
-    p.logits = r.take((size_t)x.rows * p.pieces.stride * 4);
-    p.dz = t == IGC_DATA_FLOAT ? p.logits : r.take((size_t)x.rows * p.pieces.stride * 2);
+    p.dz = r.take((size_t)x.rows * p.pieces.stride * elem);
+    p.logits = p.direct || elem == 4 ? p.dz : r.take((size_t)x.rows * p.pieces.stride * 4);
     p.dx = r.take(p.sum ? (size_t)x.rows * C * 4 : 0);
-    p.sums = r.take((size_t)((x.rows + kSlopeRows - 1) / kSlopeRows) * p.pieces.stride * 4);
-    p.room_bytes = 0;
+    p.sums = r.take((size_t)((x.rows + 255) / 256 * 256 / kLeastRows) * p.pieces.stride * 4);
+    // (the last piece may be smaller, and then take other tiles)
     for (int columns : {p.pieces.size, V - (p.pieces.count - 1) * p.pieces.size}) {
-        p.room_bytes = std::max(p.room_bytes, product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, columns)));
+        const LinearArgs logits = logits_product(x, C, p.pieces, columns);
+        p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
         if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(x, C, p.pieces, columns)));
         if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, C, p.pieces, columns)));
     }
@@ -372,7 +387,21 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
     RowPart *parts = reinterpret_cast<RowPart *>(ws + p.parts);
     float *picked = reinterpret_cast<float *>(ws + p.picked);
     int ranges = 0;
-    for (int first = 0; first < V; first += p.pieces.size) {
+    if (p.whole) {
+        LinearArgs a = logits_product(mx, C, p.pieces, V);
+        a.a = x;
+        a.b = w;
+        a.bias = static_cast<const float *>(bias);
+        CrossEnd end{};
+        end.targets = targets;
+        end.V = V;
+        end.parts = parts;
+        end.picked = picked;
+        CrossPlan taken;
+        if ((st = cross_product(handle, kRowStatistics, t, a, end, ws + p.room, p.room_bytes, &taken)) != IGC_STATUS_SUCCESS) return st;
+        ranges = (V + taken.tileColumns - 1) / taken.tileColumns;
+    }
+    for (int first = 0; first < V && !p.whole; first += p.pieces.size) {
         const int columns = std::min(p.pieces.size, V - first);
         LinearArgs a = logits_product(mx, C, p.pieces, columns);
         a.a = x;
@@ -426,15 +455,33 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
         a.a = x;
         a.b = piece;
         a.bias = bias ? static_cast<const float *>(bias) + first : nullptr;
-        a.y = ws + p.logits;
-        if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
-        SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
-                    static_cast<const float *>(logSum), static_cast<const float *>(dloss), dbias ? reinterpret_cast<float *>(ws + p.sums) : nullptr};
-        st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
-                           dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
-        if (st != IGC_STATUS_SUCCESS) return st;
+        float *sums = dbias ? reinterpret_cast<float *>(ws + p.sums) : nullptr;
+        long long sum_blocks = row_blocks;
+        if (p.direct) {
+            a.y = ws + p.dz;
+            CrossEnd end{};
+            end.targets = targets;
+            end.first = first;
+            end.V = V;
+            end.alpha = *static_cast<const float *>(alpha);
+            end.logSum = static_cast<const float *>(logSum);
+            end.dloss = static_cast<const float *>(dloss);
+            end.sums = sums;
+            end.sumStride = p.pieces.stride;
+            CrossPlan taken;
+            if ((st = cross_product(handle, kSlopes, t, a, end, ws + p.room, p.room_bytes, &taken)) != IGC_STATUS_SUCCESS) return st;
+            sum_blocks = taken.sumBlocks;
+        } else {
+            a.y = ws + p.logits;
+            if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+            SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
+                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums};
+            st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
+                               dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
+            if (st != IGC_STATUS_SUCCESS) return st;
+        }
         if (dbias) {
-            BiasGradientArgs b{q.sums, p.pieces.stride, row_blocks, columns, w_beta, static_cast<float *>(dbias) + first};
+            BiasGradientArgs b{sums, p.pieces.stride, sum_blocks, columns, w_beta, static_cast<float *>(dbias) + first};
             st = launch_kernel(reinterpret_cast<const void *>(&bias_gradient_kernel), b, dim3((unsigned)(columns + 63) / 64u), 256, handle->stream);
             if (st != IGC_STATUS_SUCCESS) return st;
         }

@@ -44,6 +44,7 @@ struct TileArgs : LinearArgs {
 struct TileKernel {
     int bm, bn, threads;
     const void *kernel;   // null: not offered
+    int wavesM;           // wavefronts along the tile's rows (ends that leave something for each)
 };
 constexpr int kTileShapes = 4, kStagedShape = 3 /* operands that the others have copied first */, kDirectShapes = 2;
 TileKernel direct_float_kernel(bool sa, bool sb, int shape);   // float operands as they are: few tokens, small products

@@ -17,6 +17,7 @@
 // Neither a quarter fewer vector instructions in f and f' nor z loaded before the last products made a difference: not kept.  Few
 // tokens are bound by the filter's bytes: 8 x 4096 -> 16384 bfloat16 23 us for the tiles, 4.5 for the sum of four ranges, 31.7 the call with the filter in no
 // cache; float 42 and 4.9 warm, 71 the call, 8 x 4001 -> 16384 45, 4.8 and 61.
+#include "igconv_cross_entropy.h"
 #include "igconv_linear_float.hpp"
 
 namespace igc {
@@ -351,6 +352,7 @@ struct TilePlan {
     int tilesM = 0, tilesN = 0, splits = 1, stepsPerSplit = 0;
     OperandPlan a, b;
     size_t partsAt = 0, sumsAt = 0, bytes = 0;   // of workspace
+    double us = 1e300;
 };
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -394,13 +396,16 @@ constexpr ShapeCost kShapeCost[kTileShapes] = {{1, 1.40, 1.40, 8.0}, {2, 0.45, 0
 constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes] = {{2, 1.10, 2.00, 2.5}, {2, 0.60, 1.00, 2.0}};
 // The second launch that adds the ranges' parts, and their bytes, written and read mostly in the last-level cache; bytes per us from memory, and what one
 // workgroup reads of them, whatever its tile (8 x 4096 -> 16384, the filter not in the last-level cache: 128 workgroups 40 us, 256 36, 512 29).
+// What the ends for cross entropy add to a tile's, by shape.
+constexpr double kCrossEnds[kTileShapes] = {4.0, 2.0, 1.0, 1.0};
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;
 
-TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room) {
+// cross: null, or the end of a product for cross entropy (bfloat16 or float, forward, in one range)
+TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room, const CrossKind *cross = nullptr) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
     const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a, a.padded_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b);
-    double best = 1e300;
+    double &best = pl.us;
     // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
     auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
         const int steps = (a.K + step - 1) / step, per = (steps + splits - 1) / splits;
@@ -431,25 +436,27 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         pl.bytes = at + parts + sum_bytes;
     };
     // (no range without a step)
-    auto most_splits = [&](int step) { return std::min(64, (a.K + step - 1) / step); };
+    auto most_splits = [&](int step) { return cross ? 1 : std::min(64, (a.K + step - 1) / step); };
+    auto more = [&](const ShapeCost &sc, int shape) { return cross ? ShapeCost{sc.per_cu, sc.alone, sc.full, sc.ends + kCrossEnds[shape]} : sc; };
     if (f32) {
         // (rows that end inside a piece begin off 16-byte boundaries as well: 1024 x 2050 -> 1000 65 steps of 32 x 128 49 us, 1024 x 2048 -> 1000 64 steps 45;
         // in parts both 42)
         const double steps = a.K % 4 != 0 && !(sa && sb) ? 1.1 : 1.0;
         if (fits(oa, sa, 4, a.a) && fits(ob, sb, 4, a.b))
             for (int shape = 0; shape < kDirectShapes; ++shape) {
-                const ShapeCost sc = kDirectCost[shape];
+                const ShapeCost sc = more(kDirectCost[shape], 2);
                 for (int splits = 1; splits <= most_splits(kFloatStep); ++splits)
-                    consider(direct_float_kernel(sa, sb, shape), {sc.per_cu, sc.alone * steps, sc.full * steps, sc.ends}, kFloatStep, splits, false);
+                    consider(cross ? cross_direct_float_kernel(*cross, shape) : direct_float_kernel(sa, sb, shape), {sc.per_cu, sc.alone * steps, sc.full * steps, sc.ends}, kFloatStep, splits, false);
             }
-        for (int splits = 1; splits <= most_splits(kFloatStep); ++splits) consider(float_kernel(), kFloatCost, kFloatStep, splits, true);
+        for (int splits = 1; splits <= most_splits(kFloatStep); ++splits) consider(cross ? cross_float_kernel(*cross) : float_kernel(), more(kFloatCost, 1), kFloatStep, splits, true);
         return pl;
     }
     // (a tile's reach stays within 31 bits)
     if ((oa.pack ? oa.toRow : oa.stride) >= (1ll << 22) || (ob.pack ? ob.toRow : ob.stride) >= (1ll << 22)) return pl;
     for (int shape = 0; shape < (oa.pack || ob.pack ? kTileShapes : kStagedShape); ++shape)
         for (int splits = 1; splits <= most_splits(kTileStep); ++splits)
-            consider(tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), kShapeCost[shape], kTileStep, splits, shape < kStagedShape);
+            consider(cross ? cross_tile_kernel(*cross, shape) : tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), more(kShapeCost[shape], shape), kTileStep, splits,
+                     shape < kStagedShape);
     return pl;
 }
 
@@ -488,22 +495,26 @@ struct SumsOut {
     float alpha = 1.f, beta = 0.f;
 };
 
+// the plan's tiles in the kernels' arguments, operands copied where it says so
+igcStatus begin_tiles(igcHandle_t handle, const TilePlan &pl, igcDataType in, const LinearArgs &a, uint8_t *ws, TileArgs &t) {
+    static_cast<LinearArgs &>(t) = a;
+    t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
+    t.group = std::min(pl.tilesM, 4);
+    t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
+    t.tilesPerXcd = (int)(((long long)pl.tilesM * pl.tilesN * pl.splits + 7) / 8);
+    t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
+    t.partsRow = round_up(a.N, 8);
+    return pack_operands(pl, in == IGC_DATA_FLOAT, a, t, ws, handle->stream);
+}
+
 igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes, const SumsOut &sums = SumsOut(),
                       bool *summed = nullptr) {
     const TilePlan pl = plan_tiles(handle, in, out, a, sums.out != nullptr, workSpace && on16(workSpace) ? bytes : 0);
     if (pl.tiles) {
         TileArgs t{};
-        static_cast<LinearArgs &>(t) = a;
         uint8_t *ws = static_cast<uint8_t *>(workSpace);
-        igcStatus rc = pack_operands(pl, in == IGC_DATA_FLOAT, a, t, ws, handle->stream);
+        igcStatus rc = begin_tiles(handle, pl, in, a, ws, t);
         if (rc != IGC_STATUS_SUCCESS) return rc;
-        t.tilesM = pl.tilesM; t.tilesN = pl.tilesN;
-        t.group = std::min(pl.tilesM, 4);
-        t.splits = pl.splits; t.stepsPerSplit = pl.stepsPerSplit;
-        const long long units = (long long)pl.tilesM * pl.tilesN * pl.splits;
-        t.tilesPerXcd = (int)((units + 7) / 8);
-        t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
-        t.partsRow = round_up(a.N, 8);
         t.columnParts = sums.out ? reinterpret_cast<float *>(ws + pl.sumsAt) : nullptr;
         rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
         if (rc == IGC_STATUS_SUCCESS && (pl.splits > 1 || sums.out)) {
@@ -554,6 +565,30 @@ igcStatus product(igcHandle_t handle, igcDataType in, igcDataType out, const Lin
     return run_product(handle, in, out, a, workSpace, bytes);
 }
 size_t product_room(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a) { return plan_tiles(handle, in, out, a, false, kNoLimit).bytes; }
+double product_us(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, size_t room) { return plan_tiles(handle, in, out, a, false, room).us; }
+
+static CrossPlan cross_plan(const TilePlan &pl) {
+    CrossPlan c;
+    if (!pl.tiles) return c;
+    c.us = pl.us;
+    c.room = pl.bytes;
+    c.tileColumns = pl.k.bn;
+    c.sumBlocks = pl.tilesM * pl.k.wavesM;
+    return c;
+}
+CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room) {
+    return cross_plan(plan_tiles(handle, in, in, a, false, room, &kind));
+}
+igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes, CrossPlan *taken) {
+    const TilePlan pl = plan_tiles(handle, in, in, a, false, bytes, &kind);
+    *taken = cross_plan(pl);
+    if (!pl.tiles) return IGC_STATUS_NOT_SUPPORTED;
+    CrossArgs t{};
+    const igcStatus rc = begin_tiles(handle, pl, in, a, static_cast<uint8_t *>(workSpace), t);
+    if (rc != IGC_STATUS_SUCCESS) return rc;
+    t.end = end;
+    return launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+}
 
 }  // namespace igc
 

@@ -49,8 +49,8 @@ __device__ __forceinline__ void write_sums(const TileArgs &p, int lane, int rang
     }
 }
 
-template <class Cfg>
-__global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const TileArgs p) {
+template <class Cfg, class TO = float, class Args = TileArgs>
+__global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Args p) {
     constexpr int FM = Cfg::FM, FN = Cfg::FN, SF = Cfg::SF, R = Cfg::REQUESTS;
     __shared__ __attribute__((aligned(16))) uint8_t lds[Cfg::LDS_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -168,8 +168,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_float_kernel(const Til
 
     __builtin_amdgcn_s_waitcnt(0x0F70);   // (nothing may be on its way into LDS)
     __syncthreads();
-    write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, float>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, tm * Cfg::BM + wm * FM * 16,
-                                                              tn * Cfg::BN + wn * FN * 16, acc);
+    TileEnd<Cfg, TO, Args>::template run<FM, FN>(p, lds, lane, wave, split, tm, tn, tm * Cfg::BM + wm * FM * 16, tn * Cfg::BN + wn * FN * 16, acc);
     if (p.columnParts) write_sums<SF>(p, lane, split * p.tilesN + tn, tm * Cfg::BM + (wm * FM + wn * SF) * 16, sums);
 }
 

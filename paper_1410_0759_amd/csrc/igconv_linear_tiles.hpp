@@ -336,8 +336,17 @@ __device__ __forceinline__ void write_results(const TileArgs &p, uint8_t *share,
     }
 }
 
-template <class Cfg, class TO>
-__global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const TileArgs p) {
+// What a workgroup does with its tile's results, all of whose LDS is free: its wavefront's are those from row m0, column n0 on.  Another TO or Args: another end.
+template <class Cfg, class TO, class Args>
+struct TileEnd {
+    template <int FM, int FN>
+    static __device__ __forceinline__ void run(const Args &p, uint8_t *lds, int lane, int wave, int split, int tm, int tn, int m0, int n0, f32x4 (&acc)[FM][FN]) {
+        write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0, n0, acc);
+    }
+};
+
+template <class Cfg, class TO, class Args = TileArgs>
+__global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Args p) {
     constexpr int BM = Cfg::BM, BN = Cfg::BN, FM = Cfg::FM, FN = Cfg::FN, SLOTS = 2 * FM, FREE = FM / 2;
     __shared__ __attribute__((aligned(16))) uint8_t lds[Cfg::LDS_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -479,7 +488,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear_tiles_kernel(const Til
 
     __builtin_amdgcn_s_waitcnt(0x0F70);   // (nothing may be on its way into LDS)
     __syncthreads();
-    write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0 + wm * FM * 16, n0 + wn * FN * 16, acc);
+    TileEnd<Cfg, TO, Args>::template run<FM, FN>(p, lds, lane, wave, split, tm, tn, m0 + wm * FM * 16, n0 + wn * FN * 16, acc);
     if constexpr (Cfg::SA) {
         if (p.columnParts) {
             typedef decltype(copyA) Copy;
