@@ -9,23 +9,12 @@
 // Layout.  A row of W is cut into blocks of 128 features in 64 bytes; word 4 g + i of a block holds features 32 i + 8 g to + 7, the first in the lowest bits.
 // So the 16 bytes that lane group g of a wavefront (16 lanes each) loads are its share of four matrix instructions of 32 features each, and every instruction's features
 // lie in one group of any size.  Scales are kept with the rows next to each other: a lane's four results have theirs in 8 bytes.
-#include "igconv_linear_tiles.hpp"
+#include "igconv_linear4.h"
 
 namespace igc {
 namespace {
 
-constexpr int kBlock = 128, kBlockBytes = 64;
-
-using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
-
-__host__ __device__ inline long long code_row(int C) { return (long long)((C + kBlock - 1) / kBlock) * kBlockBytes; }
-
-// eight codes as bfloat16 numbers
-__device__ __forceinline__ bf16x8 widen8(uint32_t codes) {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 1);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.f, 3);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
+constexpr int kBlock = kCodeBlock, kBlockBytes = kCodeBlockBytes;
 
 // ---- into four bits and back --------------------------------------------------------------------------------------------
 struct StoreArgs {
@@ -135,13 +124,6 @@ __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) 
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------
-struct Linear4Args : LinearArgs {      // a: x; M tokens, N rows of W, K features
-    const uint8_t *codes;
-    const uint16_t *scales;
-    int group;
-    long long tilesM, tilesN;
-};
-
 // A lane's eight features of a token, in bfloat16 parts.
 template <class T> struct Parts;
 template <> struct Parts<bf16_t> {
@@ -183,10 +165,10 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p
     constexpr int N = Parts<TX>::N;
     __shared__ f32x4 sums[WAVES][KB * TB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
-    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group - 1) / p.group;
+    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group4 - 1) / p.group4;
     const long long row_bytes = code_row(p.K);
-    const uint32_t last_of_group = p.group == 32 ? 0xFu : (p.group == 64 ? 0xAu : 0x8u);
-    for (long long tile = blockIdx.x; tile < p.tilesM * p.tilesN; tile += gridDim.x) {
+    const uint32_t last_of_group = p.group4 == 32 ? 0xFu : (p.group4 == 64 ? 0xAu : 0x8u);
+    for (long long tile = blockIdx.x; tile < (long long)p.tilesM * p.tilesN; tile += gridDim.x) {
         const int n0 = (int)(tile % p.tilesN) * (16 * KB);
         const long long m0 = tile / p.tilesN * (16 * TB);
         const uint8_t *row[KB];
@@ -239,25 +221,17 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p
                         for (int n = 0; n < N; ++n) part[kb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, x[tb][n], part[kb][tb], 0, 0, 0);
                 }
                 if (!(last_of_group >> i & 1)) continue;
-                const int group = (s * kBlock + 32 * i) / p.group;
+                const int group = (s * kBlock + 32 * i) / p.group4;
                 if (group >= groups) continue;      // (the last block's codes behind the row are zeros, and so is the part)
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
                     const int n = n0 + 16 * kb + 4 * g;
-                    const uint16_t *from = p.scales + (long long)group * p.N + n;
-                    Adjacent<uint16_t, 4> v{};
-                    if (n + 4 <= p.N) {
-                        v = *reinterpret_cast<const Adjacent<uint16_t, 4> *>(from);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (n + e < p.N) v.v[e] = from[e];
-                    }
+                    const f32x4 scale = widen_scales(load_scales(p.scales + (long long)group * p.N, n, p.N));
 #pragma unroll
                     for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            total[kb][tb][e] += bf16_bits_to_float(v.v[e]) * part[kb][tb][e];
+                            total[kb][tb][e] += scale[e] * part[kb][tb][e];
                             part[kb][tb][e] = 0.f;
                         }
                 }
@@ -281,6 +255,43 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p
                     if (n + e < p.N) finish_element<TO>(p, (int)m, n + e, d[e]);
         }
         __syncthreads();
+    }
+}
+
+// ---- x for the tiles -------------------------------------------------------------------------------------------------------
+struct Lay4Args {
+    const void *x;
+    uint16_t *to;
+    long long stride;
+    int M, C, toRow;
+};
+// bfloat16: rows on 16-byte boundaries, zeros up to the next eighth feature; float: three parts, kPartsTokens rows of each in turn, and zeros for the last rows.
+template <class T>
+__global__ __launch_bounds__(256) void lay_out_kernel(const Lay4Args p) {
+    constexpr int N = Parts<T>::N;
+    const int groups = p.toRow / 8;
+    const long long rows = N == 1 ? p.M : ((long long)p.M + kPartsTokens - 1) / kPartsTokens * kPartsTokens;
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < rows * groups; id += (long long)gridDim.x * 256) {
+        const long long m = id / groups;
+        const int c = (int)(id % groups) * 8;
+        Adjacent<T, 8> v;
+        const T *from = static_cast<const T *>(p.x) + m * p.stride + c;
+        if (m < p.M && c + 8 <= p.C) {
+            v = *reinterpret_cast<const Adjacent<T, 8> *>(from);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v.v[e] = T{};
+                if (m < p.M && c + e < p.C) v.v[e] = from[e];
+            }
+        }
+        bf16x8 parts[N];
+        Parts<T>::split(v, parts);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const long long row = N == 1 ? m : (m / kPartsTokens * N + n) * kPartsTokens + m % kPartsTokens;
+            *reinterpret_cast<bf16x8 *>(p.to + row * p.toRow + c) = parts[n];
+        }
     }
 }
 
@@ -316,18 +327,33 @@ igcStatus with_types(igcDataType in, igcDataType out, F f) {
     return out == IGC_DATA_FLOAT ? f(bf16_t(), float()) : f(bf16_t(), bf16_t());
 }
 
+struct Scale4Args {
+    const uint16_t *from;
+    uint16_t *to;
+    int N;
+    long long groups, toRow;
+};
+// scales into rows of an even length
+__global__ __launch_bounds__(256) void lay_out_scales_kernel(const Scale4Args p) {
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < p.groups * p.toRow; id += (long long)gridDim.x * 256) {
+        const long long group = id / p.toRow, n = id % p.toRow;
+        p.to[id] = n < p.N ? p.from[group * p.N + n] : (uint16_t)0;
+    }
+}
+
 template <int KB, int TB, class TX, class TO>
 igcStatus launch_linear4(Linear4Args a, void *stream) {
     constexpr int WAVES = KB * TB > 4 ? 8 : 16;
-    a.tilesM = ((long long)a.M + 16 * TB - 1) / (16 * TB);
+    a.tilesM = (a.M + 16 * TB - 1) / (16 * TB);
     a.tilesN = (a.N + 16 * KB - 1) / (16 * KB);
-    return launch_kernel(reinterpret_cast<const void *>(&linear4_kernel<KB, TB, WAVES, TX, TO>), a, dim3((unsigned)std::min(a.tilesM * a.tilesN, kMostGroups)), 64 * WAVES, stream);
+    return launch_kernel(reinterpret_cast<const void *>(&linear4_kernel<KB, TB, WAVES, TX, TO>), a, dim3((unsigned)std::min((long long)a.tilesM * a.tilesN, kMostGroups)), 64 * WAVES,
+                         stream);
 }
 
 template <class TX, class TO>
-igcStatus run_linear4(igcHandle_t handle, const Linear4Args &a) {
+igcStatus run_few(igcHandle_t handle, const Linear4Args &a) {
     const int tb = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
-    const long long tm = ((long long)a.M + 16 * tb - 1) / (16 * tb);
+    const long long tm = (a.M + 16 * tb - 1) / (16 * tb);
     auto enough = [&](int kb) { return tm * ((a.N + 16 * kb - 1) / (16 * kb)) >= handle->computeUnits; };
     const int kb = enough(4) ? 4 : (enough(2) ? 2 : 1);
     auto with_kb = [&](auto t) {
@@ -336,6 +362,77 @@ igcStatus run_linear4(igcHandle_t handle, const Linear4Args &a) {
         return kb == 2 ? launch_linear4<2, TB, TX, TO>(a, handle->stream) : launch_linear4<1, TB, TX, TO>(a, handle->stream);
     };
     return tb == 1 ? with_kb(Constant<1>()) : (tb == 2 ? with_kb(Constant<2>()) : with_kb(Constant<4>()));
+}
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+// The tiles for a call, or none: few tokens, or more workgroups than a launch holds.
+struct Tile4Plan {
+    TileKernel k{};
+    bool lay = false, layScales = false;       // x, the scales are laid out first, in `room` bytes
+    size_t scalesAt = 0, room = 0;
+    long long tilesM = 0, tilesN = 0;
+};
+Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, const Linear4Args &a) {
+    Tile4Plan best;
+    if (a.M <= 64 || a.K > (1 << 22)) return best;
+    const bool parts = in == IGC_DATA_FLOAT;
+    const long long row = round_up(a.K, 8);
+    Tile4Plan p;
+    // (as they lie: rows on 4-byte boundaries of whole pieces of 16 bytes, none inside another, a tile's reach below 2^31 bytes)
+    p.lay = parts || a.K % 8 != 0 || (uintptr_t)a.a % 4 != 0 || (a.M > 1 && (a.am % 2 != 0 || a.am < a.K)) || a.am >= (1 << 22);
+    p.layScales = a.N % 2 != 0 || (uintptr_t)a.scales % 4 != 0;
+    p.scalesAt = p.lay ? (size_t)round_up((parts ? round_up(a.M, kPartsTokens) * 3 : a.M) * row * 2, 256) : 0;
+    p.room = p.scalesAt + (p.layScales ? (size_t)((a.K + a.group4 - 1) / a.group4) * round_up(a.N, 2) * 2 : 0);
+    double least = 1e300;
+    for (int shape = 0; shape < kTile4Shapes; ++shape) {
+        p.k = tile4_kernel(shape, a.group4, parts, out == IGC_DATA_FLOAT);
+        if (!p.k.kernel) continue;
+        p.tilesM = (a.M + p.k.bm - 1) / p.k.bm;
+        p.tilesN = (a.N + p.k.bn - 1) / p.k.bn;
+        if (p.tilesM * p.tilesN > kMostGroups) continue;
+        const double us = (double)((p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits) * p.k.bm * p.k.bn;
+        if (us >= least) continue;
+        least = us;
+        best = p;
+    }
+    return best;
+}
+
+igcStatus run_tiles4(igcHandle_t handle, igcDataType in, const Linear4Args &a, const Tile4Plan &pl, void *workSpace) {
+    Linear4Args t = a;
+    igcStatus st = IGC_STATUS_SUCCESS;
+    if (pl.lay) {
+        Lay4Args q{a.a, static_cast<uint16_t *>(workSpace), a.am, a.M, a.K, (int)round_up(a.K, 8)};
+        const long long groups = (round_up(a.M, kPartsTokens) * (q.toRow / 8) + 255) / 256;
+        st = launch_kernel(in == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&lay_out_kernel<float>) : reinterpret_cast<const void *>(&lay_out_kernel<bf16_t>), q,
+                           dim3((unsigned)std::min(groups, kMostGroups)), 256, handle->stream);
+        if (st != IGC_STATUS_SUCCESS) return st;
+        t.a = workSpace;
+        t.am = q.toRow;
+    }
+    t.scaleRow = a.N;
+    if (pl.layScales) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workSpace) + pl.scalesAt);
+        Scale4Args q{a.scales, to, a.N, (a.K + a.group4 - 1) / a.group4, round_up(a.N, 2)};
+        st = launch_kernel(reinterpret_cast<const void *>(&lay_out_scales_kernel), q, dim3((unsigned)std::min((q.groups * q.toRow + 255) / 256, kMostGroups)), 256, handle->stream);
+        if (st != IGC_STATUS_SUCCESS) return st;
+        t.scales = to;
+        t.scaleRow = q.toRow;
+    }
+    t.tilesM = (int)pl.tilesM; t.tilesN = (int)pl.tilesN;
+    t.splits = 1;
+    t.tilesPerXcd = (int)((pl.tilesM * pl.tilesN + 7) / 8);
+    t.group = std::min(t.tilesM, 4);
+    return launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+}
+
+Linear4Args sizes_of(const Matrix &x, const igcFilterStruct &w, int group) {
+    Linear4Args a{};
+    a.am = x.stride; a.ak = 1;
+    a.M = (int)x.rows; a.N = w.k; a.K = w.c;
+    a.group4 = group;
+    return a;
 }
 
 }  // namespace
@@ -390,7 +487,7 @@ igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescrip
     Matrix x, y;
     const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = 0;
+    *sizeInBytes = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, sizes_of(x, *wDesc, group)).room;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -401,7 +498,7 @@ igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDesc
     Matrix mx, my, mr;
     const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &mx, &my);
     if (st != IGC_STATUS_SUCCESS) return st;
-    Linear4Args a{};
+    Linear4Args a = sizes_of(mx, *wDesc, group);
     a.alpha = *static_cast<const float *>(alpha);
     a.beta = *static_cast<const float *>(beta);
     if (a.beta != 0.f) {
@@ -411,16 +508,16 @@ igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDesc
         if (rDesc->dtype != yDesc->dtype || !matrix_of(*rDesc, &mr)) return IGC_STATUS_NOT_SUPPORTED;
     }
     if (off(x, elem_size(xDesc->dtype)) || off(y, elem_size(yDesc->dtype)) || off(bias, 4) || off(codes, 16) || off(scales, 2)) return IGC_STATUS_BAD_PARAM;
-    a.a = x; a.am = mx.stride; a.ak = 1;
-    a.M = (int)mx.rows; a.N = wDesc->k; a.K = wDesc->c;
+    a.a = x;
     a.bias = static_cast<const float *>(bias);
     a.act = activation;
     a.r = r; a.rs = mr.stride;
     a.y = y; a.ys = my.stride;
     a.codes = static_cast<const uint8_t *>(codes);
     a.scales = static_cast<const uint16_t *>(scales);
-    a.group = group;
-    return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_linear4<decltype(tx), decltype(ty)>(handle, a); });
+    const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
+    if (pl.k.kernel && (pl.room == 0 || (workSpace && !off(workSpace, 16) && workSpaceSizeInBytes >= pl.room))) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
+    return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_few<decltype(tx), decltype(ty)>(handle, a); });
 }
 
 }  // extern "C"
