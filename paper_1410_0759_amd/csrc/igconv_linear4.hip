@@ -124,27 +124,51 @@ __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) 
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------
-// A lane's eight features of a token, in bfloat16 parts.
-template <class T> struct Parts;
-template <> struct Parts<bf16_t> {
-    static constexpr int N = 1;
-    static __device__ __forceinline__ void split(const Adjacent<bf16_t, 8> &x, bf16x8 (&p)[1]) { p[0] = __builtin_bit_cast(bf16x8, x); }
+// A lane's eight features of a token, in registers and as bfloat16 parts.
+template <class T> struct Features;
+template <> struct Features<bf16_t> {
+    static constexpr int PARTS = 1;
+    u32x4 v;
+    __device__ __forceinline__ void load(const bf16_t *from) { v = __builtin_bit_cast(u32x4, *reinterpret_cast<const Adjacent<bf16_t, 8> *>(from)); }
+    __device__ __forceinline__ void load_some(const bf16_t *from, int there) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t lo = 0, hi = 0;
+            if (2 * e < there) lo = from[2 * e].bits;
+            if (2 * e + 1 < there) hi = from[2 * e + 1].bits;
+            v[e] = lo | hi << 16;
+        }
+    }
+    __device__ __forceinline__ void split(bf16x8 (&p)[1]) const { p[0] = __builtin_bit_cast(bf16x8, v); }
 };
-template <> struct Parts<float> {
-    static constexpr int N = 3;
+template <> struct Features<float> {
+    static constexpr int PARTS = 3;
+    f32x4 v[2];
+    __device__ __forceinline__ void load(const float *from) {
+        const Adjacent<float, 8> q = *reinterpret_cast<const Adjacent<float, 8> *>(from);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = q.v[e];
+    }
+    __device__ __forceinline__ void load_some(const float *from, int there) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e / 4][e % 4] = 0.f;
+            if (e < there) v[e / 4][e % 4] = from[e];
+        }
+    }
     // by truncation: 24 bits are three times eight.  (An infinity has no rest; an undefined number must not become one.)
-    static __device__ __forceinline__ void split(const Adjacent<float, 8> &x, bf16x8 (&p)[3]) {
+    __device__ __forceinline__ void split(bf16x8 (&p)[3]) const {
         u32x4 h, m, l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t hb[2], mb[2], lb[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float v = x.v[2 * e + i];
-                const uint32_t all = __builtin_bit_cast(uint32_t, v);
+                const float x = v[(2 * e + i) / 4][(2 * e + i) % 4];
+                const uint32_t all = __builtin_bit_cast(uint32_t, x);
                 const bool finite = (all & 0x7F800000u) != 0x7F800000u;
                 hb[i] = (!finite && (all & 0x007FFFFFu)) ? 0x7FC00000u : all & 0xFFFF0000u;
-                const float r = finite ? v - __builtin_bit_cast(float, hb[i]) : 0.f;
+                const float r = finite ? x - __builtin_bit_cast(float, hb[i]) : 0.f;
                 mb[i] = __builtin_bit_cast(uint32_t, r) & 0xFFFF0000u;
                 lb[i] = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, mb[i]));
             }
@@ -158,16 +182,112 @@ template <> struct Parts<float> {
     }
 };
 
-// Any number of tokens.  A workgroup computes 16 TB tokens x 16 KB rows of W; its wavefronts take the blocks of 128 features in turns and add their sums at
-// the end, so that a few rows of W keep a compute unit's loads under way.
-template <int KB, int TB, int WAVES, class TX, class TO>
-__global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p) {
-    constexpr int N = Parts<TX>::N;
+// A workgroup computes 16 TB tokens x 16 KB rows of W; its wavefronts take the blocks of 128 features in turns and add their sums at the end, so that a few rows of W keep a
+// compute unit's loads under way.  The last part of all of them: the sums, from LDS, with the epilogue.
+template <int KB, int TB, int WAVES, class TO>
+__device__ __forceinline__ void finish_sums(const Linear4Args &p, f32x4 (&sums)[WAVES][KB * TB][64], const f32x4 (&total)[KB][TB], int lane, int wave, long long m0, int n0) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+            if (m0 + 16 * tb + (lane & 15) < p.M) sums[wave][kb * TB + tb][lane] = total[kb][tb];
+    __syncthreads();
+    for (int at = threadIdx.x; at < KB * TB * 64; at += 64 * WAVES) {
+        const int block = at >> 6, l = at & 63;
+        const long long m = m0 + 16 * (block % TB) + (l & 15);
+        const int n = n0 + 16 * (block / TB) + 4 * (l >> 4);
+        if (m >= p.M) continue;
+        f32x4 d = sums[0][block][l];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) d += sums[w][block][l];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) finish_element<TO>(p, (int)m, n + e, d[e]);
+    }
+    __syncthreads();
+}
+
+// Sixteen tokens: everything that a wavefront needs for BATCH blocks is requested at once - at 4096 features that is all it needs - because each trip to memory that waits for
+// another shows (1 x 4096 -> 16384, groups of 128: 14.3 us block after block, 15.7 with the next block under way, @FEW@ this way).
+template <int KB, int GROUP, class TX, class TO>
+__global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
+    constexpr int WAVES = 8, N = Features<TX>::PARTS, SCALES = kBlock / GROUP, IN_GROUP = GROUP / 32;
+    constexpr int BATCH = GROUP == 32 || N == 3 ? 2 : 4;     // (registers)
+    __shared__ f32x4 sums[WAVES][KB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + GROUP - 1) / GROUP;
+    const long long row_bytes = code_row(p.K);
+    for (long long tile = blockIdx.x; tile < (long long)p.tilesM * p.tilesN; tile += gridDim.x) {
+        const int n0 = (int)(tile % p.tilesN) * (16 * KB);
+        const long long m0 = tile / p.tilesN * 16;
+        const uint8_t *row[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) row[kb] = p.codes + (long long)min(n0 + 16 * kb + l16, p.N - 1) * row_bytes + g * 16;
+        const TX *token = static_cast<const TX *>(p.a) + min(m0 + l16, (long long)p.M - 1) * p.am + 8 * g;
+        f32x4 total[KB][1];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) total[kb][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int first = wave; first < blocks; first += BATCH * WAVES) {
+            u32x4 codes[BATCH][KB];
+            u32x2 scales[BATCH][SCALES][KB];
+            Features<TX> x[BATCH][4];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int s = first + b * WAVES;
+                if (s >= blocks) continue;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) codes[b][kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if ((s + 1) * kBlock <= p.K) x[b][i].load(token + s * kBlock + 32 * i);
+                    else x[b][i].load_some(token + s * kBlock + 32 * i, p.K - s * kBlock - 8 * g - 32 * i);
+                }
+#pragma unroll
+                for (int q = 0; q < SCALES; ++q)      // (behind the row: zeros times the last group's)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) scales[b][q][kb] = load_scales(p.scales + (long long)min(s * SCALES + q, groups - 1) * p.N, n0 + 16 * kb + 4 * g, p.N);
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (first + b * WAVES >= blocks) continue;
+#pragma unroll
+                for (int q = 0; q < SCALES; ++q) {
+                    f32x4 sum[KB];
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) sum[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < IN_GROUP; ++i) {
+                        bf16x8 parts[N];
+                        x[b][q * IN_GROUP + i].split(parts);
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) {
+                            const bf16x8 w = widen8(codes[b][kb][q * IN_GROUP + i]);
+#pragma unroll
+                            for (int n = 0; n < N; ++n) sum[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, parts[n], sum[kb], 0, 0, 0);
+                        }
+                    }
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        const f32x4 scale = widen_scales(scales[b][q][kb]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) total[kb][0][e] += scale[e] * sum[kb][e];
+                    }
+                }
+            }
+        }
+        finish_sums<KB, 1, WAVES, TO>(p, sums, total, lane, wave, m0, n0);
+    }
+}
+
+// More tokens, TB pieces of sixteen: a block's codes and scales are requested while the block before is multiplied.  Sums are multiplied by their scales every 32 features,
+// whatever the group: that needs no room for sums under way.
+template <int KB, int TB, class TX, class TO>
+__global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p) {
+    constexpr int WAVES = 8, N = Features<TX>::PARTS;
     __shared__ f32x4 sums[WAVES][KB * TB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
-    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group4 - 1) / p.group4;
+    const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group4 - 1) / p.group4, shift = p.group4 == 32 ? 0 : (p.group4 == 64 ? 1 : 2);
     const long long row_bytes = code_row(p.K);
-    const uint32_t last_of_group = p.group4 == 32 ? 0xFu : (p.group4 == 64 ? 0xAu : 0x8u);
     for (long long tile = blockIdx.x; tile < (long long)p.tilesM * p.tilesN; tile += gridDim.x) {
         const int n0 = (int)(tile % p.tilesN) * (16 * KB);
         const long long m0 = tile / p.tilesN * (16 * TB);
@@ -177,84 +297,59 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_kernel(const Linear4Args p
         const TX *token[TB];
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) token[tb] = static_cast<const TX *>(p.a) + min(m0 + 16 * tb + l16, (long long)p.M - 1) * p.am + 8 * g;
-        f32x4 total[KB][TB], part[KB][TB];
+        f32x4 total[KB][TB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb) total[kb][tb] = part[kb][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        u32x4 codes[KB], next[KB];
-        auto load = [&](int s, u32x4 (&to)[KB]) __attribute__((always_inline)) {
-            if (s < blocks)
+            for (int tb = 0; tb < TB; ++tb) total[kb][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        u32x4 codes[KB], next_codes[KB];
+        u32x2 scales[4][KB], next_scales[4][KB];
+        auto load = [&](int s) __attribute__((always_inline)) {
+            if (s >= blocks) return;
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb) to[kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
+            for (int kb = 0; kb < KB; ++kb) next_codes[kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)      // (behind the row: zeros times the last group's)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    next_scales[i][kb] = load_scales(p.scales + (long long)min((4 * s + i) >> shift, groups - 1) * p.N, n0 + 16 * kb + 4 * g, p.N);
         };
-        load(wave, next);
+        load(wave);
         for (int s = wave; s < blocks; s += WAVES) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) codes[kb] = next[kb];
-            load(s + WAVES, next);
-            const int left = p.K - s * kBlock - 8 * g;      // features from this lane's first on
+            for (int kb = 0; kb < KB; ++kb) codes[kb] = next_codes[kb];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) scales[i][kb] = next_scales[i][kb];
+            load(s + WAVES);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                bf16x8 x[TB][N];
+                bf16x8 parts[TB][N];
 #pragma unroll
                 for (int tb = 0; tb < TB; ++tb) {
+                    Features<TX> here;
                     const TX *from = token[tb] + s * kBlock + 32 * i;
-                    Adjacent<TX, 8> v;
-                    if (left - 32 * i >= 8) {
-                        v = *reinterpret_cast<const Adjacent<TX, 8> *>(from);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            v.v[e] = TX{};
-                            if (e < left - 32 * i) v.v[e] = from[e];
-                        }
-                    }
-                    Parts<TX>::split(v, x[tb]);
+                    if ((s + 1) * kBlock <= p.K) here.load(from);
+                    else here.load_some(from, p.K - s * kBlock - 8 * g - 32 * i);
+                    here.split(parts[tb]);
                 }
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
                     const bf16x8 q = widen8(codes[kb][i]);
+                    const f32x4 scale = widen_scales(scales[i][kb]);
 #pragma unroll
-                    for (int tb = 0; tb < TB; ++tb)
+                    for (int tb = 0; tb < TB; ++tb) {
+                        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int n = 0; n < N; ++n) part[kb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, x[tb][n], part[kb][tb], 0, 0, 0);
-                }
-                if (!(last_of_group >> i & 1)) continue;
-                const int group = (s * kBlock + 32 * i) / p.group4;
-                if (group >= groups) continue;      // (the last block's codes behind the row are zeros, and so is the part)
+                        for (int n = 0; n < N; ++n) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, parts[tb][n], sum, 0, 0, 0);
 #pragma unroll
-                for (int kb = 0; kb < KB; ++kb) {
-                    const int n = n0 + 16 * kb + 4 * g;
-                    const f32x4 scale = widen_scales(load_scales(p.scales + (long long)group * p.N, n, p.N));
-#pragma unroll
-                    for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            total[kb][tb][e] += scale[e] * part[kb][tb][e];
-                            part[kb][tb][e] = 0.f;
-                        }
+                        for (int e = 0; e < 4; ++e) total[kb][tb][e] += scale[e] * sum[e];
+                    }
                 }
             }
         }
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb) sums[wave][kb * TB + tb][lane] = total[kb][tb];
-        __syncthreads();
-        for (int at = threadIdx.x; at < KB * TB * 64; at += 64 * WAVES) {
-            const int block = at >> 6, l = at & 63;
-            f32x4 d = sums[0][block][l];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) d += sums[w][block][l];
-            const long long m = m0 + 16 * (block % TB) + (l & 15);
-            const int n = n0 + 16 * (block / TB) + 4 * (l >> 4);
-            if (m < p.M)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < p.N) finish_element<TO>(p, (int)m, n + e, d[e]);
-        }
-        __syncthreads();
+        finish_sums<KB, TB, WAVES, TO>(p, sums, total, lane, wave, m0, n0);
     }
 }
 
@@ -268,25 +363,18 @@ struct Lay4Args {
 // bfloat16: rows on 16-byte boundaries, zeros up to the next eighth feature; float: three parts, kPartsTokens rows of each in turn, and zeros for the last rows.
 template <class T>
 __global__ __launch_bounds__(256) void lay_out_kernel(const Lay4Args p) {
-    constexpr int N = Parts<T>::N;
+    constexpr int N = Features<T>::PARTS;
     const int groups = p.toRow / 8;
     const long long rows = N == 1 ? p.M : ((long long)p.M + kPartsTokens - 1) / kPartsTokens * kPartsTokens;
     for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < rows * groups; id += (long long)gridDim.x * 256) {
         const long long m = id / groups;
         const int c = (int)(id % groups) * 8;
-        Adjacent<T, 8> v;
+        Features<T> v;
         const T *from = static_cast<const T *>(p.x) + m * p.stride + c;
-        if (m < p.M && c + 8 <= p.C) {
-            v = *reinterpret_cast<const Adjacent<T, 8> *>(from);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v.v[e] = T{};
-                if (m < p.M && c + e < p.C) v.v[e] = from[e];
-            }
-        }
+        if (m < p.M && c + 8 <= p.C) v.load(from);
+        else v.load_some(from, m < p.M ? p.C - c : 0);
         bf16x8 parts[N];
-        Parts<T>::split(v, parts);
+        v.split(parts);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const long long row = N == 1 ? m : (m / kPartsTokens * N + n) * kPartsTokens + m % kPartsTokens;
@@ -342,26 +430,28 @@ __global__ __launch_bounds__(256) void lay_out_scales_kernel(const Scale4Args p)
 }
 
 template <int KB, int TB, class TX, class TO>
-igcStatus launch_linear4(Linear4Args a, void *stream) {
-    constexpr int WAVES = KB * TB > 4 ? 8 : 16;
+igcStatus launch_few(igcHandle_t handle, Linear4Args a) {
     a.tilesM = (a.M + 16 * TB - 1) / (16 * TB);
     a.tilesN = (a.N + 16 * KB - 1) / (16 * KB);
-    return launch_kernel(reinterpret_cast<const void *>(&linear4_kernel<KB, TB, WAVES, TX, TO>), a, dim3((unsigned)std::min((long long)a.tilesM * a.tilesN, kMostGroups)), 64 * WAVES,
-                         stream);
+    const void *kernel;
+    if constexpr (TB == 1)
+        kernel = a.group4 == 32 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 32, TX, TO>)
+                                : (a.group4 == 64 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 64, TX, TO>) : reinterpret_cast<const void *>(&linear4_few_kernel<KB, 128, TX, TO>));
+    else
+        kernel = reinterpret_cast<const void *>(&linear4_pieces_kernel<KB, TB, TX, TO>);
+    return launch_kernel(kernel, a, dim3((unsigned)std::min((long long)a.tilesM * a.tilesN, kMostGroups)), 512, handle->stream);
 }
 
+// As many rows of W to a workgroup as leave one for each compute unit: fewer of them read x less often.
 template <class TX, class TO>
 igcStatus run_few(igcHandle_t handle, const Linear4Args &a) {
-    const int tb = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
-    const long long tm = (a.M + 16 * tb - 1) / (16 * tb);
-    auto enough = [&](int kb) { return tm * ((a.N + 16 * kb - 1) / (16 * kb)) >= handle->computeUnits; };
-    const int kb = enough(4) ? 4 : (enough(2) ? 2 : 1);
-    auto with_kb = [&](auto t) {
-        constexpr int TB = decltype(t)::value;
-        if (kb == 4) return launch_linear4<4, TB, TX, TO>(a, handle->stream);
-        return kb == 2 ? launch_linear4<2, TB, TX, TO>(a, handle->stream) : launch_linear4<1, TB, TX, TO>(a, handle->stream);
-    };
-    return tb == 1 ? with_kb(Constant<1>()) : (tb == 2 ? with_kb(Constant<2>()) : with_kb(Constant<4>()));
+    auto enough = [&](int kb, int tb) { return (long long)((a.M + 16 * tb - 1) / (16 * tb)) * ((a.N + 16 * kb - 1) / (16 * kb)) >= handle->computeUnits; };
+    if (a.M <= 16) {
+        if (enough(4, 1)) return launch_few<4, 1, TX, TO>(handle, a);
+        return enough(2, 1) ? launch_few<2, 1, TX, TO>(handle, a) : launch_few<1, 1, TX, TO>(handle, a);
+    }
+    if (a.M <= 32) return enough(2, 2) ? launch_few<2, 2, TX, TO>(handle, a) : launch_few<1, 2, TX, TO>(handle, a);
+    return enough(2, 4) ? launch_few<2, 4, TX, TO>(handle, a) : launch_few<1, 4, TX, TO>(handle, a);
 }
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -391,7 +481,8 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
         p.tilesM = (a.M + p.k.bm - 1) / p.k.bm;
         p.tilesN = (a.N + p.k.bn - 1) / p.k.bn;
         if (p.tilesM * p.tilesN > kMostGroups) continue;
-        const double us = (double)((p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits) * p.k.bm * p.k.bn;
+        constexpr double kBlockUs[kTile4Shapes] = {2.4, 1.2, 3.2};
+        const double us = (double)((p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits) * kBlockUs[shape];
         if (us >= least) continue;
         least = us;
         best = p;

@@ -11,6 +11,11 @@ static TileKernel of_group(int shape, bool parts, bool f32_out) {
     }
     typedef Tile4Config<128, 256, 2, 4, 1, GROUP, 6> Wide;
     typedef Tile4Config<128, 128, 2, 4, 1, GROUP, 6> Small;
+    typedef Tile4Config<256, 256, 2, 4, 1, GROUP, 3> Widest;
+    if (shape == 2 && GROUP == 32) return {};      // (spills registers: 4096 x 4096 -> 8192 324 us for 332)
+    if (shape == 2)
+        return {Widest::BM, Widest::BN, Widest::THREADS,
+                f32_out ? reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, float>) : reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, bf16_t>), Widest::WAVES_M};
     if (shape == 0)
         return {Wide::BM, Wide::BN, Wide::THREADS,
                 f32_out ? reinterpret_cast<const void *>(&linear4_tiles_kernel<Wide, float>) : reinterpret_cast<const void *>(&linear4_tiles_kernel<Wide, bf16_t>), Wide::WAVES_M};
