@@ -129,8 +129,8 @@ template <class T> struct Features;
 template <> struct Features<bf16_t> {
     static constexpr int PARTS = 1;
     u32x4 v;
-    __device__ __forceinline__ void load(const bf16_t *from) { v = __builtin_bit_cast(u32x4, *reinterpret_cast<const Adjacent<bf16_t, 8> *>(from)); }
-    __device__ __forceinline__ void load_some(const bf16_t *from, int there) {
+    __device__ __forceinline__ void load(const bf16_t *from, long long = 0) { v = __builtin_bit_cast(u32x4, *reinterpret_cast<const Adjacent<bf16_t, 8> *>(from)); }
+    __device__ __forceinline__ void load_some(const bf16_t *from, int there, long long = 0) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t lo = 0, hi = 0;
@@ -144,12 +144,12 @@ template <> struct Features<bf16_t> {
 template <> struct Features<float> {
     static constexpr int PARTS = 3;
     f32x4 v[2];
-    __device__ __forceinline__ void load(const float *from) {
+    __device__ __forceinline__ void load(const float *from, long long = 0) {
         const Adjacent<float, 8> q = *reinterpret_cast<const Adjacent<float, 8> *>(from);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = q.v[e];
     }
-    __device__ __forceinline__ void load_some(const float *from, int there) {
+    __device__ __forceinline__ void load_some(const float *from, int there, long long = 0) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e / 4][e % 4] = 0.f;
@@ -182,10 +182,35 @@ template <> struct Features<float> {
     }
 };
 
+// float features laid out in three parts (lay_out_kernel), `parts` elements apart; rows end with a whole eight
+struct Laid {
+    uint16_t bits;
+};
+template <> struct Features<Laid> {
+    static constexpr int PARTS = 3;
+    u32x4 v[3];
+    __device__ __forceinline__ void load(const Laid *from, long long parts) {
+#pragma unroll
+        for (int n = 0; n < 3; ++n) v[n] = *reinterpret_cast<const u32x4 *>(from + n * parts);
+    }
+    __device__ __forceinline__ void load_some(const Laid *from, int there, long long parts) {
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            v[n] = u32x4{0u, 0u, 0u, 0u};
+            if (there > 0) v[n] = *reinterpret_cast<const u32x4 *>(from + n * parts);
+        }
+    }
+    __device__ __forceinline__ void split(bf16x8 (&p)[3]) const {
+#pragma unroll
+        for (int n = 0; n < 3; ++n) p[n] = __builtin_bit_cast(bf16x8, v[n]);
+    }
+};
+
 // A workgroup computes 16 TB tokens x 16 KB rows of W; its wavefronts take the blocks of 128 features in turns and add their sums at the end, so that a few rows of W keep a
 // compute unit's loads under way.  The last part of all of them: the sums, from LDS, with the epilogue.
 template <int KB, int TB, int WAVES, class TO>
-__device__ __forceinline__ void finish_sums(const Linear4Args &p, f32x4 (&sums)[WAVES][KB * TB][64], const f32x4 (&total)[KB][TB], int lane, int wave, long long m0, int n0) {
+__device__ __forceinline__ void finish_sums(const Linear4Args &p, f32x4 (&sums)[WAVES][KB * TB][64], const f32x4 (&total)[KB][TB], int lane, int wave, long long m0, int n0,
+                                            int split) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -200,6 +225,10 @@ __device__ __forceinline__ void finish_sums(const Linear4Args &p, f32x4 (&sums)[
         f32x4 d = sums[0][block][l];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) d += sums[w][block][l];
+        if (p.splits > 1) {
+            if (n < p.N) *reinterpret_cast<f32x4 *>(p.parts + ((long long)split * p.M + m) * p.partsRow + n) = d;
+            continue;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (n + e < p.N) finish_element<TO>(p, (int)m, n + e, d[e]);
@@ -217,7 +246,9 @@ __global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
     const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + GROUP - 1) / GROUP;
     const long long row_bytes = code_row(p.K);
-    for (long long tile = blockIdx.x; tile < (long long)p.tilesM * p.tilesN; tile += gridDim.x) {
+    for (long long unit = blockIdx.x; unit < (long long)p.tilesM * p.tilesN * p.splits; unit += gridDim.x) {
+        const long long tile = unit / p.splits;
+        const int split = (int)(unit % p.splits), begin = split * p.stepsPerSplit, end = min(blocks, begin + p.stepsPerSplit);
         const int n0 = (int)(tile % p.tilesN) * (16 * KB);
         const long long m0 = tile / p.tilesN * 16;
         const uint8_t *row[KB];
@@ -227,14 +258,14 @@ __global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
         f32x4 total[KB][1];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) total[kb][0] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int first = wave; first < blocks; first += BATCH * WAVES) {
+        for (int first = begin + wave; first < end; first += BATCH * WAVES) {
             u32x4 codes[BATCH][KB];
             u32x2 scales[BATCH][SCALES][KB];
             Features<TX> x[BATCH][4];
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 const int s = first + b * WAVES;
-                if (s >= blocks) continue;
+                if (s >= end) continue;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) codes[b][kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
 #pragma unroll
@@ -249,7 +280,7 @@ __global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
             }
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
-                if (first + b * WAVES >= blocks) continue;
+                if (first + b * WAVES >= end) continue;
 #pragma unroll
                 for (int q = 0; q < SCALES; ++q) {
                     f32x4 sum[KB];
@@ -275,7 +306,7 @@ __global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
                 }
             }
         }
-        finish_sums<KB, 1, WAVES, TO>(p, sums, total, lane, wave, m0, n0);
+        finish_sums<KB, 1, WAVES, TO>(p, sums, total, lane, wave, m0, n0, split);
     }
 }
 
@@ -288,7 +319,9 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
     const int blocks = (p.K + kBlock - 1) / kBlock, groups = (p.K + p.group4 - 1) / p.group4, shift = p.group4 == 32 ? 0 : (p.group4 == 64 ? 1 : 2);
     const long long row_bytes = code_row(p.K);
-    for (long long tile = blockIdx.x; tile < (long long)p.tilesM * p.tilesN; tile += gridDim.x) {
+    for (long long unit = blockIdx.x; unit < (long long)p.tilesM * p.tilesN * p.splits; unit += gridDim.x) {
+        const long long tile = unit / p.splits;
+        const int split = (int)(unit % p.splits), begin = split * p.stepsPerSplit, end = min(blocks, begin + p.stepsPerSplit);
         const int n0 = (int)(tile % p.tilesN) * (16 * KB);
         const long long m0 = tile / p.tilesN * (16 * TB);
         const uint8_t *row[KB];
@@ -296,7 +329,10 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
         for (int kb = 0; kb < KB; ++kb) row[kb] = p.codes + (long long)min(n0 + 16 * kb + l16, p.N - 1) * row_bytes + g * 16;
         const TX *token[TB];
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb) token[tb] = static_cast<const TX *>(p.a) + min(m0 + 16 * tb + l16, (long long)p.M - 1) * p.am + 8 * g;
+        for (int tb = 0; tb < TB; ++tb) {
+            const long long m = min(m0 + 16 * tb + l16, (long long)p.M - 1);
+            token[tb] = static_cast<const TX *>(p.a) + (sizeof(TX) == 2 && N == 3 ? m / kPartsTokens * (3 * kPartsTokens) + m % kPartsTokens : m) * p.am + 8 * g;
+        }
         f32x4 total[KB][TB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -305,7 +341,7 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
         u32x4 codes[KB], next_codes[KB];
         u32x2 scales[4][KB], next_scales[4][KB];
         auto load = [&](int s) __attribute__((always_inline)) {
-            if (s >= blocks) return;
+            if (s >= end) return;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) next_codes[kb] = *reinterpret_cast<const u32x4 *>(row[kb] + (long long)s * kBlockBytes);
 #pragma unroll
@@ -314,8 +350,8 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
                 for (int kb = 0; kb < KB; ++kb)
                     next_scales[i][kb] = load_scales(p.scales + (long long)min((4 * s + i) >> shift, groups - 1) * p.N, n0 + 16 * kb + 4 * g, p.N);
         };
-        load(wave);
-        for (int s = wave; s < blocks; s += WAVES) {
+        load(begin + wave);
+        for (int s = begin + wave; s < end; s += WAVES) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) codes[kb] = next_codes[kb];
 #pragma unroll
@@ -330,8 +366,8 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
                 for (int tb = 0; tb < TB; ++tb) {
                     Features<TX> here;
                     const TX *from = token[tb] + s * kBlock + 32 * i;
-                    if ((s + 1) * kBlock <= p.K) here.load(from);
-                    else here.load_some(from, p.K - s * kBlock - 8 * g - 32 * i);
+                    if ((s + 1) * kBlock <= p.K) here.load(from, kPartsTokens * p.am);
+                    else here.load_some(from, p.K - s * kBlock - 8 * g - 32 * i, kPartsTokens * p.am);
                     here.split(parts[tb]);
                 }
 #pragma unroll
@@ -349,7 +385,22 @@ __global__ __launch_bounds__(512) void linear4_pieces_kernel(const Linear4Args p
                 }
             }
         }
-        finish_sums<KB, TB, WAVES, TO>(p, sums, total, lane, wave, m0, n0);
+        finish_sums<KB, TB, WAVES, TO>(p, sums, total, lane, wave, m0, n0, split);
+    }
+}
+
+// The sum of the parts of a cut reduction, with the epilogue: a thread four neighbours of a row.
+template <class TO>
+__global__ __launch_bounds__(256) void linear4_finish_kernel(const Linear4Args p) {
+    const long long groups = p.partsRow / 4, tasks = p.M * groups;
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < tasks; id += (long long)gridDim.x * 256) {
+        const int m = (int)(id / groups), n = (int)(id % groups) * 4;
+        f32x4 d = *reinterpret_cast<const f32x4 *>(p.parts + m * p.partsRow + n);
+#pragma unroll 4
+        for (int s = 1; s < p.splits; ++s) d += *reinterpret_cast<const f32x4 *>(p.parts + ((long long)s * p.M + m) * p.partsRow + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < p.N) finish_element<TO>(p, m, n + e, d[e]);
     }
 }
 
@@ -407,6 +458,7 @@ igcStatus check_product(igcTensorDescriptor_t x, igcFilterDescriptor_t w, int gr
     return IGC_STATUS_SUCCESS;
 }
 
+constexpr long long kSplitBytes = 4ll << 20;   // of codes
 constexpr long long kMostGroups = 1ll << 21;   // workgroups of a launch (times 1024 threads: a 32-bit number); more tiles are taken in turns
 
 template <class F>
@@ -429,32 +481,88 @@ __global__ __launch_bounds__(256) void lay_out_scales_kernel(const Scale4Args p)
     }
 }
 
-template <int KB, int TB, class TX, class TO>
-igcStatus launch_few(igcHandle_t handle, Linear4Args a) {
-    a.tilesM = (a.M + 16 * TB - 1) / (16 * TB);
-    a.tilesN = (a.N + 16 * KB - 1) / (16 * KB);
-    const void *kernel;
-    if constexpr (TB == 1)
-        kernel = a.group4 == 32 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 32, TX, TO>)
-                                : (a.group4 == 64 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 64, TX, TO>) : reinterpret_cast<const void *>(&linear4_few_kernel<KB, 128, TX, TO>));
-    else
-        kernel = reinterpret_cast<const void *>(&linear4_pieces_kernel<KB, TB, TX, TO>);
-    return launch_kernel(kernel, a, dim3((unsigned)std::min((long long)a.tilesM * a.tilesN, kMostGroups)), 512, handle->stream);
-}
-
-// As many rows of W to a workgroup as leave one for each compute unit: fewer of them read x less often.
-template <class TX, class TO>
-igcStatus run_few(igcHandle_t handle, const Linear4Args &a) {
-    auto enough = [&](int kb, int tb) { return (long long)((a.M + 16 * tb - 1) / (16 * tb)) * ((a.N + 16 * kb - 1) / (16 * kb)) >= handle->computeUnits; };
-    if (a.M <= 16) {
-        if (enough(4, 1)) return launch_few<4, 1, TX, TO>(handle, a);
-        return enough(2, 1) ? launch_few<2, 1, TX, TO>(handle, a) : launch_few<1, 1, TX, TO>(handle, a);
-    }
-    if (a.M <= 32) return enough(2, 2) ? launch_few<2, 2, TX, TO>(handle, a) : launch_few<1, 2, TX, TO>(handle, a);
-    return enough(2, 4) ? launch_few<2, 4, TX, TO>(handle, a) : launch_few<1, 4, TX, TO>(handle, a);
-}
-
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+// Few tokens: pieces of 16 TB tokens and 16 KB rows of W, the reduction in ranges where those are few; x in parts first where several pieces of float tokens would make
+// them again and again.
+struct FewPlan {
+    int kb = 1, tb = 1, splits = 1, per = 0;      // per: blocks to a range
+    bool lay = false;
+    size_t partsAt = 0, room = 0;
+};
+FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size_t room) {
+    FewPlan p;
+    const int blocks = (a.K + kBlock - 1) / kBlock;
+    p.tb = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
+    const long long tm = (a.M + 16 * p.tb - 1) / (16 * p.tb);
+    auto tiles = [&](int kb) { return tm * ((a.N + 16 * kb - 1) / (16 * kb)); };
+    const int most = p.tb == 1 ? 4 : 2;      // (registers)
+    // Without ranges: as many rows of W to a workgroup as leave one for each compute unit (x is read less often).
+    p.kb = most == 4 && tiles(4) >= h->computeUnits ? 4 : (tiles(2) >= h->computeUnits ? 2 : 1);
+    p.per = blocks;
+    if (in == IGC_DATA_FLOAT && p.tb > 1) {
+        const size_t bytes = (size_t)round_up(round_up(a.M, kPartsTokens) * 3 * round_up(a.K, 8) * 2, 256);
+        if (bytes <= room) p.lay = true, p.partsAt = p.room = bytes;
+    }
+    // Ranges, each of a block for every wavefront at least, where the codes are worth a second launch.
+    if (p.kb < most && (long long)a.N * code_row(a.K) >= kSplitBytes) {
+        const int splits = (int)std::min<long long>((h->computeUnits + tiles(most) - 1) / tiles(most), (blocks + 7) / 8);
+        const size_t bytes = (size_t)splits * a.M * round_up(a.N, 4) * 4;
+        if (splits > 1 && p.partsAt + bytes <= room) {
+            p.kb = most;
+            p.per = (blocks + splits - 1) / splits;
+            p.splits = (blocks + p.per - 1) / p.per;
+            p.room = p.partsAt + bytes;
+        }
+    }
+    return p;
+}
+
+template <int KB, int TB, class TX, class TO>
+const void *few_kernel(int group) {
+    if constexpr (TB == 1)
+        return group == 32 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 32, TX, TO>)
+                           : (group == 64 ? reinterpret_cast<const void *>(&linear4_few_kernel<KB, 64, TX, TO>) : reinterpret_cast<const void *>(&linear4_few_kernel<KB, 128, TX, TO>));
+    else
+        return reinterpret_cast<const void *>(&linear4_pieces_kernel<KB, TB, TX, TO>);
+}
+template <class TX, class TO>
+const void *few_kernel(const FewPlan &p, int group) {
+    if (p.tb == 1) return p.kb == 4 ? few_kernel<4, 1, TX, TO>(group) : (p.kb == 2 ? few_kernel<2, 1, TX, TO>(group) : few_kernel<1, 1, TX, TO>(group));
+    if constexpr (sizeof(TX) == 4) {
+        if (p.lay) {
+            if (p.tb == 2) return p.kb == 2 ? few_kernel<2, 2, Laid, TO>(group) : few_kernel<1, 2, Laid, TO>(group);
+            return p.kb == 2 ? few_kernel<2, 4, Laid, TO>(group) : few_kernel<1, 4, Laid, TO>(group);
+        }
+    }
+    if (p.tb == 2) return p.kb == 2 ? few_kernel<2, 2, TX, TO>(group) : few_kernel<1, 2, TX, TO>(group);
+    return p.kb == 2 ? few_kernel<2, 4, TX, TO>(group) : few_kernel<1, 4, TX, TO>(group);
+}
+
+igcStatus lay_out(igcHandle_t handle, igcDataType in, Linear4Args &t, void *to) {
+    Lay4Args q{t.a, static_cast<uint16_t *>(to), t.am, t.M, t.K, (int)round_up(t.K, 8)};
+    const long long groups = (round_up(t.M, kPartsTokens) * (q.toRow / 8) + 255) / 256;
+    t.a = to;
+    t.am = q.toRow;
+    return launch_kernel(in == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&lay_out_kernel<float>) : reinterpret_cast<const void *>(&lay_out_kernel<bf16_t>), q,
+                         dim3((unsigned)std::min(groups, kMostGroups)), 256, handle->stream);
+}
+
+template <class TX, class TO>
+igcStatus run_few(igcHandle_t handle, const Linear4Args &a, const FewPlan &p, void *workSpace) {
+    Linear4Args t = a;
+    igcStatus st = IGC_STATUS_SUCCESS;
+    if (p.lay && (st = lay_out(handle, IGC_DATA_FLOAT, t, workSpace)) != IGC_STATUS_SUCCESS) return st;
+    t.tilesM = (a.M + 16 * p.tb - 1) / (16 * p.tb);
+    t.tilesN = (a.N + 16 * p.kb - 1) / (16 * p.kb);
+    t.splits = p.splits;
+    t.stepsPerSplit = p.per;
+    t.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workSpace) + p.partsAt);
+    t.partsRow = round_up(a.N, 4);
+    st = launch_kernel(few_kernel<TX, TO>(p, a.group4), t, dim3((unsigned)std::min((long long)t.tilesM * t.tilesN * t.splits, kMostGroups)), 512, handle->stream);
+    if (st != IGC_STATUS_SUCCESS || p.splits == 1) return st;
+    return launch_kernel(reinterpret_cast<const void *>(&linear4_finish_kernel<TO>), t, dim3((unsigned)std::min((a.M * (t.partsRow / 4) + 255) / 256, kMostGroups)), 256, handle->stream);
+}
 
 // The tiles for a call, or none: few tokens, or more workgroups than a launch holds.
 struct Tile4Plan {
@@ -493,15 +601,7 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
 igcStatus run_tiles4(igcHandle_t handle, igcDataType in, const Linear4Args &a, const Tile4Plan &pl, void *workSpace) {
     Linear4Args t = a;
     igcStatus st = IGC_STATUS_SUCCESS;
-    if (pl.lay) {
-        Lay4Args q{a.a, static_cast<uint16_t *>(workSpace), a.am, a.M, a.K, (int)round_up(a.K, 8)};
-        const long long groups = (round_up(a.M, kPartsTokens) * (q.toRow / 8) + 255) / 256;
-        st = launch_kernel(in == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&lay_out_kernel<float>) : reinterpret_cast<const void *>(&lay_out_kernel<bf16_t>), q,
-                           dim3((unsigned)std::min(groups, kMostGroups)), 256, handle->stream);
-        if (st != IGC_STATUS_SUCCESS) return st;
-        t.a = workSpace;
-        t.am = q.toRow;
-    }
+    if (pl.lay && (st = lay_out(handle, in, t, workSpace)) != IGC_STATUS_SUCCESS) return st;
     t.scaleRow = a.N;
     if (pl.layScales) {
         uint16_t *to = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workSpace) + pl.scalesAt);
@@ -578,7 +678,9 @@ igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescrip
     Matrix x, y;
     const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, sizes_of(x, *wDesc, group)).room;
+    const Linear4Args a = sizes_of(x, *wDesc, group);
+    const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
+    *sizeInBytes = pl.k.kernel ? pl.room : plan_few(handle, xDesc->dtype, a, ~(size_t)0).room;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -607,8 +709,10 @@ igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDesc
     a.codes = static_cast<const uint8_t *>(codes);
     a.scales = static_cast<const uint16_t *>(scales);
     const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
-    if (pl.k.kernel && (pl.room == 0 || (workSpace && !off(workSpace, 16) && workSpaceSizeInBytes >= pl.room))) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
-    return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_few<decltype(tx), decltype(ty)>(handle, a); });
+    const size_t room = workSpace && !off(workSpace, 16) ? workSpaceSizeInBytes : 0;
+    if (pl.k.kernel && pl.room <= room) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
+    const FewPlan few = plan_few(handle, xDesc->dtype, a, room);
+    return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_few<decltype(tx), decltype(ty)>(handle, a, few, workSpace); });
 }
 
 }  // extern "C"
