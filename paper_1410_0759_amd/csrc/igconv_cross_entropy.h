@@ -45,6 +45,11 @@ struct CrossPlan {
 CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);
 igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes,
                         CrossPlan *taken);
+// The same for at most kFewTokens tokens of bfloat16 features, of any layout (igconv_cross_entropy_few.hip).  Slopes: dz in two parts, rows M to 2 M - 1 of y hold the second; x is
+// copied to z (rows zs apart, from 16-byte boundaries), twice below each other.  One block of column sums.
+constexpr int kFewTokens = 32;
+int cross_few_columns(igcHandle_t handle, int N);      // of an entry of the statistics
+igcStatus cross_few(igcHandle_t handle, CrossKind kind, const LinearArgs &a, const CrossEnd &end);
 // what an ordinary product takes, in us by the same figures, with so much room
 double product_us(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, size_t room);
 

@@ -89,6 +89,13 @@ struct LossArgs {
     float *loss, *logSum;
 };
 
+__device__ __forceinline__ void finish_loss(const LossArgs &a, long long m, RowPart row) {
+    const float log_sum = row.most == -INFINITY ? row.most + row.sum : row.most + logf(row.sum);
+    const int t = a.targets[m];
+    a.loss[m] = t >= 0 && t < a.V ? log_sum - a.picked[m] : 0.f;
+    if (a.logSum) a.logSum[m] = log_sum;
+}
+
 // 64 rows to a workgroup, its sixteen wavefronts on every sixteenth range.
 __global__ __launch_bounds__(1024) void loss_kernel(const LossArgs a) {
     __shared__ RowPart parts[16][64];
@@ -104,14 +111,30 @@ __global__ __launch_bounds__(1024) void loss_kernel(const LossArgs a) {
         if (wave == 0 && m < a.M) {
 #pragma unroll
             for (int w = 1; w < 16; ++w) mine = joined(mine, parts[w][lane]);
-            const float log_sum = mine.most == -INFINITY ? mine.most + mine.sum : mine.most + logf(mine.sum);
-            const int t = a.targets[m];
-            a.loss[m] = t >= 0 && t < a.V ? log_sum - a.picked[m] : 0.f;
-            if (a.logSum) a.logSum[m] = log_sum;
+            finish_loss(a, m, mine);
         }
         __syncthreads();
     }
 }
+
+// Few rows: a workgroup to a row, its threads on the ranges.
+__global__ __launch_bounds__(1024) void loss_row_kernel(const LossArgs a) {
+    __shared__ RowPart parts[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = blockIdx.x;
+    RowPart mine{-INFINITY, 0.f};
+#pragma unroll 4
+    for (int r = threadIdx.x; r < a.ranges; r += 1024) mine = joined(mine, a.parts[(long long)r * a.M + m]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) mine = joined(mine, {__shfl_xor(mine.most, d), __shfl_xor(mine.sum, d)});
+    if (lane == 0) parts[wave] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) mine = joined(mine, parts[w]);
+        finish_loss(a, m, mine);
+    }
+}
+constexpr int kRowLosses = 256;      // rows up to which each has a workgroup of its own (4 rows of 512 ranges: @ROWLOSS@ us, 64 rows to a workgroup 4.6)
 
 // ---- backward -----------------------------------------------------------------------------------------------------------
 struct SlopeArgs {
@@ -185,15 +208,16 @@ __global__ __launch_bounds__(256) void bias_gradient_kernel(const BiasGradientAr
     }
 }
 
-struct RoundArgs {
-    const float *from;      // packed
-    bf16_t *to;
+struct JoinArgs {
+    const float *from, *more;      // packed; more: null, or added
+    void *to;
     long long stride;
     int M, C;
     float beta;
 };
-// The pieces' sum into bfloat16 rows.
-__global__ __launch_bounds__(256) void round_kernel(const RoundArgs a) {
+// The sum over the pieces (few tokens: of dz's two parts) into dx.
+template <class TO>
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs a) {
     const int groups = (a.C + 3) / 4;
     const long long tasks = (long long)a.M * groups;
     for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < tasks; id += (long long)gridDim.x * 256) {
@@ -202,10 +226,11 @@ __global__ __launch_bounds__(256) void round_kernel(const RoundArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (c + e < a.C) {
-                bf16_t *to = a.to + m * a.stride + c + e;
+                TO *to = static_cast<TO *>(a.to) + m * a.stride + c + e;
                 float v = a.from[m * a.C + c + e];
-                if (a.beta != 0.f) v += a.beta * Stored<bf16_t>::widen(*to);
-                *to = Stored<bf16_t>::narrow(v);
+                if (a.more) v += a.more[m * a.C + c + e];
+                if (a.beta != 0.f) v += a.beta * Stored<TO>::widen(*to);
+                *to = Stored<TO>::narrow(v);
             }
     }
 }
@@ -265,8 +290,9 @@ constexpr size_t kNoLimit = ~(size_t)0;
 constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a tile's entry in the statistics and the column sums
 
 // (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
+bool few_tokens(igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens; }
 struct ForwardPlan {
-    bool whole;          // the tiles leave the statistics, no logits in memory
+    bool few, whole;     // few tokens; else whether the tiles leave the statistics, no logits in memory
     Pieces pieces;
     int ranges;          // of all columns
     size_t logits, parts, picked, room, total, room_bytes;
@@ -274,9 +300,21 @@ struct ForwardPlan {
 ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
     ForwardPlan p;
     p.pieces = pieces_of(x.rows, V, 4);
+    p.few = few_tokens(t, x);
+    if (p.few) {
+        p.whole = true;
+        p.ranges = (V + cross_few_columns(h, V) - 1) / cross_few_columns(h, V);
+        p.logits = p.room = p.room_bytes = 0;
+        Room r;
+        p.parts = r.take((size_t)x.rows * p.ranges * sizeof(RowPart));
+        p.picked = r.take((size_t)x.rows * 4);
+        p.total = r.total;
+        return p;
+    }
     // (the last piece may be smaller, and then take other tiles)
-    p.room_bytes = std::max(product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, p.pieces.size)),
-                            product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, V - (p.pieces.count - 1) * p.pieces.size)));
+    p.room_bytes = product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, p.pieces.size));
+    if (p.pieces.count > 1)
+        p.room_bytes = std::max(p.room_bytes, product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, V - (p.pieces.count - 1) * p.pieces.size)));
     const CrossPlan cross = plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, V), kNoLimit);
     p.whole = cross.us >= 0.0 && cross.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes);
     if (p.whole) p.room_bytes = cross.room;
@@ -290,50 +328,60 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
     return p;
 }
 
-LinearArgs data_product(const Matrix &x, int C, const Pieces &p, int columns) {
+LinearArgs data_product(long long rows, int C, const Pieces &p, int columns) {
     LinearArgs a{};
     a.am = p.stride; a.ak = 1; a.bn = 1; a.bk = C; a.strided_b = true; a.padded_a = true;
-    a.M = (int)x.rows; a.N = C; a.K = columns;
+    a.M = (int)rows; a.N = C; a.K = columns;
     a.alpha = 1.f;
     a.act = IGC_ACTIVATION_IDENTITY;
     return a;
 }
-LinearArgs filter_product(const Matrix &x, int C, const Pieces &p, int columns) {
+// (few tokens: x as it was copied, once for each part of dz)
+LinearArgs filter_product(const Matrix &x, bool few, int C, const Pieces &p, int columns) {
     LinearArgs a{};
-    a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = x.stride; a.strided_a = a.strided_b = true; a.padded_a = true;
-    a.M = columns; a.N = C; a.K = (int)x.rows;
+    a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = few ? round_up(C, 8) : x.stride; a.padded_b = few; a.strided_a = a.strided_b = true; a.padded_a = true;
+    a.M = columns; a.N = C; a.K = (int)(few ? 2 * x.rows : x.rows);
     a.alpha = 1.f;
     a.act = IGC_ACTIVATION_IDENTITY;
     return a;
 }
 struct BackwardPlan {
-    bool direct;         // the tiles leave dz, no logits in memory
+    bool few, direct;    // few tokens; else whether the tiles leave dz, no logits in memory
     Pieces pieces;
-    bool sum;            // dx of several pieces is summed in floats first
-    size_t logits, dz, dx, sums, room, total, room_bytes;
+    bool sum;            // dx is summed in floats first
+    long long rows;      // of dz: two parts' of few tokens
+    size_t logits, dz, dx, x, sums, room, total, room_bytes;
 };
 // dx, dw: null where that gradient is not asked for
 BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
     BackwardPlan p;
     const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
-    p.pieces = pieces_of(x.rows, V, elem);
-    const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size), kNoLimit);
-    const Pieces wide = pieces_of(x.rows, V, 4);
-    p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit);
-    p.room_bytes = p.direct ? cross.room : 0;
-    if (!p.direct) p.pieces = wide;
-    p.sum = dx && p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16;
+    p.few = few_tokens(t, x);
+    p.rows = p.few ? 2 * x.rows : x.rows;
+    p.pieces = pieces_of(p.rows, V, elem);
+    p.direct = p.few;
+    if (!p.few) {
+        const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size), kNoLimit);
+        const Pieces wide = pieces_of(x.rows, V, 4);
+        p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit);
+        if (!p.direct) p.pieces = wide;
+    }
+    p.sum = dx && (p.few || (p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16));
     Room r;
-    p.dz = r.take((size_t)x.rows * p.pieces.stride * elem);
+    p.dz = r.take((size_t)p.rows * p.pieces.stride * elem);
     p.logits = p.direct || elem == 4 ? p.dz : r.take((size_t)x.rows * p.pieces.stride * 4);
-    p.dx = r.take(p.sum ? (size_t)x.rows * C * 4 : 0);
+    p.dx = r.take(p.sum ? (size_t)p.rows * C * 4 : 0);
+    p.x = r.take(p.few && dw ? (size_t)p.rows * round_up(C, 8) * 2 : 0);
     p.sums = r.take((size_t)((x.rows + 255) / 256 * 256 / kLeastRows) * p.pieces.stride * 4);
-    // (the last piece may be smaller, and then take other tiles)
-    for (int columns : {p.pieces.size, V - (p.pieces.count - 1) * p.pieces.size}) {
+    p.room_bytes = 0;
+    for (int piece : {0, p.pieces.count - 1}) {
+        // (the last piece may be smaller, and then take other tiles)
+        const int columns = std::min(p.pieces.size, V - piece * p.pieces.size);
         const LinearArgs logits = logits_product(x, C, p.pieces, columns);
-        p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
-        if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(x, C, p.pieces, columns)));
-        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, C, p.pieces, columns)));
+        if (!p.few) p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
+        if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns)));
+        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, p.few, C, p.pieces, columns)));
+        if (p.pieces.count == 1) break;
     }
     p.room = r.take(p.room_bytes);
     p.total = r.total;
@@ -398,7 +446,9 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
         end.parts = parts;
         end.picked = picked;
         CrossPlan taken;
-        if ((st = cross_product(handle, kRowStatistics, t, a, end, ws + p.room, p.room_bytes, &taken)) != IGC_STATUS_SUCCESS) return st;
+        taken.tileColumns = cross_few_columns(handle, V);
+        st = p.few ? cross_few(handle, kRowStatistics, a, end) : cross_product(handle, kRowStatistics, t, a, end, ws + p.room, p.room_bytes, &taken);
+        if (st != IGC_STATUS_SUCCESS) return st;
         ranges = (V + taken.tileColumns - 1) / taken.tileColumns;
     }
     for (int first = 0; first < V && !p.whole; first += p.pieces.size) {
@@ -416,6 +466,7 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
         ranges += here;
     }
     LossArgs q{parts, M, V, ranges, targets, picked, static_cast<float *>(loss), static_cast<float *>(logSum)};
+    if (M <= kRowLosses) return launch_kernel(reinterpret_cast<const void *>(&loss_row_kernel), q, dim3((unsigned)M), 1024, handle->stream);
     return launch_kernel(reinterpret_cast<const void *>(&loss_kernel), q, dim3(grid_of((M + 63) / 64)), 1024, handle->stream);
 }
 
@@ -469,7 +520,15 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             end.sums = sums;
             end.sumStride = p.pieces.stride;
             CrossPlan taken;
-            if ((st = cross_product(handle, kSlopes, t, a, end, ws + p.room, p.room_bytes, &taken)) != IGC_STATUS_SUCCESS) return st;
+            taken.sumBlocks = 1;
+            if (p.few) {
+                a.z = dw && first == 0 ? ws + p.x : nullptr;
+                a.zs = round_up(C, 8);
+                st = cross_few(handle, kSlopes, a, end);
+            } else {
+                st = cross_product(handle, kSlopes, t, a, end, ws + p.room, p.room_bytes, &taken);
+            }
+            if (st != IGC_STATUS_SUCCESS) return st;
             sum_blocks = taken.sumBlocks;
         } else {
             a.y = ws + p.logits;
@@ -486,7 +545,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             if (st != IGC_STATUS_SUCCESS) return st;
         }
         if (dx) {
-            LinearArgs d = data_product(mx, C, p.pieces, columns);
+            LinearArgs d = data_product(p.rows, C, p.pieces, columns);
             d.a = ws + p.dz;
             d.b = piece;
             d.y = p.sum ? ws + p.dx : dx;
@@ -497,9 +556,9 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             if ((st = product(handle, t, p.sum ? IGC_DATA_FLOAT : dxDesc->dtype, d, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
         }
         if (dw) {
-            LinearArgs f = filter_product(mx, C, p.pieces, columns);
+            LinearArgs f = filter_product(mx, p.few, C, p.pieces, columns);
             f.a = ws + p.dz;
-            f.b = x;
+            f.b = p.few ? ws + p.x : x;
             f.y = static_cast<uint8_t *>(dw) + (size_t)first * C * elem_size(dwDesc->dtype);
             f.ys = C;
             f.r = f.y;
@@ -509,8 +568,10 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
         }
     }
     if (dx && p.sum) {
-        RoundArgs r{reinterpret_cast<const float *>(ws + p.dx), static_cast<bf16_t *>(dx), mdx.stride, M, C, dx_beta};
-        return launch_kernel(reinterpret_cast<const void *>(&round_kernel), r, dim3(grid_of(((long long)M * ((C + 3) / 4) + 255) / 256)), 256, handle->stream);
+        const float *from = reinterpret_cast<const float *>(ws + p.dx);
+        JoinArgs j{from, p.few ? from + (long long)M * C : nullptr, dx, mdx.stride, M, C, dx_beta};
+        return launch_kernel(dxDesc->dtype == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&join_kernel<float>) : reinterpret_cast<const void *>(&join_kernel<bf16_t>), j,
+                             dim3(grid_of(((long long)M * ((C + 3) / 4) + 255) / 256)), 256, handle->stream);
     }
     return IGC_STATUS_SUCCESS;
 }

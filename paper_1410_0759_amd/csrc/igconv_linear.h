@@ -14,7 +14,7 @@ struct LinearArgs {
     const void *a, *b;
     long long am, ak, bn, bk;
     bool strided_a, strided_b;   // the reduction index runs along the rows in memory (am, bn are 1)
-    bool padded_a;               // the first operand's rows in memory may be read up to the next eighth element, where zeros lie
+    bool padded_a, padded_b;     // the operand's rows in memory may be read up to the next eighth element, where (along the reduction index) zeros lie
     int M, N, K;
     // after the product: t = alpha D + bias[n]; z[m][n] = t where z is kept; t = f(t) (forward) or t f'(zin[m][n]) (backward
     // data); y[m][n] = t + beta r[m][n]

@@ -404,7 +404,7 @@ constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kW
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room, const CrossKind *cross = nullptr) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
-    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a, a.padded_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b);
+    const OperandPlan oa = operand_plan(sa, a.M, a.K, a.am, a.ak, f32, a.a, a.padded_a), ob = operand_plan(sb, a.N, a.K, a.bn, a.bk, f32, a.b, a.padded_b);
     double &best = pl.us;
     // the product by kernel k in `splits` ranges of steps of `step`, its operands copied first or not
     auto consider = [&](const TileKernel &k, const ShapeCost &sc, int step, int splits, bool copied) {
