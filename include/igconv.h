@@ -570,7 +570,7 @@ igcStatus igcLinearBackwardFilter(igcHandle_t handle, const void *alpha,
  * igcAdamWStep: one step of AdamW over any number of tensors.  With g = gradientScale * grad and t = step:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   param = param (1 - rate weightDecay) - rate (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + epsilon)
- * in fp32 for every element, whatever its types; the update takes m and v before they are rounded.  0 <= beta < 1, epsilon > 0, step >= 1; finite numbers.
+ * in fp32 for every element, whatever its types; the update takes m and v before they are rounded.  0 <= beta < 1, epsilon >= 2^-126, step >= 1; finite numbers.
  * deviceLearningRate, deviceGradientScale, deviceStep: device pointers or NULL, read when the step runs (so that a captured one
  * can be replayed): the rate in place of learningRate, a factor beside gradientScale, the step in place of step (below 1: 1).
  *

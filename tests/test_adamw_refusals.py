@@ -24,7 +24,7 @@ def params(**more):
 def test_numbers():
     nan, inf = float("nan"), float("inf")
     for bad in (dict(beta1=1.0), dict(beta1=-0.1), dict(beta1=nan), dict(beta2=1.0), dict(beta2=-1.0), dict(beta2=nan), dict(epsilon=0.0), dict(epsilon=-1.0),
-                dict(epsilon=nan), dict(epsilon=inf), dict(epsilon=1e-60), dict(step=0), dict(step=-3), dict(learning_rate=nan), dict(learning_rate=inf),
+                dict(epsilon=nan), dict(epsilon=inf), dict(epsilon=1e-60), dict(epsilon=1e-39), dict(step=0), dict(step=-3), dict(learning_rate=nan), dict(learning_rate=inf),
                 dict(gradient_scale=nan), dict(gradient_scale=inf), dict(device_step=P + 2), dict(device_learning_rate=P + 1), dict(device_gradient_scale=P + 2)):
         assert step(params(**bad), count=0) == BAD, bad
     assert step(params(), count=0) == 0

@@ -147,6 +147,20 @@ def test_large_tensor_and_small_numbers():
     assert (x.v.numpy()[used] > 0).all()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_squares_below_the_normal_numbers(bits):
+    """A first step with gradients around 1e-19 and an epsilon below their roots: steps of the rate, whatever the gradient.  (A hundredth of the square has 16 bits left at 1e-19:
+    its root is known to 2^-16.)"""
+    u = _u()
+    import paper_1410_0759_amd as ig
+    rng = np.random.default_rng(13)
+    x = u.Tensor(rng, 1000, bits=bits, fresh=True, decay=0.0)
+    x.g.put(np.copysign(1e-19 * (1 + rng.random(1000)), rng.standard_normal(1000)), x.g.dtype)
+    p, g = x.p.numpy(), x.g.numpy()
+    ig.check(ig.adamw_step(handle(), parameters(step=1, gradient_scale=1.0, epsilon=1e-30, learning_rate=0.25), u.table([x])))
+    near(x.p.numpy(), p - 0.25 * np.sign(g), 0.25 * 2.0 ** -15 + 4 * E * (np.abs(p) + 0.25), "p")
+
+
 def test_infinite_and_undefined_gradients_stay_where_they_are():
     u = _u()
     rng = np.random.default_rng(8)
