@@ -27,8 +27,8 @@ struct StoreArgs {
 };
 
 // A workgroup takes 64 rows of a block: a lane one word of it, sixteen lanes a row, so that a group's largest is found among 4, 8 or 16 lanes
-// and 64 rows' scales of a group go out next to each other.  All in exact arithmetic: the scale is the smallest bfloat16 number not below
-// a sixth of the largest, the borders between codes are products of eight bits by three.
+// and 64 rows' scales of a group go out next to each other.  The scale is the smallest bfloat16 number not below a sixth of the largest.  (16384 x 4096 bfloat16:
+// @TO4@ us for 171 MB; with a comparison for each border between codes 77.)
 template <class T>
 __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     const int lane = threadIdx.x & 63, word = lane & 15;
@@ -69,16 +69,24 @@ __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
                 scale = __builtin_bit_cast(uint32_t, (float)want) & 0xFFFF0000u;
                 if ((double)__builtin_bit_cast(float, scale) < want) scale += 0x10000u;
             }
-            const float s = __builtin_bit_cast(float, scale);
+            // w / scale, rounded once: the inverse's product and its remainder's, which is exact.  It is a border between codes only where w is one times the scale (borders
+            // have three bits, scales eight: no other w of 24 is within half a step of that).  Below 2^-100, where inverses overflow, both are taken 2^64 times.
             uint32_t codes = 0;
             if (scale != 0) {
+                const float s = __builtin_bit_cast(float, scale), up = s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up, inverse = 1.f / su;
+                float q[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float v = __builtin_fabsf(w[i][e]);
-                    // the even code of two as near
-                    const uint32_t q = (v > 0.25f * s) + (v >= 0.75f * s) + (v > 1.25f * s) + (v >= 1.75f * s) + (v > 2.5f * s) + (v >= 3.5f * s) + (v > 5.f * s);
-                    codes |= (q | (w[i][e] < 0.f && q ? 8u : 0u)) << (4 * e);
+                    const float v = w[i][e] * up, near = v * inverse;
+                    q[e] = __builtin_fmaf(__builtin_fmaf(-near, su, v), inverse, near);
                 }
+                codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, q[0], q[1], 1.f, 0);
+                codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, q[2], q[3], 1.f, 1);
+                codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, q[4], q[5], 1.f, 2);
+                codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, q[6], q[7], 1.f, 3);
+                // (no negative zeros)
+                const uint32_t size = codes & 0x77777777u, some = (size | size >> 1 | size >> 2) & 0x11111111u;
+                codes = size | (codes & some << 3);
             }
             if (k >= p.K) continue;
             *reinterpret_cast<uint32_t *>(p.codes + k * code_row(p.C) + block * kBlockBytes + at * 4) = codes;
@@ -87,36 +95,40 @@ __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     }
 }
 
+// A workgroup takes 64 rows of a block: a lane four features, so that the lanes of a store write next to each other (16384 x 4096 into float: @FROM4@ us for 306 MB; eight
+// features to a lane, whose stores of 16 bytes lie 32 apart, 92).
 template <class T>
 __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) {
-    const int lane = threadIdx.x & 63, word = lane & 15, at = 4 * (word & 3) + (word >> 2);
+    const int four = threadIdx.x & 31;
+    // (features 4 j to 4 j + 3 of a block: half of word 4 (j / 2 % 4) + j / 8)
+    const int at = (4 * ((four >> 1) & 3) + (four >> 3)) * 4 + (four & 1) * 2;
     const int blocks = (p.C + kBlock - 1) / kBlock;
     for (long long tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
-        const int block = (int)(tile % blocks), c = block * kBlock + word * 8;
-        const long long k0 = tile / blocks * 64 + (threadIdx.x >> 4);
+        const int block = (int)(tile % blocks), c = block * kBlock + four * 4;
+        const long long k0 = tile / blocks * 64 + (threadIdx.x >> 5);
         if (c >= p.C) continue;
-        uint32_t codes[4];
-        float scale[4];
+        uint32_t codes[8];
+        float scale[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const long long k = k0 + 16 * i < p.K ? k0 + 16 * i : p.K - 1;
-            codes[i] = *reinterpret_cast<const uint32_t *>(p.codes + k * code_row(p.C) + block * kBlockBytes + at * 4);
+        for (int i = 0; i < 8; ++i) {
+            const long long k = k0 + 8 * i < p.K ? k0 + 8 * i : p.K - 1;
+            codes[i] = *reinterpret_cast<const uint16_t *>(p.codes + k * code_row(p.C) + block * kBlockBytes + at);
             scale[i] = bf16_bits_to_float(p.scales[(long long)(c / p.group) * p.K + k]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const long long k = k0 + 16 * i;
+        for (int i = 0; i < 8; ++i) {
+            const long long k = k0 + 8 * i;
             if (k >= p.K) continue;
             const bf16x8 q = widen8(codes[i]);
-            Adjacent<T, 8> v;
+            Adjacent<T, 4> v;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.v[e] = Stored<T>::narrow((float)q[e] * scale[i]);
+            for (int e = 0; e < 4; ++e) v.v[e] = Stored<T>::narrow((float)q[e] * scale[i]);
             T *to = static_cast<T *>(p.out) + k * p.C + c;
-            if (c + 8 <= p.C) {
-                *reinterpret_cast<Adjacent<T, 8> *>(to) = v;
+            if (c + 4 <= p.C) {
+                *reinterpret_cast<Adjacent<T, 4> *>(to) = v;
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 4; ++e)
                     if (c + e < p.C) to[e] = v.v[e];
             }
         }
