@@ -12,7 +12,7 @@ namespace igc {
 namespace {
 
 constexpr int kRange = 2048;                         // columns of one entry of the row statistics
-constexpr size_t kPieceBytes = (size_t)256 << 20;    // of logits (or dz) at a time
+constexpr size_t kPieceBytes = (size_t)512 << 20;    // of logits (or dz) at a time
 
 // (nothing but minus infinities: a sum of zero, and no difference of infinities)
 __device__ __forceinline__ RowPart joined(RowPart a, RowPart b) {
