@@ -501,7 +501,11 @@ struct FewPlan {
     int kb = 1, tb = 1, splits = 1, per = 0;      // per: blocks to a range
     bool lay = false;
     size_t partsAt = 0, room = 0;
+    double us = 0.0;
 };
+// us of a block of 128 features of a tile, by shape (float in parts: the last), and of a wavefront's block of few tokens, by pieces of 16.  Measured: 2048 x 4096 -> 8192 one round
+// of 256 x 256, 128 us, or two of 128 x 256, 157; 1024 x 4096 -> 2048 128 x 128, 38; 2048 x 4096 -> 8192 float four rounds, 340; 60 x 4096 -> 16384 two rounds of four blocks, 44.
+constexpr double kBlockUs[kTile4Shapes] = {2.45, 1.2, 4.0}, kPartsBlockUs = 2.66, kFewBlockUs[3] = {1.5, 2.5, 5.0}, kLaunchUs = 4.0;
 FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size_t room) {
     FewPlan p;
     const int blocks = (a.K + kBlock - 1) / kBlock;
@@ -516,8 +520,8 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
         const size_t bytes = (size_t)round_up(round_up(a.M, kPartsTokens) * 3 * round_up(a.K, 8) * 2, 256);
         if (bytes <= room) p.lay = true, p.partsAt = p.room = bytes;
     }
-    // Ranges, each of a block for every wavefront at least, where the codes are worth a second launch.
-    if (p.kb < most && (long long)a.N * code_row(a.K) >= kSplitBytes) {
+    // Ranges, each of a block for every wavefront at least, where the codes (more tokens: the products) are worth a second launch.
+    if (p.kb < most && (long long)a.N * code_row(a.K) * std::max(1ll, tm * p.tb / 2) >= kSplitBytes) {
         const int splits = (int)std::min<long long>((h->computeUnits + tiles(most) - 1) / tiles(most), (blocks + 7) / 8);
         const size_t bytes = (size_t)splits * a.M * round_up(a.N, 4) * 4;
         if (splits > 1 && p.partsAt + bytes <= room) {
@@ -527,6 +531,8 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
             p.room = p.partsAt + bytes;
         }
     }
+    const long long rounds = (tiles(p.kb) * p.splits + h->computeUnits - 1) / h->computeUnits;
+    p.us = rounds * ((p.per + 7) / 8) * kFewBlockUs[p.tb / 2] + kLaunchUs * (1 + p.lay + (p.splits > 1));
     return p;
 }
 
@@ -582,6 +588,7 @@ struct Tile4Plan {
     bool lay = false, layScales = false;       // x, the scales are laid out first, in `room` bytes
     size_t scalesAt = 0, room = 0;
     long long tilesM = 0, tilesN = 0;
+    double us = 1e300;
 };
 Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, const Linear4Args &a) {
     Tile4Plan best;
@@ -594,18 +601,15 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
     p.layScales = a.N % 2 != 0 || (uintptr_t)a.scales % 4 != 0;
     p.scalesAt = p.lay ? (size_t)round_up((parts ? round_up(a.M, kPartsTokens) * 3 : a.M) * row * 2, 256) : 0;
     p.room = p.scalesAt + (p.layScales ? (size_t)((a.K + a.group4 - 1) / a.group4) * round_up(a.N, 2) * 2 : 0);
-    double least = 1e300;
     for (int shape = 0; shape < kTile4Shapes; ++shape) {
         p.k = tile4_kernel(shape, a.group4, parts, out == IGC_DATA_FLOAT);
         if (!p.k.kernel) continue;
         p.tilesM = (a.M + p.k.bm - 1) / p.k.bm;
         p.tilesN = (a.N + p.k.bn - 1) / p.k.bn;
         if (p.tilesM * p.tilesN > kMostGroups) continue;
-        constexpr double kBlockUs[kTile4Shapes] = {2.4, 1.2, 3.2};
-        const double us = (double)((p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits) * kBlockUs[shape];
-        if (us >= least) continue;
-        least = us;
-        best = p;
+        const long long rounds = (p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits;
+        p.us = rounds * ((a.K + kBlock - 1) / kBlock) * (parts ? kPartsBlockUs : kBlockUs[shape]) + kLaunchUs * (1 + p.lay + p.layScales);
+        if (p.us < best.us) best = p;
     }
     return best;
 }
@@ -692,7 +696,8 @@ igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescrip
     if (st != IGC_STATUS_SUCCESS) return st;
     const Linear4Args a = sizes_of(x, *wDesc, group);
     const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
-    *sizeInBytes = pl.k.kernel ? pl.room : plan_few(handle, xDesc->dtype, a, ~(size_t)0).room;
+    const FewPlan few = plan_few(handle, xDesc->dtype, a, ~(size_t)0);
+    *sizeInBytes = pl.us <= few.us ? pl.room : few.room;
     return IGC_STATUS_SUCCESS;
 }
 
@@ -722,8 +727,8 @@ igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDesc
     a.scales = static_cast<const uint16_t *>(scales);
     const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
     const size_t room = workSpace && !off(workSpace, 16) ? workSpaceSizeInBytes : 0;
-    if (pl.k.kernel && pl.room <= room) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
     const FewPlan few = plan_few(handle, xDesc->dtype, a, room);
+    if (pl.room <= room && pl.us <= few.us) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
     return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_few<decltype(tx), decltype(ty)>(handle, a, few, workSpace); });
 }
 
