@@ -24,6 +24,7 @@ struct CrossEnd {
     float alpha;
     const float *logSum, *dloss;
     float *sums;                // column sums of dz over each wavefront's rows, [sumBlocks][sumStride], or null
+    bool twoParts;              // dz in two bfloat16 parts, the second as M more rows below
     long long sumStride;
 };
 struct CrossArgs : TileArgs {
@@ -45,14 +46,19 @@ struct CrossPlan {
 CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);
 igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes,
                         CrossPlan *taken);
-// The same for at most kFewTokens tokens of bfloat16 features, of any layout (igconv_cross_entropy_few.hip).  Slopes: dz in two parts, rows M to 2 M - 1 of y hold the second; x is
-// copied to z (rows zs apart, from 16-byte boundaries), twice below each other.  One block of column sums.
-constexpr int kFewTokens = 32;
+// The same for at most kFewTokens tokens of bfloat16 features, of any layout (igconv_cross_entropy_few.hip).  Slopes: dz in two parts; x is copied to z (rows zs apart, from 16-byte
+// boundaries), twice below each other.  One block of column sums.
+constexpr int kFewTokens = 16;
 int cross_few_columns(igcHandle_t handle, int N);      // of an entry of the statistics
 igcStatus cross_few(igcHandle_t handle, CrossKind kind, const LinearArgs &a, const CrossEnd &end);
 // what an ordinary product takes, in us by the same figures, with so much room
 double product_us(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, size_t room);
 
+// what v rounded to bfloat16 leaves (an infinity: nothing)
+__device__ __forceinline__ float rest_of(float v) {
+    const float high = bf16_bits_to_float(to_bf16_bits(v));
+    return high - high == 0.f ? v - high : 0.f;
+}
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896f); }
 
 }  // namespace igc

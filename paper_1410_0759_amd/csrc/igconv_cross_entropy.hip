@@ -147,6 +147,7 @@ struct SlopeArgs {
     int V;
     const float *logSum, *dloss;
     float *sums;                // [rows / kSlopeRows][stride]: column sums, or null
+    int parts;                  // dz in two parts, the second M rows below
 };
 constexpr int kSlopeRows = 32;
 
@@ -179,6 +180,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
             TZ *to = static_cast<TZ *>(a.dz) + m * a.stride + n;
             if constexpr (sizeof(TZ) == 4) *reinterpret_cast<float4 *>(to) = float4{d[0], d[1], d[2], d[3]};
             else *reinterpret_cast<uint2 *>(to) = uint2{to_bf16_pair(d[0], d[1]), to_bf16_pair(d[2], d[3])};
+            if (a.parts) *reinterpret_cast<uint2 *>(to + a.M * a.stride) = uint2{to_bf16_pair(rest_of(d[0]), rest_of(d[1])), to_bf16_pair(rest_of(d[2]), rest_of(d[3]))};
         }
         if (a.sums) *reinterpret_cast<float4 *>(a.sums + block * a.stride + n) = float4{sums[0], sums[1], sums[2], sums[3]};
     }
@@ -215,7 +217,7 @@ struct JoinArgs {
     int M, C;
     float beta;
 };
-// The sum over the pieces (few tokens: of dz's two parts) into dx.
+// The sum over the pieces and over dz's parts into dx.
 template <class TO>
 __global__ __launch_bounds__(256) void join_kernel(const JoinArgs a) {
     const int groups = (a.C + 3) / 4;
@@ -232,6 +234,23 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs a) {
                 if (a.beta != 0.f) v += a.beta * Stored<TO>::widen(*to);
                 *to = Stored<TO>::narrow(v);
             }
+    }
+}
+
+struct TwiceArgs {
+    const uint16_t *from;
+    uint16_t *to;
+    long long stride, toRow;
+    int M, C;
+};
+// x once for each part of dz, rows from 16-byte boundaries below each other
+__global__ __launch_bounds__(256) void twice_kernel(const TwiceArgs a) {
+    const long long tasks = (long long)a.M * a.toRow;
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < tasks; id += (long long)gridDim.x * 256) {
+        const long long m = id / a.toRow, c = id % a.toRow;
+        const uint16_t v = c < a.C ? a.from[m * a.stride + c] : (uint16_t)0;
+        a.to[id] = v;
+        a.to[a.M * a.toRow + id] = v;
     }
 }
 
@@ -290,7 +309,12 @@ constexpr size_t kNoLimit = ~(size_t)0;
 constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a tile's entry in the statistics and the column sums
 
 // (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
-bool few_tokens(igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens; }
+// Few enough tokens and vocabulary entries for the kernel of igconv_cross_entropy_few.hip (figures there).
+bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens && V <= 128 * h->computeUnits; }
+// Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: rounded to one, a row whose gradient is nearly all its
+// target's would be off by that number's rounding, and few rows do not average it out.  (Many do, and would pay for the second part in full.)
+constexpr int kPartsRows = 32;
+bool in_parts(igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && x.rows <= kPartsRows; }
 struct ForwardPlan {
     bool few, whole;     // few tokens; else whether the tiles leave the statistics, no logits in memory
     Pieces pieces;
@@ -300,7 +324,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
     ForwardPlan p;
     p.pieces = pieces_of(x.rows, V, 4);
-    p.few = few_tokens(t, x);
+    p.few = few_tokens(h, t, x, V);
     if (p.few) {
         p.whole = true;
         p.ranges = (V + cross_few_columns(h, V) - 1) / cross_few_columns(h, V);
@@ -336,42 +360,44 @@ LinearArgs data_product(long long rows, int C, const Pieces &p, int columns) {
     a.act = IGC_ACTIVATION_IDENTITY;
     return a;
 }
-// (few tokens: x as it was copied, once for each part of dz)
-LinearArgs filter_product(const Matrix &x, bool few, int C, const Pieces &p, int columns) {
+// (parts: x as it was copied, once for each part of dz)
+LinearArgs filter_product(const Matrix &x, bool parts, int C, const Pieces &p, int columns) {
     LinearArgs a{};
-    a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = few ? round_up(C, 8) : x.stride; a.padded_b = few; a.strided_a = a.strided_b = true; a.padded_a = true;
-    a.M = columns; a.N = C; a.K = (int)(few ? 2 * x.rows : x.rows);
+    a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = parts ? round_up(C, 8) : x.stride; a.padded_b = parts; a.strided_a = a.strided_b = true; a.padded_a = true;
+    a.M = columns; a.N = C; a.K = (int)(parts ? 2 * x.rows : x.rows);
     a.alpha = 1.f;
     a.act = IGC_ACTIVATION_IDENTITY;
     return a;
 }
 struct BackwardPlan {
     bool few, direct;    // few tokens; else whether the tiles leave dz, no logits in memory
+    bool parts;          // dz is in two parts
     Pieces pieces;
     bool sum;            // dx is summed in floats first
-    long long rows;      // of dz: two parts' of few tokens
+    long long rows;      // of dz: its parts'
     size_t logits, dz, dx, x, sums, room, total, room_bytes;
 };
 // dx, dw: null where that gradient is not asked for
 BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
     BackwardPlan p;
     const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
-    p.few = few_tokens(t, x);
-    p.rows = p.few ? 2 * x.rows : x.rows;
+    p.few = few_tokens(h, t, x, V);
+    p.parts = in_parts(t, x);
+    p.rows = p.parts ? 2 * x.rows : x.rows;
     p.pieces = pieces_of(p.rows, V, elem);
     p.direct = p.few;
     if (!p.few) {
         const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size), kNoLimit);
-        const Pieces wide = pieces_of(x.rows, V, 4);
+        const Pieces wide = pieces_of(p.rows, V, 4);
         p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit);
         if (!p.direct) p.pieces = wide;
     }
-    p.sum = dx && (p.few || (p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16));
+    p.sum = dx && (p.parts || (p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16));
     Room r;
     p.dz = r.take((size_t)p.rows * p.pieces.stride * elem);
     p.logits = p.direct || elem == 4 ? p.dz : r.take((size_t)x.rows * p.pieces.stride * 4);
     p.dx = r.take(p.sum ? (size_t)p.rows * C * 4 : 0);
-    p.x = r.take(p.few && dw ? (size_t)p.rows * round_up(C, 8) * 2 : 0);
+    p.x = r.take(p.parts && dw ? (size_t)p.rows * round_up(C, 8) * 2 : 0);
     p.sums = r.take((size_t)((x.rows + 255) / 256 * 256 / kLeastRows) * p.pieces.stride * 4);
     p.room_bytes = 0;
     for (int piece : {0, p.pieces.count - 1}) {
@@ -380,7 +406,7 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
         const LinearArgs logits = logits_product(x, C, p.pieces, columns);
         if (!p.few) p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
         if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns)));
-        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, p.few, C, p.pieces, columns)));
+        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, p.parts, C, p.pieces, columns)));
         if (p.pieces.count == 1) break;
     }
     p.room = r.take(p.room_bytes);
@@ -499,6 +525,11 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
     const float dx_beta = *static_cast<const float *>(beta), w_beta = *static_cast<const float *>(paramBeta);
     uint8_t *ws = static_cast<uint8_t *>(workSpace);
     const long long row_blocks = (M + kSlopeRows - 1) / kSlopeRows;
+    if (p.parts && !p.few && dw) {
+        TwiceArgs q{static_cast<const uint16_t *>(x), reinterpret_cast<uint16_t *>(ws + p.x), mx.stride, round_up(C, 8), M, C};
+        st = launch_kernel(reinterpret_cast<const void *>(&twice_kernel), q, dim3(grid_of((M * q.toRow + 255) / 256)), 256, handle->stream);
+        if (st != IGC_STATUS_SUCCESS) return st;
+    }
     for (int first = 0; first < V; first += p.pieces.size) {
         const int columns = std::min(p.pieces.size, V - first);
         const void *piece = static_cast<const uint8_t *>(w) + (size_t)first * C * elem_size(t);
@@ -519,6 +550,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             end.dloss = static_cast<const float *>(dloss);
             end.sums = sums;
             end.sumStride = p.pieces.stride;
+            end.twoParts = p.parts;
             CrossPlan taken;
             taken.sumBlocks = 1;
             if (p.few) {
@@ -534,7 +566,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             a.y = ws + p.logits;
             if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
             SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
-                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums};
+                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums, p.parts ? 1 : 0};
             st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
                                dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
             if (st != IGC_STATUS_SUCCESS) return st;
@@ -556,9 +588,9 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             if ((st = product(handle, t, p.sum ? IGC_DATA_FLOAT : dxDesc->dtype, d, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
         }
         if (dw) {
-            LinearArgs f = filter_product(mx, p.few, C, p.pieces, columns);
+            LinearArgs f = filter_product(mx, p.parts, C, p.pieces, columns);
             f.a = ws + p.dz;
-            f.b = p.few ? ws + p.x : x;
+            f.b = p.parts ? ws + p.x : x;
             f.y = static_cast<uint8_t *>(dw) + (size_t)first * C * elem_size(dwDesc->dtype);
             f.ys = C;
             f.r = f.y;
@@ -569,7 +601,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
     }
     if (dx && p.sum) {
         const float *from = reinterpret_cast<const float *>(ws + p.dx);
-        JoinArgs j{from, p.few ? from + (long long)M * C : nullptr, dx, mdx.stride, M, C, dx_beta};
+        JoinArgs j{from, p.parts ? from + (long long)M * C : nullptr, dx, mdx.stride, M, C, dx_beta};
         return launch_kernel(dxDesc->dtype == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&join_kernel<float>) : reinterpret_cast<const void *>(&join_kernel<bf16_t>), j,
                              dim3(grid_of(((long long)M * ((C + 3) / 4) + 255) / 256)), 256, handle->stream);
     }

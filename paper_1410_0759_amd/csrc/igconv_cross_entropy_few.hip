@@ -1,9 +1,7 @@
-// Few tokens: bfloat16 logits for cross entropy straight from registers.  A workgroup computes 16 TB tokens x 16 KB vocabulary entries; its eight wavefronts take the blocks of 128
-// features in turns, a batch of blocks requested at once, and add their sums in LDS.  The vocabulary's bytes are all there is to it: 4 x 4096 -> 32768 (268 MB) @FEW@ us
-// with the joining of the statistics; as tiles of 256 x 256 in two ranges with float logits in between 77.
-//
-// dz goes out in two bfloat16 parts, as rows of their own, of the matrix that the products take: rounded to one, a row whose gradient is nearly all its target's would be
-// off by that number's rounding, and few rows do not average it out.  (Many do, and would pay for the second part in full.)
+// Sixteen tokens at most: bfloat16 logits for cross entropy straight from registers.  A workgroup computes the tokens by 16 KB vocabulary entries; its eight wavefronts take the
+// blocks of 128 features in turns, two blocks requested at once, and add their sums in LDS.  The vocabulary's bytes are all there is to it: 8 x 8192 -> 8000 39.5 us with the
+// joining of the statistics (131 MB; as tiles of 128 x 128 77), 8 x 4096 -> 32768 64.6 (66.6).  Beyond 128 entries for each compute unit the tiles, whose loads run further
+// ahead, are the faster: 8 x 4096 -> 131072 195 us, this way 224; with more than sixteen tokens, and for float, everywhere (30 x 1024 -> 50000 27 for 43; float 58 for 97).
 #include "igconv_cross_entropy.h"
 #include "igconv_linear_tiles.hpp"
 
@@ -25,28 +23,24 @@ __device__ __forceinline__ u32x4 load8_bits(const uint16_t *from, int there) {
     return v;
 }
 
-template <int KB, int TB, bool SLOPES>
+template <int KB, bool SLOPES>
 __global__ __launch_bounds__(64 * kWaves) void cross_few_kernel(const CrossArgs p) {
-    constexpr int BATCH = TB == 1 ? 2 : 1, TOKENS = 16 * TB, COLUMNS = 16 * KB;      // (registers)
-    __shared__ f32x4 sums[kWaves][KB * TB][64];
+    constexpr int BATCH = 2, TOKENS = kFewTokens, COLUMNS = 16 * KB;
+    __shared__ f32x4 sums[kWaves][KB][64];
     __shared__ float z[TOKENS][COLUMNS + 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
     const int blocks = (p.K + kBlock - 1) / kBlock;
-    const uint16_t *token[TB];
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) token[tb] = static_cast<const uint16_t *>(p.a) + (long long)min(16 * tb + l16, p.M - 1) * p.am + 8 * g;
+    const uint16_t *token = static_cast<const uint16_t *>(p.a) + (long long)min(l16, p.M - 1) * p.am + 8 * g;
     for (int tile = blockIdx.x; tile < p.tilesN; tile += gridDim.x) {
         const int n0 = tile * COLUMNS;
         const uint16_t *row[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) row[kb] = static_cast<const uint16_t *>(p.b) + (long long)min(n0 + 16 * kb + l16, p.N - 1) * p.bn + 8 * g;
-        f32x4 total[KB][TB];
+        f32x4 total[KB];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb) total[kb][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kb = 0; kb < KB; ++kb) total[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int first = wave; first < blocks; first += BATCH * kWaves) {
-            u32x4 w[BATCH][4][KB], x[BATCH][4][TB];
+            u32x4 w[BATCH][4][KB], x[BATCH][4];
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 const int s = first + b * kWaves;
@@ -57,8 +51,7 @@ __global__ __launch_bounds__(64 * kWaves) void cross_few_kernel(const CrossArgs 
                     const int c = s * kBlock + 32 * i, there = whole ? 8 : p.K - c - 8 * g;
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) w[b][i][kb] = load8_bits(row[kb] + c, there);
-#pragma unroll
-                    for (int tb = 0; tb < TB; ++tb) x[b][i][tb] = load8_bits(token[tb] + c, there);
+                    x[b][i] = load8_bits(token + c, there);
                 }
             }
 #pragma unroll
@@ -68,20 +61,16 @@ __global__ __launch_bounds__(64 * kWaves) void cross_few_kernel(const CrossArgs 
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                        for (int tb = 0; tb < TB; ++tb)
-                            total[kb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[b][i][kb]), __builtin_bit_cast(bf16x8, x[b][i][tb]), total[kb][tb], 0, 0, 0);
+                        total[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[b][i][kb]), __builtin_bit_cast(bf16x8, x[b][i]), total[kb], 0, 0, 0);
             }
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-                if (16 * tb + l16 < p.M) sums[wave][kb * TB + tb][lane] = total[kb][tb];
+            if (l16 < p.M) sums[wave][kb][lane] = total[kb];
         __syncthreads();
         // the logits, minus infinity right of the matrix
-        for (int at = threadIdx.x; at < KB * TB * 64; at += 64 * kWaves) {
-            const int block = at >> 6, l = at & 63, m = 16 * (block % TB) + (l & 15), n = 16 * (block / TB) + 4 * (l >> 4);
+        for (int at = threadIdx.x; at < KB * 64; at += 64 * kWaves) {
+            const int block = at >> 6, l = at & 63, m = l & 15, n = 16 * block + 4 * (l >> 4);
             if (m >= p.M) continue;
             f32x4 d = sums[0][block][l];
 #pragma unroll
@@ -125,8 +114,7 @@ __global__ __launch_bounds__(64 * kWaves) void cross_few_kernel(const CrossArgs 
                     if (there && t - p.end.first == n0 + n + e) v -= 1.f;
                     d[e] = there && n0 + n + e < p.N ? slope * v : 0.f;
                     z[m][n + e] = d[e];
-                    const float high = bf16_bits_to_float(to_bf16_bits(d[e]));
-                    rest[e] = high - high == 0.f ? d[e] - high : 0.f;      // (an infinity has no rest)
+                    rest[e] = rest_of(d[e]);
                 }
                 uint16_t *to = static_cast<uint16_t *>(p.y) + m * p.ys + n0 + n;
                 *reinterpret_cast<uint32_t *>(to) = to_bf16_pair(d[0], d[1]);
@@ -156,12 +144,6 @@ __global__ __launch_bounds__(64 * kWaves) void cross_few_kernel(const CrossArgs 
     }
 }
 
-template <bool SLOPES>
-const void *kernel_of(int kb, int tb) {
-    if (tb == 1) return kb == 4 ? reinterpret_cast<const void *>(&cross_few_kernel<4, 1, SLOPES>) : reinterpret_cast<const void *>(&cross_few_kernel<1, 1, SLOPES>);
-    return kb == 4 ? reinterpret_cast<const void *>(&cross_few_kernel<4, 2, SLOPES>) : reinterpret_cast<const void *>(&cross_few_kernel<1, 2, SLOPES>);
-}
-
 }  // namespace
 
 int cross_few_columns(igcHandle_t handle, int N) { return N >= 64 * handle->computeUnits / 2 ? 64 : 16; }
@@ -170,10 +152,12 @@ igcStatus cross_few(igcHandle_t handle, CrossKind kind, const LinearArgs &a, con
     CrossArgs t{};
     static_cast<LinearArgs &>(t) = a;
     t.end = end;
-    const int columns = cross_few_columns(handle, a.N), tb = a.M <= 16 ? 1 : 2;
+    const int columns = cross_few_columns(handle, a.N);
     t.tilesM = 1;
     t.tilesN = (a.N + columns - 1) / columns;
-    return launch_kernel(kind == kSlopes ? kernel_of<true>(columns / 16, tb) : kernel_of<false>(columns / 16, tb), t, dim3((unsigned)std::min(t.tilesN, 1 << 20)), 64 * kWaves, handle->stream);
+    const void *const kernels[2][2] = {{reinterpret_cast<const void *>(&cross_few_kernel<1, false>), reinterpret_cast<const void *>(&cross_few_kernel<4, false>)},
+                                       {reinterpret_cast<const void *>(&cross_few_kernel<1, true>), reinterpret_cast<const void *>(&cross_few_kernel<4, true>)}};
+    return launch_kernel(kernels[kind == kSlopes][columns == 64], t, dim3((unsigned)std::min(t.tilesN, 1 << 20)), 64 * kWaves, handle->stream);
 }
 
 }  // namespace igc

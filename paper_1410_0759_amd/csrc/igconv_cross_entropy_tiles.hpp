@@ -124,7 +124,20 @@ struct TileEnd<Cfg, Slopes<TZ>, CrossArgs> {
         q.act = IGC_ACTIVATION_IDENTITY;
         q.splits = 1;
         q.N = (p.N + 7) / 8 * 8;
-        write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TZ>(q, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0, n0, acc);
+        uint8_t *share = lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES);
+        write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TZ>(q, share, lane, split, m0, n0, acc);
+        if constexpr (sizeof(TZ) == 2) {
+            if (p.end.twoParts) {
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = rest_of(acc[i][j][e]);
+                q.y = static_cast<TZ *>(q.y) + q.M * q.ys;
+                write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TZ>(q, share, lane, split, m0, n0, acc);
+            }
+        }
     }
 };
 

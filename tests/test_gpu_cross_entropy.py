@@ -3,7 +3,7 @@
 Tolerances.  e = 2^-24.  A logit: a sum of C products and the bias, (C + 4) e of the products' magnitudes (float: products in three bfloat16 parts leave out 2^-21 +
 2^-30 of each), and e (|z| + |bias|).  exp(d) is off by 2 e |d| + 4 e of itself; a logarithm of a sum by the logits' errors at most, by the average of the exponentials'
 and by its additions, no chain of which has more than 300; then half a step.  dz: its exponential's error and, of the logits' and logarithms', e^error - 1 of it; 4 e of the
-terms; rounded to bfloat16 half a step (2^-8) of it.  A product of n terms with dz: dz's errors and (n + 8) e (float: and 2^-21 + 2^-30) of the terms, half a step
+terms; rounded to bfloat16 half a step (2^-8) of it (at most 32 rows: in two parts, 2^-16).  A product of n terms with dz: dz's errors and (n + 8) e (float: and 2^-21 + 2^-30) of the terms, half a step
 of the result, and of the sum over the pieces e for each piece."""
 import pytest
 
@@ -130,7 +130,7 @@ class Case:
         size = torch.where(there, abs(alpha) * d.abs()[:, None] * torch.exp(z - s[:, None]), 0.0)
         tdz = size * (torch.expm1(tz) + 2 * E * (z - s[:, None]).abs() + 8 * E) + 8 * E * dz.abs()
         tsum = tdz.sum(0) + (self.M + 8) * E * dz.abs().sum(0)
-        half = HALF[self.dtype] if self.dtype == "bf16" else 0.0
+        half = 0.0 if self.dtype == "f32" else (2.0 ** -16 if self.M <= 32 else HALF["bf16"])
         tdz = tdz + half * (dz.abs() + tdz)
         x, w = self.X.view.double(), self.w.double()
         what = str((self.M, self.C, self.V, self.dtype, self.layout, dx, dw, alpha, beta, pbeta))
@@ -197,6 +197,24 @@ def test_large_tiles(dtype):
     Case(1100, 520, 6000, dtype).check_backward(dtype, dtype)
     Case(4, 1024, 70000, dtype).check_forward()
     Case(4, 1024, 70000, dtype).check_backward(dtype, dtype)
+
+
+@pytest.mark.parametrize("types", [("bf16", "bf16", "bf16"), ("bf16", "f32", "f32"), ("f32", "f32", "f32")], ids="-".join)
+def test_few_tokens(types):
+    """One and two pieces of sixteen tokens, short and long rows, vocabularies of few and of many entries; thirty-three tokens."""
+    dtype, dx, dw = types
+    for i, (M, C, V) in enumerate([(1, 4100, 700), (9, 136, 40000), (17, 96, 9000), (32, 130, 515), (20, 1027, 20011), (16, 2048, 8192), (3, 129, 8193), (30, 80, 40001), (33, 96, 9000)]):
+        print("few tokens", types, M, C, V, flush=True)
+        c = Case(M, C, V, dtype, LAYOUTS[i % 4], bias=i % 2 == 0)
+        c.check_forward()
+        c.check_backward(dx, dw, beta=(0.0, 1.0)[i % 2], pbeta=(0.0, 1.0, -0.5)[i % 3], alpha=1.0 if i % 3 else 2.0)
+    # nearly all of a row's gradient is its target's: two parts hold it to 2^-16
+    if dtype == "bf16":
+        c = Case(1, 64, 50, "bf16", lost=0.0)
+        got = c.backward("f32", "f32", dbias=False)
+        dz = co.slopes(c.exact()[2], c.log_sum.double(), c.t, c.dloss.double())
+        for name, want in (("dx", dz @ c.w.double()), ("dw", dz.t() @ c.X.view.double())):
+            assert float((got[name][0] - want).norm() / want.norm()) < 2.0 ** -15, name
 
 
 def test_large_logits_and_entries_taken_out():
