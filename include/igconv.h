@@ -620,11 +620,12 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
  *   dz = alpha * dloss * (exp(z - logSum) - [v is the target]), 0 in a row without target,
  *   dx = dz w + beta * dx,   dw = dz^T x + paramBeta * dw,   dbias = column sums of dz + paramBeta * dbias
  * dx: M rows of C, dw: filter V x C x 1 x 1, each float or, for bfloat16 x, bfloat16 too; dbias: V packed floats.  Each may be NULL (its descriptor too): not computed.
- * For bfloat16 x, dz is rounded to bfloat16 in front of the two products, as their operand (dbias sums it before); the sums over
- * pieces of the vocabulary are held in floats.  A row without target adds zeros times its x to dw: that x has to be finite.
+ * For bfloat16 x, dz goes into the two products in bfloat16: rounded once, or, up to 32 rows, as its rounding and what that left off,
+ * rounded too (dbias sums it before); the sums over pieces of the vocabulary are held in floats.  A row without target adds zeros times its x to dw: that x has to be finite.
  *
- * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports, about 256 MB to 1 GB for
- * long batches; less is BAD_PARAM.  Sums in a fixed order: results repeat bit by bit. */
+ * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports; less is BAD_PARAM.  For 8192
+ * rows, 4096 features and 131072 entries that is 64 MB forward and 670 MB backward, as floats (copies of the operands in parts) 3.3 and 1.7 GB.
+ * Float products are off as igcLinearForward's.  No output may overlap an input or another output.  Sums in a fixed order: results repeat bit by bit. */
 igcStatus igcGetLinearCrossEntropyBackwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
                                                         igcFilterDescriptor_t wDesc, igcTensorDescriptor_t dxDesc,
                                                         igcFilterDescriptor_t dwDesc, size_t *sizeInBytes);
@@ -653,7 +654,7 @@ igcStatus igcDequantizeFilter4(igcHandle_t handle, int group, const void *codes,
  * as igcLinearForward has it: x M rows of C, y and r M rows of K.  x bfloat16 with y bfloat16 or float, or both float; of wDesc the sizes count (its type:
  * float or bfloat16).  The weights are not rounded on the way: products with q are exact, a group's sum is multiplied by its scale in
  * fp32 (sums of x q have to stay within float's range).  workSpace (device, 16-byte aligned, contents mean nothing): the query's bytes make long
- * prompts fast; any size will do, NULL too. */
+ * prompts fast; any size will do, NULL too (the order of sums, hence their last bits, may depend on it). */
 igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
                                             igcFilterDescriptor_t wDesc, int group,
                                             igcTensorDescriptor_t yDesc, size_t *sizeInBytes);

@@ -134,7 +134,7 @@ __global__ __launch_bounds__(1024) void loss_row_kernel(const LossArgs a) {
         finish_loss(a, m, mine);
     }
 }
-constexpr int kRowLosses = 256;      // rows up to which each has a workgroup of its own (4 rows of 512 ranges: @ROWLOSS@ us, 64 rows to a workgroup 4.6)
+constexpr int kRowLosses = 1024;     // rows up to which each has a workgroup of its own (1024 ranges, 8, 300, 1000 and 2000 rows: 5.3, 7.6, 14.4 and 23.6 us, with 64 rows to a workgroup 26)
 
 // ---- backward -----------------------------------------------------------------------------------------------------------
 struct SlopeArgs {

@@ -28,7 +28,7 @@ struct StoreArgs {
 
 // A workgroup takes 64 rows of a block: a lane one word of it, sixteen lanes a row, so that a group's largest is found among 4, 8 or 16 lanes
 // and 64 rows' scales of a group go out next to each other.  The scale is the smallest bfloat16 number not below a sixth of the largest.  (16384 x 4096 bfloat16:
-// @TO4@ us for 171 MB; with a comparison for each border between codes 77.)
+// 55 to 63 us for 171 MB; with a comparison for each border between codes 77.)
 template <class T>
 __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     const int lane = threadIdx.x & 63, word = lane & 15;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     }
 }
 
-// A workgroup takes 64 rows of a block: a lane four features, so that the lanes of a store write next to each other (16384 x 4096 into float: @FROM4@ us for 306 MB; eight
+// A workgroup takes 64 rows of a block: a lane four features, so that the lanes of a store write next to each other (16384 x 4096 into float: 72 us for 306 MB; eight
 // features to a lane, whose stores of 16 bytes lie 32 apart, 92).
 template <class T>
 __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) {
@@ -249,7 +249,7 @@ __device__ __forceinline__ void finish_sums(const Linear4Args &p, f32x4 (&sums)[
 }
 
 // Sixteen tokens: everything that a wavefront needs for BATCH blocks is requested at once - at 4096 features that is all it needs - because each trip to memory that waits for
-// another shows (1 x 4096 -> 16384, groups of 128: 14.3 us block after block, 15.7 with the next block under way, @FEW@ this way).
+// another shows (1 x 4096 -> 16384, groups of 128: 14.3 us block after block, 15.7 with the next block under way, 11.4 to 12.2 this way).
 template <int KB, int GROUP, class TX, class TO>
 __global__ __launch_bounds__(512) void linear4_few_kernel(const Linear4Args p) {
     constexpr int WAVES = 8, N = Features<TX>::PARTS, SCALES = kBlock / GROUP, IN_GROUP = GROUP / 32;
