@@ -22,9 +22,11 @@ def hashed(x):
     return x ^ (x >> np.uint64(16))
 
 
-def random_bits(n, seed, t):
-    """16 bits for each element of m, and of v."""
-    r = hashed(np.arange(n, dtype=np.uint64) ^ hashed(np.uint64(seed) ^ hashed(np.uint64(t))))
+def random_bits(n, seed, t, first=0):
+    """16 bits for each element of m, and of v, from the element `first` on."""
+    i = np.arange(first, first + n, dtype=np.uint64)
+    i = (i & np.uint64(0xFFFFFFFF)) ^ (((i >> np.uint64(32)) * np.uint64(0x9E3779B9)) & np.uint64(0xFFFFFFFF))
+    r = hashed(i ^ hashed(np.uint64(seed) ^ hashed(np.uint64(t))))
     return (r & np.uint64(0xFFFF)).astype(np.float64), (r >> np.uint64(16)).astype(np.float64)
 
 

@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWArgs a) {
     if (a.deviceRate) c.rate = *a.deviceRate;
     if (a.deviceScale) c.scale *= *a.deviceScale;
     if (a.deviceStep) {
-        step = *a.deviceStep;
+        step = max(1, *a.deviceStep);
         c.correct1 = correction(a.beta1, step);
         c.correct2 = correction(a.beta2, step);
     }
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWArgs a) {
 }
 
 bool off(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
-bool is_number(double v) { return v - v == 0.0; }
+bool is_number(double v) { return (float)v - (float)v == 0.f; }    // (as a float)
 
 igcStatus check_tensor(const igcAdamWTensor &t) {
     if (t.count < 0 || !is_number(t.weightDecay)) return IGC_STATUS_BAD_PARAM;

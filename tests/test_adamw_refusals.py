@@ -67,3 +67,9 @@ def test_arguments():
         raise AssertionError("an unknown name was taken")
     except AttributeError:
         pass
+
+
+def test_numbers_beyond_floats():
+    for bad in (dict(learning_rate=1e39), dict(gradient_scale=-1e39), dict(epsilon=1e39)):
+        assert step(params(**bad), count=0) == BAD, bad
+    assert step(weight_decay=1e39) == BAD

@@ -120,7 +120,8 @@ class Case:
             got["dbias"] = (DB[:self.V].double(), out["dbias"].double())
         return got
 
-    def check_backward(self, dx="bf16", dw="bf16", dbias=True, alpha=1.0, beta=0.0, pbeta=0.0, ones=False, pieces=1):
+    def check_backward(self, dx="bf16", dw="bf16", dbias=True, alpha=1.0, beta=0.0, pbeta=0.0, ones=False, pieces=1, entries=slice(None)):
+        """entries: of the vocabulary, where dw is looked at"""
         got = self.backward(dx, dw, dbias, alpha, beta, pbeta, ones)
         _, _, z, tz = self.exact()
         s = self.log_sum.double()
@@ -142,14 +143,16 @@ class Case:
                 tol = tol + 4 * E * (scale * old).abs()
             near(have, want, tol + HALF[out] * (want.abs() + tol) + 1e-37, name + " " + what)
 
+        if dbias:
+            check("dbias", dz.sum(0), tsum, pbeta, "f32")
         if dx:
             sizes = (dz.abs() + tdz) @ w.abs()
             check("dx", dz @ w, tdz @ w.abs() + ((self.V + 8 + 2 * pieces) * E + PART[self.dtype]) * sizes, beta, dx)
         if dw:
+            dz, tdz = dz[:, entries], tdz[:, entries]
             sizes = (dz.abs() + tdz).t() @ x.abs()
+            got["dw"] = tuple(v[entries] for v in got["dw"])
             check("dw", dz.t() @ x, tdz.t() @ x.abs() + ((self.M + 8) * E + PART[self.dtype]) * sizes, pbeta, dw)
-        if dbias:
-            check("dbias", dz.sum(0), tsum, pbeta, "f32")
 
 
 LAYOUTS = [(0, 0), (3, 1), (8, 8), (1, 0)]
@@ -336,3 +339,49 @@ def test_in_a_graph_and_on_another_stream(M):
         call(d)
     other.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(d[:5], b[:5]))
+
+
+def test_vocabulary_beyond_32_bits():
+    """w of 2.2e9 elements, 4.4 GB: its last entries lie behind 2^32 bytes, those of dw too."""
+    for M in (3, 40):
+        print("far vocabulary", M, flush=True)
+        case = Case(M, 8200, 270001, "bf16", seed=31)
+        case.t[0] = case.V - 1
+        case.check_forward()
+        entries = torch.cat([torch.arange(300), torch.arange(262000, 262300), torch.arange(case.V - 300, case.V)]).cuda()
+        case.check_backward(pieces=8, entries=entries)
+        del case
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_beyond_32_bits(dtype):
+    """Rows of x and dx 2^25 elements apart."""
+    u, ig = _u(), _u().ig
+    for M in (70, 130):
+        print("far rows", dtype, M, flush=True)
+        case = Case(M, 72, 500, dtype)
+        apart = 2 ** 25
+
+        class Far(u.Rows):
+            def __init__(self, shape, dtype, *layout):
+                self.buf = torch.empty(M * apart, dtype=u.DTYPES[dtype], device="cuda").view(M, apart)
+                self.buf[:, 72:80] = u.GUARD
+                self.view = self.buf[:, :72]
+                self.desc = ig.TensorDescriptor().set({"f32": ig.IGC_DATA_FLOAT, "bf16": ig.IGC_DATA_BFLOAT16}[dtype], M, 72, 1, 1, (apart, 1, 1, 1))
+
+            def numpy(self):
+                assert bool((self.buf[:, 72:80] == u.GUARD).all())
+                return self.view.double().cpu().numpy()
+
+        far = Far(None, dtype)
+        far.view.copy_(case.X.view)
+        case.X = far
+        case.check_forward()
+        keep, u.Rows = u.Rows, Far
+        try:
+            case.check_backward(dx=dtype, dw=dtype)
+        finally:
+            u.Rows = keep
+        del case, far
+        torch.cuda.empty_cache()

@@ -237,3 +237,76 @@ def test_repeats_in_a_graph_and_on_another_stream():
         call(z, b, other)
         other.synchronize()
         assert torch.equal(y, z)
+
+
+def test_codes_beyond_32_bits():
+    """A filter of 4.6 GB in four bits, whose last rows lie behind 2^32 bytes, and of 18 GB as bfloat16: codes, numbers, and products with one token to many."""
+    import torch
+    u, ig = _u(), _u().ig
+    K, C, group, some = 140001, 65536 + 40, 128, 24
+    rng = np.random.default_rng(21)
+    rows = np.concatenate([np.arange(some), np.arange(K - some, K)])
+    w = held(rng.standard_normal((2 * some, C)), "bf16")
+    W = torch.zeros(K, C, dtype=torch.bfloat16, device="cuda")
+    W[torch.from_numpy(rows).cuda()] = on_gpu(w, torch.bfloat16)
+    fd, h = u.filter_desc("bf16", K, C), u.handle()
+    cb, sb = ig.get_filter4_size(fd, group)
+    assert cb > 2 ** 32
+    codes, scales = (torch.full((b,), 0xA5, dtype=torch.uint8, device="cuda") for b in (cb, sb))
+    ig.check(ig.quantize_filter4(h, fd, W.data_ptr(), group, codes.data_ptr(), scales.data_ptr()))
+    wc, ws = qo.quantize(w, group)
+    at = torch.from_numpy(rows).cuda()
+    assert np.array_equal(codes.view(K, -1)[at].cpu().numpy(), qo.pack(wc))
+    assert np.array_equal(scales.view(torch.bfloat16).view(-1, K)[:, at].double().cpu().numpy(), ws)
+    assert not bool(codes.view(K, -1)[some:K - some].any())
+    W.fill_(7.0)
+    ig.check(ig.dequantize_filter4(h, group, codes.data_ptr(), scales.data_ptr(), fd, W.data_ptr()))
+    values = qo.values(wc, ws, group)
+    assert np.array_equal(W[at].double().cpu().numpy(), held(values, "bf16")) and not bool(W[some:K - some].any())
+    del W
+    for M in (1, 20, 300):
+        print("far codes", M, flush=True)
+        x = held(rng.standard_normal((M, C)), "bf16")
+        X = on_gpu(x, torch.bfloat16)
+        Y = torch.full((M, K), float("nan"), device="cuda")
+        xd, yd = ig.TensorDescriptor().set(ig.IGC_DATA_BFLOAT16, M, C, 1, 1, (C, 1, 1, 1)), ig.TensorDescriptor().set(ig.IGC_DATA_FLOAT, M, K, 1, 1, (K, 1, 1, 1))
+        space = u.Workspace(ig.get_linear4_forward_workspace_size(h, xd, fd, group, yd))
+        ig.check(ig.linear4_forward(h, 1.0, xd, X.data_ptr(), fd, group, codes.data_ptr(), scales.data_ptr(), space.buf.data_ptr(), space.size, 0, -1, 0.0, None, 0, yd,
+                                    Y.data_ptr()))
+        space.check()
+        want = x @ values.T
+        tol = (C + 2 * len(ws) + 20) * E * (np.abs(x) @ np.abs(values).T)
+        u.close(Y[:, at].double().cpu().numpy(), want, tol + E * (np.abs(want) + tol), "y of far codes, %d tokens" % M)
+        assert not bool(Y[:, some:K - some].any())
+    del codes, scales, Y, X
+    torch.cuda.empty_cache()
+
+
+def test_rows_beyond_32_bits():
+    """Rows of x and y 2^25 elements apart: the last ones lie behind 2^32 bytes."""
+    import torch
+    u, ig = _u(), _u().ig
+    C, K, group, apart = 200, 90, 64, 2 ** 25
+    for types in TYPES:
+        for M in (70, 130):
+            print("far rows", types, M, flush=True)
+            rng = np.random.default_rng(M)
+            wc, ws = qo.quantize(held(rng.standard_normal((K, C)) / 14, "bf16"), group)
+            w = qo.values(wc, ws, group)
+            x = held(rng.standard_normal((M, C)), types[0])
+            X = torch.empty(M * apart, dtype=u.DTYPES[types[0]], device="cuda").view(M, apart)
+            X[:, :C] = on_gpu(x, u.DTYPES[types[0]])
+            Y = torch.empty(M * apart, dtype=u.DTYPES[types[1]], device="cuda").view(M, apart)
+            Y[:, :K + 8] = float("nan")
+            data = {"f32": ig.IGC_DATA_FLOAT, "bf16": ig.IGC_DATA_BFLOAT16}
+            xd, yd = ig.TensorDescriptor().set(data[types[0]], M, C, 1, 1, (apart, 1, 1, 1)), ig.TensorDescriptor().set(data[types[1]], M, K, 1, 1, (apart, 1, 1, 1))
+            codes, scales, h, fd = on_gpu(qo.pack(wc)), on_gpu(ws, torch.bfloat16), u.handle(), u.filter_desc("bf16", K, C)
+            space = u.Workspace(ig.get_linear4_forward_workspace_size(h, xd, fd, group, yd))
+            ig.check(ig.linear4_forward(h, 1.0, xd, X.data_ptr(), fd, group, codes.data_ptr(), scales.data_ptr(), space.buf.data_ptr(), space.size, 0, -1, 0.0, None, 0, yd,
+                                        Y.data_ptr()))
+            want = x @ w.T
+            tol = ((3 if types[0] == "f32" else 1) * C + 2 * len(ws) + 20) * E * (np.abs(x) @ np.abs(w).T)
+            u.close(Y[:, :K].double().cpu().numpy(), want, tol + u.HALF_STEP[types[1]] * (np.abs(want) + tol), "y of far rows %s" % ((types, M),))
+            assert bool(Y[:, K:K + 8].isnan().all())
+            del X, Y
+            torch.cuda.empty_cache()
