@@ -653,8 +653,8 @@ igcStatus igcDequantizeFilter4(igcHandle_t handle, int group, const void *codes,
 /* Matrix product with such a filter:  y = f(alpha * x W^T + bias) + beta * r
  * as igcLinearForward has it: x M rows of C, y and r M rows of K.  x bfloat16 with y bfloat16 or float, or both float; of wDesc the sizes count (its type:
  * float or bfloat16).  The weights are not rounded on the way: products with q are exact, a group's sum is multiplied by its scale in
- * fp32 (sums of x q have to stay within float's range).  workSpace (device, 16-byte aligned, contents mean nothing): the query's bytes make long
- * prompts fast; any size will do, NULL too (the order of sums, hence their last bits, may depend on it). */
+ * fp32 (sums of x q have to stay within float's range).  workSpace (device, 16-byte aligned, contents mean nothing): the query's bytes make
+ * calls of more than a few tokens and of long rows fast; any size will do, NULL too (the order of sums, hence their last bits, may depend on it). */
 igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc,
                                             igcFilterDescriptor_t wDesc, int group,
                                             igcTensorDescriptor_t yDesc, size_t *sizeInBytes);

@@ -134,7 +134,9 @@ __global__ __launch_bounds__(1024) void loss_row_kernel(const LossArgs a) {
         finish_loss(a, m, mine);
     }
 }
-constexpr int kRowLosses = 1024;     // rows up to which each has a workgroup of its own (1024 ranges, 8, 300, 1000 and 2000 rows: 5.3, 7.6, 14.4 and 23.6 us, with 64 rows to a workgroup 26)
+// Rows up to which each has a workgroup of its own (1024 ranges, 8, 300, 1000 and 2000 rows: 5.3, 7.6, 14.4 and 23.6 us, with 64 rows to a workgroup 26; 40 ranges, 1023
+// rows: 7.3 and 4.9).
+constexpr int kRowLosses = 1024, kFewRowLosses = 256, kManyRanges = 256;
 
 // ---- backward -----------------------------------------------------------------------------------------------------------
 struct SlopeArgs {
@@ -492,7 +494,7 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
         ranges += here;
     }
     LossArgs q{parts, M, V, ranges, targets, picked, static_cast<float *>(loss), static_cast<float *>(logSum)};
-    if (M <= kRowLosses) return launch_kernel(reinterpret_cast<const void *>(&loss_row_kernel), q, dim3((unsigned)M), 1024, handle->stream);
+    if (M <= kRowLosses && (M <= kFewRowLosses || ranges >= kManyRanges)) return launch_kernel(reinterpret_cast<const void *>(&loss_row_kernel), q, dim3((unsigned)M), 1024, handle->stream);
     return launch_kernel(reinterpret_cast<const void *>(&loss_kernel), q, dim3(grid_of((M + 63) / 64)), 1024, handle->stream);
 }
 

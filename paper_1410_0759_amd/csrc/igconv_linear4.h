@@ -15,9 +15,9 @@ struct Linear4Args : TileArgs {      // a: x; M tokens, N rows of W, K features
     long long scaleRow;   // elements from one group's scales to the next
 };
 
-// Tiles for long prompts (igconv_linear4_tiles.hpp): x bfloat16 in rows that the tiles take, or (parts) three bfloat16 parts of float x, laid out for them.
+// Tiles for more than a few tokens (igconv_linear4_tiles.hpp), shape 3 64 x 128 for the fewer of them: x bfloat16 in rows that the tiles take, or (parts) three bfloat16 parts of float x, laid out for them.
 // Scales on 4-byte boundaries, scaleRow even.
-constexpr int kTile4Shapes = 3, kPartsTokens = 64;      // tokens of a tile of the parts
+constexpr int kTile4Shapes = 4, kPartsTokens = 64;      // tokens of a tile of the parts
 TileKernel tile4_kernel(int shape, int group, bool parts, bool f32_out);
 
 using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));

@@ -143,6 +143,7 @@ template <> struct Features<bf16_t> {
     u32x4 v;
     __device__ __forceinline__ void load(const bf16_t *from, long long = 0) { v = __builtin_bit_cast(u32x4, *reinterpret_cast<const Adjacent<bf16_t, 8> *>(from)); }
     __device__ __forceinline__ void load_some(const bf16_t *from, int there, long long = 0) {
+        if (there >= 8) return load(from);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t lo = 0, hi = 0;
@@ -162,6 +163,7 @@ template <> struct Features<float> {
         for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = q.v[e];
     }
     __device__ __forceinline__ void load_some(const float *from, int there, long long = 0) {
+        if (there >= 8) return load(from);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             v[e / 4][e % 4] = 0.f;
@@ -470,7 +472,6 @@ igcStatus check_product(igcTensorDescriptor_t x, igcFilterDescriptor_t w, int gr
     return IGC_STATUS_SUCCESS;
 }
 
-constexpr long long kSplitBytes = 4ll << 20;   // of codes
 constexpr long long kMostGroups = 1ll << 21;   // workgroups of a launch (times 1024 threads: a 32-bit number); more tiles are taken in turns
 
 template <class F>
@@ -503,9 +504,14 @@ struct FewPlan {
     size_t partsAt = 0, room = 0;
     double us = 0.0;
 };
-// us of a block of 128 features of a tile, by shape (float in parts: the last), and of a wavefront's block of few tokens, by pieces of 16.  Measured: 2048 x 4096 -> 8192 one round
-// of 256 x 256, 128 us, or two of 128 x 256, 157; 1024 x 4096 -> 2048 128 x 128, 38; 2048 x 4096 -> 8192 float four rounds, 340; 60 x 4096 -> 16384 two rounds of four blocks, 44.
-constexpr double kBlockUs[kTile4Shapes] = {2.45, 1.2, 4.0}, kPartsBlockUs = 2.66, kFewBlockUs[3] = {1.5, 2.5, 5.0}, kLaunchUs = 4.0;
+// us, measured, for the choice between kernels.  Of a block of 128 features: by the shape of a tile (of 64 x 128 one on a compute unit and two; float in parts: 64 x 256 and
+// 64 x 128), at groups of 64; of 17 to 32 and more tokens in the few-token kernels, a block to each wavefront (kCrooked: bfloat16 rows off 16-byte boundaries); of a launch and a
+// tile's start; bytes per us of ranges' sums that are stored and read.  2048 x 4096 -> 8192 one round of 256 x 256, 128 us, or two of 128 x 256, 157; 64 x 4096 -> 16384, groups of
+// 128: 64 x 128 in one, two, four and eight ranges 27.7, 23.1, 23.8 and 31.5 us, 128 x 128 39.5, 29.1, 35.7 and 46.8, few-token kernel 44.8; 64 x 1024 -> 2048 tiles 9.5, few-token
+// kernel 7.4; float 64 x 4096 -> 10880 and the like 33 and 107; 100 x 5001 -> 2003 20 and 36.
+constexpr double kBlockUs[kTile4Shapes] = {2.45, 1.2, 4.0, 0.8}, kTwoBlocksUs = 1.45, kPartsBlockUs[kTile4Shapes] = {2.1, 0.0, 0.0, 1.35}, kFewBlockUs[3] = {0.0, 2.5, 4.6},
+                 kFewPartsBlockUs[3] = {0.0, 4.5, 11.5}, kCrooked = 1.7, kLaunchUs = 3.5, kStartUs = 1.5, kSumBytes = 6e6;
+double sums_us(long long splits, const Linear4Args &a) { return splits > 1 ? kLaunchUs + (double)splits * a.M * a.N * 8 / kSumBytes : 0.0; }
 FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size_t room) {
     FewPlan p;
     const int blocks = (a.K + kBlock - 1) / kBlock;
@@ -520,19 +526,35 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
         const size_t bytes = (size_t)round_up(round_up(a.M, kPartsTokens) * 3 * round_up(a.K, 8) * 2, 256);
         if (bytes <= room) p.lay = true, p.partsAt = p.room = bytes;
     }
-    // Ranges, each of a block for every wavefront at least, where the codes (more tokens: the products) are worth a second launch.
-    if (p.kb < most && (long long)a.N * code_row(a.K) * std::max(1ll, tm * p.tb / 2) >= kSplitBytes) {
-        const int splits = (int)std::min<long long>((h->computeUnits + tiles(most) - 1) / tiles(most), (blocks + 7) / 8);
+    const bool parts = in == IGC_DATA_FLOAT;
+    const bool crooked = !parts && (a.K % 8 != 0 || a.am % 8 != 0), small = a.group4 == 32;
+    // a block: of sixteen tokens by rows of W and tokens (1 x 4096 -> 4096, groups of 128: 16 rows and no ranges 5.8 us, 64 rows and four ranges 8.9; 16 x 16000 -> 333 one and
+    // twelve ranges 17 and 10), of more by its shape
+    auto block_us = [&](int kb) {
+        if (p.tb > 1) return (parts ? kFewPartsBlockUs : kFewBlockUs)[p.tb / 2] * (crooked ? kCrooked : 1.0);
+        const double tokens = a.M * (crooked ? 0.15 : 0.045) + (crooked && small ? 0.9 : 0.0);
+        return tokens + (parts ? (small ? 1.05 + 0.85 * kb : 1.2 + 0.6 * kb) : (small ? 0.35 + 0.65 * kb : 0.35 + 0.4 * kb));
+    };
+    auto cost = [&](const FewPlan &q) {
+        const long long rounds = (tiles(q.kb) * q.splits + h->computeUnits - 1) / h->computeUnits;
+        return rounds * ((q.per + 7) / 8) * block_us(q.kb) + kLaunchUs * (1 + q.lay) + sums_us(q.splits, a);
+    };
+    p.us = cost(p);
+    // Ranges, each of a block for every wavefront at least, where they cost less with the second launch.
+    if (p.kb < most) {
+        // (of more than sixteen tokens a workgroup fills a compute unit: 64 x 5001 -> 2003 bfloat16 in 5 ranges 32 us, in 4 23; fewer tokens have two beside each other: float
+        // 4096 -> 10880 and the like 22 us, in one range less 25)
+        const long long fit = parts && p.tb == 1 ? (h->computeUnits + tiles(most) - 1) / tiles(most) : std::max(1ll, h->computeUnits / tiles(most));
+        const int splits = (int)std::min<long long>(fit, (blocks + 7) / 8);
         const size_t bytes = (size_t)splits * a.M * round_up(a.N, 4) * 4;
-        if (splits > 1 && p.partsAt + bytes <= room) {
-            p.kb = most;
-            p.per = (blocks + splits - 1) / splits;
-            p.splits = (blocks + p.per - 1) / p.per;
-            p.room = p.partsAt + bytes;
-        }
+        FewPlan q = p;
+        q.kb = most;
+        q.per = (blocks + splits - 1) / splits;
+        q.splits = (blocks + q.per - 1) / q.per;
+        q.room = p.partsAt + bytes;
+        q.us = cost(q);
+        if (splits > 1 && q.room <= room && q.us < p.us) return q;
     }
-    const long long rounds = (tiles(p.kb) * p.splits + h->computeUnits - 1) / h->computeUnits;
-    p.us = rounds * ((p.per + 7) / 8) * kFewBlockUs[p.tb / 2] + kLaunchUs * (1 + p.lay + (p.splits > 1));
     return p;
 }
 
@@ -566,6 +588,11 @@ igcStatus lay_out(igcHandle_t handle, igcDataType in, Linear4Args &t, void *to) 
                          dim3((unsigned)std::min(groups, kMostGroups)), 256, handle->stream);
 }
 
+igcStatus finish(igcHandle_t handle, igcDataType out, const Linear4Args &t) {
+    return launch_kernel(out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear4_finish_kernel<float>) : reinterpret_cast<const void *>(&linear4_finish_kernel<bf16_t>), t,
+                         dim3((unsigned)std::min((t.M * (t.partsRow / 4) + 255) / 256, kMostGroups)), 256, handle->stream);
+}
+
 template <class TX, class TO>
 igcStatus run_few(igcHandle_t handle, const Linear4Args &a, const FewPlan &p, void *workSpace) {
     Linear4Args t = a;
@@ -579,20 +606,21 @@ igcStatus run_few(igcHandle_t handle, const Linear4Args &a, const FewPlan &p, vo
     t.partsRow = round_up(a.N, 4);
     st = launch_kernel(few_kernel<TX, TO>(p, a.group4), t, dim3((unsigned)std::min((long long)t.tilesM * t.tilesN * t.splits, kMostGroups)), 512, handle->stream);
     if (st != IGC_STATUS_SUCCESS || p.splits == 1) return st;
-    return launch_kernel(reinterpret_cast<const void *>(&linear4_finish_kernel<TO>), t, dim3((unsigned)std::min((a.M * (t.partsRow / 4) + 255) / 256, kMostGroups)), 256, handle->stream);
+    return finish(handle, sizeof(TO) == 4 ? IGC_DATA_FLOAT : IGC_DATA_BFLOAT16, t);
 }
 
 // The tiles for a call, or none: few tokens, or more workgroups than a launch holds.
 struct Tile4Plan {
     TileKernel k{};
     bool lay = false, layScales = false;       // x, the scales are laid out first, in `room` bytes
-    size_t scalesAt = 0, room = 0;
+    size_t scalesAt = 0, partsAt = 0, room = 0;
+    int splits = 1, per = 0;      // per: blocks to a range
     long long tilesM = 0, tilesN = 0;
     double us = 1e300;
 };
 Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, const Linear4Args &a) {
     Tile4Plan best;
-    if (a.M <= 64 || a.K > (1 << 22)) return best;
+    if (a.M <= 16 || a.K > (1 << 22)) return best;
     const bool parts = in == IGC_DATA_FLOAT;
     const long long row = round_up(a.K, 8);
     Tile4Plan p;
@@ -600,21 +628,32 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
     p.lay = parts || a.K % 8 != 0 || (uintptr_t)a.a % 4 != 0 || (a.M > 1 && (a.am % 2 != 0 || a.am < a.K)) || a.am >= (1 << 22);
     p.layScales = a.N % 2 != 0 || (uintptr_t)a.scales % 4 != 0;
     p.scalesAt = p.lay ? (size_t)round_up((parts ? round_up(a.M, kPartsTokens) * 3 : a.M) * row * 2, 256) : 0;
-    p.room = p.scalesAt + (p.layScales ? (size_t)((a.K + a.group4 - 1) / a.group4) * round_up(a.N, 2) * 2 : 0);
+    p.partsAt = p.scalesAt + (p.layScales ? (size_t)round_up((a.K + a.group4 - 1) / a.group4 * round_up(a.N, 2) * 2, 256) : 0);
+    const int blocks = (a.K + kBlock - 1) / kBlock;
+    // (groups' sums and scales)
+    const double scaled = a.group4 == 32 ? 1.15 : (a.group4 == 64 ? 1.0 : 0.9);
     for (int shape = 0; shape < kTile4Shapes; ++shape) {
         p.k = tile4_kernel(shape, a.group4, parts, out == IGC_DATA_FLOAT);
         if (!p.k.kernel) continue;
         p.tilesM = (a.M + p.k.bm - 1) / p.k.bm;
         p.tilesN = (a.N + p.k.bn - 1) / p.k.bn;
         if (p.tilesM * p.tilesN > kMostGroups) continue;
-        const long long rounds = (p.tilesM * p.tilesN + h->computeUnits - 1) / h->computeUnits;
-        p.us = rounds * ((a.K + kBlock - 1) / kBlock) * (parts ? kPartsBlockUs : kBlockUs[shape]) + kLaunchUs * (1 + p.lay + p.layScales);
-        if (p.us < best.us) best = p;
+        const double one = scaled * (parts ? kPartsBlockUs : kBlockUs)[shape], two = shape == 3 && !parts ? scaled * kTwoBlocksUs : 2.0 * one;
+        // the reduction in ranges of two blocks and more
+        for (int splits = 1; splits == 1 || (shape != 2 && splits <= std::min(16, blocks / 2) && p.tilesM * p.tilesN * (splits - 1) < 2 * h->computeUnits); ++splits) {
+            p.per = (blocks + splits - 1) / splits;
+            p.splits = (blocks + p.per - 1) / p.per;
+            const long long rounds = (p.tilesM * p.tilesN * p.splits + h->computeUnits - 1) / h->computeUnits;
+            p.us = kStartUs + p.per * (rounds / 2 * two + rounds % 2 * one) + kLaunchUs * (1 + p.lay + p.layScales) + sums_us(p.splits, a);
+            if (p.us >= best.us) continue;
+            best = p;
+            best.room = p.partsAt + (p.splits > 1 ? (size_t)p.splits * a.M * round_up(a.N, 8) * 4 : 0);
+        }
     }
     return best;
 }
 
-igcStatus run_tiles4(igcHandle_t handle, igcDataType in, const Linear4Args &a, const Tile4Plan &pl, void *workSpace) {
+igcStatus run_tiles4(igcHandle_t handle, igcDataType in, igcDataType out, const Linear4Args &a, const Tile4Plan &pl, void *workSpace) {
     Linear4Args t = a;
     igcStatus st = IGC_STATUS_SUCCESS;
     if (pl.lay && (st = lay_out(handle, in, t, workSpace)) != IGC_STATUS_SUCCESS) return st;
@@ -628,10 +667,15 @@ igcStatus run_tiles4(igcHandle_t handle, igcDataType in, const Linear4Args &a, c
         t.scaleRow = q.toRow;
     }
     t.tilesM = (int)pl.tilesM; t.tilesN = (int)pl.tilesN;
-    t.splits = 1;
-    t.tilesPerXcd = (int)((pl.tilesM * pl.tilesN + 7) / 8);
+    t.splits = pl.splits;
+    t.stepsPerSplit = pl.per;
+    t.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workSpace) + pl.partsAt);
+    t.partsRow = round_up(a.N, 8);
+    t.tilesPerXcd = (int)((pl.tilesM * pl.tilesN * pl.splits + 7) / 8);
     t.group = std::min(t.tilesM, 4);
-    return launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+    st = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+    if (st != IGC_STATUS_SUCCESS || pl.splits == 1) return st;
+    return finish(handle, out, t);
 }
 
 Linear4Args sizes_of(const Matrix &x, const igcFilterStruct &w, int group) {
@@ -728,7 +772,7 @@ igcStatus igcLinear4Forward(igcHandle_t handle, const void *alpha, igcTensorDesc
     const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
     const size_t room = workSpace && !off(workSpace, 16) ? workSpaceSizeInBytes : 0;
     const FewPlan few = plan_few(handle, xDesc->dtype, a, room);
-    if (pl.room <= room && pl.us <= few.us) return run_tiles4(handle, xDesc->dtype, a, pl, workSpace);
+    if (pl.room <= room && pl.us <= few.us) return run_tiles4(handle, xDesc->dtype, yDesc->dtype, a, pl, workSpace);
     return with_types(xDesc->dtype, yDesc->dtype, [&](auto tx, auto ty) { return run_few<decltype(tx), decltype(ty)>(handle, a, few, workSpace); });
 }
 

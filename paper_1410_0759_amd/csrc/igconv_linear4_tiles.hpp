@@ -3,7 +3,7 @@
 // know of the copies, would wait for all of them with it (2048 x 4096 -> 8192, groups of 64, tiles of 128 x 256: 198 us that way, 160 this way).
 //
 // A group's products are summed from zero, and multiplied by the group's scale into the result: 4 multiply-adds for each matrix instruction that ends
-// a group (groups of 32: all of them, of 128: every fourth).  They follow the next unit's matrix instructions, which do not wait for them nor they for these.
+// a group (groups of 32: all of them, of 128: every fourth).  Few tiles: the reduction in ranges of blocks, added by linear4_finish_kernel.  They follow the next unit's matrix instructions, which do not wait for them nor they for these.
 #ifndef IGCONV_LINEAR4_TILES_HPP_
 #define IGCONV_LINEAR4_TILES_HPP_
 
@@ -42,13 +42,14 @@ struct Copies4 {
     const uint16_t *scales_from;
     long long codes_left, scale_row;
     uint32_t row_bytes, code_at;
-    int t0, N, K, lane, wave, blocks, groups, steps;
-    int x_requested = 0, x_slot = 0, requested = 0, code_slot = 0, scale_slot = 0;
+    int t0, N, K, lane, wave, first, blocks, groups, steps;     // blocks, steps: the range's ends
+    int x_requested, x_slot = 0, requested, code_slot = 0, scale_slot = 0;
     u32x4 code_buf;
     uint32_t code_to, scale_to;
     int code_block;
 
-    __device__ __forceinline__ void init(const Linear4Args &p, uint8_t *lds_, int tm, int tn, int lane_, int wave_) {
+    // (the range `split` of the blocks)
+    __device__ __forceinline__ void init(const Linear4Args &p, uint8_t *lds_, int tm, int tn, int split, int lane_, int wave_) {
         lds = lds_;
         lds_codes = lds + Cfg::X_SLOTS * Cfg::X_BYTES;
         lds_scales = lds_codes + Cfg::CODE_SLOTS * Cfg::CODE_BYTES;
@@ -58,9 +59,11 @@ struct Copies4 {
         N = p.N;
         K = p.K;
         x.init(p.a, p.am, 1, tm * Cfg::ROWS, Cfg::PARTS == 1 ? p.M : p.tilesM * Cfg::ROWS, K, lane, wave);
-        blocks = (K + kCodeBlock - 1) / kCodeBlock;
+        first = requested = split * p.stepsPerSplit;
+        blocks = min((K + kCodeBlock - 1) / kCodeBlock, first + p.stepsPerSplit);
+        x_requested = 2 * first;
         groups = (K + Cfg::GROUP - 1) / Cfg::GROUP;
-        steps = (K + 63) / 64;
+        steps = min((K + 63) / 64, 2 * blocks);
         // Codes: a request of a wavefront is 16 rows' blocks of 64 bytes, four lanes a row, so that neighbours read neighbours; the four pieces of a row are permuted by
         // an exclusive or with the row's number, for the lanes of a read, which go down the rows, to lie in different banks.
         row_bytes = (uint32_t)code_row(K);
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_tiles_kernel(const Li
     if (!tile_of(p, &tm, &tn, &split)) return;
     const int m0 = tm * Cfg::BM, n0 = tn * Cfg::BN + wn * FN * 16;
     Copies4<Cfg> copies;
-    copies.init(p, lds, tm, tn, lane, wave);
+    copies.init(p, lds, tm, tn, split, lane, wave);
     constexpr int R = Copies4<Cfg>::R, RC = Copies4<Cfg>::RC;
     OperandReads<Cfg::ROWS, FM, false, 2> reads;
     reads.init(wm * FM * 16, lane);
@@ -182,7 +185,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_tiles_kernel(const Li
     read_codes(0, codes);
     bf16x8 q = widen8(codes[0][0]);
     int xs = 0, cs = 0, ss = 0;       // places of the step's x, the block's codes and scales
-    for (int block = 0; block < copies.blocks; ++block) {
+    for (int block = copies.first; block < copies.blocks; ++block) {
         int ended = FN - 1, ended_in = IN_GROUP == 1 ? (FN - 1) & 1 : FN - 1;      // column of the group that ended last, with the block before, and where its sum is
 #pragma unroll
         for (int i32 = 0; i32 < 4; ++i32) {
@@ -213,9 +216,12 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_tiles_kernel(const Li
             for (int j = 0; j < FN; ++j) {
                 const int b = IN_GROUP == 1 ? j & 1 : j;
                 // (a request to a unit: all wavefronts' at once wait for each other; codes and scales of a block between the first middle and the second)
-                static_assert(R <= FN && RC <= FN, "");
-                if (kk == 1 && j < R) copies.request_x(j);
-                if (i32 == 2 && j < RC) copies.request_codes(j);
+                if (kk == 1)
+#pragma unroll
+                    for (int r = j; r < R; r += FN) copies.request_x(r);
+                if (i32 == 2)
+#pragma unroll
+                    for (int r = j; r < RC; r += FN) copies.request_codes(r);
                 const bf16x8 then = widen8(j + 1 < FN ? codes[j + 1][i32] : (i32 < 3 ? codes[0][i32 + 1] : next_codes[0][0]));
 #pragma unroll
                 for (int n = 0; n < PARTS; ++n)
@@ -248,7 +254,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_tiles_kernel(const Li
     add(IN_GROUP == 1 ? (FN - 1) & 1 : FN - 1, FN - 1);
     __builtin_amdgcn_s_waitcnt(requests_left(0));   // (nothing may be on its way into LDS)
     __syncthreads();
-    write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES / 256 * 256, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES / 256 * 256), lane, 0, m0 + wm * FM * 16, n0, total);
+    write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES / 256 * 256, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES / 256 * 256), lane, split, m0 + wm * FM * 16, n0, total);
 }
 
 // The same with 256 x 256 results: a wavefront's 128 tokens share its 64 rows' decoded codes, a step's at a time, and go through one block of 16 tokens after the other, so that
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Lin
     int tm, tn, split;
     if (!tile_of(p, &tm, &tn, &split)) return;
     Copies4<Cfg> copies;
-    copies.init(p, lds, tm, tn, lane, wave);
+    copies.init(p, lds, tm, tn, split, lane, wave);
     constexpr int R = Copies4<Cfg>::R, RC = Copies4<Cfg>::RC;
     OperandReads<Cfg::ROWS, FM, false, 2> reads;
     reads.init(wm * FM * 16, lane);
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Lin
     __builtin_amdgcn_s_waitcnt(requests_left(R));
     asm volatile("s_barrier" ::: "memory");
     int xs = 0, cs = 0, ss = 0;       // places of the step's x, the block's codes and scales
-    for (int block = 0; block < copies.blocks; ++block) {
+    for (int block = copies.first; block < copies.blocks; ++block) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const uint8_t *here = lds + xs * Cfg::X_BYTES;

@@ -310,3 +310,13 @@ def test_rows_beyond_32_bits():
             assert bool(Y[:, K:K + 8].isnan().all())
             del X, Y
             torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+def test_ranges_of_the_reduction(types):
+    """Few rows of W and long ones: ranges of blocks, which end anywhere in the rows, added in a second launch."""
+    for M, C, K, group in ((3, 16000, 100, 32), (16, 9001, 65, 128), (20, 5001, 333, 64), (17, 4096, 40, 32), (33, 3000, 700, 128), (64, 4096, 600, 64), (100, 8000, 130, 32),
+                           (129, 2500, 257, 64), (257, 3000, 260, 128), (500, 1500, 130, 32)):
+        for layout in ((0, 0), (1, 1)):
+            print("four-bit product in ranges", types, M, C, K, group, layout, flush=True)
+            product(M, C, K, group, types, layout, "silu", residual=True)
