@@ -25,15 +25,30 @@ struct CrossEnd {
     const float *logSum, *dloss;
     float *sums;                // column sums of dz over each wavefront's rows, [sumBlocks][sumStride], or null
     bool twoParts;              // dz in two bfloat16 parts, the second as M more rows below
+    float *rests;               // [M]: what rounding to bfloat16 left of dz at the targets, or null
     long long sumStride;
 };
 struct CrossArgs : TileArgs {
     CrossEnd end;
 };
 
-enum CrossKind { kRowStatistics, kSlopes };
+// A product of dz with rows added before its results are rounded: to row m, where i = rowOf[m] - first is one of 0 to count - 1, factor[m] (null: 1) times row i of `from`.
+template <class TO> struct WithRows {};
+struct RowAddend {
+    const int *rowOf;
+    const float *factor;
+    const uint16_t *from;
+    long long stride;
+    int first, count;
+};
+struct AddendArgs : TileArgs {
+    RowAddend add;
+};
+
+enum CrossKind { kRowStatistics, kSlopes, kDataWithRows, kFilterWithRows };
 // The kernels with these ends: bfloat16 tiles (as tile_kernel_rows), float operands as they are, float in parts.
 TileKernel cross_tile_kernel(CrossKind kind, int shape);
+TileKernel with_rows_tile_kernel(CrossKind kind, int shape, bool f32_out);
 TileKernel cross_direct_float_kernel(CrossKind kind, int shape);
 TileKernel cross_float_kernel(CrossKind kind);
 
@@ -46,6 +61,9 @@ struct CrossPlan {
 CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);
 igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes,
                         CrossPlan *taken);
+// A product of bfloat16 operands with rows added (of a layout that the tiles do not take: without them), and its room.
+igcStatus product_with_rows(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a, const RowAddend &add, void *workSpace, size_t bytes);
+size_t product_with_rows_room(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a);
 // The same for at most kFewTokens tokens of bfloat16 features, of any layout (igconv_cross_entropy_few.hip).  Slopes: dz in two parts; x is copied to z (rows zs apart, from 16-byte
 // boundaries), twice below each other.  One block of column sums.
 constexpr int kFewTokens = 16;

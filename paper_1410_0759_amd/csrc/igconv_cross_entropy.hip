@@ -7,6 +7,7 @@
 // logit of each row and range of columns and the sum of exp(z - largest); a last kernel joins them.  Backward, the piece's logits are made again, become dz, and go
 // into two products.
 #include "igconv_cross_entropy.h"
+#include "igconv_linear_tiles.hpp"
 
 namespace igc {
 namespace {
@@ -150,6 +151,7 @@ struct SlopeArgs {
     const float *logSum, *dloss;
     float *sums;                // [rows / kSlopeRows][stride]: column sums, or null
     int parts;                  // dz in two parts, the second M rows below
+    float *rests;               // [M]: what rounding left of dz at the targets, or null
 };
 constexpr int kSlopeRows = 32;
 
@@ -178,6 +180,7 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
                 const float p = sizeof(TZ) == 4 ? expf(z[e] - log_sum) : exp_of(z[e] - log_sum);
                 d[e] = there && n + e < a.columns ? slope * (t - a.first == n + e ? p - 1.f : p) : 0.f;
                 sums[e] += d[e];
+                if (a.rests && there && n + e < a.columns && t - a.first == n + e) a.rests[m] = rest_of(d[e]);
             }
             TZ *to = static_cast<TZ *>(a.dz) + m * a.stride + n;
             if constexpr (sizeof(TZ) == 4) *reinterpret_cast<float4 *>(to) = float4{d[0], d[1], d[2], d[3]};
@@ -185,30 +188,6 @@ __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
             if (a.parts) *reinterpret_cast<uint2 *>(to + a.M * a.stride) = uint2{to_bf16_pair(rest_of(d[0]), rest_of(d[1])), to_bf16_pair(rest_of(d[2]), rest_of(d[3]))};
         }
         if (a.sums) *reinterpret_cast<float4 *>(a.sums + block * a.stride + n) = float4{sums[0], sums[1], sums[2], sums[3]};
-    }
-}
-
-struct BiasGradientArgs {
-    const float *sums;
-    long long stride, blocks;
-    int columns;
-    float beta;
-    float *out;
-};
-// 64 columns to a workgroup, its four wavefronts on every fourth block of rows
-__global__ __launch_bounds__(256) void bias_gradient_kernel(const BiasGradientArgs a) {
-    __shared__ float sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)blockIdx.x * 64 + lane;
-    float sum = 0.f;
-    if (n < a.columns)
-#pragma unroll 4
-        for (long long b = wave; b < a.blocks; b += 4) sum += a.sums[b * a.stride + n];
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && n < a.columns) {
-        float v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-        if (a.beta != 0.f) v += a.beta * a.out[n];
-        a.out[n] = v;
     }
 }
 
@@ -253,6 +232,106 @@ __global__ __launch_bounds__(256) void twice_kernel(const TwiceArgs a) {
         const uint16_t v = c < a.C ? a.from[m * a.stride + c] : (uint16_t)0;
         a.to[id] = v;
         a.to[a.M * a.toRow + id] = v;
+    }
+}
+
+// ---- what rounding dz leaves at the targets -------------------------------------------------------------------------------
+// Nearly all of a row's gradient is its target's, and its rounding would be half of what the results are off by (with their own: 1.41 times theirs).  The rest of it goes
+// back in: dx[m] += rest[m] w[t], dw[v] += the sum of rest[m] x[m] over the rows m with target v, which the first of these rows makes.  (4096 x 4096 -> 65536: @RESTS@)
+struct AfterSlopesArgs {
+    // the bias gradient
+    const float *sums;
+    long long stride, blocks;
+    float beta;
+    float *out;
+    int biasGroups;             // workgroups that make it, in front of the others
+    // the targets
+    const int *targets;
+    int M, first, columns;
+    int *firstOf, *lastOf;      // [columns]: the first and last row with this target, INT_MAX and -1 without one
+};
+constexpr int kTargetRange = 512;     // entries to a workgroup, which looks at all rows
+// 64 columns of the bias gradient to a workgroup, its four wavefronts on every fourth block of rows; or a range of entries.  (One launch: of 777 rows each is mostly start.)
+__global__ __launch_bounds__(256) void after_slopes_kernel(const AfterSlopesArgs a) {
+    if ((int)blockIdx.x < a.biasGroups) {
+        __shared__ float sums[4][64];
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)blockIdx.x * 64 + lane;
+        float sum = 0.f;
+        if (n < a.columns)
+#pragma unroll 4
+            for (long long b = wave; b < a.blocks; b += 4) sum += a.sums[b * a.stride + n];
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && n < a.columns) {
+            float v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            if (a.beta != 0.f) v += a.beta * a.out[n];
+            a.out[n] = v;
+        }
+        return;
+    }
+    __shared__ int first_of[kTargetRange], last_of[kTargetRange];
+    const int v0 = ((int)blockIdx.x - a.biasGroups) * kTargetRange;
+    for (int i = threadIdx.x; i < kTargetRange; i += 256) first_of[i] = 0x7FFFFFFF, last_of[i] = -1;
+    __syncthreads();
+#pragma unroll 8
+    for (int m = threadIdx.x; m < a.M; m += 256) {
+        const uint32_t v = (uint32_t)a.targets[m] - (uint32_t)a.first - (uint32_t)v0;
+        if (v >= kTargetRange) continue;
+        atomicMin(&first_of[v], m);
+        atomicMax(&last_of[v], m);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTargetRange && v0 + i < a.columns; i += 256) {
+        a.firstOf[v0 + i] = first_of[i];
+        a.lastOf[v0 + i] = last_of[i];
+    }
+}
+
+struct RestRowsArgs {
+    const int *targets;
+    int M, first, columns, C;
+    const int *firstOf, *lastOf;
+    const float *rests;
+    const uint16_t *x;
+    long long stride, toRow;
+    uint16_t *to;               // [M][toRow]: of a target's first row
+};
+constexpr int kRestColumns = 2048;
+__global__ __launch_bounds__(256) void rest_rows_kernel(const RestRowsArgs a) {
+    __shared__ unsigned long long same[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.y * kRestColumns + (int)threadIdx.x * 8;
+    for (int m0 = blockIdx.x; m0 < a.M; m0 += (int)gridDim.x) {
+        const int t = a.targets[m0];
+        const uint32_t v = (uint32_t)t - (uint32_t)a.first;
+        if (v >= (uint32_t)a.columns || a.firstOf[v] != m0) continue;
+        const int last = a.lastOf[v];
+        float sum[8] = {};
+        auto add = [&](int m) {
+            const float rest = a.rests[m];
+            const uint16_t *from = a.x + m * a.stride + c;
+            if (c + 8 <= a.C) {
+                const Adjacent<uint16_t, 8> q = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(from);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += rest * bf16_bits_to_float(q.v[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < a.C) sum[e] += rest * bf16_bits_to_float(from[e]);
+            }
+        };
+        add(m0);
+        for (int m = m0 + 1; m <= last; m += 256) {
+            const int mine = m + (int)threadIdx.x;
+            const unsigned long long here = __ballot(mine <= last && a.targets[mine] == t);
+            __syncthreads();
+            if (lane == 0) same[wave] = here;
+            __syncthreads();
+            for (int w = 0; w < 4; ++w)
+                for (unsigned long long left = same[w]; left; left &= left - 1) add(m + 64 * w + __builtin_ctzll(left));
+        }
+        if (c >= a.toRow) continue;
+        uint16_t *to = a.to + m0 * a.toRow + c;
+        *reinterpret_cast<uint4 *>(to) = uint4{to_bf16_pair(sum[0], sum[1]), to_bf16_pair(sum[2], sum[3]), to_bf16_pair(sum[4], sum[5]), to_bf16_pair(sum[6], sum[7])};
     }
 }
 
@@ -376,8 +455,9 @@ struct BackwardPlan {
     bool parts;          // dz is in two parts
     Pieces pieces;
     bool sum;            // dx is summed in floats first
+    bool rests;          // what rounding dz leaves at the targets goes back in
     long long rows;      // of dz: its parts'
-    size_t logits, dz, dx, x, sums, room, total, room_bytes;
+    size_t logits, dz, dx, x, sums, restsAt, firstOf, lastOf, restRows, room, total, room_bytes;
 };
 // dx, dw: null where that gradient is not asked for
 BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
@@ -401,14 +481,29 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
     p.dx = r.take(p.sum ? (size_t)p.rows * C * 4 : 0);
     p.x = r.take(p.parts && dw ? (size_t)p.rows * round_up(C, 8) * 2 : 0);
     p.sums = r.take((size_t)((x.rows + 255) / 256 * 256 / kLeastRows) * p.pieces.stride * 4);
+    p.rests = t == IGC_DATA_BFLOAT16 && !p.parts && (dx || dw);
+    p.restsAt = r.take(p.rests ? (size_t)x.rows * 4 : 0);
+    p.firstOf = r.take(p.rests && dw ? (size_t)p.pieces.size * 4 : 0);
+    p.lastOf = r.take(p.rests && dw ? (size_t)p.pieces.size * 4 : 0);
+    p.restRows = r.take(p.rests && dw ? (size_t)x.rows * round_up(C, 8) * 2 : 0);
     p.room_bytes = 0;
     for (int piece : {0, p.pieces.count - 1}) {
         // (the last piece may be smaller, and then take other tiles)
         const int columns = std::min(p.pieces.size, V - piece * p.pieces.size);
         const LinearArgs logits = logits_product(x, C, p.pieces, columns);
         if (!p.few) p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
-        if (dx) p.room_bytes = std::max(p.room_bytes, product_room(h, t, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns)));
-        if (dw) p.room_bytes = std::max(p.room_bytes, product_room(h, t, dw->dtype, filter_product(x, p.parts, C, p.pieces, columns)));
+        auto room_of = [&](CrossKind kind, igcDataType out, const LinearArgs &a) {
+            p.room_bytes = std::max(p.room_bytes, p.rests ? product_with_rows_room(h, kind, out, a) : product_room(h, t, out, a));
+        };
+        if (dx) room_of(kDataWithRows, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns));
+        if (dw) {
+            LinearArgs f = filter_product(x, p.parts, C, p.pieces, columns);
+            room_of(kFilterWithRows, dw->dtype, f);
+            if (elem == 2) {      // (x off 4-byte boundaries: copied, else it would go element by element)
+                f.b = reinterpret_cast<const void *>(2);
+                room_of(kFilterWithRows, dw->dtype, f);
+            }
+        }
         if (p.pieces.count == 1) break;
     }
     p.room = r.take(p.room_bytes);
@@ -527,6 +622,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
     const float dx_beta = *static_cast<const float *>(beta), w_beta = *static_cast<const float *>(paramBeta);
     uint8_t *ws = static_cast<uint8_t *>(workSpace);
     const long long row_blocks = (M + kSlopeRows - 1) / kSlopeRows;
+    float *rests = p.rests ? reinterpret_cast<float *>(ws + p.restsAt) : nullptr;
     if (p.parts && !p.few && dw) {
         TwiceArgs q{static_cast<const uint16_t *>(x), reinterpret_cast<uint16_t *>(ws + p.x), mx.stride, round_up(C, 8), M, C};
         st = launch_kernel(reinterpret_cast<const void *>(&twice_kernel), q, dim3(grid_of((M * q.toRow + 255) / 256)), 256, handle->stream);
@@ -553,6 +649,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             end.sums = sums;
             end.sumStride = p.pieces.stride;
             end.twoParts = p.parts;
+            end.rests = rests;
             CrossPlan taken;
             taken.sumBlocks = 1;
             if (p.few) {
@@ -568,14 +665,17 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             a.y = ws + p.logits;
             if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
             SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
-                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums, p.parts ? 1 : 0};
+                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums, p.parts ? 1 : 0, rests};
             st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
                                dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
             if (st != IGC_STATUS_SUCCESS) return st;
         }
-        if (dbias) {
-            BiasGradientArgs b{sums, p.pieces.stride, sum_blocks, columns, w_beta, static_cast<float *>(dbias) + first};
-            st = launch_kernel(reinterpret_cast<const void *>(&bias_gradient_kernel), b, dim3((unsigned)(columns + 63) / 64u), 256, handle->stream);
+        int *first_of = reinterpret_cast<int *>(ws + p.firstOf), *last_of = reinterpret_cast<int *>(ws + p.lastOf);
+        if (dbias || (dw && p.rests)) {
+            AfterSlopesArgs b{sums, p.pieces.stride, sum_blocks, w_beta, dbias ? static_cast<float *>(dbias) + first : nullptr, dbias ? (columns + 63) / 64 : 0,
+                              targets, M, first, columns, first_of, last_of};
+            const int ranges = dw && p.rests ? (columns + kTargetRange - 1) / kTargetRange : 0;
+            st = launch_kernel(reinterpret_cast<const void *>(&after_slopes_kernel), b, dim3((unsigned)(b.biasGroups + ranges)), 256, handle->stream);
             if (st != IGC_STATUS_SUCCESS) return st;
         }
         if (dx) {
@@ -587,7 +687,10 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             d.r = d.y;
             d.rs = d.ys;
             d.beta = first > 0 ? 1.f : (p.sum ? 0.f : dx_beta);
-            if ((st = product(handle, t, p.sum ? IGC_DATA_FLOAT : dxDesc->dtype, d, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+            const igcDataType out = p.sum ? IGC_DATA_FLOAT : dxDesc->dtype;
+            const RowAddend add{targets, rests, static_cast<const uint16_t *>(piece), C, first, columns};
+            st = p.rests ? product_with_rows(handle, kDataWithRows, out, d, add, ws + p.room, p.room_bytes) : product(handle, t, out, d, ws + p.room, p.room_bytes);
+            if (st != IGC_STATUS_SUCCESS) return st;
         }
         if (dw) {
             LinearArgs f = filter_product(mx, p.parts, C, p.pieces, columns);
@@ -598,7 +701,17 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             f.r = f.y;
             f.rs = C;
             f.beta = w_beta;
-            if ((st = product(handle, t, dwDesc->dtype, f, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+            if (!p.rests) {
+                if ((st = product(handle, t, dwDesc->dtype, f, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
+                continue;
+            }
+            uint16_t *rest_rows = reinterpret_cast<uint16_t *>(ws + p.restRows);
+            const RestRowsArgs s{targets, M, first, columns, C, first_of, last_of, rests, static_cast<const uint16_t *>(x), mx.stride, round_up(C, 8), rest_rows};
+            const long long across = (C + kRestColumns - 1) / kRestColumns;
+            st = launch_kernel(reinterpret_cast<const void *>(&rest_rows_kernel), s, dim3((unsigned)std::min<long long>(M, std::max(kMostGroups / across, 1ll)), (unsigned)across), 256, handle->stream);
+            if (st != IGC_STATUS_SUCCESS) return st;
+            const RowAddend add{first_of, nullptr, rest_rows, s.toRow, 0, M};
+            if ((st = product_with_rows(handle, kFilterWithRows, dwDesc->dtype, f, add, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
         }
     }
     if (dx && p.sum) {

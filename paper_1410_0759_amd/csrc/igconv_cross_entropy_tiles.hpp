@@ -24,6 +24,21 @@ __device__ __forceinline__ void finish_logits(const CrossArgs &p, int n0, int la
         }
 }
 
+// four neighbours of a row of bfloat16 numbers (zeros behind its N elements)
+__device__ __forceinline__ f32x4 four_of(const uint16_t *row, int n, int N) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (n + 4 <= N) {
+        const Adjacent<uint16_t, 4> q = *reinterpret_cast<const Adjacent<uint16_t, 4> *>(row + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = bf16_bits_to_float(q.v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) v[e] = bf16_bits_to_float(row[n + e]);
+    }
+    return v;
+}
+
 template <class Cfg>
 struct TileEnd<Cfg, RowStatistics, CrossArgs> {
     template <int FM, int FN>
@@ -99,6 +114,7 @@ struct TileEnd<Cfg, Slopes<TZ>, CrossArgs> {
                     float v = sizeof(TZ) == 4 ? expf(acc[i][j][e] - log_sum) : exp_of(acc[i][j][e] - log_sum);
                     if (at == 16 * j + e) v -= 1.f;
                     v = there && n0 + 16 * j + 4 * g + e < p.N ? slope * v : 0.f;
+                    if (sizeof(TZ) == 2 && p.end.rests && at == 16 * j + e && n0 + 16 * j + 4 * g + e < p.N) p.end.rests[m] = rest_of(v);
                     acc[i][j][e] = v;
                     sums[j][e] += v;
                 }
@@ -138,6 +154,37 @@ struct TileEnd<Cfg, Slopes<TZ>, CrossArgs> {
                 write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TZ>(q, share, lane, split, m0, n0, acc);
             }
         }
+    }
+};
+
+template <class Cfg, class TO>
+struct TileEnd<Cfg, WithRows<TO>, AddendArgs> {
+    template <int FM, int FN>
+    static __device__ __forceinline__ void run(const AddendArgs &p, uint8_t *lds, int lane, int wave, int split, int, int, int m0, int n0, f32x4 (&acc)[FM][FN]) {
+        const int l16 = lane & 15, g = lane >> 4;
+        if (split == 0) {
+            uint32_t at[FM];
+            float factor[FM];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int m = m0 + 16 * i + l16;
+                at[i] = m < p.M ? (uint32_t)p.add.rowOf[m] - (uint32_t)p.add.first : 0xFFFFFFFFu;
+                factor[i] = 1.f;
+                if (m < p.M && p.add.factor) factor[i] = p.add.factor[m];
+            }
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                if (at[i] >= (uint32_t)p.add.count) continue;
+                const uint16_t *from = p.add.from + (long long)at[i] * p.add.stride;
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const f32x4 row = four_of(from, n0 + 16 * j + 4 * g, p.N);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += factor[i] * row[e];
+                }
+            }
+        }
+        write_results<FM, FN, Cfg::LDS_BYTES / Cfg::WAVES, TO>(p, lds + wave * (Cfg::LDS_BYTES / Cfg::WAVES), lane, split, m0, n0, acc);
     }
 };
 

@@ -400,7 +400,7 @@ constexpr ShapeCost kFloatCost = {1, 1.09, 1.09, 4.0}, kDirectCost[kDirectShapes
 constexpr double kCrossEnds[kTileShapes] = {4.0, 2.0, 1.0, 1.0};
 constexpr double kPartsLaunch = 2.5, kPartsBytes = 6e6, kMemoryBytes = 4.9e6, kWorkgroupBytes = 16e3;
 
-// cross: null, or the end of a product for cross entropy (bfloat16 or float, forward, in one range)
+// cross: null, or the end of a product for cross entropy (of logits: bfloat16 or float, in one range; with rows added: bfloat16)
 TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const LinearArgs &a, bool sums, size_t room, const CrossKind *cross = nullptr) {
     TilePlan pl;
     const bool f32 = in == IGC_DATA_FLOAT, sa = a.strided_a, sb = a.strided_b;
@@ -436,8 +436,8 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
         pl.bytes = at + parts + sum_bytes;
     };
     // (no range without a step)
-    auto most_splits = [&](int step) { return cross ? 1 : std::min(64, (a.K + step - 1) / step); };
-    auto more = [&](const ShapeCost &sc, int shape) { return cross ? ShapeCost{sc.per_cu, sc.alone, sc.full, sc.ends + kCrossEnds[shape]} : sc; };
+    auto most_splits = [&](int step) { return cross && *cross <= kSlopes ? 1 : std::min(64, (a.K + step - 1) / step); };
+    auto more = [&](const ShapeCost &sc, int shape) { return cross && *cross <= kSlopes ? ShapeCost{sc.per_cu, sc.alone, sc.full, sc.ends + kCrossEnds[shape]} : sc; };
     if (f32) {
         // (rows that end inside a piece begin off 16-byte boundaries as well: 1024 x 2050 -> 1000 65 steps of 32 x 128 49 us, 1024 x 2048 -> 1000 64 steps 45;
         // in parts both 42)
@@ -455,8 +455,9 @@ TilePlan plan_tiles(const igcContext *h, igcDataType in, igcDataType out, const 
     if ((oa.pack ? oa.toRow : oa.stride) >= (1ll << 22) || (ob.pack ? ob.toRow : ob.stride) >= (1ll << 22)) return pl;
     for (int shape = 0; shape < (oa.pack || ob.pack ? kTileShapes : kStagedShape); ++shape)
         for (int splits = 1; splits <= most_splits(kTileStep); ++splits)
-            consider(cross ? cross_tile_kernel(*cross, shape) : tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT), more(kShapeCost[shape], shape), kTileStep, splits,
-                     shape < kStagedShape);
+            consider(!cross ? tile_kernel(sa, sb, shape, out == IGC_DATA_FLOAT)
+                            : (*cross <= kSlopes ? cross_tile_kernel(*cross, shape) : with_rows_tile_kernel(*cross, shape, out == IGC_DATA_FLOAT)),
+                     more(kShapeCost[shape], shape), kTileStep, splits, shape < kStagedShape);
     return pl;
 }
 
@@ -505,6 +506,15 @@ igcStatus begin_tiles(igcHandle_t handle, const TilePlan &pl, igcDataType in, co
     t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
     t.partsRow = round_up(a.N, 8);
     return pack_operands(pl, in == IGC_DATA_FLOAT, a, t, ws, handle->stream);
+}
+
+// after tiles in ranges
+igcStatus join_ranges(igcHandle_t handle, igcDataType out, const TileArgs &t) {
+    FinishArgs f{};
+    static_cast<TileArgs &>(f) = t;
+    f.partsGroups = (t.M * (t.partsRow / 8) + 255) / 256;
+    return launch_kernel(out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_finish_kernel<float>) : reinterpret_cast<const void *>(&linear_finish_kernel<bf16_t>), f,
+                         dim3((unsigned)f.partsGroups), 256, handle->stream);
 }
 
 igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes, const SumsOut &sums = SumsOut(),
@@ -588,6 +598,20 @@ igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, cons
     if (rc != IGC_STATUS_SUCCESS) return rc;
     t.end = end;
     return launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+}
+
+igcStatus product_with_rows(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a, const RowAddend &add, void *workSpace, size_t bytes) {
+    const TilePlan pl = plan_tiles(handle, IGC_DATA_BFLOAT16, out, a, false, bytes, &kind);
+    if (!pl.tiles) return product(handle, IGC_DATA_BFLOAT16, out, a, workSpace, bytes);
+    AddendArgs t{};
+    igcStatus rc = begin_tiles(handle, pl, IGC_DATA_BFLOAT16, a, static_cast<uint8_t *>(workSpace), t);
+    if (rc != IGC_STATUS_SUCCESS) return rc;
+    t.add = add;
+    rc = launch_kernel(pl.k.kernel, t, dim3((unsigned)t.tilesPerXcd * 8u), pl.k.threads, handle->stream);
+    return rc == IGC_STATUS_SUCCESS && pl.splits > 1 ? join_ranges(handle, out, t) : rc;
+}
+size_t product_with_rows_room(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a) {
+    return plan_tiles(handle, IGC_DATA_BFLOAT16, out, a, false, kNoLimit, &kind).bytes;
 }
 
 }  // namespace igc

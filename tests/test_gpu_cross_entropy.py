@@ -3,7 +3,7 @@
 Tolerances.  e = 2^-24.  A logit: a sum of C products and the bias, (C + 4) e of the products' magnitudes (float: products in three bfloat16 parts leave out 2^-21 +
 2^-30 of each), and e (|z| + |bias|).  exp(d) is off by 2 e |d| + 4 e of itself; a logarithm of a sum by the logits' errors at most, by the average of the exponentials'
 and by its additions, no chain of which has more than 300; then half a step.  dz: its exponential's error and, of the logits' and logarithms', e^error - 1 of it; 4 e of the
-terms; rounded to bfloat16 half a step (2^-8) of it (at most 32 rows: in two parts, 2^-16).  A product of n terms with dz: dz's errors and (n + 8) e (float: and 2^-21 + 2^-30) of the terms, half a step
+terms; rounded to bfloat16 to the number next to it, or to either of two where its error reaches a border (at most 32 rows, and at the targets: in two parts, 2^-16).  A product of n terms with dz: dz's errors and (n + 8) e (float: and 2^-21 + 2^-30) of the terms, half a step
 of the result, and of the sum over the pieces e for each piece."""
 import pytest
 
@@ -131,8 +131,11 @@ class Case:
         size = torch.where(there, abs(alpha) * d.abs()[:, None] * torch.exp(z - s[:, None]), 0.0)
         tdz = size * (torch.expm1(tz) + 2 * E * (z - s[:, None]).abs() + 8 * E) + 8 * E * dz.abs()
         tsum = tdz.sum(0) + (self.M + 8) * E * dz.abs().sum(0)
-        half = 0.0 if self.dtype == "f32" else (2.0 ** -16 if self.M <= 32 else HALF["bf16"])
-        tdz = tdz + half * (dz.abs() + tdz)
+        # dz as the products take it: from the lowest to the highest number that it may have been rounded to
+        fine = (torch.arange(self.V, device="cuda")[None, :] == self.t[:, None]) | (self.M <= 32) | (self.dtype == "f32")
+        parts = tdz + (0.0 if self.dtype == "f32" else 2.0 ** -16) * (dz.abs() + tdz)
+        low, high = (torch.where(fine, dz + f, (dz + q).float().to(torch.bfloat16).double()) for q, f in ((-tdz, -parts), (tdz, parts)))
+        dbz, dz, tdz = dz.sum(0), (low + high) / 2, (high - low) / 2
         x, w = self.X.view.double(), self.w.double()
         what = str((self.M, self.C, self.V, self.dtype, self.layout, dx, dw, alpha, beta, pbeta))
 
@@ -144,7 +147,7 @@ class Case:
             near(have, want, tol + HALF[out] * (want.abs() + tol) + 1e-37, name + " " + what)
 
         if dbias:
-            check("dbias", dz.sum(0), tsum, pbeta, "f32")
+            check("dbias", dbz, tsum, pbeta, "f32")
         if dx:
             sizes = (dz.abs() + tdz) @ w.abs()
             check("dx", dz @ w, tdz @ w.abs() + ((self.V + 8 + 2 * pieces) * E + PART[self.dtype]) * sizes, beta, dx)
@@ -385,3 +388,18 @@ def test_rows_beyond_32_bits(dtype):
             u.Rows = keep
         del case, far
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("types", [("bf16", "bf16", "bf16"), ("bf16", "f32", "f32")], ids="-".join)
+def test_targets_that_repeat(types):
+    """All rows of one target, of two, of neighbours; across pieces, in ranges of the reduction, in copies."""
+    for M, C, V, layout in ((33, 64, 100, (0, 0)), (600, 70, 50, (1, 1)), (1500, 2100, 300, (8, 8)), (3000, 40, 130, (0, 0)), (2000, 64, 140001, (0, 0))):
+        for how in ("one", "two", "neighbours", "last"):
+            print("targets that repeat", types, M, C, V, layout, how, flush=True)
+            case = Case(M, C, V, types[0], layout, bias=True, lost=0.0)
+            m = torch.arange(M, device="cuda")
+            case.t = {"one": 0 * m + V // 2, "two": m % 2 * (V - 1), "neighbours": m % V, "last": V - 1 - m // 700}[how].to(torch.int32)
+            case.t[M // 3] = -100
+            case.check_backward(types[1], types[2], alpha=1.0 / M, beta=0.5 if how == "two" else 0.0, pbeta=0.5 if how == "two" else 0.0, pieces=4)
+            del case
+    torch.cuda.empty_cache()
