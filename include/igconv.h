@@ -620,8 +620,8 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
  *   dz = alpha * dloss * (exp(z - logSum) - [v is the target]), 0 in a row without target,
  *   dx = dz w + beta * dx,   dw = dz^T x + paramBeta * dw,   dbias = column sums of dz + paramBeta * dbias
  * dx: M rows of C, dw: filter V x C x 1 x 1, each float or, for bfloat16 x, bfloat16 too; dbias: V packed floats.  Each may be NULL (its descriptor too): not computed.
- * For bfloat16 x, dz goes into the two products in bfloat16: rounded once, or, up to 32 rows, as its rounding and what that left off,
- * rounded too (dbias sums it before); the sums over pieces of the vocabulary are held in floats.  A row without target adds zeros times its x to dw: that x has to be finite.
+ * For bfloat16 x, dz goes into the two products in bfloat16 (dbias sums it before), its rounding and what that left off, rounded too: of
+ * all elements up to 32 rows, else of the targets, which are nearly all of a gradient; the sums over pieces of the vocabulary are held in floats.  A row without target adds zeros times its x to dw: that x has to be finite.
  *
  * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports; less is BAD_PARAM.  For 8192
  * rows, 4096 features and 131072 entries that is 64 MB forward and 670 MB backward, as floats (copies of the operands in parts) 3.3 and 1.7 GB.

@@ -237,7 +237,8 @@ __global__ __launch_bounds__(256) void twice_kernel(const TwiceArgs a) {
 
 // ---- what rounding dz leaves at the targets -------------------------------------------------------------------------------
 // Nearly all of a row's gradient is its target's, and its rounding would be half of what the results are off by (with their own: 1.41 times theirs).  The rest of it goes
-// back in: dx[m] += rest[m] w[t], dw[v] += the sum of rest[m] x[m] over the rows m with target v, which the first of these rows makes.  (4096 x 4096 -> 65536: @RESTS@)
+// back in: dx[m] += rest[m] w[t], dw[v] += the sum of rest[m] x[m] over the rows m with target v, which the first of these rows makes.  (Beside the products: 4096 x 4096 -> 65536
+// 30 us of 5100, 777 x 1000 -> 10007 16 of 110.)
 struct AfterSlopesArgs {
     // the bias gradient
     const float *sums;
@@ -296,9 +297,9 @@ struct RestRowsArgs {
     long long stride, toRow;
     uint16_t *to;               // [M][toRow]: of a target's first row
 };
-constexpr int kRestColumns = 2048;
+constexpr int kRestColumns = 2048, kRestRows = 2048;     // rows looked at at once, eight to a thread
 __global__ __launch_bounds__(256) void rest_rows_kernel(const RestRowsArgs a) {
-    __shared__ unsigned long long same[4];
+    __shared__ int list[kRestRows], counts[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.y * kRestColumns + (int)threadIdx.x * 8;
     for (int m0 = blockIdx.x; m0 < a.M; m0 += (int)gridDim.x) {
         const int t = a.targets[m0];
@@ -306,29 +307,50 @@ __global__ __launch_bounds__(256) void rest_rows_kernel(const RestRowsArgs a) {
         if (v >= (uint32_t)a.columns || a.firstOf[v] != m0) continue;
         const int last = a.lastOf[v];
         float sum[8] = {};
-        auto add = [&](int m) {
-            const float rest = a.rests[m];
-            const uint16_t *from = a.x + m * a.stride + c;
-            if (c + 8 <= a.C) {
-                const Adjacent<uint16_t, 8> q = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(from);
+        // four rows at once, added one after the other
+        auto add = [&](const int *rows, int n) __attribute__((always_inline)) {
+            Adjacent<uint16_t, 8> q[4];
+            float rest[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += rest * bf16_bits_to_float(q.v[e]);
-            } else {
+            for (int k = 0; k < 4; ++k) {
+                const int m = rows[k < n ? k : 0];
+                const uint16_t *from = a.x + m * a.stride + c;
+                rest[k] = a.rests[m];
+                if (c + 8 <= a.C) q[k] = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(from);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q[k].v[e] = c + e < a.C ? from[e] : (uint16_t)0;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < n)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += rest[k] * bf16_bits_to_float(q[k].v[e]);
+        };
+        if (last == m0) add(&m0, 1);
+        else
+            for (long long from = m0; from <= last; from += kRestRows) {
+                const long long m = from + (int)threadIdx.x * 8;
+                uint32_t same = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (c + e < a.C) sum[e] += rest * bf16_bits_to_float(from[e]);
+                    if (m + e <= last && a.targets[m + e] == t) same |= 1u << e;
+                int place = __builtin_popcount(same);
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int before = __shfl_up(place, d);
+                    if (lane >= d) place += before;
+                }
+                __syncthreads();
+                if (lane == 63) counts[wave] = place;
+                __syncthreads();
+                place -= __builtin_popcount(same);
+                for (int w = 0; w < wave; ++w) place += counts[w];
+                for (; same; same &= same - 1) list[place++] = (int)m + __builtin_ctz(same);
+                const int n = counts[0] + counts[1] + counts[2] + counts[3];
+                __syncthreads();
+                for (int k = 0; k < n; k += 4) add(list + k, n - k);
             }
-        };
-        add(m0);
-        for (int m = m0 + 1; m <= last; m += 256) {
-            const int mine = m + (int)threadIdx.x;
-            const unsigned long long here = __ballot(mine <= last && a.targets[mine] == t);
-            __syncthreads();
-            if (lane == 0) same[wave] = here;
-            __syncthreads();
-            for (int w = 0; w < 4; ++w)
-                for (unsigned long long left = same[w]; left; left &= left - 1) add(m + 64 * w + __builtin_ctzll(left));
-        }
         if (c >= a.toRow) continue;
         uint16_t *to = a.to + m0 * a.toRow + c;
         *reinterpret_cast<uint4 *>(to) = uint4{to_bf16_pair(sum[0], sum[1]), to_bf16_pair(sum[2], sum[3]), to_bf16_pair(sum[4], sum[5]), to_bf16_pair(sum[6], sum[7])};
@@ -392,8 +414,8 @@ constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a
 // (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
 // Few enough tokens and vocabulary entries for the kernel of igconv_cross_entropy_few.hip (figures there).
 bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens && V <= 128 * h->computeUnits; }
-// Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: rounded to one, a row whose gradient is nearly all its
-// target's would be off by that number's rounding, and few rows do not average it out.  (Many do, and would pay for the second part in full.)
+// Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: a tile's 64 rows have room for both.  More rows would pay for the
+// second part in full, and put back what is left at the targets instead.
 constexpr int kPartsRows = 32;
 bool in_parts(igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && x.rows <= kPartsRows; }
 struct ForwardPlan {
