@@ -27,7 +27,7 @@ struct AdamWEntry {
     long long count;
     long long firstUnit;
     float decay;
-    int kind;      // 1: bfloat16 param, 2: bfloat16 gradient, 4: states in 8 bits
+    int kind;      // 1: bfloat16 param, 2: bfloat16 gradient, 4: states in 8 bits, 8: read as a stream
 };
 struct AdamWArgs {
     double beta1, beta2;
@@ -62,11 +62,14 @@ struct __attribute__((packed, aligned(sizeof(T)))) Near {
     T v[N];
 };
 
-template <class T>
+// (STREAM: not kept in caches, as whatever is stored: nothing is read again soon)
+template <class T, bool STREAM>
 __device__ __forceinline__ void load4(const void *from, long long at, int left, float (&to)[4]) {
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(T)), aligned(sizeof(T))));
     const T *p = static_cast<const T *>(from) + at;
     if (left >= 4) {
-        const Near<T, 4> q = *reinterpret_cast<const Near<T, 4> *>(p);
+        const Words *words = reinterpret_cast<const Words *>(p);
+        const Near<T, 4> q = __builtin_bit_cast(Near<T, 4>, STREAM ? __builtin_nontemporal_load(words) : *words);
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = Stored<T>::widen(q.v[e]);
     } else {
@@ -84,16 +87,22 @@ __device__ __forceinline__ void store4(void *to, long long at, int left, const f
         Near<T, 4> q;
 #pragma unroll
         for (int e = 0; e < 4; ++e) q.v[e] = Stored<T>::narrow(from[e]);
-        *reinterpret_cast<Near<T, 4> *>(p) = q;
+        typedef uint32_t Words __attribute__((ext_vector_type(sizeof(T)), aligned(sizeof(T))));
+        __builtin_nontemporal_store(__builtin_bit_cast(Words, q), reinterpret_cast<Words *>(p));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (e < left) p[e] = Stored<T>::narrow(from[e]);
     }
 }
+template <bool STREAM>
 __device__ __forceinline__ uint32_t load_codes(const void *from, long long at, int left) {
+    typedef uint32_t Word __attribute__((aligned(1)));
     const uint8_t *p = static_cast<const uint8_t *>(from) + at;
-    if (left >= 4) return __builtin_bit_cast(uint32_t, *reinterpret_cast<const Near<uint8_t, 4> *>(p));
+    if (left >= 4) {
+        const Word *word = reinterpret_cast<const Word *>(p);
+        return STREAM ? __builtin_nontemporal_load(word) : *word;
+    }
     uint32_t r = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -103,7 +112,8 @@ __device__ __forceinline__ uint32_t load_codes(const void *from, long long at, i
 __device__ __forceinline__ void store_codes(void *to, long long at, int left, uint32_t codes) {
     uint8_t *p = static_cast<uint8_t *>(to) + at;
     if (left >= 4) {
-        *reinterpret_cast<Near<uint8_t, 4> *>(p) = __builtin_bit_cast(Near<uint8_t, 4>, codes);
+        typedef uint32_t Word __attribute__((aligned(1)));
+        __builtin_nontemporal_store(codes, reinterpret_cast<Word *>(p));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -208,7 +218,7 @@ struct Constants {
 };
 
 // A wavefront's part of a unit: kUnit / 4 elements from `begin` on, in blocks of 256, all loads in front.
-template <class TP, class TG, bool EIGHT>
+template <class TP, class TG, bool EIGHT, bool STREAM>
 __device__ __forceinline__ void update(const AdamWEntry &t, const Constants &c, long long begin, int lane) {
 #pragma clang fp contract(off)   // (m and v as written: each operation rounded once)
     constexpr int BLOCKS = kUnit / (kThreads / 64) / kBlock;
@@ -218,16 +228,16 @@ __device__ __forceinline__ void update(const AdamWEntry &t, const Constants &c, 
     for (int b = 0; b < BLOCKS; ++b) {
         const long long block = begin + b * kBlock, at = block + lane * 4, rest = t.count - at;
         const int left = rest >= 4 ? 4 : (rest < 0 ? 0 : (int)rest);
-        load4<TP>(t.param, at, left, p[b]);
-        load4<TG>(t.grad, at, left, g[b]);
+        load4<TP, STREAM>(t.param, at, left, p[b]);
+        load4<TG, STREAM>(t.grad, at, left, g[b]);
         if constexpr (EIGHT) {
-            mc[b] = load_codes(t.m, at, left);
-            vc[b] = load_codes(t.v, at, left);
+            mc[b] = load_codes<STREAM>(t.m, at, left);
+            vc[b] = load_codes<STREAM>(t.v, at, left);
             ms[b] = vs[b] = 0.f;
             if (block < t.count) ms[b] = t.mScale[block / kBlock], vs[b] = t.vScale[block / kBlock];
         } else {
-            load4<float>(t.m, at, left, m[b]);
-            load4<float>(t.v, at, left, v[b]);
+            load4<float, STREAM>(t.m, at, left, m[b]);
+            load4<float, STREAM>(t.v, at, left, v[b]);
         }
     }
     const float shrink = 1.f - c.rate * t.decay;
@@ -286,17 +296,30 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWArgs a) {
         const AdamWEntry &t = a.entry[i];
         const long long begin = (unit - t.firstUnit) * kUnit + wave * (kUnit / (kThreads / 64));
         switch (t.kind) {
-        case 0: update<float, float, false>(t, c, begin, lane); break;
-        case 1: update<bf16_t, float, false>(t, c, begin, lane); break;
-        case 2: update<float, bf16_t, false>(t, c, begin, lane); break;
-        case 3: update<bf16_t, bf16_t, false>(t, c, begin, lane); break;
-        case 4: update<float, float, true>(t, c, begin, lane); break;
-        case 5: update<bf16_t, float, true>(t, c, begin, lane); break;
-        case 6: update<float, bf16_t, true>(t, c, begin, lane); break;
-        default: update<bf16_t, bf16_t, true>(t, c, begin, lane); break;
+        case 0: update<float, float, false, false>(t, c, begin, lane); break;
+        case 1: update<bf16_t, float, false, false>(t, c, begin, lane); break;
+        case 2: update<float, bf16_t, false, false>(t, c, begin, lane); break;
+        case 3: update<bf16_t, bf16_t, false, false>(t, c, begin, lane); break;
+        case 4: update<float, float, true, false>(t, c, begin, lane); break;
+        case 5: update<bf16_t, float, true, false>(t, c, begin, lane); break;
+        case 6: update<float, bf16_t, true, false>(t, c, begin, lane); break;
+        case 7: update<bf16_t, bf16_t, true, false>(t, c, begin, lane); break;
+        case 8: update<float, float, false, true>(t, c, begin, lane); break;
+        case 9: update<bf16_t, float, false, true>(t, c, begin, lane); break;
+        case 10: update<float, bf16_t, false, true>(t, c, begin, lane); break;
+        case 11: update<bf16_t, bf16_t, false, true>(t, c, begin, lane); break;
+        case 12: update<float, float, true, true>(t, c, begin, lane); break;
+        case 13: update<bf16_t, float, true, true>(t, c, begin, lane); break;
+        case 14: update<float, bf16_t, true, true>(t, c, begin, lane); break;
+        default: update<bf16_t, bf16_t, true, true>(t, c, begin, lane); break;
         }
     }
 }
+
+// Elements of a call from which on what lies on 128-byte boundaries is read past the caches too (that of the step before has left them; off the boundaries a line's two halves are
+// read by two wavefronts).  5.4e8 float elements 3030 us, with it 2810, before stores went past the caches 3130; 4e8 with 8 bits 1250, 1169, 1276; at odd places 1265, 1444,
+// 1363; 1e6 float elements 8.6, 9.1, 10.4.
+constexpr long long kStreamed = 1ll << 24;
 
 bool off(const void *p, size_t to) { return (uintptr_t)p % to != 0; }
 bool is_number(double v) { return (float)v - (float)v == 0.f; }    // (as a float)
@@ -326,9 +349,11 @@ extern "C" igcStatus igcAdamWStep(igcHandle_t handle, const igcAdamWParameters *
         (!q.deviceLearningRate && !is_number(q.learningRate)) || (!q.deviceStep && q.step < 1) || (float)q.epsilon < 0x1p-126f || off(q.deviceLearningRate, 4) ||
         off(q.deviceGradientScale, 4) || off(q.deviceStep, 4))
         return IGC_STATUS_BAD_PARAM;
+    long long elements = 0;
     for (int i = 0; i < tensors; ++i) {
         const igcStatus st = check_tensor(list[i]);
         if (st != IGC_STATUS_SUCCESS) return st;
+        elements += std::min(list[i].count, kStreamed);
     }
     AdamWArgs a{};
     a.beta1 = q.beta1; a.beta2 = q.beta2;
@@ -349,7 +374,8 @@ extern "C" igcStatus igcAdamWStep(igcHandle_t handle, const igcAdamWParameters *
             e.count = t.count;
             e.firstUnit = a.units;
             e.decay = (float)t.weightDecay;
-            e.kind = (t.paramType == IGC_DATA_BFLOAT16 ? 1 : 0) | (t.gradType == IGC_DATA_BFLOAT16 ? 2 : 0) | (t.stateBits == 8 ? 4 : 0);
+            e.kind = (t.paramType == IGC_DATA_BFLOAT16 ? 1 : 0) | (t.gradType == IGC_DATA_BFLOAT16 ? 2 : 0) | (t.stateBits == 8 ? 4 : 0) |
+                     (elements < kStreamed || off(t.param, 128) || off(t.grad, 128) || off(t.m, 128) || off(t.v, 128) ? 0 : 8);
             a.units += (t.count + kUnit - 1) / kUnit;
         }
         if (a.tensors == 0) continue;

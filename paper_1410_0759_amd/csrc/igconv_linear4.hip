@@ -28,7 +28,7 @@ struct StoreArgs {
 
 // A workgroup takes 64 rows of a block: a lane one word of it, sixteen lanes a row, so that a group's largest is found among 4, 8 or 16 lanes
 // and 64 rows' scales of a group go out next to each other.  The scale is the smallest bfloat16 number not below a sixth of the largest.  (16384 x 4096 bfloat16:
-// 55 to 63 us for 171 MB; with a comparison for each border between codes 77.)
+// 46 to 50 us for 171 MB; with a sixth in double precision 55 to 63, with a comparison for each border between codes 77.)
 template <class T>
 __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     const int lane = threadIdx.x & 63, word = lane & 15;
@@ -65,9 +65,12 @@ __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
             for (int d = 1; d < p.group / 8; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
             uint32_t scale = 0x7FC00000u;
             if (most < 0x7F800000u) {
-                const double want = (double)__builtin_bit_cast(float, most) / 6.0;
-                scale = __builtin_bit_cast(uint32_t, (float)want) & 0xFFFF0000u;
-                if ((double)__builtin_bit_cast(float, scale) < want) scale += 0x10000u;
+                // (six times a bfloat16 number is exact; a sixth is off by a last digit, so that at most two steps are missing)
+                const float largest = __builtin_bit_cast(float, most);
+                scale = __builtin_bit_cast(uint32_t, largest * (1.f / 6.f)) & 0xFFFF0000u;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    if (6.f * __builtin_bit_cast(float, scale) < largest) scale += 0x10000u;
             }
             // w / scale, rounded once: the inverse's product and its remainder's, which is exact.  It is a border between codes only where w is one times the scale (borders
             // have three bits, scales eight: no other w of 24 is within half a step of that).  Below 2^-100, where inverses overflow, both are taken 2^64 times.
@@ -95,8 +98,8 @@ __global__ __launch_bounds__(256) void to_four_bits_kernel(const StoreArgs p) {
     }
 }
 
-// A workgroup takes 64 rows of a block: a lane four features, so that the lanes of a store write next to each other (16384 x 4096 into float: 72 us for 306 MB; eight
-// features to a lane, whose stores of 16 bytes lie 32 apart, 92).
+// A workgroup takes 64 rows of a block: a lane four features, so that the lanes of a store write next to each other (16384 x 4096 into float: 51 us for 306 MB; with
+// stores that stay in the caches 72, with eight features to a lane, whose stores of 16 bytes lie 32 apart, 92).
 template <class T>
 __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) {
     const int four = threadIdx.x & 31;
@@ -125,7 +128,8 @@ __global__ __launch_bounds__(256) void from_four_bits_kernel(const StoreArgs p) 
             for (int e = 0; e < 4; ++e) v.v[e] = Stored<T>::narrow((float)q[e] * scale[i]);
             T *to = static_cast<T *>(p.out) + k * p.C + c;
             if (c + 4 <= p.C) {
-                *reinterpret_cast<Adjacent<T, 4> *>(to) = v;
+                typedef uint32_t Words __attribute__((ext_vector_type(sizeof(T)), aligned(sizeof(T))));
+                __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words *>(to));
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
