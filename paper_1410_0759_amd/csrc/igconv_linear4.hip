@@ -422,20 +422,33 @@ __global__ __launch_bounds__(256) void linear4_finish_kernel(const Linear4Args p
     }
 }
 
-// ---- x for the tiles -------------------------------------------------------------------------------------------------------
+// ---- x and scales for the tiles ------------------------------------------------------------------------------------------------
 struct Lay4Args {
     const void *x;
     uint16_t *to;
     long long stride;
     int M, C, toRow;
+    unsigned groupsX;           // workgroups for x; the others lay out scales
+    const uint16_t *scales;
+    uint16_t *toScales;
+    int N;
+    long long scaleGroups, scaleRow;
 };
-// bfloat16: rows on 16-byte boundaries, zeros up to the next eighth feature; float: three parts, kPartsTokens rows of each in turn, and zeros for the last rows.
+// x: bfloat16 in rows on 16-byte boundaries, zeros up to the next eighth feature; float in three parts, kPartsTokens rows of each in turn, and zeros for the last rows.
+// Scales: in rows of an even length.
 template <class T>
 __global__ __launch_bounds__(256) void lay_out_kernel(const Lay4Args p) {
     constexpr int N = Features<T>::PARTS;
+    if (blockIdx.x >= p.groupsX) {
+        for (long long id = (long long)(blockIdx.x - p.groupsX) * 256 + threadIdx.x; id < p.scaleGroups * p.scaleRow; id += (long long)(gridDim.x - p.groupsX) * 256) {
+            const long long group = id / p.scaleRow, n = id % p.scaleRow;
+            p.toScales[id] = n < p.N ? p.scales[group * p.N + n] : (uint16_t)0;
+        }
+        return;
+    }
     const int groups = p.toRow / 8;
     const long long rows = N == 1 ? p.M : ((long long)p.M + kPartsTokens - 1) / kPartsTokens * kPartsTokens;
-    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < rows * groups; id += (long long)gridDim.x * 256) {
+    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < rows * groups; id += (long long)p.groupsX * 256) {
         const long long m = id / groups;
         const int c = (int)(id % groups) * 8;
         Features<T> v;
@@ -482,20 +495,6 @@ template <class F>
 igcStatus with_types(igcDataType in, igcDataType out, F f) {
     if (in == IGC_DATA_FLOAT) return f(float(), float());
     return out == IGC_DATA_FLOAT ? f(bf16_t(), float()) : f(bf16_t(), bf16_t());
-}
-
-struct Scale4Args {
-    const uint16_t *from;
-    uint16_t *to;
-    int N;
-    long long groups, toRow;
-};
-// scales into rows of an even length
-__global__ __launch_bounds__(256) void lay_out_scales_kernel(const Scale4Args p) {
-    for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < p.groups * p.toRow; id += (long long)gridDim.x * 256) {
-        const long long group = id / p.toRow, n = id % p.toRow;
-        p.to[id] = n < p.N ? p.from[group * p.N + n] : (uint16_t)0;
-    }
 }
 
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
@@ -583,13 +582,23 @@ const void *few_kernel(const FewPlan &p, int group) {
     return p.kb == 2 ? few_kernel<2, 4, TX, TO>(group) : few_kernel<1, 4, TX, TO>(group);
 }
 
-igcStatus lay_out(igcHandle_t handle, igcDataType in, Linear4Args &t, void *to) {
-    Lay4Args q{t.a, static_cast<uint16_t *>(to), t.am, t.M, t.K, (int)round_up(t.K, 8)};
-    const long long groups = (round_up(t.M, kPartsTokens) * (q.toRow / 8) + 255) / 256;
-    t.a = to;
-    t.am = q.toRow;
+// to, toScales: null where x, the scales stay as they are
+igcStatus lay_out(igcHandle_t handle, igcDataType in, Linear4Args &t, void *to, void *toScales = nullptr) {
+    Lay4Args q{t.a, static_cast<uint16_t *>(to), t.am, t.M, t.K, (int)round_up(t.K, 8), 0, t.scales, static_cast<uint16_t *>(toScales), t.N,
+               (t.K + t.group4 - 1) / t.group4, round_up(t.N, 2)};
+    long long groups = 0;
+    if (to) {
+        q.groupsX = (unsigned)std::min((round_up(t.M, kPartsTokens) * (q.toRow / 8) + 255) / 256, kMostGroups);
+        t.a = to;
+        t.am = q.toRow;
+    }
+    if (toScales) {
+        groups = std::min((q.scaleGroups * q.scaleRow + 255) / 256, kMostGroups);
+        t.scales = q.toScales;
+        t.scaleRow = q.scaleRow;
+    }
     return launch_kernel(in == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&lay_out_kernel<float>) : reinterpret_cast<const void *>(&lay_out_kernel<bf16_t>), q,
-                         dim3((unsigned)std::min(groups, kMostGroups)), 256, handle->stream);
+                         dim3((unsigned)(q.groupsX + groups)), 256, handle->stream);
 }
 
 igcStatus finish(igcHandle_t handle, igcDataType out, const Linear4Args &t) {
@@ -648,7 +657,7 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
             p.per = (blocks + splits - 1) / splits;
             p.splits = (blocks + p.per - 1) / p.per;
             const long long rounds = (p.tilesM * p.tilesN * p.splits + h->computeUnits - 1) / h->computeUnits;
-            p.us = kStartUs + p.per * (rounds / 2 * two + rounds % 2 * one) + kLaunchUs * (1 + p.lay + p.layScales) + sums_us(p.splits, a);
+            p.us = kStartUs + p.per * (rounds / 2 * two + rounds % 2 * one) + kLaunchUs * (1 + (p.lay || p.layScales)) + sums_us(p.splits, a);
             if (p.us >= best.us) continue;
             best = p;
             best.room = p.partsAt + (p.splits > 1 ? (size_t)p.splits * a.M * round_up(a.N, 8) * 4 : 0);
@@ -660,20 +669,13 @@ Tile4Plan plan_tiles4(const igcContext *h, igcDataType in, igcDataType out, cons
 igcStatus run_tiles4(igcHandle_t handle, igcDataType in, igcDataType out, const Linear4Args &a, const Tile4Plan &pl, void *workSpace) {
     Linear4Args t = a;
     igcStatus st = IGC_STATUS_SUCCESS;
-    if (pl.lay && (st = lay_out(handle, in, t, workSpace)) != IGC_STATUS_SUCCESS) return st;
     t.scaleRow = a.N;
-    if (pl.layScales) {
-        uint16_t *to = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workSpace) + pl.scalesAt);
-        Scale4Args q{a.scales, to, a.N, (a.K + a.group4 - 1) / a.group4, round_up(a.N, 2)};
-        st = launch_kernel(reinterpret_cast<const void *>(&lay_out_scales_kernel), q, dim3((unsigned)std::min((q.groups * q.toRow + 255) / 256, kMostGroups)), 256, handle->stream);
-        if (st != IGC_STATUS_SUCCESS) return st;
-        t.scales = to;
-        t.scaleRow = q.toRow;
-    }
+    uint8_t *ws = static_cast<uint8_t *>(workSpace);
+    if ((pl.lay || pl.layScales) && (st = lay_out(handle, in, t, pl.lay ? ws : nullptr, pl.layScales ? ws + pl.scalesAt : nullptr)) != IGC_STATUS_SUCCESS) return st;
     t.tilesM = (int)pl.tilesM; t.tilesN = (int)pl.tilesN;
     t.splits = pl.splits;
     t.stepsPerSplit = pl.per;
-    t.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workSpace) + pl.partsAt);
+    t.parts = reinterpret_cast<float *>(ws + pl.partsAt);
     t.partsRow = round_up(a.N, 8);
     t.tilesPerXcd = (int)((pl.tilesM * pl.tilesN * pl.splits + 7) / 8);
     t.group = std::min(t.tilesM, 4);
