@@ -744,10 +744,14 @@ igcStatus igcGetLinear4ForwardWorkspaceSize(igcHandle_t handle, igcTensorDescrip
     Matrix x, y;
     const igcStatus st = check_product(xDesc, wDesc, group, yDesc, &x, &y);
     if (st != IGC_STATUS_SUCCESS) return st;
-    const Linear4Args a = sizes_of(x, *wDesc, group);
-    const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
+    Linear4Args a = sizes_of(x, *wDesc, group);
     const FewPlan few = plan_few(handle, xDesc->dtype, a, ~(size_t)0);
-    *sizeInBytes = pl.us <= few.us ? pl.room : few.room;
+    *sizeInBytes = 0;
+    for (int off_words : {0, 1}) {      // (x and scales on 4-byte boundaries and off them)
+        if (off_words) a.a = a.scales = reinterpret_cast<const uint16_t *>(2);
+        const Tile4Plan pl = plan_tiles4(handle, xDesc->dtype, yDesc->dtype, a);
+        *sizeInBytes = std::max(*sizeInBytes, pl.us <= few.us ? pl.room : few.room);
+    }
     return IGC_STATUS_SUCCESS;
 }
 

@@ -69,3 +69,10 @@ def test_product_refuses():
     assert status(lambda: ig.get_linear4_forward_workspace_size(h, rows(B, 4, 63), filt(B, 8, 64), 32, rows(B, 4, 8))) == BAD
     assert status(lambda: ig.get_linear4_forward_workspace_size(h, rows(F, 4, 64), filt(B, 8, 64), 32, rows(B, 4, 8))) == UNSUPPORTED
     assert ig.get_linear4_forward_workspace_size(h, rows(F, 4, 64), filt(F, 8, 64), 32, rows(F, 4, 8)) >= 0
+
+
+def test_workspace_holds_copies_of_what_lies_off_words():
+    """bfloat16 rows may begin at any 2 bytes: a prompt's room holds their copy whatever the descriptor says."""
+    h = ig.Handle()
+    for M, C, K in ((2048, 4096, 8192), (700, 520, 602), (64, 4096, 16384)):
+        assert ig.get_linear4_forward_workspace_size(h, rows(B, M, C), filt(B, K, C), 64, rows(B, M, K)) >= 2 * M * C

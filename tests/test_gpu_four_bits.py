@@ -320,3 +320,22 @@ def test_ranges_of_the_reduction(types):
         for layout in ((0, 0), (1, 1)):
             print("four-bit product in ranges", types, M, C, K, group, layout, flush=True)
             product(M, C, K, group, types, layout, "silu", residual=True)
+
+
+def test_off_words():
+    """x of even rows and scales that begin 2 bytes behind a word."""
+    import torch
+    u, ig = _u(), _u().ig
+    for M, C, K, group in ((20, 4096, 300, 32), (64, 512, 200, 64), (700, 520, 602, 128)):
+        rng = np.random.default_rng(M)
+        wc, ws = qo.quantize(held(rng.standard_normal((K, C)) / 20, "bf16"), group)
+        w, x = qo.values(wc, ws, group), held(rng.standard_normal((M, C)), "bf16")
+        X, Y, h, fd = u.Rows(x, "bf16", 8, 1), u.Rows((M, K), "f32", 0, 0, fill=float("nan")), u.handle(), u.filter_desc("bf16", K, C)
+        codes, scales = on_gpu(qo.pack(wc)), torch.zeros(ws.size + 1, dtype=torch.bfloat16, device="cuda")
+        scales[1:] = on_gpu(ws.reshape(-1), torch.bfloat16)
+        space = u.Workspace(ig.get_linear4_forward_workspace_size(h, X.desc, fd, group, Y.desc))
+        ig.check(ig.linear4_forward(h, 1.0, X.desc, X.ptr, fd, group, codes.data_ptr(), scales[1:].data_ptr(), space.buf.data_ptr(), space.size, 0, -1, 0.0, None, 0, Y.desc, Y.ptr))
+        space.check()
+        want = x @ w.T
+        tol = (C + 2 * len(ws) + 20) * E * (np.abs(x) @ np.abs(w).T)
+        u.close(Y.numpy(), want, tol + E * (np.abs(want) + tol), "y off words %s" % ((M, C, K, group),))
