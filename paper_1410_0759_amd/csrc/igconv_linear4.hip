@@ -522,8 +522,6 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
     const long long tm = (a.M + 16 * p.tb - 1) / (16 * p.tb);
     auto tiles = [&](int kb) { return tm * ((a.N + 16 * kb - 1) / (16 * kb)); };
     const int most = p.tb == 1 ? 4 : 2;      // (registers)
-    // Without ranges: as many rows of W to a workgroup as leave one for each compute unit (x is read less often).
-    p.kb = most == 4 && tiles(4) >= h->computeUnits ? 4 : (tiles(2) >= h->computeUnits ? 2 : 1);
     p.per = blocks;
     if (in == IGC_DATA_FLOAT && p.tb > 1) {
         const size_t bytes = (size_t)round_up(round_up(a.M, kPartsTokens) * 3 * round_up(a.K, 8) * 2, 256);
@@ -542,11 +540,19 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
         const long long rounds = (tiles(q.kb) * q.splits + h->computeUnits - 1) / h->computeUnits;
         return rounds * ((q.per + 7) / 8) * block_us(q.kb) + kLaunchUs * (1 + q.lay) + sums_us(q.splits, a);
     };
+    // Without ranges: of sixteen tokens as many rows of W to a workgroup as cost least (1 x 4096 -> 10880 and the like, groups of 128: 16, 32 and 64 rows 15.8, 14.6 and 12.1 us,
+    // 1 x 8192 -> 8192 16.6, 14.4 and 19.7), of more 32 where that leaves one workgroup for each compute unit.
     p.us = cost(p);
+    for (FewPlan q = p; q.kb < most;) {
+        q.kb *= 2;
+        if (p.tb > 1 && tiles(q.kb) < h->computeUnits) break;
+        q.us = cost(q);
+        if (q.us < p.us || p.tb > 1) p.kb = q.kb, p.us = q.us;
+    }
     // Ranges, each of a block for every wavefront at least, where they cost less with the second launch.
-    if (p.kb < most) {
-        // (of more than sixteen tokens a workgroup fills a compute unit: 64 x 5001 -> 2003 bfloat16 in 5 ranges 32 us, in 4 23; fewer tokens have two beside each other: float
-        // 4096 -> 10880 and the like 22 us, in one range less 25)
+    if (p.kb < most || p.tb == 1) {
+        // (of more than sixteen tokens a workgroup fills a compute unit: 64 x 5001 -> 2003 bfloat16 in 5 ranges 32 us, in 4 23; of fewer float
+        // tokens two run beside each other: 1 x 4096 -> 10880 and the like 22 us in two ranges, 25 in one)
         const long long fit = parts && p.tb == 1 ? (h->computeUnits + tiles(most) - 1) / tiles(most) : std::max(1ll, h->computeUnits / tiles(most));
         const int splits = (int)std::min<long long>(fit, (blocks + 7) / 8);
         const size_t bytes = (size_t)splits * a.M * round_up(a.N, 4) * 4;
