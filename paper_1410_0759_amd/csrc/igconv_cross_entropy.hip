@@ -149,24 +149,26 @@ struct SlopeArgs {
     const int *targets;
     int V;
     const float *logSum, *dloss;
-    float *sums;                // [rows / kSlopeRows][stride]: column sums, or null
+    float *sums;                // [rows / rowsEach][stride]: column sums, or null
+    int rowsEach;
     int parts;                  // dz in two parts, the second M rows below
     float *rests;               // [M]: what rounding left of dz at the targets, or null
 };
-constexpr int kSlopeRows = 32;
+// Rows to a workgroup, and where there would be less than one for each compute unit (40 rows of 5003: 24 us with 32 rows to each, 5.2 with 4).
+constexpr int kSlopeRows = 32, kSlopeRowsFew = 4;
 
-// A thread takes four columns of kSlopeRows rows.
+// A thread takes four columns of rowsEach rows.
 template <class TZ>
 __global__ __launch_bounds__(256) void slope_kernel(const SlopeArgs a) {
     const int across = (int)((a.stride + 1023) / 1024);
-    const long long tasks = (long long)across * ((a.M + kSlopeRows - 1) / kSlopeRows);
+    const long long tasks = (long long)across * ((a.M + a.rowsEach - 1) / a.rowsEach);
     for (long long task = blockIdx.x; task < tasks; task += gridDim.x) {
         const int n = (int)(task % across) * 1024 + (int)threadIdx.x * 4;
-        const long long block = task / across, m0 = block * kSlopeRows;
+        const long long block = task / across, m0 = block * a.rowsEach;
         if (n >= a.columns && (n & ~7) >= a.columns) continue;      // (nothing of the last eight)
         float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int r = 0; r < kSlopeRows; ++r) {
+        for (int r = 0; r < a.rowsEach; ++r) {
             const long long m = m0 + r;
             if (m >= a.M) break;
             const float4 q = *reinterpret_cast<const float4 *>(a.logits + m * a.stride + n);
@@ -479,6 +481,7 @@ struct BackwardPlan {
     bool sum;            // dx is summed in floats first
     bool rests;          // what rounding dz leaves at the targets goes back in
     long long rows;      // of dz: its parts'
+    int slopeRows;       // rows to a workgroup of slope_kernel
     size_t logits, dz, dx, x, sums, restsAt, firstOf, lastOf, restRows, room, total, room_bytes;
 };
 // dx, dw: null where that gradient is not asked for
@@ -502,7 +505,8 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
     p.logits = p.direct || elem == 4 ? p.dz : r.take((size_t)x.rows * p.pieces.stride * 4);
     p.dx = r.take(p.sum ? (size_t)p.rows * C * 4 : 0);
     p.x = r.take(p.parts && dw ? (size_t)p.rows * round_up(C, 8) * 2 : 0);
-    p.sums = r.take((size_t)((x.rows + 255) / 256 * 256 / kLeastRows) * p.pieces.stride * 4);
+    p.slopeRows = (p.pieces.stride + 1023) / 1024 * ((x.rows + kSlopeRows - 1) / kSlopeRows) < h->computeUnits ? kSlopeRowsFew : kSlopeRows;
+    p.sums = r.take((size_t)std::max((x.rows + 255) / 256 * 256 / kLeastRows, p.direct ? 0ll : (x.rows + p.slopeRows - 1) / p.slopeRows) * p.pieces.stride * 4);
     p.rests = t == IGC_DATA_BFLOAT16 && !p.parts && (dx || dw);
     p.restsAt = r.take(p.rests ? (size_t)x.rows * 4 : 0);
     p.firstOf = r.take(p.rests && dw ? (size_t)p.pieces.size * 4 : 0);
@@ -643,7 +647,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
     if (workSpaceSizeInBytes < p.total) return IGC_STATUS_BAD_PARAM;
     const float dx_beta = *static_cast<const float *>(beta), w_beta = *static_cast<const float *>(paramBeta);
     uint8_t *ws = static_cast<uint8_t *>(workSpace);
-    const long long row_blocks = (M + kSlopeRows - 1) / kSlopeRows;
+    const long long row_blocks = (M + p.slopeRows - 1) / p.slopeRows;
     float *rests = p.rests ? reinterpret_cast<float *>(ws + p.restsAt) : nullptr;
     if (p.parts && !p.few && dw) {
         TwiceArgs q{static_cast<const uint16_t *>(x), reinterpret_cast<uint16_t *>(ws + p.x), mx.stride, round_up(C, 8), M, C};
@@ -687,7 +691,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             a.y = ws + p.logits;
             if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
             SlopeArgs q{reinterpret_cast<const float *>(ws + p.logits), ws + p.dz, p.pieces.stride, M, columns, first, *static_cast<const float *>(alpha), targets, V,
-                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums, p.parts ? 1 : 0, rests};
+                        static_cast<const float *>(logSum), static_cast<const float *>(dloss), sums, p.slopeRows, p.parts ? 1 : 0, rests};
             st = launch_kernel(t == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&slope_kernel<float>) : reinterpret_cast<const void *>(&slope_kernel<bf16_t>), q,
                                dim3(grid_of((p.pieces.stride + 1023) / 1024 * row_blocks)), 256, handle->stream);
             if (st != IGC_STATUS_SUCCESS) return st;
