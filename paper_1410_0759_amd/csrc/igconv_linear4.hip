@@ -511,7 +511,7 @@ struct FewPlan {
 // 64 x 128), at groups of 64; of 17 to 32 and more tokens in the few-token kernels, a block to each wavefront (kCrooked: bfloat16 rows off 16-byte boundaries); of a launch and a
 // tile's start; bytes per us of ranges' sums that are stored and read.  2048 x 4096 -> 8192 one round of 256 x 256, 128 us, or two of 128 x 256, 157; 64 x 4096 -> 16384, groups of
 // 128: 64 x 128 in one, two, four and eight ranges 27.7, 23.1, 23.8 and 31.5 us, 128 x 128 39.5, 29.1, 35.7 and 46.8, few-token kernel 44.8; 64 x 1024 -> 2048 tiles 9.5, few-token
-// kernel 7.4; float 64 x 4096 -> 10880 and the like 33 and 107; 100 x 5001 -> 2003 20 and 36.
+// kernel 7.4; float 64 x 4096 -> 10880 30 and 77; 100 x 5001 -> 2003 20 and 36.
 constexpr double kBlockUs[kTile4Shapes] = {2.45, 1.2, 4.0, 0.8}, kTwoBlocksUs = 1.45, kPartsBlockUs[kTile4Shapes] = {2.1, 0.0, 0.0, 1.35}, kFewBlockUs[3] = {0.0, 2.5, 4.6},
                  kFewPartsBlockUs[3] = {0.0, 4.5, 11.5}, kCrooked = 1.7, kLaunchUs = 3.5, kStartUs = 1.5, kSumBytes = 6e6;
 double sums_us(long long splits, const Linear4Args &a) { return splits > 1 ? kLaunchUs + (double)splits * a.M * a.N * 8 / kSumBytes : 0.0; }
@@ -540,7 +540,7 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
         const long long rounds = (tiles(q.kb) * q.splits + h->computeUnits - 1) / h->computeUnits;
         return rounds * ((q.per + 7) / 8) * block_us(q.kb) + kLaunchUs * (1 + q.lay) + sums_us(q.splits, a);
     };
-    // Without ranges: of sixteen tokens as many rows of W to a workgroup as cost least (1 x 4096 -> 10880 and the like, groups of 128: 16, 32 and 64 rows 15.8, 14.6 and 12.1 us,
+    // Without ranges: of sixteen tokens as many rows of W to a workgroup as cost least (1 x 4096 -> 10880, groups of 128: 16, 32 and 64 rows 15.8, 14.6 and 12.1 us,
     // 1 x 8192 -> 8192 16.6, 14.4 and 19.7), of more 32 where that leaves one workgroup for each compute unit.
     p.us = cost(p);
     for (FewPlan q = p; q.kb < most;) {
@@ -551,10 +551,8 @@ FewPlan plan_few(const igcContext *h, igcDataType in, const Linear4Args &a, size
     }
     // Ranges, each of a block for every wavefront at least, where they cost less with the second launch.
     if (p.kb < most || p.tb == 1) {
-        // (of more than sixteen tokens a workgroup fills a compute unit: 64 x 5001 -> 2003 bfloat16 in 5 ranges 32 us, in 4 23; of fewer float
-        // tokens two run beside each other: 1 x 4096 -> 10880 and the like 22 us in two ranges, 25 in one)
-        const long long fit = parts && p.tb == 1 ? (h->computeUnits + tiles(most) - 1) / tiles(most) : std::max(1ll, h->computeUnits / tiles(most));
-        const int splits = (int)std::min<long long>(fit, (blocks + 7) / 8);
+        // (no more workgroups than compute units: 64 x 5001 -> 2003 bfloat16 in 5 ranges 32 us, in 4 23; 1 x 4096 -> 10880 float in two 21, in one 16)
+        const int splits = (int)std::min<long long>(std::max(1ll, h->computeUnits / tiles(most)), (blocks + 7) / 8);
         const size_t bytes = (size_t)splits * a.M * round_up(a.N, 4) * 4;
         FewPlan q = p;
         q.kb = most;
