@@ -300,37 +300,48 @@ struct RestRowsArgs {
     uint16_t *to;               // [M][toRow]: of a target's first row
 };
 constexpr int kRestColumns = 2048, kRestRows = 2048;     // rows looked at at once, eight to a thread
-__global__ __launch_bounds__(256) void rest_rows_kernel(const RestRowsArgs a) {
+// (4096 x 4096 -> 8000 in all: 671 us with targets at random, 1404 with all of them the same, which one workgroup's rows add four at a time; eight at a time 697 and 1254.)
+__global__ __launch_bounds__(256, 5) void rest_rows_kernel(const RestRowsArgs a) {
     __shared__ int list[kRestRows], counts[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.y * kRestColumns + (int)threadIdx.x * 8;
+    __shared__ float sums[256][8];
+    // a row by as many threads as it has eighths, rows in turns by the others
+    int across = 256;
+    while (across > 1 && across / 2 * 8 >= a.toRow) across /= 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turns = 256 / across, turn = (int)threadIdx.x / across;
+    const int c = (int)blockIdx.y * kRestColumns + ((int)threadIdx.x % across) * 8;
     for (int m0 = blockIdx.x; m0 < a.M; m0 += (int)gridDim.x) {
         const int t = a.targets[m0];
         const uint32_t v = (uint32_t)t - (uint32_t)a.first;
         if (v >= (uint32_t)a.columns || a.firstOf[v] != m0) continue;
         const int last = a.lastOf[v];
         float sum[8] = {};
-        // four rows at once, added one after the other
-        auto add = [&](const int *rows, int n) __attribute__((always_inline)) {
-            Adjacent<uint16_t, 8> q[4];
-            float rest[4];
+        // up to AT_ONCE rows at once, added one after the other (beyond the last: the first again, not added; no branches between the loads)
+        auto add = [&](auto at_once, const int *rows, int n) __attribute__((always_inline)) {
+            constexpr int AT_ONCE = decltype(at_once)::value;
+            Adjacent<uint16_t, 8> q[AT_ONCE];
+            float rest[AT_ONCE];
+            int m[AT_ONCE];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int m = rows[k < n ? k : 0];
-                const uint16_t *from = a.x + m * a.stride + c;
-                rest[k] = a.rests[m];
-                if (c + 8 <= a.C) q[k] = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(from);
-                else
+            for (int k = 0; k < AT_ONCE; ++k) m[k] = rows[k * turns < n ? k * turns : 0];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) q[k].v[e] = c + e < a.C ? from[e] : (uint16_t)0;
-            }
+            for (int k = 0; k < AT_ONCE; ++k) rest[k] = a.rests[m[k]];
+            if (c + 8 <= a.C)
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k < n)
+                for (int k = 0; k < AT_ONCE; ++k) q[k] = *reinterpret_cast<const Adjacent<uint16_t, 8> *>(a.x + m[k] * a.stride + c);
+            else
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q[k].v[e] = c + e < a.C ? a.x[m[k] * a.stride + c + e] : (uint16_t)0;
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (k * turns < n)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] += rest[k] * bf16_bits_to_float(q[k].v[e]);
         };
-        if (last == m0) add(&m0, 1);
-        else
+        if (last == m0) {
+            if (turn == 0) add(std::integral_constant<int, 1>(), &m0, 1);
+        } else {
             for (long long from = m0; from <= last; from += kRestRows) {
                 const long long m = from + (int)threadIdx.x * 8;
                 uint32_t same = 0;
@@ -351,9 +362,19 @@ __global__ __launch_bounds__(256) void rest_rows_kernel(const RestRowsArgs a) {
                 for (; same; same &= same - 1) list[place++] = (int)m + __builtin_ctz(same);
                 const int n = counts[0] + counts[1] + counts[2] + counts[3];
                 __syncthreads();
-                for (int k = 0; k < n; k += 4) add(list + k, n - k);
+                for (int k = turn; k < n; k += 4 * turns) add(std::integral_constant<int, 4>(), list + k, n - k);
             }
-        if (c >= a.toRow) continue;
+            if (turns > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sums[threadIdx.x][e] = sum[e];
+                __syncthreads();
+                for (int w = 1; w < turns && turn == 0; ++w)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += sums[threadIdx.x + w * across][e];
+            }
+        }
+        if (c >= a.toRow || turn > 0) continue;
         uint16_t *to = a.to + m0 * a.toRow + c;
         *reinterpret_cast<uint4 *>(to) = uint4{to_bf16_pair(sum[0], sum[1]), to_bf16_pair(sum[2], sum[3]), to_bf16_pair(sum[4], sum[5]), to_bf16_pair(sum[6], sum[7])};
     }
