@@ -29,7 +29,7 @@ __all__ = [
     "get_linear_backward_filter_workspace_size", "linear_backward_filter",
     "AdamWParameters", "AdamWTensor", "adamw_step",
     "get_linear_cross_entropy_forward_workspace_size", "linear_cross_entropy_forward", "get_linear_cross_entropy_backward_workspace_size",
-    "linear_cross_entropy_backward",
+    "linear_cross_entropy_backward", "set_cross_entropy_slopes", "get_cross_entropy_slopes",
     "get_filter4_size", "quantize_filter4", "dequantize_filter4", "get_linear4_forward_workspace_size", "linear4_forward",
 ]
 
@@ -140,6 +140,8 @@ DECLARED_SYMBOLS = {
     "igcAdamWStep": (_i, [_vp, _P(AdamWParameters), _i, _P(AdamWTensor)]),
     "igcGetLinearCrossEntropyForwardWorkspaceSize": (_i, [_vp] * 3 + [_P(_sz)]),
     "igcLinearCrossEntropyForward": (_i, [_vp] * 8 + [_sz, _vp, _vp]),
+    "igcSetCrossEntropySlopes": (_i, [_vp, _i]),
+    "igcGetCrossEntropySlopes": (_i, [_vp, _P(_i)]),
     "igcGetLinearCrossEntropyBackwardWorkspaceSize": (_i, [_vp] * 5 + [_P(_sz)]),
     "igcLinearCrossEntropyBackward": (_i, [_vp] * 11 + [_sz] + [_vp] * 7),
     "igcGetFilter4Size": (_i, [_vp, _i, _P(_sz), _P(_sz)]),
@@ -555,6 +557,17 @@ def linear_cross_entropy_forward(handle, xdesc, x_ptr, wdesc, w_ptr, bias_ptr, t
     """igcLinearCrossEntropyForward; the bias and log_sum pointers may be 0.  targets: 32-bit integers."""
     return lib().igcLinearCrossEntropyForward(handle.ptr, xdesc.ptr, _vp(x_ptr), wdesc.ptr, _vp(w_ptr), _vp(bias_ptr), _vp(targets_ptr), _vp(workspace_ptr),
                                               workspace_bytes, _vp(loss_ptr), _vp(log_sum_ptr))
+
+
+def set_cross_entropy_slopes(handle, dtype):
+    """IGC_DATA_BFLOAT16 (at first) or IGC_DATA_FLOAT: what the logits' gradients of bfloat16 features go into the products as."""
+    check(lib().igcSetCrossEntropySlopes(handle.ptr, dtype), "igcSetCrossEntropySlopes")
+
+
+def get_cross_entropy_slopes(handle):
+    out = _i()
+    check(lib().igcGetCrossEntropySlopes(handle.ptr, ctypes.byref(out)), "igcGetCrossEntropySlopes")
+    return out.value
 
 
 def get_linear_cross_entropy_backward_workspace_size(handle, xdesc, wdesc, dxdesc, dwdesc):

@@ -437,10 +437,10 @@ constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a
 // (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
 // Few enough tokens and vocabulary entries for the kernel of igconv_cross_entropy_few.hip (figures there).
 bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens && V <= 128 * h->computeUnits; }
-// Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: a tile's 64 rows have room for both.  More rows would pay for the
-// second part in full, and put back what is left at the targets instead.
+// Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: a tile's 64 rows have room for both.  More rows pay for the second part
+// in full (4096 x 4096 -> 65536 8290 us for 5180, 777 x 1000 -> 10007 143 for 112): by the handle's choice; else what is left at the targets is put back instead.
 constexpr int kPartsRows = 32;
-bool in_parts(igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && x.rows <= kPartsRows; }
+bool in_parts(igcHandle_t h, igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && (x.rows <= kPartsRows || h->crossEntropySlopes == IGC_DATA_FLOAT); }
 struct ForwardPlan {
     bool few, whole;     // few tokens; else whether the tiles leave the statistics, no logits in memory
     Pieces pieces;
@@ -510,7 +510,7 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
     BackwardPlan p;
     const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
     p.few = few_tokens(h, t, x, V);
-    p.parts = in_parts(t, x);
+    p.parts = in_parts(h, t, x);
     p.rows = p.parts ? 2 * x.rows : x.rows;
     p.pieces = pieces_of(p.rows, V, elem);
     p.direct = p.few;
@@ -565,6 +565,8 @@ igcStatus check_sizes(igcTensorDescriptor_t x, igcFilterDescriptor_t w, Matrix *
     if ((x->dtype != IGC_DATA_FLOAT && x->dtype != IGC_DATA_BFLOAT16) || w->dtype != x->dtype || !matrix_of(*x, mx) || w->k > kMostColumns) return IGC_STATUS_NOT_SUPPORTED;
     return IGC_STATUS_SUCCESS;
 }
+// (two parts: their rows are counted as a product's)
+igcStatus check_rows(igcHandle_t h, igcDataType t, const Matrix &x) { return in_parts(h, t, x) && x.rows > kMostRows / 2 ? IGC_STATUS_NOT_SUPPORTED : IGC_STATUS_SUCCESS; }
 igcStatus check_gradients(igcTensorDescriptor_t x, igcFilterDescriptor_t w, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, Matrix *mdx) {
     const auto type = [&](igcDataType t) { return t == IGC_DATA_FLOAT || (t == IGC_DATA_BFLOAT16 && x->dtype == IGC_DATA_BFLOAT16); };
     if ((dx && !dx->set) || (dw && !dw->set)) return IGC_STATUS_NOT_INITIALIZED;
@@ -640,12 +642,26 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
     return launch_kernel(reinterpret_cast<const void *>(&loss_kernel), q, dim3(grid_of((M + 63) / 64)), 1024, handle->stream);
 }
 
+igcStatus igcSetCrossEntropySlopes(igcHandle_t handle, igcDataType type) {
+    if (!handle || (type != IGC_DATA_BFLOAT16 && type != IGC_DATA_FLOAT)) return IGC_STATUS_BAD_PARAM;
+    handle->crossEntropySlopes = type;
+    return IGC_STATUS_SUCCESS;
+}
+
+igcStatus igcGetCrossEntropySlopes(igcHandle_t handle, igcDataType *type) {
+    if (!handle || !type) return IGC_STATUS_BAD_PARAM;
+    *type = handle->crossEntropySlopes;
+    return IGC_STATUS_SUCCESS;
+}
+
 igcStatus igcGetLinearCrossEntropyBackwardWorkspaceSize(igcHandle_t handle, igcTensorDescriptor_t xDesc, igcFilterDescriptor_t wDesc, igcTensorDescriptor_t dxDesc,
                                                         igcFilterDescriptor_t dwDesc, size_t *sizeInBytes) {
     if (!handle || !sizeInBytes) return IGC_STATUS_BAD_PARAM;
     Matrix x, dx;
     igcStatus st = check_sizes(xDesc, wDesc, &x);
-    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &dx)) != IGC_STATUS_SUCCESS) return st;
+    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &dx)) != IGC_STATUS_SUCCESS ||
+        (st = check_rows(handle, xDesc->dtype, x)) != IGC_STATUS_SUCCESS)
+        return st;
     *sizeInBytes = plan_backward(handle, xDesc->dtype, dxDesc, dwDesc, x, wDesc->c, wDesc->k).total;
     return IGC_STATUS_SUCCESS;
 }
@@ -658,7 +674,9 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
     if (!handle || !alpha || !beta || !paramBeta || !x || !w || !targets || !logSum || !workSpace || (!dx && !dw && !dbias) || (dx && !dxDesc) || (dw && !dwDesc)) return IGC_STATUS_BAD_PARAM;
     Matrix mx, mdx;
     igcStatus st = check_sizes(xDesc, wDesc, &mx);
-    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &mdx)) != IGC_STATUS_SUCCESS) return st;
+    if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &mdx)) != IGC_STATUS_SUCCESS ||
+        (st = check_rows(handle, xDesc->dtype, mx)) != IGC_STATUS_SUCCESS)
+        return st;
     const igcDataType t = xDesc->dtype;
     if (off(x, elem_size(t)) || off(w, elem_size(t)) || off(bias, 4) || off(targets, 4) || off(logSum, 4) || off(dloss, 4) || off(workSpace, 16) ||
         (dx && off(dx, elem_size(dxDesc->dtype))) || (dw && off(dw, elem_size(dwDesc->dtype))) || off(dbias, 4))

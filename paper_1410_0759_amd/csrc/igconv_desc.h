@@ -11,6 +11,7 @@ struct igcContext {
     void *stream = nullptr;
     int kernelOverride = -1;
     int computeUnits = 256;   // of the device current when the handle was created (MI355X's 256 when there is none)
+    igcDataType crossEntropySlopes = IGC_DATA_BFLOAT16;   // what dz of bfloat16 features goes into the products as
 };
 
 struct igcTensorStruct {

@@ -17,7 +17,7 @@ ENDS = {"loss": ("false, false", "RowStatistics"), "slopes": ("false, false", "S
 def check_names(names, ends):
     for end in ends.split():
         kernel, what = ENDS[end]
-        assert any(LARGE + kernel in n and what in n for n in names), (end, names)
+        assert any(LARGE + kernel in n and "igc::" + what in n for n in names), (end, names)
 
 
 def a_case(M, C, V, layout=(0, 0), units=256, repeat=0, **more):
