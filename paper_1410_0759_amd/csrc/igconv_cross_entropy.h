@@ -61,7 +61,7 @@ struct CrossPlan {
 CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);
 igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, const CrossEnd &end, void *workSpace, size_t bytes,
                         CrossPlan *taken);
-// A product of bfloat16 operands with rows added (of a layout that the tiles do not take: without them), and its room.
+// A product of bfloat16 operands with rows added, of any layout, and its room.
 igcStatus product_with_rows(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a, const RowAddend &add, void *workSpace, size_t bytes);
 size_t product_with_rows_room(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a);
 // The same for at most kFewTokens tokens of bfloat16 features, of any layout (igconv_cross_entropy_few.hip).  Slopes: dz in two parts; x is copied to z (rows zs apart, from 16-byte

@@ -78,8 +78,19 @@ __device__ __forceinline__ void load_any(const void *from, long long sr, long lo
     }
 }
 
-template <class T, class TO>
-__global__ __launch_bounds__(256) void linear_any_kernel(const LinearArgs p) {
+struct AnyAddendArgs : LinearArgs {
+    RowAddend add;
+};
+// a result of the product, with what is added before the epilogue
+__device__ __forceinline__ float with_addend(const LinearArgs &, int, int, float d) { return d; }
+__device__ __forceinline__ float with_addend(const AnyAddendArgs &p, int m, int n, float d) {
+    const uint32_t at = (uint32_t)p.add.rowOf[m] - (uint32_t)p.add.first;
+    if (at >= (uint32_t)p.add.count) return d;
+    return d + (p.add.factor ? p.add.factor[m] : 1.f) * bf16_bits_to_float(p.add.from[at * p.add.stride + n]);
+}
+
+template <class T, class TO, class Args = LinearArgs>
+__global__ __launch_bounds__(256) void linear_any_kernel(const Args p) {
     typedef AnyTile<T> Tile;
     __shared__ __attribute__((aligned(16))) typename Tile::lds_t la[kAnyTile * Tile::ROW], lb[kAnyTile * Tile::ROW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
@@ -103,7 +114,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(const LinearArgs p) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int n = n0 + wn + 8 * (v >> 2) + 4 * half + (v & 3);
-            if (m < p.M && n < p.N) finish_element<TO>(p, m, n, acc[v]);
+            if (m < p.M && n < p.N) finish_element<TO>(p, m, n, with_addend(p, m, n, acc[v]));
         }
     }
 }
@@ -517,6 +528,10 @@ igcStatus join_ranges(igcHandle_t handle, igcDataType out, const TileArgs &t) {
                          dim3((unsigned)f.partsGroups), 256, handle->stream);
 }
 
+dim3 any_grid(const LinearArgs &a) {
+    return dim3((unsigned)std::min((long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile), kMostGroups));
+}
+
 igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const LinearArgs &a, void *workSpace, size_t bytes, const SumsOut &sums = SumsOut(),
                       bool *summed = nullptr) {
     const TilePlan pl = plan_tiles(handle, in, out, a, sums.out != nullptr, workSpace && on16(workSpace) ? bytes : 0);
@@ -541,10 +556,8 @@ igcStatus run_product(igcHandle_t handle, igcDataType in, igcDataType out, const
         }
         return rc;
     }
-    const long long tiles = (long long)((a.M + kAnyTile - 1) / kAnyTile) * ((a.N + kAnyTile - 1) / kAnyTile);
     return by_types(in, out, [&](auto ti, auto to) {
-        return launch_kernel(reinterpret_cast<const void *>(&linear_any_kernel<decltype(ti), decltype(to)>), a, dim3((unsigned)std::min(tiles, kMostGroups)), 256,
-                             handle->stream);
+        return launch_kernel(reinterpret_cast<const void *>(&linear_any_kernel<decltype(ti), decltype(to)>), a, any_grid(a), 256, handle->stream);
     });
 }
 
@@ -602,7 +615,13 @@ igcStatus cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, cons
 
 igcStatus product_with_rows(igcHandle_t handle, CrossKind kind, igcDataType out, const LinearArgs &a, const RowAddend &add, void *workSpace, size_t bytes) {
     const TilePlan pl = plan_tiles(handle, IGC_DATA_BFLOAT16, out, a, false, bytes, &kind);
-    if (!pl.tiles) return product(handle, IGC_DATA_BFLOAT16, out, a, workSpace, bytes);
+    if (!pl.tiles) {
+        AnyAddendArgs t{};
+        static_cast<LinearArgs &>(t) = a;
+        t.add = add;
+        return launch_kernel(out == IGC_DATA_FLOAT ? reinterpret_cast<const void *>(&linear_any_kernel<bf16_t, float, AnyAddendArgs>)
+                                                   : reinterpret_cast<const void *>(&linear_any_kernel<bf16_t, bf16_t, AnyAddendArgs>), t, any_grid(a), 256, handle->stream);
+    }
     AddendArgs t{};
     igcStatus rc = begin_tiles(handle, pl, IGC_DATA_BFLOAT16, a, static_cast<uint8_t *>(workSpace), t);
     if (rc != IGC_STATUS_SUCCESS) return rc;
