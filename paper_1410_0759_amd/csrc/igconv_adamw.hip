@@ -240,7 +240,8 @@ __device__ __forceinline__ void update(const AdamWEntry &t, const Constants &c, 
             load4<float, STREAM>(t.v, at, left, v[b]);
         }
     }
-    const float shrink = 1.f - c.rate * t.decay;
+    // (subtracted as it is: 1 - rate decay has steps of 2^-24, a fifth of a decay of 1e-7 and all of one of 2e-8.  An infinite weight stays one.)
+    const float decay = c.rate * t.decay, largest = 0x1.fffffep127f;
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
         const long long block = begin + b * kBlock, at = block + lane * 4, rest = t.count - at;
@@ -256,7 +257,8 @@ __device__ __forceinline__ void update(const AdamWEntry &t, const Constants &c, 
             if constexpr (EIGHT) m[b][e] *= ms[b], v[b][e] *= vs[b];
             m[b][e] = m[b][e] * c.keep1 + gs * c.take1;
             v[b][e] = v[b][e] * c.keep2 + gs * gs * c.take2;
-            p[b][e] = p[b][e] * shrink - c.rate * (m[b][e] * c.correct1 * __builtin_amdgcn_rcpf(root(v[b][e] * c.correct2) + c.epsilon));
+            const float change = c.rate * (m[b][e] * c.correct1 * __builtin_amdgcn_rcpf(root(v[b][e] * c.correct2) + c.epsilon));
+            p[b][e] -= __builtin_fmaf(decay, __builtin_amdgcn_fmed3f(p[b][e], -largest, largest), change);
         }
         store4<TP>(t.param, at, left, p[b]);
         if (t.copy) store4<bf16_t>(t.copy, at, left, p[b]);
