@@ -56,6 +56,7 @@ TileKernel cross_float_kernel(CrossKind kind);
 struct CrossPlan {
     double us = -1.0;
     size_t room = 0;
+    bool copiesB = false;      // the second operand is copied first
     int tileColumns = 0, sumBlocks = 0;
 };
 CrossPlan plan_cross_product(igcHandle_t handle, CrossKind kind, igcDataType in, const LinearArgs &a, size_t room);

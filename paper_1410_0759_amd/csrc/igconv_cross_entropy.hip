@@ -389,12 +389,13 @@ unsigned grid_of(long long groups) { return (unsigned)std::min(std::max(groups, 
 
 // The vocabulary in pieces of `size` entries, a multiple of 256 unless it is the whole; `bytes` to an entry of a row.  (Tiles take rows of less than 2^22
 // elements.)
+constexpr long long kMostEntries = 1ll << 20;
 struct Pieces {
     int size, count;
     long long stride;      // of the rows of a piece, elements
 };
-Pieces pieces_of(long long M, int V, size_t bytes) {
-    const long long most = std::min(std::max((long long)(kPieceBytes / bytes) / M / 256 * 256, 256ll), 1ll << 20);
+Pieces pieces_of(long long M, int V, size_t bytes, long long limit = kMostEntries) {
+    const long long most = std::min(std::max((long long)(kPieceBytes / bytes) / M / 256 * 256, 256ll), limit);
     Pieces p;
     if (V <= most) {
         p.size = V;
@@ -415,6 +416,9 @@ struct Room {
         return at;
     }
 };
+
+// Where w is copied first, it goes by pieces of so many entries: kPieceBytes of copies.
+long long copied_entries(igcDataType t, int C) { return std::max((long long)kPieceBytes / (t == IGC_DATA_FLOAT ? round_up(C, 32) * 6 : round_up(C, 8) * 2) / 256 * 256, 256ll); }
 
 LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns) {
     LinearArgs a{};
@@ -453,6 +457,7 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
     p.few = few_tokens(h, t, x, V);
     if (p.few) {
         p.whole = true;
+        p.pieces = Pieces{V, 1, 0};
         p.ranges = (V + cross_few_columns(h, V) - 1) / cross_few_columns(h, V);
         p.logits = p.room = p.room_bytes = 0;
         Room r;
@@ -462,12 +467,27 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
         return p;
     }
     // (the last piece may be smaller, and then take other tiles)
-    p.room_bytes = product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, p.pieces.size));
-    if (p.pieces.count > 1)
-        p.room_bytes = std::max(p.room_bytes, product_room(h, t, IGC_DATA_FLOAT, logits_product(x, C, p.pieces, V - (p.pieces.count - 1) * p.pieces.size)));
-    const CrossPlan cross = plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, V), kNoLimit);
-    p.whole = cross.us >= 0.0 && cross.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes);
-    if (p.whole) p.room_bytes = cross.room;
+    auto most_room = [&](const Pieces &q, auto room) {
+        return q.count > 1 ? std::max(room(logits_product(x, C, q, q.size)), room(logits_product(x, C, q, V - (q.count - 1) * q.size))) : room(logits_product(x, C, q, V));
+    };
+    auto cross = [&](int columns) { return plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, columns), kNoLimit); };
+    auto in_memory = [&](const LinearArgs &a) { return product_room(h, t, IGC_DATA_FLOAT, a); };
+    Pieces whole{V, 1, 0};
+    CrossPlan all = cross(V);
+    if (all.us < 0.0 || all.copiesB) whole = pieces_of(1, V, 4, copied_entries(t, C));
+    if (all.us < 0.0) {
+        all = cross(whole.size);
+        all.us *= whole.count;
+    }
+    p.room_bytes = most_room(p.pieces, in_memory);
+    p.whole = all.us >= 0.0 && all.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes);
+    if (p.whole) {
+        p.pieces = whole;
+        p.room_bytes = most_room(whole, [&](const LinearArgs &a) { return plan_cross_product(h, kRowStatistics, t, a, kNoLimit).room; });
+    } else if ((t == IGC_DATA_FLOAT || C % 8 != 0) && p.room_bytes > kPieceBytes) {
+        p.pieces = pieces_of(x.rows, V, 4, copied_entries(t, C));
+        p.room_bytes = most_room(p.pieces, in_memory);
+    }
     p.ranges = p.whole ? (V + kLeastColumns - 1) / kLeastColumns : (p.pieces.size + kRange - 1) / kRange * p.pieces.count;
     Room r;
     p.logits = r.take(p.whole ? 0 : (size_t)x.rows * p.pieces.stride * 4);
@@ -607,28 +627,26 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
     RowPart *parts = reinterpret_cast<RowPart *>(ws + p.parts);
     float *picked = reinterpret_cast<float *>(ws + p.picked);
     int ranges = 0;
-    if (p.whole) {
-        LinearArgs a = logits_product(mx, C, p.pieces, V);
-        a.a = x;
-        a.b = w;
-        a.bias = static_cast<const float *>(bias);
-        CrossEnd end{};
-        end.targets = targets;
-        end.V = V;
-        end.parts = parts;
-        end.picked = picked;
-        CrossPlan taken;
-        taken.tileColumns = cross_few_columns(handle, V);
-        st = p.few ? cross_few(handle, kRowStatistics, a, end) : cross_product(handle, kRowStatistics, t, a, end, ws + p.room, p.room_bytes, &taken);
-        if (st != IGC_STATUS_SUCCESS) return st;
-        ranges = (V + taken.tileColumns - 1) / taken.tileColumns;
-    }
-    for (int first = 0; first < V && !p.whole; first += p.pieces.size) {
+    for (int first = 0; first < V; first += p.pieces.size) {
         const int columns = std::min(p.pieces.size, V - first);
         LinearArgs a = logits_product(mx, C, p.pieces, columns);
         a.a = x;
         a.b = static_cast<const uint8_t *>(w) + (size_t)first * C * elem_size(t);
         a.bias = bias ? static_cast<const float *>(bias) + first : nullptr;
+        if (p.whole) {
+            CrossEnd end{};
+            end.targets = targets;
+            end.first = first;
+            end.V = V;
+            end.parts = parts + (long long)ranges * M;
+            end.picked = picked;
+            CrossPlan taken;
+            taken.tileColumns = cross_few_columns(handle, V);
+            st = p.few ? cross_few(handle, kRowStatistics, a, end) : cross_product(handle, kRowStatistics, t, a, end, ws + p.room, p.room_bytes, &taken);
+            if (st != IGC_STATUS_SUCCESS) return st;
+            ranges += (columns + taken.tileColumns - 1) / taken.tileColumns;
+            continue;
+        }
         a.y = ws + p.logits;
         if ((st = product(handle, t, IGC_DATA_FLOAT, a, ws + p.room, p.room_bytes)) != IGC_STATUS_SUCCESS) return st;
         const int here = (columns + kRange - 1) / kRange;

@@ -595,6 +595,7 @@ static CrossPlan cross_plan(const TilePlan &pl) {
     if (!pl.tiles) return c;
     c.us = pl.us;
     c.room = pl.bytes;
+    c.copiesB = pl.b.pack;
     c.tileColumns = pl.k.bn;
     c.sumBlocks = pl.tilesM * pl.k.wavesM;
     return c;
