@@ -626,8 +626,9 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
  * the row of dw of an entry that is nobody's target.  igcSetCrossEntropySlopes(handle, IGC_DATA_FLOAT) has the second part of all elements go in, with any number of rows (up to
  * 2^29), in later calls and queries on the handle (which is asked for both): 2^-16 everywhere, about what exp leaves of it, for up to 1.6 times the time.  A row without target adds zeros times its x to dw: that x has to be finite.
  *
- * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports; less is BAD_PARAM.  For 8192
- * rows, 4096 features and 131072 entries that is 67 MB forward and 839 MB backward (slopes in two parts: 1.0 GB), as floats (copies of the operands in parts) 0.7 and 1.8 GB.
+ * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports, which counts x and w off 4-byte boundaries too; less than a call needs is
+ * BAD_PARAM.  For 8192 rows, 4096 features and 131072 entries that is 201 MB forward and 839 MB backward (slopes in two parts: 1.0 GB), as floats (copies of the operands in parts) 0.7 and
+ * 1.8 GB.
  * Float products are off as igcLinearForward's.  No output may overlap an input or another output.  Sums in a fixed order: results repeat bit by bit. */
 igcStatus igcSetCrossEntropySlopes(igcHandle_t handle, igcDataType type);      /* IGC_DATA_BFLOAT16 (at first) or IGC_DATA_FLOAT */
 igcStatus igcGetCrossEntropySlopes(igcHandle_t handle, igcDataType *type);

@@ -417,11 +417,42 @@ struct Room {
     }
 };
 
-// Where w is copied first, it goes by pieces of so many entries: kPieceBytes of copies.
-long long copied_entries(igcDataType t, int C) { return std::max((long long)kPieceBytes / (t == IGC_DATA_FLOAT ? round_up(C, 32) * 6 : round_up(C, 8) * 2) / 256 * 256, 256ll); }
+// Where the operands lie, as far as plans go by it: on 4-byte boundaries (null), x off them, or w, with which x may be.  The queries take the most that any place needs; calls have the room of
+// their own place asked of them.
+struct Places {
+    const void *x = nullptr, *w = nullptr;
+};
+constexpr uintptr_t kOff = 2;
+Places places_of(const void *x, const void *w) {
+    const void *off = reinterpret_cast<const void *>(kOff);
+    return (uintptr_t)w % 4 != 0 ? Places{off, off} : ((uintptr_t)x % 4 != 0 ? Places{off, nullptr} : Places());
+}
+// Rows from which on operands off the boundaries are copied for the tiles; fewer have tiles that take them through registers, in the room of those on boundaries.  (w off, x 4096 wide,
+// 32768 entries, loss and gradient: 256 rows copied 218 and 626 us, through registers 183 and 542, 1024 rows 382 and 1134, 663 and 1605; 777 x 1000 -> 10007 49 and 129, 71 and 200.)
+constexpr int kPlaceRows = 512;
+Places copied_places(const Matrix &x, const Places &at) { return x.rows < kPlaceRows ? Places() : at; }
 
-LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns) {
+template <class F>
+size_t most_of_places(igcDataType t, const Matrix &x, F total) {
+    const void *off = reinterpret_cast<const void *>(kOff);
+    size_t most = total(Places());
+    if (t == IGC_DATA_BFLOAT16) most = std::max(most, total(places_of(off, nullptr)));
+    if (t == IGC_DATA_BFLOAT16 && x.rows >= kPlaceRows) most = std::max(most, total(places_of(off, off)));
+    return most;
+}
+
+// Where w is copied first, it goes by pieces of so many entries: kPieceBytes of copies, less of a w that needs them for its place alone, for which every call's room is asked.
+constexpr size_t kPlaceBytes = (size_t)64 << 20;
+size_t copied_bytes(igcDataType t, int C) { return t == IGC_DATA_FLOAT || C % 8 != 0 ? kPieceBytes : kPlaceBytes; }
+long long copied_entries(igcDataType t, int C) {
+    const long long entry = t == IGC_DATA_FLOAT ? round_up(C, 32) * 6 : round_up(C, 8) * 2;
+    return std::max((long long)copied_bytes(t, C) / entry / 256 * 256, 256ll);
+}
+
+LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns, const Places &at = Places()) {
     LinearArgs a{};
+    a.a = at.x;
+    a.b = at.w;
     a.am = x.stride; a.ak = 1; a.bn = C; a.bk = 1;
     a.M = (int)x.rows; a.N = columns; a.K = C;
     a.alpha = 1.f;
@@ -432,13 +463,12 @@ LinearArgs logits_product(const Matrix &x, int C, const Pieces &p, int columns) 
 
 // Logits in memory are written and read once more, at bytes per us, by a second launch.
 constexpr double kLogitsBytes = 4.5e6, kLaunch = 3.0;
-double through_memory_us(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V, const Pieces &p, double bytes, size_t room) {
-    return p.count * (product_us(h, t, IGC_DATA_FLOAT, logits_product(x, C, p, p.size), room) + kLaunch) + (double)x.rows * V * bytes / kLogitsBytes;
+double through_memory_us(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V, const Pieces &p, double bytes, size_t room, const Places &at) {
+    return p.count * (product_us(h, t, IGC_DATA_FLOAT, logits_product(x, C, p, p.size, at), room) + kLaunch) + (double)x.rows * V * bytes / kLogitsBytes;
 }
 constexpr size_t kNoLimit = ~(size_t)0;
 constexpr int kLeastColumns = 128, kLeastRows = 32;     // of a wavefront's or a tile's entry in the statistics and the column sums
 
-// (Plans are made without the operands' addresses, in the query and in the call: rows off 4-byte boundaries take another kernel in the same room.)
 // Few enough tokens and vocabulary entries for the kernel of igconv_cross_entropy_few.hip (figures there).
 bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t == IGC_DATA_BFLOAT16 && x.rows <= kFewTokens && V <= 128 * h->computeUnits; }
 // Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: a tile's 64 rows have room for both.  More rows pay for the second part
@@ -451,7 +481,8 @@ struct ForwardPlan {
     int ranges;          // of all columns
     size_t logits, parts, picked, room, total, room_bytes;
 };
-ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
+ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V, const Places &places) {
+    const Places at = copied_places(x, places);
     ForwardPlan p;
     p.pieces = pieces_of(x.rows, V, 4);
     p.few = few_tokens(h, t, x, V);
@@ -468,9 +499,9 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
     }
     // (the last piece may be smaller, and then take other tiles)
     auto most_room = [&](const Pieces &q, auto room) {
-        return q.count > 1 ? std::max(room(logits_product(x, C, q, q.size)), room(logits_product(x, C, q, V - (q.count - 1) * q.size))) : room(logits_product(x, C, q, V));
+        return q.count > 1 ? std::max(room(logits_product(x, C, q, q.size, at)), room(logits_product(x, C, q, V - (q.count - 1) * q.size, at))) : room(logits_product(x, C, q, V, at));
     };
-    auto cross = [&](int columns) { return plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, columns), kNoLimit); };
+    auto cross = [&](int columns) { return plan_cross_product(h, kRowStatistics, t, logits_product(x, C, p.pieces, columns, at), kNoLimit); };
     auto in_memory = [&](const LinearArgs &a) { return product_room(h, t, IGC_DATA_FLOAT, a); };
     Pieces whole{V, 1, 0};
     CrossPlan all = cross(V);
@@ -480,11 +511,11 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
         all.us *= whole.count;
     }
     p.room_bytes = most_room(p.pieces, in_memory);
-    p.whole = all.us >= 0.0 && all.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes);
+    p.whole = all.us >= 0.0 && all.us <= through_memory_us(h, t, x, C, V, p.pieces, 8.0, p.room_bytes, at);
     if (p.whole) {
         p.pieces = whole;
         p.room_bytes = most_room(whole, [&](const LinearArgs &a) { return plan_cross_product(h, kRowStatistics, t, a, kNoLimit).room; });
-    } else if ((t == IGC_DATA_FLOAT || C % 8 != 0) && p.room_bytes > kPieceBytes) {
+    } else if ((t == IGC_DATA_FLOAT || C % 8 != 0 || at.w) && p.room_bytes > copied_bytes(t, C)) {
         p.pieces = pieces_of(x.rows, V, 4, copied_entries(t, C));
         p.room_bytes = most_room(p.pieces, in_memory);
     }
@@ -498,8 +529,9 @@ ForwardPlan plan_forward(igcHandle_t h, igcDataType t, const Matrix &x, int C, i
     return p;
 }
 
-LinearArgs data_product(long long rows, int C, const Pieces &p, int columns) {
+LinearArgs data_product(long long rows, int C, const Pieces &p, int columns, const Places &at) {
     LinearArgs a{};
+    a.b = at.w;
     a.am = p.stride; a.ak = 1; a.bn = 1; a.bk = C; a.strided_b = true; a.padded_a = true;
     a.M = (int)rows; a.N = C; a.K = columns;
     a.alpha = 1.f;
@@ -507,8 +539,9 @@ LinearArgs data_product(long long rows, int C, const Pieces &p, int columns) {
     return a;
 }
 // (parts: x as it was copied, once for each part of dz)
-LinearArgs filter_product(const Matrix &x, bool parts, int C, const Pieces &p, int columns) {
+LinearArgs filter_product(const Matrix &x, bool parts, int C, const Pieces &p, int columns, const Places &at) {
     LinearArgs a{};
+    a.b = parts ? nullptr : at.x;
     a.am = 1; a.ak = p.stride; a.bn = 1; a.bk = parts ? round_up(C, 8) : x.stride; a.padded_b = parts; a.strided_a = a.strided_b = true; a.padded_a = true;
     a.M = columns; a.N = C; a.K = (int)(parts ? 2 * x.rows : x.rows);
     a.alpha = 1.f;
@@ -526,20 +559,28 @@ struct BackwardPlan {
     size_t logits, dz, dx, x, sums, restsAt, firstOf, lastOf, restRows, room, total, room_bytes;
 };
 // dx, dw: null where that gradient is not asked for
-BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V) {
+BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, const Matrix &x, int C, int V, const Places &places) {
+    const Places at = copied_places(x, places);
     BackwardPlan p;
     const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
     p.few = few_tokens(h, t, x, V);
     p.parts = in_parts(h, t, x);
     p.rows = p.parts ? 2 * x.rows : x.rows;
-    p.pieces = pieces_of(p.rows, V, elem);
-    p.direct = p.few;
-    if (!p.few) {
-        const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size), kNoLimit);
-        const Pieces wide = pieces_of(p.rows, V, 4);
-        p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit);
+    auto in_pieces = [&](long long limit) {
+        p.pieces = pieces_of(p.rows, V, elem, limit);
+        p.direct = p.few;
+        if (p.few) return;
+        const CrossPlan cross = plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size, at), kNoLimit);
+        const Pieces wide = pieces_of(p.rows, V, 4, limit);
+        p.direct = cross.us >= 0.0 && cross.us * p.pieces.count <= through_memory_us(h, t, x, C, V, wide, 8.0 + elem, kNoLimit, at);
         if (!p.direct) p.pieces = wide;
-    }
+    };
+    in_pieces(kMostEntries);
+    // (w copied for its place alone: in smaller pieces)
+    if (at.w && C % 8 == 0 && p.pieces.size > copied_entries(t, C) &&
+        (plan_cross_product(h, kSlopes, t, logits_product(x, C, p.pieces, p.pieces.size, at), kNoLimit).copiesB ||
+         plan_cross_product(h, kDataWithRows, t, data_product(p.rows, C, p.pieces, p.pieces.size, at), kNoLimit).copiesB))
+        in_pieces(copied_entries(t, C));
     p.sum = dx && (p.parts || (p.pieces.count > 1 && dx->dtype == IGC_DATA_BFLOAT16));
     Room r;
     p.dz = r.take((size_t)p.rows * p.pieces.stride * elem);
@@ -557,20 +598,13 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
     for (int piece : {0, p.pieces.count - 1}) {
         // (the last piece may be smaller, and then take other tiles)
         const int columns = std::min(p.pieces.size, V - piece * p.pieces.size);
-        const LinearArgs logits = logits_product(x, C, p.pieces, columns);
+        const LinearArgs logits = logits_product(x, C, p.pieces, columns, at);
         if (!p.few) p.room_bytes = std::max(p.room_bytes, p.direct ? plan_cross_product(h, kSlopes, t, logits, kNoLimit).room : product_room(h, t, IGC_DATA_FLOAT, logits));
         auto room_of = [&](CrossKind kind, igcDataType out, const LinearArgs &a) {
             p.room_bytes = std::max(p.room_bytes, p.rests ? product_with_rows_room(h, kind, out, a) : product_room(h, t, out, a));
         };
-        if (dx) room_of(kDataWithRows, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns));
-        if (dw) {
-            LinearArgs f = filter_product(x, p.parts, C, p.pieces, columns);
-            room_of(kFilterWithRows, dw->dtype, f);
-            if (elem == 2) {      // (x off 4-byte boundaries: copied, else it would go element by element)
-                f.b = reinterpret_cast<const void *>(2);
-                room_of(kFilterWithRows, dw->dtype, f);
-            }
-        }
+        if (dx) room_of(kDataWithRows, p.sum ? IGC_DATA_FLOAT : dx->dtype, data_product(p.rows, C, p.pieces, columns, at));
+        if (dw) room_of(kFilterWithRows, dw->dtype, filter_product(x, p.parts, C, p.pieces, columns, places));      // (x off a boundary: copied, else it would go element by element)
         if (p.pieces.count == 1) break;
     }
     p.room = r.take(p.room_bytes);
@@ -608,7 +642,7 @@ igcStatus igcGetLinearCrossEntropyForwardWorkspaceSize(igcHandle_t handle, igcTe
     Matrix x;
     const igcStatus st = check_sizes(xDesc, wDesc, &x);
     if (st != IGC_STATUS_SUCCESS) return st;
-    *sizeInBytes = plan_forward(handle, xDesc->dtype, x, wDesc->c, wDesc->k).total;
+    *sizeInBytes = most_of_places(xDesc->dtype, x, [&](const Places &at) { return plan_forward(handle, xDesc->dtype, x, wDesc->c, wDesc->k, at).total; });
     return IGC_STATUS_SUCCESS;
 }
 
@@ -621,7 +655,7 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
     const igcDataType t = xDesc->dtype;
     if (off(x, elem_size(t)) || off(w, elem_size(t)) || off(bias, 4) || off(targets, 4) || off(loss, 4) || off(logSum, 4) || off(workSpace, 16)) return IGC_STATUS_BAD_PARAM;
     const int C = wDesc->c, V = wDesc->k, M = (int)mx.rows;
-    const ForwardPlan p = plan_forward(handle, t, mx, C, V);
+    const ForwardPlan p = plan_forward(handle, t, mx, C, V, places_of(x, w));
     if (workSpaceSizeInBytes < p.total) return IGC_STATUS_BAD_PARAM;
     uint8_t *ws = static_cast<uint8_t *>(workSpace);
     RowPart *parts = reinterpret_cast<RowPart *>(ws + p.parts);
@@ -680,7 +714,7 @@ igcStatus igcGetLinearCrossEntropyBackwardWorkspaceSize(igcHandle_t handle, igcT
     if (st != IGC_STATUS_SUCCESS || (st = check_gradients(xDesc, wDesc, dxDesc, dwDesc, &dx)) != IGC_STATUS_SUCCESS ||
         (st = check_rows(handle, xDesc->dtype, x)) != IGC_STATUS_SUCCESS)
         return st;
-    *sizeInBytes = plan_backward(handle, xDesc->dtype, dxDesc, dwDesc, x, wDesc->c, wDesc->k).total;
+    *sizeInBytes = most_of_places(xDesc->dtype, x, [&](const Places &at) { return plan_backward(handle, xDesc->dtype, dxDesc, dwDesc, x, wDesc->c, wDesc->k, at).total; });
     return IGC_STATUS_SUCCESS;
 }
 
@@ -700,7 +734,8 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
         (dx && off(dx, elem_size(dxDesc->dtype))) || (dw && off(dw, elem_size(dwDesc->dtype))) || off(dbias, 4))
         return IGC_STATUS_BAD_PARAM;
     const int C = wDesc->c, V = wDesc->k, M = (int)mx.rows;
-    const BackwardPlan p = plan_backward(handle, t, dxDesc, dwDesc, mx, C, V);
+    const Places at = places_of(x, w);
+    const BackwardPlan p = plan_backward(handle, t, dxDesc, dwDesc, mx, C, V, at);
     if (workSpaceSizeInBytes < p.total) return IGC_STATUS_BAD_PARAM;
     const float dx_beta = *static_cast<const float *>(beta), w_beta = *static_cast<const float *>(paramBeta);
     uint8_t *ws = static_cast<uint8_t *>(workSpace);
@@ -762,7 +797,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             if (st != IGC_STATUS_SUCCESS) return st;
         }
         if (dx) {
-            LinearArgs d = data_product(p.rows, C, p.pieces, columns);
+            LinearArgs d = data_product(p.rows, C, p.pieces, columns, at);
             d.a = ws + p.dz;
             d.b = piece;
             d.y = p.sum ? ws + p.dx : dx;
@@ -776,7 +811,7 @@ igcStatus igcLinearCrossEntropyBackward(igcHandle_t handle, const void *alpha, i
             if (st != IGC_STATUS_SUCCESS) return st;
         }
         if (dw) {
-            LinearArgs f = filter_product(mx, p.parts, C, p.pieces, columns);
+            LinearArgs f = filter_product(mx, p.parts, C, p.pieces, columns, at);
             f.a = ws + p.dz;
             f.b = p.parts ? ws + p.x : x;
             f.y = static_cast<uint8_t *>(dw) + (size_t)first * C * elem_size(dwDesc->dtype);
