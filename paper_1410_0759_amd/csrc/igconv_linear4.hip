@@ -509,7 +509,7 @@ struct FewPlan {
 };
 // us, measured, for the choice between kernels.  Of a block of 128 features: by the shape of a tile (of 64 x 128 one on a compute unit and two; float in parts: 64 x 256 and
 // 64 x 128), at groups of 64; of 17 to 32 and more tokens in the few-token kernels, a block to each wavefront (kCrooked: bfloat16 rows off 16-byte boundaries); of a launch and a
-// tile's start; bytes per us of ranges' sums that are stored and read.  2048 x 4096 -> 8192 one round of 256 x 256, 128 us, or two of 128 x 256, 157; 64 x 4096 -> 16384, groups of
+// tile's start; bytes per us of ranges' sums that are stored and read.  2048 x 4096 -> 8192 one round of 256 x 256, after some calls 128 us, or two of 128 x 256, 157; 64 x 4096 -> 16384, groups of
 // 128: 64 x 128 in one, two, four and eight ranges 27.7, 23.1, 23.8 and 31.5 us, 128 x 128 39.5, 29.1, 35.7 and 46.8, few-token kernel 44.8; 64 x 1024 -> 2048 tiles 9.5, few-token
 // kernel 7.4; float 64 x 4096 -> 10880 30 and 77; 100 x 5001 -> 2003 20 and 36.
 constexpr double kBlockUs[kTile4Shapes] = {2.45, 1.2, 4.0, 0.8}, kTwoBlocksUs = 1.45, kPartsBlockUs[kTile4Shapes] = {2.1, 0.0, 0.0, 1.35}, kFewBlockUs[3] = {0.0, 2.5, 4.6},

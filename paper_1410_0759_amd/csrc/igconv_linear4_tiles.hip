@@ -18,10 +18,11 @@ static TileKernel of_group(int shape, bool parts, bool f32_out) {
     if (shape == 3)
         return {Low::BM, Low::BN, Low::THREADS,
                 f32_out ? reinterpret_cast<const void *>(&linear4_tiles_kernel<Low, float>) : reinterpret_cast<const void *>(&linear4_tiles_kernel<Low, bf16_t>), Low::WAVES_M};
-    if (shape == 2 && GROUP == 32) return {};      // (spills registers: 4096 x 4096 -> 8192 324 us for 332)
-    if (shape == 2)
-        return {Widest::BM, Widest::BN, Widest::THREADS,
-                f32_out ? reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, float>) : reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, bf16_t>), Widest::WAVES_M};
+    if (shape == 2) {
+        if constexpr (GROUP == 32) return {};      // (spills registers: 4096 x 4096 -> 8192 324 us for 332)
+        else return {Widest::BM, Widest::BN, Widest::THREADS,
+                     f32_out ? reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, float>) : reinterpret_cast<const void *>(&linear4_wide_kernel<Widest, bf16_t>), Widest::WAVES_M};
+    }
     if (shape == 0)
         return {Wide::BM, Wide::BN, Wide::THREADS,
                 f32_out ? reinterpret_cast<const void *>(&linear4_tiles_kernel<Wide, float>) : reinterpret_cast<const void *>(&linear4_tiles_kernel<Wide, bf16_t>), Wide::WAVES_M};

@@ -3,7 +3,8 @@
 // know of the copies, would wait for all of them with it (2048 x 4096 -> 8192, groups of 64, tiles of 128 x 256: 198 us that way, 160 this way).
 //
 // A group's products are summed from zero, and multiplied by the group's scale into the result: 4 multiply-adds for each matrix instruction that ends
-// a group (groups of 32: all of them, of 128: every fourth).  Few tiles: the reduction in ranges of blocks, added by linear4_finish_kernel.  They follow the next unit's matrix instructions, which do not wait for them nor they for these.
+// a group (groups of 32: all of them, of 128: every fourth).  They follow the next unit's matrix instructions, which do not wait for them nor they for these.  Few tiles: the
+// reduction in ranges of blocks, added by linear4_finish_kernel.
 #ifndef IGCONV_LINEAR4_TILES_HPP_
 #define IGCONV_LINEAR4_TILES_HPP_
 
@@ -258,18 +259,19 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_tiles_kernel(const Li
 }
 
 // The same with 256 x 256 results: a wavefront's 128 tokens share its 64 rows' decoded codes, a step's at a time, and go through one block of 16 tokens after the other, so that
-// the groups' sums are 16 tokens by 64 rows at a time.  A group of 128 is added in two halves.  (2048 x 4096 -> 8192, groups of 64: 142 us, 160 with tiles of 128 x 256: half the
-// decoding, twice the matrix instructions between barriers.)
+// the groups' sums are 16 tokens by 64 rows at a time.  A group of 128 is added in two halves.  (2048 x 4096 -> 8192, groups of 64, the first 50 calls: 143 us, 160 with tiles of 128 x 256: half
+// the decoding, twice the matrix instructions between barriers.  After 150 calls 124.)
 template <class Cfg, class TO>
 __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Linear4Args p) {
-    constexpr int FM = Cfg::FM, FN = Cfg::FN, ENDS = Cfg::GROUP == 32 ? 2 : 1;      // groups' sums that end within a step (a half of one of 128)
+    static_assert(Cfg::GROUP >= 64, "");      // a step's sums are one group's, or half of one
+    constexpr int FM = Cfg::FM, FN = Cfg::FN;
     __shared__ __attribute__((aligned(16))) uint8_t lds[Cfg::LDS_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wm = wave / Cfg::WAVES_N, wn = wave % Cfg::WAVES_N;
     int tm, tn, split;
     if (!tile_of(p, &tm, &tn, &split)) return;
     Copies4<Cfg> copies;
-    copies.init(p, lds, tm, tn, split, lane, wave);
+    copies.init(p, lds, tm, tn, 0, lane, wave);      // (never in ranges)
     constexpr int R = Copies4<Cfg>::R, RC = Copies4<Cfg>::RC;
     OperandReads<Cfg::ROWS, FM, false, 2> reads;
     reads.init(wm * FM * 16, lane);
@@ -303,7 +305,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Lin
         for (int half = 0; half < 2; ++half) {
             const uint8_t *here = lds + xs * Cfg::X_BYTES;
             bf16x8 q[2][FN], x[2][2];
-            u32x2 scale[ENDS][FN];
+            u32x2 scale[FN];
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) x[0][kk] = reads.read(here, kk, 0);
 #pragma unroll
@@ -311,8 +313,7 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Lin
                 const u32x2 c = *reinterpret_cast<const u32x2 *>(copies.codes_of(cs, wn * FN + j) + half * 8);
                 q[0][j] = widen8(c[0]);
                 q[1][j] = widen8(c[1]);
-#pragma unroll
-                for (int s = 0; s < ENDS; ++s) scale[s][j] = copies.scales_of(ss, (half * 64 + s * 32) / Cfg::GROUP, wn * FN + j);
+                scale[j] = copies.scales_of(ss, half * 64 / Cfg::GROUP, wn * FN + j);
             }
             copies.begin_x();
             if (half == 0) copies.begin_codes();
@@ -328,19 +329,18 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void linear4_wide_kernel(const Lin
                 else if (half == 0 && i - R < RC) copies.request_codes(i - R);
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
-                    const int b = ENDS == 2 ? kk : i & 1;
+                    const int b = i & 1;
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) part[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[kk][j], x[i & 1][kk], ENDS == 2 || kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[b][j], 0, 0, 0);
+                    for (int j = 0; j < FN; ++j) part[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[kk][j], x[b][kk], kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[b][j], 0, 0, 0);
                     // the sums that ended before these began
-                    const int row = ENDS == 2 && kk == 1 ? i : i - 1;
-                    if (row < 0 || (ENDS == 1 && kk == 0)) continue;
+                    if (i == 0 || kk == 0) continue;
 #pragma unroll
-                    for (int j = 0; j < FN; ++j) add(total[row][j], scale[ENDS == 2 ? b ^ 1 : 0][j], part[b ^ 1][j]);
+                    for (int j = 0; j < FN; ++j) add(total[i - 1][j], scale[j], part[b ^ 1][j]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) add(total[FM - 1][j], scale[ENDS - 1][j], part[1][j]);
+            for (int j = 0; j < FN; ++j) add(total[FM - 1][j], scale[j], part[(FM - 1) & 1][j]);
             arrived();
             xs = xs == Cfg::X_SLOTS - 1 ? 0 : xs + 1;
         }
