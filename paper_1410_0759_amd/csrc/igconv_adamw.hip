@@ -41,6 +41,7 @@ struct AdamWArgs {
 };
 static_assert(sizeof(AdamWArgs) <= 4096, "a launch's arguments");
 
+// A published hash of 32 bits, multiplications and shifted exclusive ors, whose constants and shifts Chris Wellons found by a search for the least bias ("Prospecting for Hash Functions", 2018).
 __host__ __device__ inline uint32_t mixed(uint32_t x) {
     x = (x ^ (x >> 16)) * 0x7FEB352Du;
     x = (x ^ (x >> 15)) * 0x846CA68Bu;
@@ -140,7 +141,7 @@ __device__ __forceinline__ bool is_finite(float v) { return (__builtin_bit_cast(
 template <bool SQUARES> struct Eight;   // the formats: bits behind the leading one, largest number
 template <> struct Eight<false> {
     static constexpr int KEPT = 3;
-    static constexpr float MOST = 448.f, LEAST = 0.f;
+    static constexpr float MOST = 448.f;
     static __device__ __forceinline__ uint32_t narrow(const float (&y)[4]) {
         const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
         return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
@@ -265,7 +266,7 @@ __device__ __forceinline__ void update(const AdamWEntry &t, const Constants &c, 
         if constexpr (EIGHT) {
             // (four elements from a multiple of four on)
             uint32_t random[4];
-            const uint32_t from = (uint32_t)at ^ c.key ^ ((uint32_t)(at >> 32) * 0x9E3779B9u);
+            const uint32_t from = (uint32_t)at ^ c.key ^ ((uint32_t)(at >> 32) * 0x9E3779B9u);      // (2^32 over the golden ratio)
 #pragma unroll
             for (int e = 0; e < 4; ++e) random[e] = mixed(from ^ (uint32_t)e);
             float sm, sv;
