@@ -474,7 +474,14 @@ bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t
 // Rows up to which dz is held in two bfloat16 parts, as rows of their own of the matrix that the products take: a tile's 64 rows have room for both.  More rows pay for the second part
 // in full (4096 x 4096 -> 65536 8290 us for 5180, 777 x 1000 -> 10007 143 for 112): by the handle's choice; else what is left at the targets is put back instead.
 constexpr int kPartsRows = 32;
-bool in_parts(igcHandle_t h, igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && (x.rows <= kPartsRows || h->crossEntropySlopes == IGC_DATA_FLOAT); }
+// Of a few entries' gradients what is left at the targets is a long sum for each entry, which one workgroup makes in order (a row of 1024 features 0.1 us, of 4096 0.2): with both parts
+// of dz there is none, for about 24 bytes a feature of x (16384 x 1024 -> 2, 8, 16 and 32 rounded 903, 294, 195 and 142 us, in two parts 145, 158, 158 and 154; 16384 x 4096 -> 4, 8 and 16
+// 1030, 626 and 425 us, in two parts 632 each; 2048 x 1024 -> 2 134 and 58).
+constexpr int kFewEntriesRows = 512;
+bool few_entries(const Matrix &x, int C, int V) { return x.rows >= kFewEntriesRows && x.rows <= kMostRows / 2 && (long long)V * std::max(C, 2048) <= 16 * 2048; }
+bool in_parts(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
+    return t == IGC_DATA_BFLOAT16 && (x.rows <= kPartsRows || h->crossEntropySlopes == IGC_DATA_FLOAT || few_entries(x, C, V));
+}
 struct ForwardPlan {
     bool few, whole;     // few tokens; else whether the tiles leave the statistics, no logits in memory
     Pieces pieces;
@@ -564,7 +571,7 @@ BackwardPlan plan_backward(igcHandle_t h, igcDataType t, igcTensorDescriptor_t d
     BackwardPlan p;
     const size_t elem = t == IGC_DATA_FLOAT ? 4 : 2;
     p.few = few_tokens(h, t, x, V);
-    p.parts = in_parts(h, t, x);
+    p.parts = in_parts(h, t, x, C, V);
     p.rows = p.parts ? 2 * x.rows : x.rows;
     auto in_pieces = [&](long long limit) {
         p.pieces = pieces_of(p.rows, V, elem, limit);
@@ -620,7 +627,7 @@ igcStatus check_sizes(igcTensorDescriptor_t x, igcFilterDescriptor_t w, Matrix *
     return IGC_STATUS_SUCCESS;
 }
 // (two parts: their rows are counted as a product's)
-igcStatus check_rows(igcHandle_t h, igcDataType t, const Matrix &x) { return in_parts(h, t, x) && x.rows > kMostRows / 2 ? IGC_STATUS_NOT_SUPPORTED : IGC_STATUS_SUCCESS; }
+igcStatus check_rows(igcHandle_t h, igcDataType t, const Matrix &x) { return t == IGC_DATA_BFLOAT16 && h->crossEntropySlopes == IGC_DATA_FLOAT && x.rows > kMostRows / 2 ? IGC_STATUS_NOT_SUPPORTED : IGC_STATUS_SUCCESS; }
 igcStatus check_gradients(igcTensorDescriptor_t x, igcFilterDescriptor_t w, igcTensorDescriptor_t dx, igcFilterDescriptor_t dw, Matrix *mdx) {
     const auto type = [&](igcDataType t) { return t == IGC_DATA_FLOAT || (t == IGC_DATA_BFLOAT16 && x->dtype == IGC_DATA_BFLOAT16); };
     if ((dx && !dx->set) || (dw && !dw->set)) return IGC_STATUS_NOT_INITIALIZED;
