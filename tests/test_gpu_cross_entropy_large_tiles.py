@@ -32,7 +32,7 @@ def a_case(M, C, V, layout=(0, 0), units=256, repeat=0, **more):
 
 # (sizes, what of them takes the large tiles)
 SIZES = [((2047, 1000, 16381, (8, 8)), "slopes filter"), ((4090, 4096, 8185, (0, 0)), "slopes data filter"), ((4095, 2056, 16381, (2, 2)), "slopes data"), ((2303, 1024, 16383, (0, 0)), "data filter"),
-         ((2305, 1024, 16385, (8, 8)), "data"), ((4095, 2056, 9001, (2, 2)), "data"), ((4095, 4104, 8193, (0, 0)), "")]
+         ((2305, 1024, 16385, (8, 8)), "data"), ((4095, 2056, 9001, (2, 2)), "data"), ((4095, 4104, 8193, (0, 0)), ""), ((9047, 3136, 2265, (0, 0)), "filter")]
 
 
 def test_loss():
