@@ -622,9 +622,9 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
  * dx: M rows of C, dw: filter V x C x 1 x 1, each float or, for bfloat16 x, bfloat16 too; dbias: V packed floats.  Each may be NULL (its descriptor too): not computed.
  * For bfloat16 x, dz goes into the two products in bfloat16 (dbias sums it before), its rounding and what that left off, rounded too: of
  * all elements up to 32 rows, or of up to 16 entries (fewer of more than 2048 features), else of the targets, which are nearly all of a gradient; the sums over pieces of the vocabulary are held in floats.  So elsewhere a
- * float dx or dw is no more exact than that: dz is off by 2^-16 of itself at the targets, by up to 2^-8 (1.7e-3 on the average) elsewhere, which is all there is to
+ * float dx or dw is no more exact than that: dz is off by 2^-16 of itself at the targets, by up to 2^-8 (1.9e-3 by the norm) elsewhere, which is all there is to
  * the row of dw of an entry that is nobody's target.  igcSetCrossEntropySlopes(handle, IGC_DATA_FLOAT) has the second part of all elements go in, with any number of rows (up to
- * 2^29), in later calls and queries on the handle (which is asked for both): 2^-16 everywhere, about what exp leaves of it, for up to 1.6 times the time.  A row without target adds zeros times its x to dw: that x has to be finite.
+ * 2^29), in later calls and queries on the handle (which is asked for both): 2^-16 everywhere, about what exp leaves of it, for up to 1.7 times the time.  A row without target adds zeros times its x to dw: that x has to be finite.
  *
  * Both: workSpace (device, 16-byte aligned, contents mean nothing) has to have the size that the query reports, which counts x and w off 4-byte boundaries too; less than a call needs is
  * BAD_PARAM.  For 8192 rows, 4096 features and 131072 entries that is 201 MB forward and 839 MB backward (slopes in two parts: 1.0 GB), as floats (copies of the operands in parts) 0.7 and

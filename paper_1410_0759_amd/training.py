@@ -47,7 +47,7 @@ class _Module:
 class VocabularyHead(_Module):
     """The last product and the cross entropy of its logits, which are never held.  Weights of the compute type, float gradients.
     slopes: what the logits' gradients go into the products as, where the weights are bfloat16: torch.float32, as exact as float gradients are to be, or torch.bfloat16,
-    for up to 1.6 times the speed."""
+    for up to 1.7 times the speed."""
 
     def __init__(self, width, entries, dtype=torch.bfloat16, bias=False, device="cuda", seed=0, slopes=torch.float32):
         device = torch.device("cuda", torch.cuda.current_device()) if str(device) == "cuda" else torch.device(device)
