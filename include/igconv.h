@@ -621,7 +621,7 @@ igcStatus igcLinearCrossEntropyForward(igcHandle_t handle, igcTensorDescriptor_t
  *   dx = dz w + beta * dx,   dw = dz^T x + paramBeta * dw,   dbias = column sums of dz + paramBeta * dbias
  * dx: M rows of C, dw: filter V x C x 1 x 1, each float or, for bfloat16 x, bfloat16 too; dbias: V packed floats.  Each may be NULL (its descriptor too): not computed.
  * For bfloat16 x, dz goes into the two products in bfloat16 (dbias sums it before), its rounding and what that left off, rounded too: of
- * all elements up to 32 rows, or of up to 16 entries (fewer of more than 2048 features), else of the targets, which are nearly all of a gradient; the sums over pieces of the vocabulary are held in floats.  So elsewhere a
+ * all elements up to 32 rows, or of up to 16 entries (fewer of more than 2048 features, an x of up to 2^26), else of the targets, which are nearly all of a gradient; the sums over pieces of the vocabulary are held in floats.  So elsewhere a
  * float dx or dw is no more exact than that: dz is off by 2^-16 of itself at the targets, by up to 2^-8 (1.9e-3 by the norm) elsewhere, which is all there is to
  * the row of dw of an entry that is nobody's target.  igcSetCrossEntropySlopes(handle, IGC_DATA_FLOAT) has the second part of all elements go in, with any number of rows (up to
  * 2^29), in later calls and queries on the handle (which is asked for both): 2^-16 everywhere, about what exp leaves of it, for up to 1.7 times the time.  A row without target adds zeros times its x to dw: that x has to be finite.

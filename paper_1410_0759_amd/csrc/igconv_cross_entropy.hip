@@ -476,9 +476,10 @@ bool few_tokens(igcHandle_t h, igcDataType t, const Matrix &x, int V) { return t
 constexpr int kPartsRows = 32;
 // Of a few entries' gradients what is left at the targets is a long sum for each entry, which one workgroup makes in order (a row of 1024 features 0.1 us, of 4096 0.2): with both parts
 // of dz there is none, for about 24 bytes a feature of x (16384 x 1024 -> 2, 8, 16 and 32 rounded 903, 294, 195 and 142 us, in two parts 145, 158, 158 and 154; 16384 x 4096 -> 4, 8 and 16
-// 1030, 626 and 425 us, in two parts 632 each; 2048 x 1024 -> 2 134 and 58).
+// 1030, 626 and 425 us, in two parts 632 each; 2048 x 1024 -> 2 134 and 58).  Up to kFewEntriesFeatures of x: the parts of dx and x take 12 bytes each of room.
 constexpr int kFewEntriesRows = 512;
-bool few_entries(const Matrix &x, int C, int V) { return x.rows >= kFewEntriesRows && x.rows <= kMostRows / 2 && (long long)V * std::max(C, 2048) <= 16 * 2048; }
+constexpr long long kFewEntriesFeatures = 1ll << 26;
+bool few_entries(const Matrix &x, int C, int V) { return x.rows >= kFewEntriesRows && x.rows * C <= kFewEntriesFeatures && (long long)V * std::max(C, 2048) <= 16 * 2048; }
 bool in_parts(igcHandle_t h, igcDataType t, const Matrix &x, int C, int V) {
     return t == IGC_DATA_BFLOAT16 && (x.rows <= kPartsRows || h->crossEntropySlopes == IGC_DATA_FLOAT || few_entries(x, C, V));
 }

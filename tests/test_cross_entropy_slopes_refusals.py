@@ -37,3 +37,10 @@ def test_workspace_and_rows():
     most = 1 << 29
     assert status(lambda: query(b, most, 1, 1)) == OK and status(lambda: query(b, most + 1, 1, 1)) == UNSUPPORTED and call(b, most + 1, 1, 1, 1 << 50) == UNSUPPORTED
     assert status(lambda: query(a, most + 1, 1, 1)) == OK
+
+
+def test_room_of_a_few_entries():
+    """Beyond 2^26 features of x the parts are not held at once: no more room than twice x, and logits and dz in 64 columns."""
+    h = ig.Handle()
+    for M, C in ((1 << 21, 4096), ((1 << 26) // 64 + 1, 64), (70000, 1000)):
+        assert ig.get_linear_cross_entropy_backward_workspace_size(h, rows(B, M, C), filt(B, 2, C), rows(B, M, C), filt(B, 2, C)) < 2 * M * C * 2 + M * 64 * (4 + 2) + (1 << 27)

@@ -29,15 +29,15 @@ def test_many_rows_of_a_few_entries(types):
         c.check(*types, beta=0.5, got=got)
 
 
-def test_a_million_rows_of_two_entries():
-    c = a_case(1000003, 72, 2, (0, 0), "any")
+def test_nearly_a_million_rows_of_two_entries():
+    c = a_case(932003, 72, 2, (0, 0), "any")
     c.check("bf16", "f32")
     torch.cuda.empty_cache()
 
 
-def test_more_entries_and_fewer_rows_are_as_they_were():
+def test_more_entries_fewer_rows_and_more_features_are_as_they_were():
     from tests.kernel_names import launched
-    for M, C, V in ((2000, 130, 17), (700, 4096, 9), (511, 40, 2)):
+    for M, C, V in ((2000, 130, 17), (700, 4096, 9), (511, 40, 2), (66000, 1017, 2)):
         c = a_case(M, C, V, (0, 0), "any")
         _, names = launched(lambda: c.backward("bf16", "bf16"))
         assert any("rest_rows" in n for n in names), names
